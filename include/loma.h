@@ -21,6 +21,13 @@
  *   loma_compress_step     the t <m> queries over the uncompressed tail, fused
  *                          with the in-place compaction of the cache
  *                          (Section 3.1 steps 2-3; Appendix A, compress_last_chunk)
+ *   loma_decode_attn_shared, loma_decode_attn_shared_paged
+ *                          one generated token over a prefix that the whole batch shares and
+ *                          the sequences' own entries, with grouped heads
+ *   loma_qk_norm_rope_fwd, _bwd, _append
+ *                          per-head RMS norm of q and k with the rotary embedding (training
+ *                          layout; packed new tokens into cache pages)
+ *   loma_paged_extend      block tables and slot maps from request lengths
  *   loma_layout_index      row -> (chunk, zone, offset, source token, position id)
  *                          (Section 4.1; Section 4.5, Eq. 14)
  *   loma_generation_index  generated token -> cache slot / position / compress flag
@@ -673,6 +680,144 @@ LOMA_API int loma_compress_step_ragged(const void* q_mem, const void* k_mem, con
                                        int B, int H, int D, int cap,
                                        const int32_t* mem_lens, int max_mem_len, int c, int t, int tc,
                                        loma_dtype dtype, float softmax_scale, unsigned flags, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * loma_paged_extend -- block tables and slot maps for the paged entry points, from the requests'
+ * lengths: which page and row every new entry of every sequence goes to (the paper keeps one cache
+ * per sequence; this is Appendix A's append for an engine that hands out cache memory page by page).
+ * With ps = page_size and M = max_pages, for sequence b:
+ *     len   = cache_lens[b] clamped to [0, M ps]; a negative entry is a slot of the batch without a request
+ *     n     = new_lens[b] (negative counts as 0; 1 each when new_lens is NULL; 0 without a request)
+ *     h     = held[b] clamped to [0, M]: pages its table row already names.  LoMA's lengths also fall (a
+ *             compress step turns tc entries into t) while the pages stay with the sequence, so this is the
+ *             caller's count; NULL: ceil(len / ps)
+ *     fresh = max(0, ceil(min(len + n, M ps) / ps) - h), 0 if n == 0
+ * Fresh pages are drawn from free_pages in order, sequence by sequence, and written to
+ * block_table[b][h ..]; past the end of free_pages -1 is written.  Nothing else of the table is touched.
+ * New entry i of sequence b is packed row r = row_start[b] + i.
+ *
+ *   cache_lens, new_lens, held, pos0 [in]   int32 [B]; all but cache_lens may be NULL
+ *   free_pages   [in]      int32 [n_free] page numbers
+ *   taken        [in/out]  int32 [1]: pages of free_pages drawn by earlier calls; the call starts behind them and
+ *                          stores page_start[B].  NULL: starts at 0
+ *   block_table  [in/out]  int32 [B, max_pages]
+ *   row_start    [out]     int32 [B+1]: exclusive sums of n (row_start[B] = rows of the packed batch)
+ *   page_start   [out]     int32 [B+1]: taken + exclusive sums of fresh; page_start[B] > n_free: the free list
+ *                          was too short by the difference
+ *   held_out     [out]     int32 [B]: h plus the fresh pages the sequence got; may be the array `held`
+ *   slots        [out]     int32 [max_rows]: page * ps + row in page of every packed row; -1 where there is no page
+ *                          (list exhausted, entry beyond M ps, table entry negative) and for rows behind the last
+ *   row_seq      [out]     int32 [max_rows]: sequence of the row, -1 behind the last
+ *   row_pos      [out]     int32 [max_rows]: (pos0 ? pos0[b] : len) + i, the row's position id; 0 behind the last
+ * Sums and positions beyond INT_MAX are stored as INT_MAX.  Rows at and beyond max_rows are not written.
+ * on_device != 0: every pointer is [device] and the work is enqueued on `stream` (one launch up to 4096
+ * sequences when nothing is updated in place, else two); on_device == 0: every pointer is [host], no CUDA call.
+ * Errors: INVALID_ARG (page size not a power of two <= 65536, max_pages * page_size > INT_MAX, a required
+ * pointer NULL, outputs that overlap inputs or each other), ALIGNMENT (4 bytes), UNSUPPORTED, CUDA.
+ * ------------------------------------------------------------------------- */
+LOMA_API int loma_paged_extend(int B, int page_size, int max_pages, int max_rows, int n_free, const int32_t* cache_lens,
+                               const int32_t* new_lens, const int32_t* held, const int32_t* pos0,
+                               const int32_t* free_pages, int32_t* taken, int32_t* block_table, int32_t* row_start,
+                               int32_t* page_start, int32_t* held_out, int32_t* slots, int32_t* row_seq,
+                               int32_t* row_pos, int on_device, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * loma_qk_norm_rope_fwd, loma_qk_norm_rope_bwd -- RMS norm of every head of q and k and the rotary
+ * embedding of loma_rope_apply in one pass, for models that normalise queries and keys per head before
+ * rotating them.  For a row x of D features with gain w and position id p (Section 4.5, as in loma_rope_apply):
+ *     y = R(p) (w * x * r),   r = (mean_d x_d^2 + eps)^(-1/2)
+ * and the gradients, with g = dL/dy and u = R(-p) g:
+ *     dw = sum over rows of u * x r       dx = r (w u - x r^2 mean_d(w u x))
+ * All in fp32 with one rounding at the end; dw is summed in a fixed order (no atomics): results repeat bit for bit.
+ *
+ *   q, k         [device, in]   [B, Hq, S, D] and [B, Hk, S, D]; Hq, Hk may differ, and one may be 0 (its
+ *                               pointers are then ignored)
+ *   wq, wk       [device, in]   [D] each, shared by the heads; NULL: ones
+ *   q_out, k_out [device, out]  shape and strides of q and k; q_out == q and k_out == k is allowed
+ *   d_q_out, d_k_out [device, in], dq, dk [device, out]   shape and strides of q and k; outputs must not alias inputs
+ *   dwq, dwk     [device, out]  [D] each, or NULL (not computed)
+ *   q_strides, k_strides [host] int64 [3]: batch, head and row stride in elements (multiples of 16 bytes; rows must
+ *                               not overlap)
+ *   n_chunks .. tail_read, flags, position_type (0 or 1), theta_base   as in loma_rope_apply
+ *   eps          <= 0 selects 1e-6
+ *   workspace    [device]       backward: loma_qk_norm_rope_bwd_workspace_bytes(...) bytes, 256-byte aligned
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA.  No rows: a no-op (backward: dwq, dwk become 0).
+ * ------------------------------------------------------------------------- */
+LOMA_API int loma_qk_norm_rope_fwd(const void* q, const void* k, const void* wq, const void* wk, void* q_out,
+                                   void* k_out, int B, int Hq, int Hk, int D, int n_chunks, int c, int t, int tc,
+                                   int tail_read, const int64_t* q_strides, const int64_t* k_strides, loma_dtype dtype,
+                                   float eps, float theta_base, int position_type, unsigned flags, void* stream);
+LOMA_API int loma_qk_norm_rope_bwd(const void* q, const void* k, const void* wq, const void* wk, const void* d_q_out,
+                                   const void* d_k_out, void* dq, void* dk, void* dwq, void* dwk, int B, int Hq, int Hk,
+                                   int D, int n_chunks, int c, int t, int tc, int tail_read, const int64_t* q_strides,
+                                   const int64_t* k_strides, loma_dtype dtype, float eps, float theta_base,
+                                   int position_type, unsigned flags, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+LOMA_API size_t loma_qk_norm_rope_bwd_workspace_bytes(int B, int Hq, int Hk, int D, int n_chunks, int c, int t,
+                                                      int tail_read, unsigned flags);
+
+/* ---------------------------------------------------------------------------
+ * loma_qk_norm_rope_append -- the same norm and rotation for T packed new tokens of any requests, with the
+ * rotated keys (rounded to the storage type) and the values written straight to their cache entries: what
+ * a generation step or a prompt piece does before its attention.  Positions are the requests' own
+ * (Appendix A, inference_input: cursor + i).
+ *
+ *   q            [device, in]   T rows of Hq heads of D features, element (r, h, d) at r*q_strides[0] + h*q_strides[1] + d;
+ *                               k_new, v_new likewise with Hk heads (views of one projection's output, for instance)
+ *   q_out        [device, out]  [T, Hq, D] contiguous; every row is written.  May be q if q is contiguous
+ *   k_pool, v_pool [device, out] [n_pages, Hk, page_size, D]; a contiguous cache [B, Hk, cap, D] is the pool of B
+ *                               pages of cap rows.  page_size need not be a power of two
+ *   slots        [device, in]   int32 [T]: page * page_size + row (loma_paged_extend); a row whose slot lies outside
+ *                               [0, n_pages * page_size) stores no key and value.  No two rows may name one slot
+ *   positions    [device, in]   int32 [T]
+ *   q_strides, k_strides, v_strides [host] int64 [2]: row and head stride in elements
+ *   wq, wk, eps, theta_base     as above
+ * Hq or Hk may be 0.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA.  T == 0 is a no-op.
+ * ------------------------------------------------------------------------- */
+LOMA_API int loma_qk_norm_rope_append(const void* q, const void* k_new, const void* v_new, const void* wq, const void* wk,
+                                      void* q_out, void* k_pool, void* v_pool, const int32_t* slots,
+                                      const int32_t* positions, int T, int Hq, int Hk, int D, int page_size, int n_pages,
+                                      const int64_t* q_strides, const int64_t* k_strides, const int64_t* v_strides,
+                                      loma_dtype dtype, float eps, float theta_base, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * loma_decode_attn_shared, loma_decode_attn_shared_paged -- one new token per sequence for a batch whose
+ * sequences share a long prefix (a system prompt, compressed once): the decode step of loma_decode_attn_ragged
+ * in which the first prefix_len entries are the same for every sequence and stored once, with grouped heads.
+ * Query head hq of sequence b attends, under one softmax, to the prefix's entries [0, prefix_len) of kv head
+ * hq / (Hq / Hkv), to the sequence's own entries [0, cache_lens[b]) and to its new token.  The prefix part is
+ * computed for all sequences together (the prefix is read once).
+ *
+ *   q, o           [device]          [B, Hq, 1, D] contiguous; Hq is a multiple of Hkv
+ *   k_new, v_new   [device, in]      [B, Hkv, 1, D] contiguous; both NULL: the token's K/V already sit at entry
+ *                                    cache_lens[b] (after loma_qk_norm_rope_append)
+ *   k_prefix, v_prefix [device, in]  [Hkv, prefix_cap, D] contiguous; rows at and beyond prefix_len are not used
+ *   k_cache, v_cache [device, in/out] [B, Hkv, cap, D] contiguous: the sequences' own entries; entry cache_lens[b] is
+ *                                    written when k_new is given, nothing else
+ *   lse            [device, out]     fp32 [B, Hq] or NULL
+ *   cache_lens     [device, in]      int32 [B]: own entries before this token; values above max_cache_len count as
+ *                                    max_cache_len; negative: a slot without a request, whose o, lse and cache are left
+ *                                    as they are
+ *   max_cache_len  [host]            an upper bound that sizes the launch and the workspace; max_cache_len < cap
+ *   workspace      [device]          loma_decode_shared_workspace_bytes(...) bytes, 16-byte aligned; contents need not
+ *                                    be kept.  Calls that may overlap need workspaces of their own
+ * paged: pools [n_pages, Hkv, page_size, D] hold prefix and own entries; prefix_table int32 [prefix_pages] and block_table
+ * int32 [B, max_pages] name the pages (clamped to the pool on the device); prefix_len <= prefix_pages * page_size,
+ * max_cache_len < max_pages * page_size.  No page may be both a prefix page and a page a new token is written to.
+ * Errors: INVALID_ARG (Hq not a multiple of Hkv, ...), UNSUPPORTED, ALIGNMENT, CAPACITY, WORKSPACE, CUDA.  B*Hq == 0 is a no-op.
+ * ------------------------------------------------------------------------- */
+LOMA_API int loma_decode_attn_shared(const void* q, const void* k_new, const void* v_new, const void* k_prefix,
+                                     const void* v_prefix, void* k_cache, void* v_cache, void* o, float* lse, int B,
+                                     int Hq, int Hkv, int D, int prefix_cap, int prefix_len, int cap,
+                                     const int32_t* cache_lens, int max_cache_len, loma_dtype dtype, float softmax_scale,
+                                     unsigned flags, void* workspace, size_t workspace_bytes, void* stream);
+LOMA_API int loma_decode_attn_shared_paged(const void* q, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
+                                           const int32_t* prefix_table, const int32_t* block_table, void* o, float* lse,
+                                           int B, int Hq, int Hkv, int D, int page_size, int prefix_pages, int prefix_len,
+                                           int max_pages, int n_pages, const int32_t* cache_lens, int max_cache_len,
+                                           loma_dtype dtype, float softmax_scale, unsigned flags, void* workspace,
+                                           size_t workspace_bytes, void* stream);
+LOMA_API size_t loma_decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int prefix_len, int max_cache_len);
 
 /* Synchronises `stream`, then returns the device status word of the current
  * device: LOMA_OK, or LOMA_ERR_TIMEOUT if a bounded wait inside a kernel has

@@ -70,3 +70,43 @@ def loma_rope(q, k, n_chunks: int, c: int, t: int, tail_read: int = 0, flags: in
     """Rotary embedding of q and k at the layout's position ids as a differentiable torch op (out of place;
     the gradient is the rotation by the opposite angle, run by the same kernel)."""
     return _Rope.apply(q, k, n_chunks, c, t, tail_read, flags, theta_base, position_type)
+
+
+class _QkNormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, wq, wk, n_chunks, c, t, tail_read, flags, eps, theta_base, position_type):
+        if not (q.is_cuda and k.is_cuda):
+            raise RuntimeError("loma_qk_norm_rope needs CUDA tensors (there is no CPU path)")
+        q, k = q.contiguous(), k.contiguous()
+        wq, wk = (None if w is None else w.contiguous() for w in (wq, wk))
+        q_out, k_out = torch.empty_like(q), torch.empty_like(k)
+        ctx.layout = (n_chunks, c, t, tail_read, flags)
+        ctx.norm = (eps, theta_base, position_type)
+        with torch.cuda.device(q.device):
+            L.loma_qk_norm_rope_fwd(q, k, wq, wk, q_out, k_out, *ctx.layout, *ctx.norm)
+        ctx.save_for_backward(q, k, wq, wk)
+        return q_out, k_out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_q_out, d_k_out):
+        q, k, wq, wk = ctx.saved_tensors
+        n_chunks, c, t, tail_read, flags = ctx.layout
+        eps, theta_base, position_type = ctx.norm
+        d_q_out, d_k_out = d_q_out.contiguous(), d_k_out.contiguous()
+        dq, dk = torch.empty_like(q), torch.empty_like(k)
+        dwq, dwk = (torch.empty_like(w) if w is not None and need else None
+                    for w, need in ((wq, ctx.needs_input_grad[2]), (wk, ctx.needs_input_grad[3])))
+        nbytes = L.loma_qk_norm_rope_bwd_workspace_bytes(q.shape[0], q.shape[1], k.shape[1], q.shape[3], n_chunks, c, t, tail_read, flags)
+        ws = torch.empty(max(256, nbytes), dtype=torch.uint8, device=q.device)
+        with torch.cuda.device(q.device):
+            L.loma_qk_norm_rope_bwd(q, k, wq, wk, d_q_out, d_k_out, dq, dk, dwq, dwk, n_chunks, c, t, tail_read, flags, ws, eps,
+                                    theta_base, position_type)
+        return dq, dk, dwq, dwk, None, None, None, None, None, None, None, None
+
+
+def loma_qk_norm_rope(q, k, wq, wk, n_chunks: int, c: int, t: int, tail_read: int = 0, flags: int = 0, eps: float = 0.0,
+                      theta_base: float = 0.0, position_type: int = 0):
+    """Per-head RMS norm of q [B, Hq, S, D] and k [B, Hk, S, D] with gains wq, wk ([D] or None) and the rotary embedding at the
+    layout's position ids as one differentiable torch op; returns (q_out, k_out).  Gradients flow to q, k, wq and wk."""
+    return _QkNormRope.apply(q, k, wq, wk, n_chunks, c, t, tail_read, flags, eps, theta_base, position_type)

@@ -71,6 +71,16 @@ SIGNATURES = {
     "loma_compress_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _u]),
     "loma_compress_step_paged": (_i, [_p, _p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _p, _i, _i, _i, _i, _i, _f, _u, _p]),
     "loma_compress_step_ragged": (_i, [_p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _p, _i, _i, _i, _i, _i, _f, _u, _p]),
+    "loma_paged_extend": (_i, [_i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _p]),
+    "loma_qk_norm_rope_fwd": (_i, [_p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _i, _i, _i, _p, _p, _i, _f, _f, _i, _u, _p]),
+    "loma_qk_norm_rope_bwd": (_i, [_p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _i, _i, _i, _p, _p, _i, _f, _f,
+                                   _i, _u, _p, _sz, _p]),
+    "loma_qk_norm_rope_bwd_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i, _i, _i, _u]),
+    "loma_qk_norm_rope_append": (_i, [_p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _p, _p, _p, _i, _f, _f, _p]),
+    "loma_decode_attn_shared": (_i, [_p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _i, _p, _i, _i, _f, _u, _p, _sz, _p]),
+    "loma_decode_attn_shared_paged": (_i, [_p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _i, _i, _i, _p, _i, _i, _f, _u,
+                                           _p, _sz, _p]),
+    "loma_decode_shared_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
     "loma_device_status": (_i, [_p]),
     "loma_selftest_bounded_wait": (_i, [_p]),
     "loma_launch_count": (ctypes.c_uint64, []),
@@ -652,3 +662,209 @@ def loma_compress_step(q_mem, k_mem, v_mem, k_cache, v_cache, o_mem, lse, mem_le
                                   _ptr(o_mem), _ptr(lse), B, H, D, cap, mem_len, c, t, c * t, _dtype_code(q_mem),
                                   float(softmax_scale), int(flags), _ptr(workspace), ws_bytes, _stream(stream))
     _check(rc, "loma_compress_step")
+
+
+# ---- one serving step: page tables, norm + rotation into the pages, attention over a shared prefix -----------------------
+
+def _same_device(where: str, *tensors):
+    """The tensors of a device call share one device, and it is the current one: a pointer of another would reach the
+    wrong GPU's kernel."""
+    dev = None
+    for x in tensors:
+        if x is None:
+            continue
+        if dev is None:
+            dev = x.device
+        elif x.device != dev:
+            raise ValueError(f"{where}: tensors on {dev} and {x.device}")
+    if dev is not None and dev.type == "cuda" and dev.index != torch.cuda.current_device():
+        raise ValueError(f"{where}: tensors on {dev}, but the current device is cuda:{torch.cuda.current_device()}")
+    return dev
+
+
+def _int32(where: str, name: str, x, numel: Optional[int] = None):
+    if x is not None and (x.dtype != torch.int32 or not x.is_contiguous() or (numel is not None and x.numel() != numel)):
+        raise ValueError(f"{where}: {name} must be contiguous int32" + ("" if numel is None else f" with {numel} entries"))
+
+
+def _expect(where: str, name: str, x, shape, dtype):
+    if x is not None and (tuple(x.shape) != tuple(shape) or x.dtype != dtype or not x.is_contiguous()):
+        raise ValueError(f"{where}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+
+
+def _strides(x, axes):
+    """[host] int64 array; an axis of one element has no stride of its own (torch reports any number there)."""
+    return (ctypes.c_int64 * len(axes))(*[x.stride(a) if x.shape[a] > 1 else 0 for a in axes])
+
+
+def loma_paged_extend(cache_lens, new_lens, held, pos0, free_pages, taken, block_table, page_size: int, row_start, page_start,
+                      held_out, slots, row_seq, row_pos, stream=None) -> None:
+    """Block table and slot maps from request lengths (see include/loma.h).  int32 tensors, all on the device or all on the
+    host: cache_lens, new_lens, held, pos0 [B] (all but cache_lens may be None), free_pages, taken [1] or None, block_table
+    [B, max_pages] (in/out); outputs row_start, page_start [B+1], held_out [B] (may be `held`), slots, row_seq, row_pos [rows]."""
+    w = "loma_paged_extend"
+    B = cache_lens.numel()
+    for name, x, n in (("cache_lens", cache_lens, B), ("new_lens", new_lens, B), ("held", held, B), ("pos0", pos0, B),
+                       ("free_pages", free_pages, None), ("taken", taken, 1), ("row_start", row_start, B + 1),
+                       ("page_start", page_start, B + 1), ("held_out", held_out, B), ("slots", slots, None),
+                       ("row_seq", row_seq, slots.numel()), ("row_pos", row_pos, slots.numel())):
+        _int32(w, name, x, n)
+    _int32(w, "block_table", block_table)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError(f"{w}: block_table must be [B, max_pages]")
+    dev = _same_device(w, cache_lens, new_lens, held, pos0, free_pages, taken, block_table, row_start, page_start, held_out, slots,
+                       row_seq, row_pos)
+    on_device = dev.type == "cuda"
+    rc = lib().loma_paged_extend(B, int(page_size), block_table.shape[1], slots.numel(), 0 if free_pages is None else free_pages.numel(),
+                                 _ptr(cache_lens), _ptr(new_lens), _ptr(held), _ptr(pos0), _ptr(free_pages), _ptr(taken),
+                                 _ptr(block_table), _ptr(row_start), _ptr(page_start), _ptr(held_out), _ptr(slots), _ptr(row_seq),
+                                 _ptr(row_pos), int(on_device), _stream(stream) if on_device else None)
+    _check(rc, w)
+
+
+def _norm_args(where, q, k, wq, wk, pairs, gains):
+    """Checks of the training-layout norm; returns (B, Hq, Hk, D, dtype code, q strides, k strides)."""
+    if q.dim() != 4 or k.dim() != 4 or q.shape[0] != k.shape[0] or q.shape[2:] != k.shape[2:] or q.dtype != k.dtype:
+        raise ValueError(f"{where}: q [B, Hq, S, D] and k [B, Hk, S, D] must share B, S, D and dtype")
+    D = q.shape[3]
+    for x in (q, k):
+        if x.stride(3) != 1:
+            raise ValueError(f"{where}: head dimension must be contiguous")
+    for ref, x in pairs:
+        if x.shape != ref.shape or x.dtype != ref.dtype or any(n > 1 and a != b for n, a, b in zip(x.shape, x.stride(), ref.stride())):
+            raise ValueError(f"{where}: every tensor that goes with q or k must have its shape, strides and dtype")
+    for name, x in gains:
+        _expect(where, name, x, (D,), q.dtype)
+    _same_device(where, q, k, *[x for _, x in pairs], *[x for _, x in gains])
+    return q.shape[0], q.shape[1], k.shape[1], D, _dtype_code(q), _strides(q, (0, 1, 2)), _strides(k, (0, 1, 2))
+
+
+def _norm_rows(where, q, n_chunks, c, t, tail_read, flags):
+    S = n_chunks * ((c * t + t) if (flags & LOMA_FLAG_NO_REP_ZONE) else (2 * c * t + t)) + tail_read
+    if q.shape[2] != S:
+        raise ValueError(f"{where}: the layout has {S} rows, the tensors {q.shape[2]}")
+
+
+def loma_qk_norm_rope_fwd(q, k, wq, wk, q_out, k_out, n_chunks: int, c: int, t: int, tail_read: int = 0, flags: int = 0,
+                          eps: float = 0.0, theta_base: float = 0.0, position_type: int = 0, stream=None) -> None:
+    """RMS norm of every head of q [B, Hq, S, D] and k [B, Hk, S, D] (gains wq, wk [D] or None) and the rotary embedding at the
+    layout's position ids, in one pass.  q_out, k_out: shape and strides of q and k; q and k themselves are allowed."""
+    w = "loma_qk_norm_rope_fwd"
+    B, Hq, Hk, D, dt, qs, ks = _norm_args(w, q, k, wq, wk, [(q, q_out), (k, k_out)], [("wq", wq), ("wk", wk)])
+    _norm_rows(w, q, n_chunks, c, t, tail_read, flags)
+    rc = lib().loma_qk_norm_rope_fwd(_ptr(q), _ptr(k), _ptr(wq), _ptr(wk), _ptr(q_out), _ptr(k_out), B, Hq, Hk, D, n_chunks, c, t, c * t,
+                                     tail_read, qs, ks, dt, float(eps), float(theta_base), int(position_type), int(flags),
+                                     _stream(stream))
+    _check(rc, w)
+
+
+def loma_qk_norm_rope_bwd_workspace_bytes(B: int, Hq: int, Hk: int, D: int, n_chunks: int, c: int, t: int, tail_read: int = 0,
+                                          flags: int = 0) -> int:
+    return int(lib().loma_qk_norm_rope_bwd_workspace_bytes(B, Hq, Hk, D, n_chunks, c, t, tail_read, int(flags)))
+
+
+def loma_qk_norm_rope_bwd(q, k, wq, wk, d_q_out, d_k_out, dq, dk, dwq, dwk, n_chunks: int, c: int, t: int, tail_read: int = 0,
+                          flags: int = 0, workspace=None, eps: float = 0.0, theta_base: float = 0.0, position_type: int = 0,
+                          stream=None) -> None:
+    """Gradients of loma_qk_norm_rope_fwd at q, k, wq, wk.  d_q_out, dq have q's shape and strides, d_k_out, dk those of k;
+    dwq, dwk [D] or None; workspace: a device byte buffer of loma_qk_norm_rope_bwd_workspace_bytes(...) bytes."""
+    w = "loma_qk_norm_rope_bwd"
+    B, Hq, Hk, D, dt, qs, ks = _norm_args(w, q, k, wq, wk, [(q, d_q_out), (q, dq), (k, d_k_out), (k, dk)],
+                                          [("wq", wq), ("wk", wk), ("dwq", dwq), ("dwk", dwk)])
+    _norm_rows(w, q, n_chunks, c, t, tail_read, flags)
+    _same_device(w, q, workspace)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib().loma_qk_norm_rope_bwd(_ptr(q), _ptr(k), _ptr(wq), _ptr(wk), _ptr(d_q_out), _ptr(d_k_out), _ptr(dq), _ptr(dk), _ptr(dwq),
+                                     _ptr(dwk), B, Hq, Hk, D, n_chunks, c, t, c * t, tail_read, qs, ks, dt, float(eps),
+                                     float(theta_base), int(position_type), int(flags), _ptr(workspace), ws_bytes, _stream(stream))
+    _check(rc, w)
+
+
+def loma_qk_norm_rope_append(q, k_new, v_new, wq, wk, q_out, k_pool, v_pool, slots, positions, eps: float = 0.0,
+                             theta_base: float = 0.0, stream=None) -> None:
+    """Norm and rotation of T packed new tokens: q [T, Hq, D] into q_out (contiguous), k_new [T, Hk, D] and, copied, v_new into
+    the pools [n_pages, Hk, page_size, D] at slots[r] = page * page_size + row (a slot outside the pool: not stored).
+    slots, positions: int32 [T].  q, k_new, v_new may be views of one projection's output."""
+    w = "loma_qk_norm_rope_append"
+    if q.dim() != 3 or k_new.dim() != 3 or k_pool.dim() != 4:
+        raise ValueError(f"{w}: q [T, Hq, D], k_new, v_new [T, Hk, D], pools [n_pages, Hk, page_size, D]")
+    T, Hq, D = q.shape
+    n_pages, Hk, page_size, _ = k_pool.shape
+    if k_new.shape != (T, Hk, D) or v_new.shape != (T, Hk, D) or k_new.dtype != q.dtype or v_new.dtype != q.dtype:
+        raise ValueError(f"{w}: k_new and v_new must be [T, Hk, D] in q's dtype")
+    for x in (q, k_new, v_new):
+        if x.numel() and x.stride(2) != 1:
+            raise ValueError(f"{w}: head dimension must be contiguous")
+    _expect(w, "q_out", q_out, (T, Hq, D), q.dtype)
+    _expect(w, "k_pool", k_pool, (n_pages, Hk, page_size, D), q.dtype)
+    _expect(w, "v_pool", v_pool, (n_pages, Hk, page_size, D), q.dtype)
+    _expect(w, "wq", wq, (D,), q.dtype)
+    _expect(w, "wk", wk, (D,), q.dtype)
+    _int32(w, "slots", slots, T)
+    _int32(w, "positions", positions, T)
+    _same_device(w, q, k_new, v_new, wq, wk, q_out, k_pool, v_pool, slots, positions)
+    rc = lib().loma_qk_norm_rope_append(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(wq), _ptr(wk), _ptr(q_out), _ptr(k_pool), _ptr(v_pool),
+                                        _ptr(slots), _ptr(positions), T, Hq, Hk, D, page_size, n_pages, _strides(q, (0, 1)),
+                                        _strides(k_new, (0, 1)), _strides(v_new, (0, 1)), _dtype_code(q), float(eps), float(theta_base),
+                                        _stream(stream))
+    _check(rc, w)
+
+
+def loma_decode_shared_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, prefix_len: int, max_cache_len: int) -> int:
+    return int(lib().loma_decode_shared_workspace_bytes(B, Hq, Hkv, D, int(prefix_len), int(max_cache_len)))
+
+
+def _shared_common(where, q, k_new, v_new, o, lse, cache_lens, Hkv, workspace):
+    if q.dim() != 4 or q.shape[2] != 1:
+        raise ValueError(f"{where}: q must be [B, Hq, 1, D]")
+    B, Hq, _, D = q.shape
+    _expect(where, "q", q, q.shape, q.dtype)
+    _expect(where, "o", o, q.shape, q.dtype)
+    _expect(where, "k_new", k_new, (B, Hkv, 1, D), q.dtype)
+    _expect(where, "v_new", v_new, (B, Hkv, 1, D), q.dtype)
+    _expect(where, "lse", lse, (B, Hq), torch.float32)
+    _int32(where, "cache_lens", cache_lens, B)
+    return B, Hq, D, 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def loma_decode_attn_shared(q, k_new, v_new, k_prefix, v_prefix, prefix_len: int, k_cache, v_cache, o, lse, cache_lens,
+                            max_cache_len: int, workspace=None, flags: int = 0, softmax_scale: float = 0.0, stream=None) -> None:
+    """Decode step over a prefix shared by the batch.  q, o: [B, Hq, 1, D]; k_new, v_new: [B, Hkv, 1, D] or None (already
+    stored); k_prefix, v_prefix: [Hkv, prefix_cap, D]; own caches [B, Hkv, cap, D]; cache_lens: int32 [B], negative = no request;
+    workspace: loma_decode_shared_workspace_bytes(...) bytes."""
+    w = "loma_decode_attn_shared"
+    _, Hkv, cap, D = k_cache.shape
+    B, Hq, D, ws_bytes = _shared_common(w, q, k_new, v_new, o, lse, cache_lens, Hkv, workspace)
+    _expect(w, "k_cache", k_cache, (B, Hkv, cap, D), q.dtype)
+    _expect(w, "v_cache", v_cache, (B, Hkv, cap, D), q.dtype)
+    prefix_cap = 0 if k_prefix is None else k_prefix.shape[1]
+    _expect(w, "k_prefix", k_prefix, (Hkv, prefix_cap, D), q.dtype)
+    _expect(w, "v_prefix", v_prefix, (Hkv, prefix_cap, D), q.dtype)
+    _same_device(w, q, k_new, v_new, k_prefix, v_prefix, k_cache, v_cache, o, lse, cache_lens, workspace)
+    rc = lib().loma_decode_attn_shared(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_prefix), _ptr(v_prefix), _ptr(k_cache), _ptr(v_cache),
+                                       _ptr(o), _ptr(lse), B, Hq, Hkv, D, prefix_cap, int(prefix_len), cap, _ptr(cache_lens),
+                                       int(max_cache_len), _dtype_code(q), float(softmax_scale), int(flags), _ptr(workspace), ws_bytes,
+                                       _stream(stream))
+    _check(rc, w)
+
+
+def loma_decode_attn_shared_paged(q, k_new, v_new, k_pool, v_pool, prefix_table, prefix_len: int, block_table, o, lse, cache_lens,
+                                  max_cache_len: int, workspace=None, flags: int = 0, softmax_scale: float = 0.0, stream=None) -> None:
+    """loma_decode_attn_shared over a pool [n_pages, Hkv, page_size, D] that holds the prefix (prefix_table: int32
+    [prefix_pages]) and the sequences' own entries (block_table: int32 [B, max_pages])."""
+    w = "loma_decode_attn_shared_paged"
+    n_pages, Hkv, page_size, D = k_pool.shape
+    B, Hq, D, ws_bytes = _shared_common(w, q, k_new, v_new, o, lse, cache_lens, Hkv, workspace)
+    _expect(w, "k_pool", k_pool, (n_pages, Hkv, page_size, D), q.dtype)
+    _expect(w, "v_pool", v_pool, (n_pages, Hkv, page_size, D), q.dtype)
+    _int32(w, "prefix_table", prefix_table)
+    _int32(w, "block_table", block_table)
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError(f"{w}: block_table must be [B, max_pages]")
+    _same_device(w, q, k_new, v_new, k_pool, v_pool, prefix_table, block_table, o, lse, cache_lens, workspace)
+    rc = lib().loma_decode_attn_shared_paged(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_pool), _ptr(v_pool), _ptr(prefix_table),
+                                             _ptr(block_table), _ptr(o), _ptr(lse), B, Hq, Hkv, D, page_size,
+                                             0 if prefix_table is None else prefix_table.numel(), int(prefix_len), block_table.shape[1],
+                                             n_pages, _ptr(cache_lens), int(max_cache_len), _dtype_code(q), float(softmax_scale),
+                                             int(flags), _ptr(workspace), ws_bytes, _stream(stream))
+    _check(rc, w)

@@ -32,7 +32,7 @@ static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t
 static inline size_t elt_size(loma_dtype dt) { return dt == LOMA_F32 ? 4 : 2; }
 
 // B200 check, cached per device.  Returns LOMA_OK / LOMA_ERR_UNSUPPORTED / LOMA_ERR_CUDA.
-static int check_device() {
+int check_device() {
     static int cached[64];
     static bool have[64] = {false};
     int dev = 0;
@@ -48,7 +48,7 @@ static int check_device() {
     return cached[dev];
 }
 
-static int make_layout(int n_chunks, int c, int t, int tail_read, unsigned flags, Layout* L) {
+int make_layout(int n_chunks, int c, int t, int tail_read, unsigned flags, Layout* L) {
     if (n_chunks < 0 || c < 1 || t < 0 || tail_read < 0) return LOMA_ERR_INVALID_ARG;
     if (t == 0 && n_chunks != 0) return LOMA_ERR_INVALID_ARG;
     const int64_t tc = (int64_t)c * t;
@@ -59,6 +59,14 @@ static int make_layout(int n_chunks, int c, int t, int tail_read, unsigned flags
     L->n_chunks = n_chunks; L->c = c; L->t = t; L->tc = (int)tc; L->s = (int)s;
     L->tail_read = tail_read; L->S = (int)S; L->flags = flags;
     return LOMA_OK;
+}
+
+// page_size must be a power of two; returns its log2 or -1
+int log2_exact(int x) {
+    if (x <= 0 || (x & (x - 1))) return -1;
+    int l = 0;
+    while ((1 << l) < x) ++l;
+    return l;
 }
 
 }  // namespace loma
@@ -431,8 +439,6 @@ int loma_compress_step_layers(int n_layers, const void* const* q_mem, const void
     return LOMA_OK;
 }
 
-static int log2_exact(int x);   // defined with the paged entry points below
-
 // The three forms of the prompt piece over a cache.  cache_len: the uniform length, or (cache_lens given) the bound the
 // per-sequence lengths are clamped to; pg.table given: the cache is the paged pool and cap = max_pages * page_size.
 static int prefill_attn_impl(const void* q, const void* k_new, const void* v_new, void* k_cache, void* v_cache, void* o,
@@ -702,14 +708,6 @@ int loma_decode_attn_ragged_rope(const void* q, const void* k_new, const void* v
     return loma_decode_attn_ragged_impl(q, k_new, v_new, k_cache, v_cache, o, lse, B, H, D, cap, cache_lens,
                                         max_cache_len, dtype, softmax_scale, flags, workspace, workspace_bytes,
                                         stream, rope);
-}
-
-// page_size must be a power of two; returns its log2 or -1
-static int log2_exact(int x) {
-    if (x <= 0 || (x & (x - 1))) return -1;
-    int l = 0;
-    while ((1 << l) < x) ++l;
-    return l;
 }
 
 static int loma_decode_attn_paged_impl(const void* q, const void* k_new, const void* v_new, void* k_pool, void* v_pool,

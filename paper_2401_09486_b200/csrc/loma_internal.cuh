@@ -178,6 +178,64 @@ cudaError_t launch_compress_generic(const void* q_mem, const void* k_mem, const 
 cudaError_t launch_rope(void* q, void* k, int B, int H, int D, const Layout& L, int64_t sb, int64_t sh, int64_t ss,
                         loma_dtype dt, double theta_base, int position_type, cudaStream_t st);
 
+// RMS norm of every head of q and k with the rotary embedding (qk_norm_rope.cu).  A HeadsView is one [B, H, S, D] tensor:
+// row (b, h, i) lies b*sb + h*sh + i*ss elements from the base.
+struct HeadsView {
+    const void* in = nullptr;    // q or k
+    const void* grad = nullptr;  // backward: gradient of the operator's output
+    void* out = nullptr;         // the operator's output, or (backward) the gradient of q or k
+    const void* w = nullptr;     // gain, D elements, or NULL (all ones)
+    void* dw = nullptr;          // backward: its gradient, or NULL
+    int H = 0;
+    int64_t sb = 0, sh = 0, ss = 0;
+};
+size_t qk_norm_rope_bwd_workspace_bytes(int B, int Hq, int Hk, int D, const Layout& L);
+cudaError_t launch_qk_norm_rope(const HeadsView& q, const HeadsView& k, int B, int D, const Layout& L, loma_dtype dt, float eps,
+                                double theta_base, int position_type, bool backward, void* ws, cudaStream_t st);
+struct AppendArgs {
+    const void *q = nullptr, *k = nullptr, *v = nullptr, *wq = nullptr, *wk = nullptr;
+    void *q_out = nullptr, *k_pool = nullptr, *v_pool = nullptr;
+    const int32_t *slots = nullptr, *positions = nullptr;
+    int T = 0, Hq = 0, Hk = 0, page_size = 0, n_pages = 0;
+    int64_t q_row = 0, q_head = 0, k_row = 0, k_head = 0, v_row = 0, v_head = 0;   // strides in elements
+    float eps = 0.f;
+    double log2_base = 0.0;
+};
+cudaError_t launch_qk_norm_rope_append(const AppendArgs& a, int D, loma_dtype dt, cudaStream_t st);
+
+// block tables and slot maps from request lengths (paged_extend.cu)
+struct ExtendArgs {
+    int B, log2_ps, max_pages, max_rows, n_free;
+    const int32_t *cache_lens, *new_lens, *held, *pos0, *free_pages;
+    int32_t *taken, *block_table, *row_start, *page_start, *held_out, *slots, *row_seq, *row_pos;
+};
+void host_paged_extend(const ExtendArgs& a);
+cudaError_t launch_paged_extend(const ExtendArgs& a, cudaStream_t st);
+
+// one new token per sequence over a prefix the whole batch shares and the sequence's own cache (decode_shared.cu).
+// Query row m of kv head h, m = b*g + j, is query head h*g + j of sequence b.
+struct SharedArgs {
+    const void *q = nullptr, *k_new = nullptr, *v_new = nullptr;   // [B, Hq, D], [B, Hkv, D]; k_new, v_new may be NULL
+    const void *k_prefix = nullptr, *v_prefix = nullptr;           // [Hkv, prefix_cap, D], or the pool (prefix_table)
+    void *k_cache = nullptr, *v_cache = nullptr;                   // [B, Hkv, cap, D], or the pool (pg.table)
+    void* o = nullptr;                                             // [B, Hq, D]
+    float* lse = nullptr;                                          // [B, Hq] or NULL
+    const int32_t* cache_lens = nullptr;                           // [B]; negative: no request, nothing is written
+    const int32_t* prefix_table = nullptr;                         // pages of the prefix, in order
+    Paging pg;
+    int B = 0, Hq = 0, Hkv = 0, g = 0;
+    int prefix_len = 0, prefix_cap = 0, cap = 0, max_len = 0;
+    float scale = 0.f;
+    void* ws = nullptr;
+};
+size_t decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int prefix_len, int max_len);
+cudaError_t launch_decode_shared(const SharedArgs& a, int D, loma_dtype dt, bool generic, cudaStream_t st);
+
+// ---- argument checks shared by the entry points (loma_api.cu) ----
+int check_device();
+int make_layout(int n_chunks, int c, int t, int tail_read, unsigned flags, Layout* L);
+int log2_exact(int x);   // log2 of a power of two, or -1
+
 // ---- launch accounting -------------------------------------------------------
 void count_launches(int n);   // called by every launcher with the number of kernels it enqueued
 
@@ -204,5 +262,29 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);   // .x = lo (low half), .y = hi
     return *reinterpret_cast<uint32_t*>(&p);
 }
+
+template <typename T>
+struct Vec16;   // 16 bytes of adjacent elements <-> floats
+template <>
+struct Vec16<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
+        x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+};
+template <>
+struct Vec16<__nv_bfloat16> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
+        x[0] = bf16lo(v.x); x[1] = bf16hi(v.x); x[2] = bf16lo(v.y); x[3] = bf16hi(v.y);
+        x[4] = bf16lo(v.z); x[5] = bf16hi(v.z); x[6] = bf16lo(v.w); x[7] = bf16hi(v.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+        return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    }
+};
 
 }  // namespace loma

@@ -20,30 +20,6 @@
 
 namespace loma {
 
-template <typename T>
-struct Vec16;   // 16 bytes of adjacent elements <-> floats
-template <>
-struct Vec16<float> {
-    static constexpr int N = 4;
-    static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
-        x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
-    }
-    static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
-        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-    }
-};
-template <>
-struct Vec16<__nv_bfloat16> {
-    static constexpr int N = 8;
-    static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
-        x[0] = bf16lo(v.x); x[1] = bf16hi(v.x); x[2] = bf16lo(v.y); x[3] = bf16hi(v.y);
-        x[4] = bf16lo(v.z); x[5] = bf16hi(v.z); x[6] = bf16lo(v.w); x[7] = bf16hi(v.w);
-    }
-    static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
-        return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-    }
-};
-
 constexpr int ROPE_WARPS = 8;
 
 // A lane owns N = 16 / sizeof(T) adjacent features d0.. of the first half and their partners d0 + D/2..
