@@ -786,7 +786,7 @@ LOMA_API int loma_qk_norm_rope_append(const void* q, const void* k_new, const vo
  * in which the first prefix_len entries are the same for every sequence and stored once, with grouped heads.
  * Query head hq of sequence b attends, under one softmax, to the prefix's entries [0, prefix_len) of kv head
  * hq / (Hq / Hkv), to the sequence's own entries [0, cache_lens[b]) and to its new token.  The prefix part is
- * computed for all sequences together (the prefix is read once).
+ * computed for all sequences together (the prefix is read once, on the tensor cores for bf16).
  *
  *   q, o           [device]          [B, Hq, 1, D] contiguous; Hq is a multiple of Hkv
  *   k_new, v_new   [device, in]      [B, Hkv, 1, D] contiguous; both NULL: the token's K/V already sit at entry
@@ -804,6 +804,7 @@ LOMA_API int loma_qk_norm_rope_append(const void* q, const void* k_new, const vo
  * paged: pools [n_pages, Hkv, page_size, D] hold prefix and own entries; prefix_table int32 [prefix_pages] and block_table
  * int32 [B, max_pages] name the pages (clamped to the pool on the device); prefix_len <= prefix_pages * page_size,
  * max_cache_len < max_pages * page_size.  No page may be both a prefix page and a page a new token is written to.
+ * bf16 over a prefix in pages of fewer than 8 rows, and fp32, run the prefix on CUDA cores.
  * Errors: INVALID_ARG (Hq not a multiple of Hkv, ...), UNSUPPORTED, ALIGNMENT, CAPACITY, WORKSPACE, CUDA.  B*Hq == 0 is a no-op.
  * ------------------------------------------------------------------------- */
 LOMA_API int loma_decode_attn_shared(const void* q, const void* k_new, const void* v_new, const void* k_prefix,

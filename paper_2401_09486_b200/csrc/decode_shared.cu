@@ -5,7 +5,8 @@
 // with weights 2^(lse_i - max), so the parts are computed where they are cheap and joined at the end:
 //
 //   prefix   all B g query rows of a kv head against the same K and V: a matrix product, 128 rows at a time, that reads
-//            the prefix once for the batch instead of once per sequence (shared_prefix_simt_kernel)
+//            the prefix once for the batch instead of once per sequence (bf16: tcgen05, decode_shared_tc.cu; fp32 and
+//            page sizes below 8: shared_prefix_simt_kernel)
 //   own      one query row per head of a group against rows nobody else reads: a stream bound by HBM.  bf16:
 //            shared_own_mma_kernel, where the g heads of a kv head are rows of a warp-level m16n8k16 product, so a K or
 //            V row is loaded once for all of them; fp32: shared_own_stream_kernel on CUDA cores
@@ -41,7 +42,7 @@ __device__ __forceinline__ int64_t prefix_row(const SharedArgs& a, int h, int j)
 // ------------------------------------------------------------------ own cache, bf16
 // D += A B, m16n8k16, rows 8..15 of A all zero (their results are not kept)
 __device__ __forceinline__ void mma_lo(float (&d)[2], uint32_t a0, uint32_t a2, uint32_t b0, uint32_t b1) {
-    float x, y;
+    [[maybe_unused]] float x, y;
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%10,%10};"
         : "+f"(d[0]), "+f"(d[1]), "=f"(x), "=f"(y)
         : "r"(a0), "r"(0u), "r"(a2), "r"(0u), "r"(b0), "r"(b1), "f"(0.f));
@@ -143,7 +144,7 @@ shared_own_mma_kernel(const SharedArgs a, const SharedPlan p) {
         }
         const int next = key0 + OWN_WARPS * 16;
         if (next < end) load_k(next);   // in flight during the softmax and P V of this block
-        uint32_t pf[R][2];              // P rounded to bf16: off by 2^-9 of its value at most, the sums stay in fp32
+        uint32_t pf[R][2];              // P rounded to bf16: off by 2^-8 of its value at most; the sums stay in fp32
 #pragma unroll
         for (int t = 0; t < R; ++t) {
             float mx = -INFINITY;
@@ -559,7 +560,9 @@ static cudaError_t shared_t(const SharedArgs& a, bool generic, cudaStream_t st) 
     const SharedPlan p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len);
     cudaError_t e = cudaSuccess;
     if (p.p_splits > 0) {
-        e = prefix_simt<T, D>(a, p, st);
+        e = cudaErrorNotSupported;
+        if (sizeof(T) == 2 && !generic) e = launch_shared_prefix_tc(a, p, D, st);
+        if (e == cudaErrorNotSupported) e = prefix_simt<T, D>(a, p, st);
         if (e != cudaSuccess) return e;
     }
     bool done = false;

@@ -1,0 +1,358 @@
+// The prefix part of the shared-prefix decode step on the 5th-generation tensor cores (bf16).
+//
+// The B g query rows of a kv head all see the same prefix keys, so their scores and outputs are two matrix products with
+// an online softmax between them: S = Q K^T, O = sum over keys of P V.  No mask but the end of the prefix.  A CTA takes 128
+// query rows (one row per TMEM lane) and a range of keys; ranges are joined by the merge kernel.  With few rows the kernel
+// is bound by HBM (the prefix is read once per 128 rows), with many by the chain tensor pipe -> softmax -> tensor pipe, so
+// two CTAs share an SM and fill each other's waits: each has 256 of the 512 TMEM columns and half of the shared memory.
+//
+//   warps 0-3  softmax: thread = query row.  64 keys (an "event") at a time: scores out of TMEM, row maximum, probabilities
+//              2^(s scale - ref) as bf16 back over the scores.  The reference maximum only moves, and the accumulator in TMEM
+//              is only rescaled, when a row's maximum has grown by more than 2^8, which bounds a probability by 2^8
+//   warp 4     TMA: K and V in tiles of 64 keys through one ring of NS slots, in the order in which they are used
+//              K0 K1 V0 K2 V1 K3 V2 ...
+//   warp 5     MMA: S(e+2) is issued right after P V(e) into the score buffer that event e has left, so the tensor pipe works
+//              on one buffer while the warpgroup works on the other
+// P is rounded to bf16 for the second product (off by 2^-8 of its value at most); row sums are taken in fp32 before the
+// rounding, scores, maxima, sums and outputs are fp32 throughout.
+#include "decode_shared.cuh"
+#include "tcgen05_common.cuh"
+
+namespace loma {
+
+struct SharedMaps {
+    CUtensorMap k, v;
+};
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+                 : "memory");
+}
+
+constexpr int SHT_THREADS = 192, SHT_KEYS = 64, SHT_TMEM = 256;
+
+template <int D>
+struct ShtSmem {
+    static constexpr int PANELS = D / 64;
+    static constexpr int Q_PANEL = SHP_ROWS * 128, KV_PANEL = SHT_KEYS * 128;      // 64 features of every row
+    static constexpr int SLOT = PANELS * KV_PANEL;
+    static constexpr int NS = D == 128 ? 5 : 10;                                   // ring slots: 80 KB either way
+    static constexpr int RING = PANELS * Q_PANEL;
+    // 1 KB more than the tiles: they start on a 1 KB boundary, and the gap before or behind them holds the barriers.  Twice
+    // this and the 1 KB the system takes per CTA is exactly an SM's 228 KB.
+    static constexpr int TILES = RING + NS * SLOT, TOTAL = TILES + 1024;
+};
+
+struct ShtShared {   // in the gap (512 bytes at least)
+    uint64_t full[10], empty[10], sf[2], pf[2], of[2];
+    uint32_t tmem;
+    int abort_flag;
+};
+
+struct ShtParams {
+    const __nv_bfloat16* q;
+    const int32_t* prefix_table;   // NULL: contiguous
+    float *o, *lse;                // partial results (see SharedPlan)
+    int* status;
+    int B, Hq, Hkv, g, m_tiles, prefix_len, p_len, log2_ps, n_pages, box_rows;
+    float scale_log2;
+};
+
+template <int D>
+__global__ void __launch_bounds__(SHT_THREADS, 2)
+shared_prefix_tc_kernel(const __grid_constant__ SharedMaps maps, const ShtParams p) {
+    using SM = ShtSmem<D>;
+    constexpr int PANELS = SM::PANELS, NS = SM::NS;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u, before = base - raw;
+    uint8_t* tiles = smem_raw + before;
+    ShtShared* sh = reinterpret_cast<ShtShared*>(before >= 512 ? smem_raw + ((16u - (raw & 15u)) & 15u) : tiles + SM::TILES);
+    static_assert(sizeof(ShtShared) <= 496, "the barriers fit in the gap");
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    auto bar = [&](uint64_t* b) { return smem_u32(b); };
+
+    // m-tiles of one kv head and key range are neighbours: they read the same K and V at about the same time
+    int x = blockIdx.x;
+    const int mt = x % p.m_tiles; x /= p.m_tiles;
+    const int h = x % p.Hkv, split = x / p.Hkv;
+    const int begin = split * p.p_len, end = min(p.prefix_len, begin + p.p_len);
+    const int E = (end - begin + SHT_KEYS - 1) / SHT_KEYS;   // events: at least one
+    volatile int* abortp = &sh->abort_flag;
+
+    if (threadIdx.x == 0) {
+        sh->abort_flag = 0;
+        for (int i = 0; i < NS; ++i) { mbar_init(bar(&sh->full[i]), 1); mbar_init(bar(&sh->empty[i]), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar(&sh->sf[i]), 1); mbar_init(bar(&sh->pf[i]), 128); mbar_init(bar(&sh->of[i]), 1); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem)), "r"(SHT_TMEM) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    // query rows into the swizzled panels: row m of the kv head is head h g + m mod g of sequence m div g; rows past the last are zero
+    for (int i = threadIdx.x; i < SHP_ROWS * (D / 8); i += SHT_THREADS) {
+        const int r = i / (D / 8), c = i % (D / 8), m = mt * SHP_ROWS + r;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (m < p.B * p.g) {
+            const int b = m / p.g;
+            v = __ldg(reinterpret_cast<const uint4*>(p.q + ((int64_t)b * p.Hq + h * p.g + (m - b * p.g)) * D) + c);
+        }
+        *reinterpret_cast<uint4*>(tiles + (c >> 3) * SM::Q_PANEL + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
+    }
+    fence_async_smem();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh->tmem;   // score buffers at +0 and +64, output accumulator at +128
+
+    if (warp == 4) {
+        // ------------------------------------------------------------ TMA producer: item n = 0 .. 2E-1 into slot n mod NS
+        bool ok = true;
+        const int pages_per = p.prefix_table ? SHT_KEYS / p.box_rows : 1;   // boxes per tile and panel
+        int e_k = 0, e_v = 0;
+        for (int n = 0; n < 2 * E; ++n) {
+            const bool is_k = e_k < E && e_k < e_v + 2;
+            const int e = is_k ? e_k++ : e_v++;
+            const int slot = n % NS;
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(&sh->empty[slot]), ((n / NS) & 1) ^ 1, abortp, p.status));
+            if (!ok) break;
+            const uint32_t full = bar(&sh->full[slot]), dst = base + SM::RING + slot * SM::SLOT;
+            if (lane == 0) mbar_expect_tx(full, pages_per * p.box_rows * 128 * PANELS);
+            __syncwarp();
+            const CUtensorMap* map = is_k ? &maps.k : &maps.v;
+            if (lane < pages_per * PANELS) {
+                const int pn = lane % PANELS, part = lane / PANELS;
+                int row = begin + e * SHT_KEYS + part * p.box_rows, z = h;
+                if (p.prefix_table) {
+                    // past the last page of the prefix the last entry's page is loaded again (its rows are masked)
+                    const int at = min(row, p.prefix_len - 1);
+                    const int page = min(max(__ldg(p.prefix_table + (at >> p.log2_ps)), 0), p.n_pages - 1);
+                    z = page * p.Hkv + h;
+                    row &= (1 << p.log2_ps) - 1;
+                }
+                tma_load_3d(dst + pn * SM::KV_PANEL + part * p.box_rows * 128, map, full, pn * 64, row, z);
+            }
+        }
+        if (!ok) {
+            // leaving early: give copies already in flight a bounded time to land in this CTA's shared memory
+            const long long t0 = clock64();
+            while (clock64() - t0 < 2000000ll) {}
+        }
+    } else if (warp == 5) {
+        // ------------------------------------------------------------ MMA issuer: uniform control flow, one elected lane issues
+        // instruction descriptors: fp32 accumulate, bf16 x bf16, M = 128; N = 64 keys, or N = D with V as the MN-major operand
+        constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
+        constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
+        const uint64_t qd = smem_desc(base, 16, 1024);
+        int n = 0;   // items used
+        bool ok = true;
+        auto take = [&]() {
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(&sh->full[n % NS]), (n / NS) & 1, abortp, p.status));
+            return n++ % NS;
+        };
+        auto scores = [&](int e) {
+            const int slot = take();
+            if (!ok) return;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t kd = smem_desc(base + SM::RING + slot * SM::SLOT, 16, 1024);
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk)
+                    mma_ss(tmem + (e & 1) * 64, qd + (uint64_t)(((kk >> 2) * SM::Q_PANEL + (kk & 3) * 32) >> 4),
+                           kd + (uint64_t)(((kk >> 2) * SM::KV_PANEL + (kk & 3) * 32) >> 4), IDESC_S, kk > 0);
+                tc_commit(bar(&sh->empty[slot]));
+                tc_commit(bar(&sh->sf[e & 1]));
+            }
+            __syncwarp();
+        };
+        scores(0);
+        if (ok && E > 1) scores(1);
+        for (int e = 0; ok && e < E; ++e) {
+            const int b = e & 1;
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(&sh->pf[b]), (e >> 1) & 1, abortp, p.status));
+            if (!ok) break;
+            const int slot = take();
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t vd = smem_desc(base + SM::RING + slot * SM::SLOT, SM::KV_PANEL, 1024);
+#pragma unroll
+                for (int k4 = 0; k4 < 4; ++k4)
+                    mma_ts(tmem + 128, tmem + b * 64 + k4 * 8, vd + (uint64_t)((k4 * 2048) >> 4), IDESC_PV, e > 0 || k4 > 0);
+                tc_commit(bar(&sh->empty[slot]));
+                tc_commit(bar(&sh->of[b]));   // last: whoever leaves on it leaves no arrival behind
+            }
+            __syncwarp();
+            if (e + 2 < E) scores(e + 2);
+        }
+    } else {
+        // ------------------------------------------------------------ softmax and partial results
+        const int rr = threadIdx.x;
+        const uint32_t lane_addr = tmem + ((uint32_t)(warp * 32) << 16), o_addr = lane_addr + 128;
+        float m_used = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int e = 0; e < E; ++e) {
+            const int b = e & 1;
+            const uint32_t s_addr = lane_addr + b * 64;
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(&sh->sf[b]), (e >> 1) & 1, abortp, p.status));
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t s[64];
+            tmem_ld32(s_addr, s);
+            tmem_ld32(s_addr + 32, s + 32);
+            tmem_wait_ld();
+            const int valid = end - (begin + e * SHT_KEYS);
+            if (valid < SHT_KEYS) {
+                // the last tile of the prefix: keys past its end are blocked, and V rows there become zero (a page or an
+                // unused row may hold anything, and 0 x NaN is not 0)
+#pragma unroll
+                for (int i = 0; i < 64; ++i)
+                    if (i >= valid) s[i] = 0xff800000u;
+                const int n = 2 * E - 1, slot = n % NS;   // V of the last event is the last item
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(&sh->full[slot]), (n / NS) & 1, abortp, p.status));
+                if (!ok) break;
+                uint8_t* v = tiles + SM::RING + slot * SM::SLOT;
+                for (int i = rr; i < (SHT_KEYS - valid) * 8 * PANELS; i += 128) {
+                    const int pn = i / ((SHT_KEYS - valid) * 8), rest = i - pn * (SHT_KEYS - valid) * 8;
+                    *reinterpret_cast<uint4*>(v + pn * SM::KV_PANEL + valid * 128 + rest * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_async_smem();
+            }
+            float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 64; i += 8) {
+                mx0 = max3(mx0, __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+                mx1 = max3(mx1, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3]));
+                mx2 = max3(mx2, __uint_as_float(s[i + 4]), __uint_as_float(s[i + 5]));
+                mx3 = max3(mx3, __uint_as_float(s[i + 6]), __uint_as_float(s[i + 7]));
+            }
+            const float mrow = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * p.scale_log2;
+            const bool need = mrow > m_used + 8.f;
+            if (e > 0 && __any_sync(0xffffffffu, need)) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(&sh->of[b ^ 1]), ((e - 1) >> 1) & 1, abortp, p.status));
+                if (!ok) break;
+                tc_fence_after();
+                const float alpha = need ? fast_ex2(m_used - mrow) : 1.f;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t r[32];
+                    tmem_ld32(o_addr + c * 32, r);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+                    tmem_st32(o_addr + c * 32, r);
+                }
+                l *= alpha;
+            }
+            if (need) m_used = mrow;
+            const float neg_ref = m_used == -INFINITY ? 0.f : -m_used;
+            const uint64_t sc2 = pack2(p.scale_log2, p.scale_log2), nr2 = pack2(neg_ref, neg_ref);
+            uint64_t lsa = pack2(0.f, 0.f), lsb = lsa;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t pk[16];
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    float x0, x1, x2, x3;
+                    unpack2(fma2(pack2(__uint_as_float(s[c * 32 + i]), __uint_as_float(s[c * 32 + i + 1])), sc2, nr2), x0, x1);
+                    unpack2(fma2(pack2(__uint_as_float(s[c * 32 + i + 2]), __uint_as_float(s[c * 32 + i + 3])), sc2, nr2), x2, x3);
+                    const float p0 = fast_ex2(x0), p1 = fast_ex2(x1), p2 = fast_ex2(x2), p3 = fast_ex2(x3);
+                    lsa = add2(lsa, pack2(p0, p1));
+                    lsb = add2(lsb, pack2(p2, p3));
+                    pk[i >> 1] = pack_bf16(p0, p1);
+                    pk[(i >> 1) + 1] = pack_bf16(p2, p3);
+                }
+                tmem_st16(s_addr + c * 16, pk);
+            }
+            {
+                float a0, a1, b0, b1;
+                unpack2(lsa, a0, a1);
+                unpack2(lsb, b0, b1);
+                l += (a0 + a1) + (b0 + b1);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(bar(&sh->pf[b]));
+        }
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(&sh->of[(E - 1) & 1]), ((E - 1) >> 1) & 1, abortp, p.status));
+        if (ok) {
+            tc_fence_after();
+            const float inv = 1.f / l;
+            const int64_t tile = ((int64_t)split * p.Hkv + h) * p.m_tiles + mt;
+            float4* out = reinterpret_cast<float4*>(p.o + tile * SHP_ROWS * D) + rr;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t r[32];
+                tmem_ld32(o_addr + c * 32, r);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    out[(c * 8 + i) * SHP_ROWS] = make_float4(__uint_as_float(r[4 * i]) * inv, __uint_as_float(r[4 * i + 1]) * inv,
+                                                             __uint_as_float(r[4 * i + 2]) * inv, __uint_as_float(r[4 * i + 3]) * inv);
+            }
+            p.lse[tile * SHP_ROWS + rr] = m_used + log2f(l);
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 5) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(SHT_TMEM) : "memory");
+    }
+}
+
+// ------------------------------------------------------------------ host side
+// (features, rows, heads or page-heads) of the prefix; box: 64 features of box_rows rows.
+static bool encode_prefix(CUtensorMap* map, const void* p, int D, int64_t rows, int64_t row_stride_outer, int64_t outer, int box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)rows, (cuuint64_t)outer};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)row_stride_outer * D * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, es[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+static cudaError_t prefix_tc_t(const SharedArgs& a, const SharedPlan& p, cudaStream_t st) {
+    ShtParams t;
+    SharedMaps maps;
+    const int ps = 1 << a.pg.log2_ps;
+    int64_t rows, step, outer;
+    if (a.prefix_table) {
+        if (ps < 8) return cudaErrorNotSupported;   // a box would start inside an 8-row swizzle group
+        t.box_rows = std::min(ps, SHT_KEYS);
+        rows = ps; step = ps; outer = (int64_t)a.pg.n_pages * a.Hkv;
+    } else {
+        t.box_rows = std::min(a.prefix_len, SHT_KEYS);
+        rows = a.prefix_len; step = a.prefix_cap; outer = a.Hkv;
+    }
+    if (outer > INT_MAX || !encode_prefix(&maps.k, a.k_prefix, D, rows, step, outer, t.box_rows) ||
+        !encode_prefix(&maps.v, a.v_prefix, D, rows, step, outer, t.box_rows))
+        return cudaErrorNotSupported;
+    float* ws = static_cast<float*>(a.ws);
+    t.q = static_cast<const __nv_bfloat16*>(a.q);
+    t.prefix_table = a.prefix_table;
+    t.o = ws + p.p_o;
+    t.lse = ws + p.p_lse;
+    t.status = device_status_word();
+    if (!t.status) return cudaErrorUnknown;
+    t.B = a.B; t.Hq = a.Hq; t.Hkv = a.Hkv; t.g = a.g; t.m_tiles = p.m_tiles; t.prefix_len = a.prefix_len; t.p_len = p.p_len;
+    t.log2_ps = a.pg.log2_ps; t.n_pages = a.pg.n_pages;
+    t.scale_log2 = a.scale * 1.4426950408889634f;
+    const int64_t ctas = (int64_t)p.p_splits * a.Hkv * p.m_tiles;
+    if (ctas > INT_MAX) return cudaErrorNotSupported;
+    constexpr int smem = ShtSmem<D>::TOTAL;
+    cudaError_t e = cudaFuncSetAttribute(shared_prefix_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    shared_prefix_tc_kernel<D><<<(unsigned)ctas, SHT_THREADS, smem, st>>>(maps, t);
+    count_launches(1);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_shared_prefix_tc(const SharedArgs& a, const SharedPlan& p, int D, cudaStream_t st) {
+    return D == 64 ? prefix_tc_t<64>(a, p, st) : prefix_tc_t<128>(a, p, st);
+}
+
+}  // namespace loma
