@@ -72,6 +72,7 @@ shared_prefix_tc_kernel(const __grid_constant__ SharedMaps maps, const ShtParams
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     auto bar = [&](uint64_t* b) { return smem_u32(b); };
 
+    let_next_start();
     // m-tiles of one kv head and key range are neighbours: they read the same K and V at about the same time
     int x = blockIdx.x;
     const int mt = x % p.m_tiles; x /= p.m_tiles;
@@ -344,11 +345,7 @@ static cudaError_t prefix_tc_t(const SharedArgs& a, const SharedPlan& p, cudaStr
     const int64_t ctas = (int64_t)p.p_splits * a.Hkv * p.m_tiles;
     if (ctas > INT_MAX) return cudaErrorNotSupported;
     constexpr int smem = ShtSmem<D>::TOTAL;
-    cudaError_t e = cudaFuncSetAttribute(shared_prefix_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-    shared_prefix_tc_kernel<D><<<(unsigned)ctas, SHT_THREADS, smem, st>>>(maps, t);
-    count_launches(1);
-    return cudaGetLastError();
+    return launch_behind(shared_prefix_tc_kernel<D>, dim3((unsigned)ctas), SHT_THREADS, smem, st, false, maps, t);
 }
 
 cudaError_t launch_shared_prefix_tc(const SharedArgs& a, const SharedPlan& p, int D, cudaStream_t st) {
