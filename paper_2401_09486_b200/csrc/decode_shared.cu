@@ -48,10 +48,10 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
     const SeqBlocks sb{a};
     const int per = sb.scan<OWN_WARPS>(scan, wsum, blockIdx.x == 0 ? reinterpret_cast<int64_t*>(ws + p.cum) : nullptr);
     const int64_t total = scan[(a.B + per - 1) / per] * a.Hkv * p.g_tiles;
-    const int64_t W = min((int64_t)p.workers, total), w = (int64_t)warp * gridDim.x + blockIdx.x;
+    const int64_t W = own_workers(total, p.workers), w = (int64_t)warp * gridDim.x + blockIdx.x;
     if (w < W) {
-        int64_t t = own_first(w, total, W);
-        const int64_t t_end = own_first(w + 1, total, W);
+        int64_t t = first_block(w, total, W);
+        const int64_t t_end = first_block(w + 1, total, W);
         SeqBlocks::Cursor c = sb.find(t, scan, per);
         const float scale_log2 = a.scale * 1.4426950408889634f;
         float q[G][N], acc[G][N], m[G], l[G];
@@ -159,7 +159,7 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
 // ------------------------------------------------------------------ prefix on CUDA cores (fp32, small pages, second opinion)
 // 32 query rows against 64 keys at a time, all in fp32 in shared memory: scores with 2 x 4 and outputs with 4 x (D / 32)
 // values per thread in registers.  Query row m of kv head h is head h g + m mod g of sequence m / g.
-constexpr int SIMT_R = 32, SIMT_K = 64, SIMT_THREADS = 256;
+constexpr int SIMT_R = 32, SIMT_K = SHP_KEYS, SIMT_THREADS = 256;
 
 template <typename T, int D>
 struct SimtSmem {
@@ -176,170 +176,201 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
     extern __shared__ __align__(16) float sm[];
     let_next_start();
     const int tid = threadIdx.x, rows = a.B * a.g;
-    const int h = blockIdx.y, split = blockIdx.z, row0 = blockIdx.x * SIMT_R;
-    const int begin = split * p.p_len, end = min(a.prefix_len, begin + p.p_len);
     const float scale_log2 = a.scale * 1.4426950408889634f;
-    for (int idx = tid; idx < SIMT_R * LPK; idx += SIMT_THREADS) {
-        const int r = idx / LPK, c = idx - r * LPK, m = min(row0 + r, rows - 1);
-        const T* qp = static_cast<const T*>(a.q) + ((int64_t)(m / a.g) * a.Hq + h * a.g + m % a.g) * D;
-        float f[N];
-        V::unpack(__ldg(reinterpret_cast<const uint4*>(qp) + c), f);
-#pragma unroll
-        for (int e = 0; e < N; ++e) sm[SM::Q + r * (D + 4) + c * N + e] = f[e] * scale_log2;
-    }
-    if (tid < SIMT_R) { sm[SM::ML + tid] = -INFINITY; sm[SM::ML + SIMT_R + tid] = 0.f; }
-    float acc[4][DC];
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int c = 0; c < DC; ++c) acc[u][c] = 0.f;
+    const int worker = blockIdx.x / p.m_tiles, mt = blockIdx.x - worker * p.m_tiles;
+    const int64_t blocks = (int64_t)a.Hkv * p.p_blocks;
+    int64_t t = first_block(worker, blocks, p.p_workers);
+    const int64_t t_end = first_block(worker + 1, blocks, p.p_workers);
+    const int r_in = blockIdx.y * SIMT_R, row0 = mt * SHP_ROWS + r_in;   // 32 rows of the tile per blockIdx.y
+    if (row0 >= rows) return;
     const int sr = (tid >> 4) * 2, sk = tid & 15;         // scores: rows sr, sr+1; keys sk + 16 u
     const int orow = (tid >> 5) * 4, oc = tid & 31;       // outputs: rows orow .. +3 (a warp's own); features oc*DC ..
-    for (int k0 = begin; k0 < end; k0 += SIMT_K) {
+    while (t < t_end) {                                   // segments of the CTA's share
+        const int h = (int)(t / p.p_blocks), blk0 = (int)(t - (int64_t)h * p.p_blocks);
+        const int blk1 = (int)min((int64_t)p.p_blocks, blk0 + (t_end - t));
+        t += blk1 - blk0;
+        const int begin = blk0 * SHP_KEYS, end = min(a.prefix_len, blk1 * SHP_KEYS);
+        const int64_t seg = (int64_t)(worker + h) * p.m_tiles + mt;
         __syncthreads();
-        for (int idx = tid; idx < SIMT_K * LPK; idx += SIMT_THREADS) {
-            const int r = idx / LPK, c = idx - r * LPK;
-            const int64_t row = prefix_row(a, h, min(k0 + r, a.prefix_len - 1)) * D;   // keys past the end repeat the last one
+        for (int idx = tid; idx < SIMT_R * LPK; idx += SIMT_THREADS) {
+            const int r = idx / LPK, c = idx - r * LPK, m = min(row0 + r, rows - 1);
+            const T* qp = static_cast<const T*>(a.q) + ((int64_t)(m / a.g) * a.Hq + h * a.g + m % a.g) * D;
             float f[N];
-            V::unpack(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.k_prefix) + row) + c), f);
+            V::unpack(__ldg(reinterpret_cast<const uint4*>(qp) + c), f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) sm[SM::K + r * (D + 4) + c * N + e] = f[e];
-            V::unpack(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.v_prefix) + row) + c), f);
-#pragma unroll
-            for (int e = 0; e < N; ++e) sm[SM::V + r * D + c * N + e] = f[e];
+            for (int e = 0; e < N; ++e) sm[SM::Q + r * (D + 4) + c * N + e] = f[e] * scale_log2;
         }
-        __syncthreads();
-        float s[2][4] = {};
+        if (tid < SIMT_R) { sm[SM::ML + tid] = -INFINITY; sm[SM::ML + SIMT_R + tid] = 0.f; }
+        float acc[4][DC];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int c = 0; c < DC; ++c) acc[u][c] = 0.f;
+        for (int k0 = begin; k0 < end; k0 += SIMT_K) {
+            __syncthreads();
+            for (int idx = tid; idx < SIMT_K * LPK; idx += SIMT_THREADS) {
+                const int r = idx / LPK, c = idx - r * LPK;
+                const int64_t row = prefix_row(a, h, min(k0 + r, a.prefix_len - 1)) * D;   // keys past the end repeat the last one
+                float f[N];
+                V::unpack(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.k_prefix) + row) + c), f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) sm[SM::K + r * (D + 4) + c * N + e] = f[e];
+                V::unpack(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.v_prefix) + row) + c), f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) sm[SM::V + r * D + c * N + e] = f[e];
+            }
+            __syncthreads();
+            float s[2][4] = {};
 #pragma unroll 4
-        for (int d = 0; d < D; d += 4) {
-            float4 qv[2], kv[4];
+            for (int d = 0; d < D; d += 4) {
+                float4 qv[2], kv[4];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) qv[u] = *reinterpret_cast<const float4*>(&sm[SM::Q + (sr + u) * (D + 4) + d]);
+                for (int u = 0; u < 2; ++u) qv[u] = *reinterpret_cast<const float4*>(&sm[SM::Q + (sr + u) * (D + 4) + d]);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) kv[u] = *reinterpret_cast<const float4*>(&sm[SM::K + (sk + 16 * u) * (D + 4) + d]);
+                for (int u = 0; u < 4; ++u) kv[u] = *reinterpret_cast<const float4*>(&sm[SM::K + (sk + 16 * u) * (D + 4) + d]);
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    s[u][w] = fmaf(qv[u].x, kv[w].x, fmaf(qv[u].y, kv[w].y, fmaf(qv[u].z, kv[w].z, fmaf(qv[u].w, kv[w].w, s[u][w]))));
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {   // 16 lanes share a row
-            float mx = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                if (k0 + sk + 16 * w >= end) s[u][w] = -INFINITY;
-                mx = fmaxf(mx, s[u][w]);
+                    for (int w = 0; w < 4; ++w)
+                        s[u][w] = fmaf(qv[u].x, kv[w].x, fmaf(qv[u].y, kv[w].y, fmaf(qv[u].z, kv[w].z, fmaf(qv[u].w, kv[w].w, s[u][w]))));
             }
 #pragma unroll
-            for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            const float m_old = sm[SM::ML + sr + u], m_new = fmaxf(m_old, mx), ref = m_new == -INFINITY ? 0.f : m_new;
-            float sum = 0.f;
+            for (int u = 0; u < 2; ++u) {   // 16 lanes share a row
+                float mx = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float e = exp2f(s[u][w] - ref);
-                sum += e;
-                sm[SM::S + (sr + u) * (SIMT_K + 4) + sk + 16 * w] = e;
+                for (int w = 0; w < 4; ++w) {
+                    if (k0 + sk + 16 * w >= end) s[u][w] = -INFINITY;
+                    mx = fmaxf(mx, s[u][w]);
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                const float m_old = sm[SM::ML + sr + u], m_new = fmaxf(m_old, mx), ref = m_new == -INFINITY ? 0.f : m_new;
+                float sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float e = exp2f(s[u][w] - ref);
+                    sum += e;
+                    sm[SM::S + (sr + u) * (SIMT_K + 4) + sk + 16 * w] = e;
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                __syncwarp();
+                if ((tid & 15) == 0) {
+                    const float alpha = exp2f(m_old - ref);
+                    sm[SM::ML + sr + u] = m_new;
+                    sm[SM::ML + SIMT_R + sr + u] = sm[SM::ML + SIMT_R + sr + u] * alpha + sum;
+                    sm[SM::ML + 2 * SIMT_R + sr + u] = alpha;
+                }
             }
+            __syncthreads();
 #pragma unroll
-            for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            __syncwarp();
-            if ((tid & 15) == 0) {
-                const float alpha = exp2f(m_old - ref);
-                sm[SM::ML + sr + u] = m_new;
-                sm[SM::ML + SIMT_R + sr + u] = sm[SM::ML + SIMT_R + sr + u] * alpha + sum;
-                sm[SM::ML + 2 * SIMT_R + sr + u] = alpha;
+            for (int u = 0; u < 4; ++u) {
+                const float alpha = sm[SM::ML + 2 * SIMT_R + orow + u];
+#pragma unroll
+                for (int c = 0; c < DC; ++c) acc[u][c] *= alpha;
             }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const float alpha = sm[SM::ML + 2 * SIMT_R + orow + u];
-#pragma unroll
-            for (int c = 0; c < DC; ++c) acc[u][c] *= alpha;
-        }
 #pragma unroll 4
-        for (int k = 0; k < SIMT_K; k += 4) {
-            float4 pv[4];
+            for (int k = 0; k < SIMT_K; k += 4) {
+                float4 pv[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) pv[u] = *reinterpret_cast<const float4*>(&sm[SM::S + (orow + u) * (SIMT_K + 4) + k]);
+                for (int u = 0; u < 4; ++u) pv[u] = *reinterpret_cast<const float4*>(&sm[SM::S + (orow + u) * (SIMT_K + 4) + k]);
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-                float vv[DC];
+                for (int kk = 0; kk < 4; ++kk) {
+                    float vv[DC];
 #pragma unroll
-                for (int c = 0; c < DC; ++c) vv[c] = sm[SM::V + (k + kk) * D + oc * DC + c];
+                    for (int c = 0; c < DC; ++c) vv[c] = sm[SM::V + (k + kk) * D + oc * DC + c];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float pr = kk == 0 ? pv[u].x : kk == 1 ? pv[u].y : kk == 2 ? pv[u].z : pv[u].w;
+                    for (int u = 0; u < 4; ++u) {
+                        const float pr = kk == 0 ? pv[u].x : kk == 1 ? pv[u].y : kk == 2 ? pv[u].z : pv[u].w;
 #pragma unroll
-                    for (int c = 0; c < DC; ++c) acc[u][c] = fmaf(pr, vv[c], acc[u][c]);
+                        for (int c = 0; c < DC; ++c) acc[u][c] = fmaf(pr, vv[c], acc[u][c]);
+                    }
                 }
             }
         }
-    }
-    __syncthreads();
-    float* ws = static_cast<float*>(a.ws);
-    const int mt = row0 / SHP_ROWS, r_in = row0 % SHP_ROWS;
-    const int64_t tile = ((int64_t)split * a.Hkv + h) * p.m_tiles + mt;
+        __syncthreads();
+        float* ws = static_cast<float*>(a.ws);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const float inv = 1.f / sm[SM::ML + SIMT_R + orow + u];
+        for (int u = 0; u < 4; ++u) {
+            const float inv = 1.f / sm[SM::ML + SIMT_R + orow + u];
 #pragma unroll
-        for (int c = 0; c < DC; ++c) {
-            const int d = oc * DC + c;
-            ws[p.p_o + tile * SHP_ROWS * D + ((int64_t)(d >> 2) * SHP_ROWS + r_in + orow + u) * 4 + (d & 3)] = acc[u][c] * inv;
+            for (int c = 0; c < DC; ++c) {
+                const int d = oc * DC + c;
+                ws[p.p_o + seg * SHP_ROWS * D + ((int64_t)(d >> 2) * SHP_ROWS + r_in + orow + u) * 4 + (d & 3)] = acc[u][c] * inv;
+            }
         }
+        if (tid < SIMT_R) ws[p.p_lse + seg * SHP_ROWS + r_in + tid] = sm[SM::ML + tid] + log2f(sm[SM::ML + SIMT_R + tid]);
     }
-    if (tid < SIMT_R) ws[p.p_lse + tile * SHP_ROWS + r_in + tid] = sm[SM::ML + tid] + log2f(sm[SM::ML + SIMT_R + tid]);
 }
 
 // ------------------------------------------------------------------ merge
-// CTA: 32 query rows of one kv head (lanes) x 8 groups of 4 features (warps).
-constexpr int MERGE_THREADS = 256;
+// CTA: 32 query rows of one kv head (lanes) x 8 groups of 4 features (warps).  The time is that of its chain of dependent
+// loads, so partial results are taken MERGE_AT_ONCE at a time, values and log2-sum-exps together, under a running maximum.
+constexpr int MERGE_THREADS = 256, MERGE_AT_ONCE = 8;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(MERGE_THREADS)
 shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
     const int lane = threadIdx.x & 31, c4 = blockIdx.y * 8 + (threadIdx.x >> 5);
-    // before any thread may leave: the kernel after this one counts on all three having finished
-    wait_for_previous();
-    const int h = blockIdx.z, row = blockIdx.x * 32 + lane;
-    if (row >= a.B * a.g) return;
+    const int h = blockIdx.z, row = min((int)(blockIdx.x * 32 + lane), a.B * a.g - 1);   // rows past the last repeat it
     const int b = row / a.g, j = row - b * a.g;
-    if (__ldg(a.cache_lens + b) < 0) return;
+    const int len = __ldg(a.cache_lens + b);
     const float* ws = static_cast<const float*>(a.ws);
     const int mt = row / SHP_ROWS, r = row - mt * SHP_ROWS;
-    const int64_t tile0 = (int64_t)h * p.m_tiles + mt, tile_step = (int64_t)a.Hkv * p.m_tiles;
+    // the prefix segments of this tile
+    const int64_t p_all = (int64_t)a.Hkv * p.p_blocks;
+    int64_t p_first = 0;
+    int n_prefix = 0;
+    if (p.p_blocks > 0) {
+        const int64_t w0 = block_worker((int64_t)h * p.p_blocks, p_all, p.p_workers);
+        n_prefix = (int)(block_worker((int64_t)(h + 1) * p.p_blocks - 1, p_all, p.p_workers) - w0) + 1;
+        p_first = (w0 + h) * p.m_tiles + mt;
+    }
     const int gt = j / p.g_rows, x = j - gt * p.g_rows;
     const int64_t hh = (int64_t)h * p.g_tiles + gt;
+    // before any thread may leave: the kernel after this one counts on all three having finished
+    wait_for_previous();
     const int64_t* cum = reinterpret_cast<const int64_t*>(ws + p.cum);
-    const int64_t per_head = cum[a.B], blocks = per_head * a.Hkv * p.g_tiles, W = min((int64_t)p.workers, blocks);
-    const int64_t t0 = hh * per_head + cum[b], t1 = hh * per_head + cum[b + 1];   // the sequence's blocks: at least one
-    const int64_t w0 = own_worker(t0, blocks, W), first = w0 + hh * a.B + b;           // its segments are consecutive
-    const int n_own = (int)(own_worker(t1 - 1, blocks, W) - w0) + 1;
-    const float* own_lse = ws + p.own_lse + first * p.g_rows + x;
-    const float* own_o = ws + p.own_o + (first * p.g_rows + x) * D + c4 * 4;
-    float M = -INFINITY;
-#pragma unroll 4
-    for (int s = 0; s < p.p_splits; ++s) M = fmaxf(M, ws[p.p_lse + (tile0 + s * tile_step) * SHP_ROWS + r]);
-    for (int s = 0; s < n_own; ++s) M = fmaxf(M, own_lse[(int64_t)s * p.g_rows]);
-    float total = 0.f;
+    const int64_t per_head = __ldcg(cum + a.B), cum0 = __ldcg(cum + b), cum1 = __ldcg(cum + b + 1);
+    float M = -INFINITY, total = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](float lse, float4 v) {
-        const float f = lse == -INFINITY ? 0.f : exp2f(lse - M);   // no weight at all: scores of -inf
-        if (f == 0.f) return;                                      // (its outputs are 0/0)
-        total += f;
-        o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+    // n partial results of this row and these features: log2-sum-exps at lse[s * lse_step], values at v[s * v_step]
+    auto add = [&](int n, const float* lse, int64_t lse_step, const float* v, int64_t v_step) {
+        for (int s0 = 0; s0 < n; s0 += MERGE_AT_ONCE) {
+            float e[MERGE_AT_ONCE];
+            float4 y[MERGE_AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < MERGE_AT_ONCE; ++u) {
+                e[u] = -INFINITY;
+                if (s0 + u < n) {
+                    e[u] = __ldcg(lse + (s0 + u) * lse_step);
+                    y[u] = __ldcg(reinterpret_cast<const float4*>(v + (s0 + u) * v_step));
+                }
+            }
+            float m = M;
+#pragma unroll
+            for (int u = 0; u < MERGE_AT_ONCE; ++u) m = fmaxf(m, e[u]);
+            const float keep = M == -INFINITY ? 0.f : exp2f(M - m);
+            M = m;
+            total *= keep;
+            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+#pragma unroll
+            for (int u = 0; u < MERGE_AT_ONCE; ++u) {
+                if (e[u] == -INFINITY) continue;   // no weight: past the last, or scores of -inf (values 0/0)
+                const float f = exp2f(e[u] - m);
+                total += f;
+                o.x = fmaf(f, y[u].x, o.x); o.y = fmaf(f, y[u].y, o.y); o.z = fmaf(f, y[u].z, o.z); o.w = fmaf(f, y[u].w, o.w);
+            }
+        }
     };
-#pragma unroll 4
-    for (int s = 0; s < p.p_splits; ++s) {
-        const int64_t tile = tile0 + s * tile_step;
-        add(ws[p.p_lse + tile * SHP_ROWS + r],
-            *reinterpret_cast<const float4*>(ws + p.p_o + tile * SHP_ROWS * D + ((int64_t)c4 * SHP_ROWS + r) * 4));
-    }
-#pragma unroll 2
-    for (int s = 0; s < n_own; ++s)
-        add(own_lse[(int64_t)s * p.g_rows], *reinterpret_cast<const float4*>(own_o + (int64_t)s * p.g_rows * D));
+    add(n_prefix, ws + p.p_lse + p_first * SHP_ROWS + r, (int64_t)p.m_tiles * SHP_ROWS,
+        ws + p.p_o + p_first * SHP_ROWS * D + ((int64_t)c4 * SHP_ROWS + r) * 4, (int64_t)p.m_tiles * SHP_ROWS * D);
+    if (len < 0) return;   // no request
+    const int64_t all = per_head * a.Hkv * p.g_tiles, W = own_workers(all, p.workers);
+    const int64_t w0 = block_worker(hh * per_head + cum0, all, W), first = w0 + hh * a.B + b;
+    const int n_own = (int)(block_worker(hh * per_head + cum1 - 1, all, W) - w0) + 1;
+    add(n_own, ws + p.own_lse + first * p.g_rows + x, p.g_rows, ws + p.own_o + (first * p.g_rows + x) * D + c4 * 4, (int64_t)p.g_rows * D);
+    if (blockIdx.x * 32 + lane >= a.B * a.g) return;
     const float inv = 1.f / total;
     const int64_t out = (int64_t)b * a.Hq + h * a.g + j;
     if constexpr (sizeof(T) == 2)
@@ -352,7 +383,7 @@ shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
 
 // ------------------------------------------------------------------ host side
 size_t decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int prefix_len, int max_len) {
-    (void)max_len;   // the lengths decide how the own part is cut, not how many pieces it has
+    (void)max_len;   // the lengths decide how the own part is cut, not into how many pieces
     const int64_t n = std::max(make_shared_plan(B, Hq, Hkv, D, prefix_len, false).total, make_shared_plan(B, Hq, Hkv, D, prefix_len, true).total);
     return (size_t)n * sizeof(float);
 }
@@ -367,13 +398,13 @@ template <typename T, int D>
 static cudaError_t prefix_simt(const SharedArgs& a, const SharedPlan& p, cudaStream_t st) {
     constexpr int smem = SimtSmem<T, D>::FLOATS * (int)sizeof(float);
     const int rows = a.B * a.g;
-    return launch_behind(shared_prefix_simt_kernel<T, D>, dim3((rows + SIMT_R - 1) / SIMT_R, a.Hkv, p.p_splits), SIMT_THREADS, smem, st, false, a, p);
+    return launch_behind(shared_prefix_simt_kernel<T, D>, dim3(p.p_workers * p.m_tiles, std::min(SHP_ROWS / SIMT_R, (rows + SIMT_R - 1) / SIMT_R)), SIMT_THREADS, smem, st, false, a, p);
 }
 
 template <typename T, int D>
 static cudaError_t shared_t(const SharedArgs& a, bool generic, cudaStream_t st) {
     SharedPlan p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, false);
-    const bool prefix = p.p_splits > 0, tc = sizeof(T) == 2 && !generic;
+    const bool prefix = p.p_blocks > 0, tc = sizeof(T) == 2 && !generic;
     cudaError_t e = cudaErrorNotSupported;
     if (prefix) {
         if (tc) e = launch_shared_prefix_tc(a, p, D, st);

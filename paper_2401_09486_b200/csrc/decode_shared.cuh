@@ -8,64 +8,64 @@
 namespace loma {
 
 constexpr int SHP_ROWS = 128;   // query rows of a prefix tile
-constexpr int SHP_CTAS = 148;   // prefix CTAs a call is cut into where its keys allow it
+constexpr int SHP_KEYS = 64;    // prefix keys per block
+constexpr int OWN_KEYS = 16;    // own keys per block
+constexpr int OWN_WARPS = 4;    // an own worker is a warp
+constexpr int OWN_CTAS = 148, STREAM_CTAS = 4 * 148;
+
+// Prefix CTAs that a call is cut for: one per SM, so that the own kernel runs beside it.  (Two per SM fill each other's waits,
+// but the own kernel then has to wait for them: B128 Hq32 Hkv8, prefix 16384 and up to 1500 own entries, 127 us against 95;
+// without own entries 49 against 52 us, and an HBM-bound prefix, B32 H32 prefix 8192, 39 against 36 us.)
+constexpr int SHP_CTAS = 148;
 
 // The cut of a call.  Depends on the sizes alone, so results repeat and the workspace can be sized before the call.
 //
-// Prefix: tiles of SHP_ROWS query rows times key ranges of equal length.
-//
-// Own caches: lengths are known on the device only and may be anything from nothing to max_len, so the work is cut there:
-// a sequence of n keys is ceil(n / 16) blocks, the blocks of all (kv head, head tile, sequence) are numbered through, and
-// worker w of W takes blocks [T w / W, T (w + 1) / W): equal shares whatever the lengths.  A worker's stay in one (kv head,
-// head tile, sequence) is a segment with one partial result; segment w + index of that triple is a slot of its own, since
-// along the numbering either the worker or the triple moves on.
+// Both parts are cut into equal shares whatever their shape.  The blocks of all units of work are numbered through -- prefix:
+// unit = kv head, SHP_KEYS keys a block; own: unit = (kv head, head tile, sequence), OWN_KEYS keys a block -- and worker w of
+// W takes blocks [T w / W, T (w + 1) / W).  A worker's stay in one unit is a segment with a partial result in slot w + unit:
+// along the numbering either the worker or the unit moves on, so no two segments share a slot, and the segments of one unit
+// lie behind one another.  Own lengths are known on the device only, so T is found there.
+// A prefix worker is m_tiles CTAs, one per tile of SHP_ROWS query rows: they walk the same keys at the same time, so K and V
+// come out of HBM once and reach the other tiles through L2 while the own kernel streams through it.
 struct SharedPlan {
-    int m_tiles;      // prefix: tiles of SHP_ROWS query rows per kv head
-    int p_splits;     // prefix: key ranges (0: no prefix)
-    int p_len;        //         keys per range, a multiple of 128
-    int g_rows;       // own: query heads of a kv head per head tile (8 or 16 rows of a warp-level product, or fewer heads)
-    int g_tiles;      //      head tiles per kv head
-    int workers;      //      W, before it is cut down to the number of blocks
-    // partial results in the workspace, as offsets in floats.  Prefix tile (split, kv head, tile): outputs [D/4][128][4]
-    // (so that a warp whose lanes are rows stores 512 contiguous bytes) and 128 log2-sum-exps.  Own segment: outputs
-    // [g_rows][D] and g_rows log2-sum-exps.  cum: int64 [B + 1], blocks before sequence b within one (kv head, head tile).
+    int m_tiles;        // prefix: tiles of SHP_ROWS query rows per kv head
+    int p_blocks;       //         blocks per kv head (0: no prefix)
+    int p_workers;      //         W: m_tiles CTAs each
+    int g_rows;         // own: query heads of a kv head per head tile (8 or 16 rows of a warp-level product, or fewer heads)
+    int g_tiles;        //      head tiles per kv head
+    int workers;        //      W, before it is cut down for few blocks
+    // partial results in the workspace, as offsets in floats.  Prefix segment: outputs [D/4][128][4] (so that a warp whose lanes
+    // are rows stores 512 contiguous bytes) and 128 log2-sum-exps.  Own segment: outputs [g_rows][D] and g_rows
+    // log2-sum-exps.  cum: int64 [B + 1], blocks before sequence b within one (kv head, head tile).
     int64_t p_o, p_lse, own_o, own_lse, cum, total;
 };
-
-constexpr int OWN_KEYS = 16;                  // keys per block
-constexpr int OWN_WARPS = 4;                  // a worker is a warp
-constexpr int OWN_CTAS = 148, STREAM_CTAS = 4 * 148;
 
 __host__ __device__ inline int64_t own_blocks(int len) { return len < 0 ? 0 : len / OWN_KEYS + 1; }   // keys 0 .. len: len is the new token
 
 // the worker that block t of T belongs to, and the first block of worker w (W <= T)
-__host__ __device__ inline int64_t own_worker(int64_t t, int64_t T, int64_t W) { return ((t + 1) * W - 1) / T; }
-__host__ __device__ inline int64_t own_first(int64_t w, int64_t T, int64_t W) { return T / W * w + T % W * w / W; }
+__host__ __device__ inline int64_t block_worker(int64_t t, int64_t T, int64_t W) { return ((t + 1) * W - 1) / T; }
+__host__ __device__ inline int64_t first_block(int64_t w, int64_t T, int64_t W) { return T / W * w + T % W * w / W; }
+
+__host__ __device__ inline int64_t own_workers(int64_t T, int workers) { return T < workers ? T : workers; }
 
 // cuda_cores: the own part runs on shared_own_stream_kernel (fp32, small pages, second opinion)
 inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len, bool cuda_cores) {
     SharedPlan p;
     const int64_t g = Hq / Hkv, rows = (int64_t)B * g;
     p.m_tiles = (int)((rows + SHP_ROWS - 1) / SHP_ROWS);
-    p.p_splits = 0;
-    p.p_len = 128;
-    if (prefix_len > 0) {
-        // one CTA per SM (the other half of the SM works on the own caches); a range is never shorter than 128 keys
-        const int64_t tiles = (int64_t)p.m_tiles * Hkv, key_tiles = (prefix_len + 127) / 128;
-        int64_t splits = std::max<int64_t>(1, SHP_CTAS / tiles);
-        splits = std::min<int64_t>(std::min<int64_t>(splits, key_tiles), 64);
-        const int64_t per = (key_tiles + splits - 1) / splits;
-        p.p_len = (int)per * 128;
-        p.p_splits = (int)((key_tiles + per - 1) / per);
-    }
+    p.p_blocks = (prefix_len + SHP_KEYS - 1) / SHP_KEYS;
+    int64_t w = std::max(1, SHP_CTAS / p.m_tiles);
+    // whole kv heads per worker, or whole workers per kv head, where that costs less than a segment more per worker would
+    if (w >= Hkv && w / Hkv * Hkv * 10 >= w * 9) w = w / Hkv * Hkv;
+    p.p_workers = (int)std::min<int64_t>(w, (int64_t)Hkv * ((p.p_blocks + 1) / 2));   // two blocks each at least
     p.g_rows = cuda_cores ? (g < 3 ? (int)g : 4) : (g <= 8 ? (int)g : 16);
     p.g_tiles = (int)((g + p.g_rows - 1) / p.g_rows);
     p.workers = (cuda_cores ? STREAM_CTAS : OWN_CTAS) * OWN_WARPS;
     int64_t at = 0;
     auto take = [&](int64_t n) { const int64_t o = at; at += (n + 63) / 64 * 64; return o; };
-    const int64_t p_tiles = (int64_t)p.p_splits * Hkv * p.m_tiles, segments = p.workers + (int64_t)B * Hkv * p.g_tiles;
-    p.p_o = take(p_tiles * SHP_ROWS * D);
-    p.p_lse = take(p_tiles * SHP_ROWS);
+    const int64_t p_segments = p.p_blocks ? (int64_t)(p.p_workers + Hkv) * p.m_tiles : 0, segments = p.workers + (int64_t)B * Hkv * p.g_tiles;
+    p.p_o = take(p_segments * SHP_ROWS * D);
+    p.p_lse = take(p_segments * SHP_ROWS);
     p.own_o = take(segments * p.g_rows * D);
     p.own_lse = take(segments * p.g_rows);
     p.cum = take(2 * ((int64_t)B + 1));
