@@ -5,6 +5,8 @@ point it calls, takes torch tensors (device memory) or plain ints, pulls out
 pointers, shapes and strides, and raises :class:`LomaError` on a negative
 status.  No arithmetic of the method happens in Python, and there is no
 fallback: if the library has not been built, loading fails with an error.
+The serving-step functions at the end take a few microseconds on the GPU; their
+arguments are checked and passed on by a small extension module (csrc/marshal.cpp).
 """
 
 from __future__ import annotations
@@ -666,55 +668,24 @@ def loma_compress_step(q_mem, k_mem, v_mem, k_cache, v_cache, o_mem, lse, mem_le
 
 # ---- one serving step: page tables, norm + rotation into the pages, attention over a shared prefix -----------------------
 
-# Small calls are bound by the host, and a check of a tensor costs more than a kernel argument: the checks below ask each
-# tensor only what they need (dtype objects are singletons, get_device() is -1 on the host), and name the culprit only
-# once something is wrong.
-
-def _addr(x) -> Optional[int]:
-    return None if x is None else x.data_ptr()
+_marshal = None
 
 
-def _on_current(where: str, dev: int) -> None:
-    """A pointer of another device than the current one would reach the wrong GPU's kernel."""
-    if dev < 0:
-        raise ValueError(f"{where}: tensors must be on a CUDA device")
-    if dev != torch.cuda.current_device():
-        raise ValueError(f"{where}: tensors on cuda:{dev}, but the current device is cuda:{torch.cuda.current_device()}")
-
-
-def _raw_stream(stream, dev: int) -> int:
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(dev)
-    return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
-
-
-def _int32(where: str, dev: int, name: str, x, numel: int) -> None:
-    """x is None, or contiguous int32 on device `dev` with `numel` entries (any number if negative)."""
-    if x is not None and (x.dtype is not torch.int32 or x.get_device() != dev or not x.is_contiguous()
-                          or (numel >= 0 and x.numel() != numel)):
-        raise ValueError(f"{where}: {name} must be a contiguous int32 tensor on the call's device"
-                         + (f" with {numel} entries" if numel >= 0 else ""))
-
-
-def _expect(where: str, dev: int, name: str, x, shape, dtype) -> None:
-    """x is None, or a contiguous tensor on device `dev` of this shape and dtype."""
-    if x is not None and (x.dtype is not dtype or x.get_device() != dev or x.shape != shape or not x.is_contiguous()):
-        raise ValueError(f"{where}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the call's device")
-
-
-def _scratch(where: str, dev: int, x) -> int:
-    """Bytes of a workspace tensor."""
-    if x is None:
-        return 0
-    if x.get_device() != dev or not x.is_contiguous():
-        raise ValueError(f"{where}: workspace must be a contiguous tensor on the call's device")
-    return x.numel() * x.element_size()
-
-
-def _strides(x, axes):
-    """[host] int64 array; an axis of one element has no stride of its own (torch reports any number there)."""
-    shape, stride = x.shape, x.stride()
-    return (ctypes.c_int64 * len(axes))(*[stride[a] if shape[a] > 1 else 0 for a in axes])
+def _native():
+    """The marshalling module, bound to the loaded library.  Raises if it has not been built."""
+    global _marshal
+    if _marshal is None:
+        handle = lib()
+        try:
+            from . import _marshal as module
+        except ImportError as e:
+            raise RuntimeError(f"the extension module _marshal.so is missing or broken ({e}): build it with "
+                               "`python -m paper_2401_09486_b200.build` (there is no fallback path)") from e
+        names = ("loma_paged_extend", "loma_qk_norm_rope_fwd", "loma_qk_norm_rope_bwd", "loma_qk_norm_rope_append",
+                 "loma_decode_attn_shared", "loma_decode_attn_shared_paged")
+        module.bind(*[ctypes.cast(getattr(handle, n), ctypes.c_void_p).value for n in names])
+        _marshal = module
+    return _marshal
 
 
 def loma_paged_extend(cache_lens, new_lens, held, pos0, free_pages, taken, block_table, page_size: int, row_start, page_start,
@@ -722,67 +693,16 @@ def loma_paged_extend(cache_lens, new_lens, held, pos0, free_pages, taken, block
     """Block table and slot maps from request lengths (see include/loma.h).  int32 tensors, all on the device or all on the
     host: cache_lens, new_lens, held, pos0 [B] (all but cache_lens may be None), free_pages, taken [1] or None, block_table
     [B, max_pages] (in/out); outputs row_start, page_start [B+1], held_out [B] (may be `held`), slots, row_seq, row_pos [rows]."""
-    w = "loma_paged_extend"
-    B, dev, rows = cache_lens.numel(), cache_lens.get_device(), slots.numel()
-    _int32(w, dev, "cache_lens", cache_lens, B)
-    _int32(w, dev, "new_lens", new_lens, B)
-    _int32(w, dev, "held", held, B)
-    _int32(w, dev, "pos0", pos0, B)
-    _int32(w, dev, "free_pages", free_pages, -1)
-    _int32(w, dev, "taken", taken, 1)
-    _int32(w, dev, "block_table", block_table, -1)
-    _int32(w, dev, "row_start", row_start, B + 1)
-    _int32(w, dev, "page_start", page_start, B + 1)
-    _int32(w, dev, "held_out", held_out, B)
-    _int32(w, dev, "slots", slots, rows)
-    _int32(w, dev, "row_seq", row_seq, rows)
-    _int32(w, dev, "row_pos", row_pos, rows)
-    if block_table.dim() != 2 or block_table.shape[0] != B:
-        raise ValueError(f"{w}: block_table must be [B, max_pages]")
-    if dev >= 0:
-        _on_current(w, dev)
-    rc = lib().loma_paged_extend(B, page_size, block_table.shape[1], rows, 0 if free_pages is None else free_pages.numel(),
-                                 cache_lens.data_ptr(), _addr(new_lens), _addr(held), _addr(pos0), _addr(free_pages), _addr(taken),
-                                 block_table.data_ptr(), row_start.data_ptr(), page_start.data_ptr(), held_out.data_ptr(),
-                                 slots.data_ptr(), row_seq.data_ptr(), row_pos.data_ptr(), int(dev >= 0),
-                                 _raw_stream(stream, dev) if dev >= 0 else None)
-    _check(rc, w)
-
-
-def _norm_args(where, q, k, wq, wk, pairs, gains, n_chunks, c, t, tail_read, flags):
-    """Checks of the training-layout norm; returns (device, B, Hq, Hk, D, dtype code, q strides, k strides)."""
-    if q.dim() != 4 or k.dim() != 4 or q.shape[0] != k.shape[0] or q.shape[2:] != k.shape[2:] or q.dtype is not k.dtype:
-        raise ValueError(f"{where}: q [B, Hq, S, D] and k [B, Hk, S, D] must share B, S, D and dtype")
-    B, Hq, S, D = q.shape
-    Hk, dev, dtype = k.shape[1], q.get_device(), q.dtype
-    if q.stride(3) != 1 or k.stride(3) != 1:
-        raise ValueError(f"{where}: head dimension must be contiguous")
-    if k.get_device() != dev:
-        raise ValueError(f"{where}: q and k on different devices")
-    for ref, x in pairs:
-        if x.dtype is not dtype or x.get_device() != dev or x.shape != ref.shape or (
-                x.stride() != ref.stride() and any(n > 1 and a != b for n, a, b in zip(x.shape, x.stride(), ref.stride()))):
-            raise ValueError(f"{where}: every tensor that goes with q or k must have its shape, strides, dtype and device")
-    for name, x in gains:
-        _expect(where, dev, name, x, (D,), dtype)
-    rows = n_chunks * ((c * t + t) if (flags & LOMA_FLAG_NO_REP_ZONE) else (2 * c * t + t)) + tail_read
-    if S != rows:
-        raise ValueError(f"{where}: the layout has {rows} rows, the tensors {S}")
-    _on_current(where, dev)
-    return dev, B, Hq, Hk, D, _dtype_code(q), _strides(q, (0, 1, 2)), _strides(k, (0, 1, 2))
+    _check((_marshal or _native()).paged_extend(cache_lens, new_lens, held, pos0, free_pages, taken, block_table, page_size, row_start,
+                                                page_start, held_out, slots, row_seq, row_pos, stream), "loma_paged_extend")
 
 
 def loma_qk_norm_rope_fwd(q, k, wq, wk, q_out, k_out, n_chunks: int, c: int, t: int, tail_read: int = 0, flags: int = 0,
                           eps: float = 0.0, theta_base: float = 0.0, position_type: int = 0, stream=None) -> None:
     """RMS norm of every head of q [B, Hq, S, D] and k [B, Hk, S, D] (gains wq, wk [D] or None) and the rotary embedding at the
     layout's position ids, in one pass.  q_out, k_out: shape and strides of q and k; q and k themselves are allowed."""
-    w = "loma_qk_norm_rope_fwd"
-    dev, B, Hq, Hk, D, dt, qs, ks = _norm_args(w, q, k, wq, wk, ((q, q_out), (k, k_out)), (("wq", wq), ("wk", wk)), n_chunks, c, t,
-                                               tail_read, flags)
-    rc = lib().loma_qk_norm_rope_fwd(q.data_ptr(), k.data_ptr(), _addr(wq), _addr(wk), q_out.data_ptr(), k_out.data_ptr(), B, Hq, Hk, D,
-                                     n_chunks, c, t, c * t, tail_read, qs, ks, dt, eps, theta_base, position_type, flags,
-                                     _raw_stream(stream, dev))
-    _check(rc, w)
+    _check((_marshal or _native()).qk_norm_rope_fwd(q, k, wq, wk, q_out, k_out, n_chunks, c, t, tail_read, flags, eps, theta_base,
+                                                    position_type, stream), "loma_qk_norm_rope_fwd")
 
 
 def loma_qk_norm_rope_bwd_workspace_bytes(B: int, Hq: int, Hk: int, D: int, n_chunks: int, c: int, t: int, tail_read: int = 0,
@@ -795,15 +715,8 @@ def loma_qk_norm_rope_bwd(q, k, wq, wk, d_q_out, d_k_out, dq, dk, dwq, dwk, n_ch
                           stream=None) -> None:
     """Gradients of loma_qk_norm_rope_fwd at q, k, wq, wk.  d_q_out, dq have q's shape and strides, d_k_out, dk those of k;
     dwq, dwk [D] or None; workspace: a device byte buffer of loma_qk_norm_rope_bwd_workspace_bytes(...) bytes."""
-    w = "loma_qk_norm_rope_bwd"
-    dev, B, Hq, Hk, D, dt, qs, ks = _norm_args(w, q, k, wq, wk, ((q, d_q_out), (q, dq), (k, d_k_out), (k, dk)),
-                                               (("wq", wq), ("wk", wk), ("dwq", dwq), ("dwk", dwk)), n_chunks, c, t, tail_read, flags)
-    ws_bytes = _scratch(w, dev, workspace)
-    rc = lib().loma_qk_norm_rope_bwd(q.data_ptr(), k.data_ptr(), _addr(wq), _addr(wk), d_q_out.data_ptr(), d_k_out.data_ptr(),
-                                     dq.data_ptr(), dk.data_ptr(), _addr(dwq), _addr(dwk), B, Hq, Hk, D, n_chunks, c, t, c * t, tail_read,
-                                     qs, ks, dt, eps, theta_base, position_type, flags, _addr(workspace), ws_bytes,
-                                     _raw_stream(stream, dev))
-    _check(rc, w)
+    _check((_marshal or _native()).qk_norm_rope_bwd(q, k, wq, wk, d_q_out, d_k_out, dq, dk, dwq, dwk, n_chunks, c, t, tail_read, flags,
+                                                    workspace, eps, theta_base, position_type, stream), "loma_qk_norm_rope_bwd")
 
 
 def loma_qk_norm_rope_append(q, k_new, v_new, wq, wk, q_out, k_pool, v_pool, slots, positions, eps: float = 0.0,
@@ -811,49 +724,12 @@ def loma_qk_norm_rope_append(q, k_new, v_new, wq, wk, q_out, k_pool, v_pool, slo
     """Norm and rotation of T packed new tokens: q [T, Hq, D] into q_out (contiguous), k_new [T, Hk, D] and, copied, v_new into
     the pools [n_pages, Hk, page_size, D] at slots[r] = page * page_size + row (a slot outside the pool: not stored).
     slots, positions: int32 [T].  q, k_new, v_new may be views of one projection's output."""
-    w = "loma_qk_norm_rope_append"
-    if q.dim() != 3 or k_new.dim() != 3 or k_pool.dim() != 4:
-        raise ValueError(f"{w}: q [T, Hq, D], k_new, v_new [T, Hk, D], pools [n_pages, Hk, page_size, D]")
-    T, Hq, D = q.shape
-    n_pages, Hk, page_size, _ = k_pool.shape
-    dev, dtype = q.get_device(), q.dtype
-    for x in (k_new, v_new):
-        if x.dtype is not dtype or x.get_device() != dev or x.shape != (T, Hk, D):
-            raise ValueError(f"{w}: k_new and v_new must be [T, Hk, D] in q's dtype, on its device")
-    for x in (q, k_new, v_new):
-        if x.stride(2) != 1 and x.numel():
-            raise ValueError(f"{w}: head dimension must be contiguous")
-    _expect(w, dev, "q_out", q_out, (T, Hq, D), dtype)
-    _expect(w, dev, "k_pool", k_pool, (n_pages, Hk, page_size, D), dtype)
-    _expect(w, dev, "v_pool", v_pool, (n_pages, Hk, page_size, D), dtype)
-    _expect(w, dev, "wq", wq, (D,), dtype)
-    _expect(w, dev, "wk", wk, (D,), dtype)
-    _int32(w, dev, "slots", slots, T)
-    _int32(w, dev, "positions", positions, T)
-    _on_current(w, dev)
-    rc = lib().loma_qk_norm_rope_append(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _addr(wq), _addr(wk), q_out.data_ptr(),
-                                        k_pool.data_ptr(), v_pool.data_ptr(), slots.data_ptr(), positions.data_ptr(), T, Hq, Hk, D,
-                                        page_size, n_pages, _strides(q, (0, 1)), _strides(k_new, (0, 1)), _strides(v_new, (0, 1)),
-                                        _dtype_code(q), eps, theta_base, _raw_stream(stream, dev))
-    _check(rc, w)
+    _check((_marshal or _native()).qk_norm_rope_append(q, k_new, v_new, wq, wk, q_out, k_pool, v_pool, slots, positions, eps, theta_base,
+                                                       stream), "loma_qk_norm_rope_append")
 
 
 def loma_decode_shared_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, prefix_len: int, max_cache_len: int) -> int:
     return int(lib().loma_decode_shared_workspace_bytes(B, Hq, Hkv, D, int(prefix_len), int(max_cache_len)))
-
-
-def _shared_common(where, q, k_new, v_new, o, lse, cache_lens, Hkv, workspace):
-    """Checks that both forms share; returns (device, dtype, B, Hq, D, workspace bytes)."""
-    if q.dim() != 4 or q.shape[2] != 1 or not q.is_contiguous():
-        raise ValueError(f"{where}: q must be a contiguous [B, Hq, 1, D] tensor")
-    B, Hq, _, D = q.shape
-    dev, dtype = q.get_device(), q.dtype
-    _expect(where, dev, "o", o, q.shape, dtype)
-    _expect(where, dev, "k_new", k_new, (B, Hkv, 1, D), dtype)
-    _expect(where, dev, "v_new", v_new, (B, Hkv, 1, D), dtype)
-    _expect(where, dev, "lse", lse, (B, Hq), torch.float32)
-    _int32(where, dev, "cache_lens", cache_lens, B)
-    return dev, dtype, B, Hq, D, _scratch(where, dev, workspace)
 
 
 def loma_decode_attn_shared(q, k_new, v_new, k_prefix, v_prefix, prefix_len: int, k_cache, v_cache, o, lse, cache_lens,
@@ -861,39 +737,14 @@ def loma_decode_attn_shared(q, k_new, v_new, k_prefix, v_prefix, prefix_len: int
     """Decode step over a prefix shared by the batch.  q, o: [B, Hq, 1, D]; k_new, v_new: [B, Hkv, 1, D] or None (already
     stored); k_prefix, v_prefix: [Hkv, prefix_cap, D]; own caches [B, Hkv, cap, D]; cache_lens: int32 [B], negative = no request;
     workspace: loma_decode_shared_workspace_bytes(...) bytes."""
-    w = "loma_decode_attn_shared"
-    Hkv, cap = k_cache.shape[1], k_cache.shape[2]
-    dev, dtype, B, Hq, D, ws_bytes = _shared_common(w, q, k_new, v_new, o, lse, cache_lens, Hkv, workspace)
-    _expect(w, dev, "k_cache", k_cache, (B, Hkv, cap, D), dtype)
-    _expect(w, dev, "v_cache", v_cache, (B, Hkv, cap, D), dtype)
-    prefix_cap = 0 if k_prefix is None else k_prefix.shape[1]
-    _expect(w, dev, "k_prefix", k_prefix, (Hkv, prefix_cap, D), dtype)
-    _expect(w, dev, "v_prefix", v_prefix, (Hkv, prefix_cap, D), dtype)
-    _on_current(w, dev)
-    rc = lib().loma_decode_attn_shared(q.data_ptr(), _addr(k_new), _addr(v_new), _addr(k_prefix), _addr(v_prefix), k_cache.data_ptr(),
-                                       v_cache.data_ptr(), o.data_ptr(), _addr(lse), B, Hq, Hkv, D, prefix_cap, prefix_len, cap,
-                                       cache_lens.data_ptr(), max_cache_len, _dtype_code(q), softmax_scale, flags, _addr(workspace),
-                                       ws_bytes, _raw_stream(stream, dev))
-    _check(rc, w)
+    _check((_marshal or _native()).decode_attn_shared(q, k_new, v_new, k_prefix, v_prefix, prefix_len, k_cache, v_cache, o, lse, cache_lens,
+                                                      max_cache_len, workspace, flags, softmax_scale, stream), "loma_decode_attn_shared")
 
 
 def loma_decode_attn_shared_paged(q, k_new, v_new, k_pool, v_pool, prefix_table, prefix_len: int, block_table, o, lse, cache_lens,
                                   max_cache_len: int, workspace=None, flags: int = 0, softmax_scale: float = 0.0, stream=None) -> None:
     """loma_decode_attn_shared over a pool [n_pages, Hkv, page_size, D] that holds the prefix (prefix_table: int32
     [prefix_pages]) and the sequences' own entries (block_table: int32 [B, max_pages])."""
-    w = "loma_decode_attn_shared_paged"
-    n_pages, Hkv, page_size, _ = k_pool.shape
-    dev, dtype, B, Hq, D, ws_bytes = _shared_common(w, q, k_new, v_new, o, lse, cache_lens, Hkv, workspace)
-    _expect(w, dev, "k_pool", k_pool, (n_pages, Hkv, page_size, D), dtype)
-    _expect(w, dev, "v_pool", v_pool, (n_pages, Hkv, page_size, D), dtype)
-    _int32(w, dev, "prefix_table", prefix_table, -1)
-    _int32(w, dev, "block_table", block_table, -1)
-    if block_table.dim() != 2 or block_table.shape[0] != B:
-        raise ValueError(f"{w}: block_table must be [B, max_pages]")
-    _on_current(w, dev)
-    rc = lib().loma_decode_attn_shared_paged(q.data_ptr(), _addr(k_new), _addr(v_new), k_pool.data_ptr(), v_pool.data_ptr(),
-                                             _addr(prefix_table), block_table.data_ptr(), o.data_ptr(), _addr(lse), B, Hq, Hkv, D, page_size,
-                                             0 if prefix_table is None else prefix_table.numel(), prefix_len, block_table.shape[1], n_pages,
-                                             cache_lens.data_ptr(), max_cache_len, _dtype_code(q), softmax_scale, flags, _addr(workspace),
-                                             ws_bytes, _raw_stream(stream, dev))
-    _check(rc, w)
+    _check((_marshal or _native()).decode_attn_shared_paged(q, k_new, v_new, k_pool, v_pool, prefix_table, prefix_len, block_table, o, lse,
+                                                            cache_lens, max_cache_len, workspace, flags, softmax_scale, stream),
+           "loma_decode_attn_shared_paged")

@@ -1,4 +1,5 @@
-"""Builds libloma.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libloma.so (the C-ABI CUDA library, nvcc for sm_100a) and _marshal.so (argument marshalling for its shortest calls,
+g++ against torch's headers) in-tree."""
 
 from __future__ import annotations
 
@@ -7,12 +8,15 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG_DIR, "libloma.so")
+MARSHAL_SRC = os.path.join(CSRC, "marshal.cpp")
+MARSHAL_PATH = os.path.join(PKG_DIR, "_marshal.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -33,27 +37,44 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB_PATH):
-        return True
-    built = os.path.getmtime(LIB_PATH)
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(INCLUDE, "*.h"))
-    return any(os.path.getmtime(p) > built for p in deps)
+def _older(path: str, deps) -> bool:
+    return not os.path.exists(path) or any(os.path.getmtime(p) > os.path.getmtime(path) for p in deps)
 
 
-def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compile every csrc/*.cu into one shared library; returns its path."""
-    if not force and not _stale():
-        return LIB_PATH
-    cmd = [_nvcc(), *NVCC_FLAGS, "-I", INCLUDE, "-I", CSRC, "-o", LIB_PATH, *sources()]
+def _run(cmd, what: str, verbose: bool) -> None:
     if verbose:
-        cmd[1:1] = ["-Xptxas", "-v"]
         print(" ".join(cmd), file=sys.stderr)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+        raise RuntimeError(f"{what} failed:\n" + res.stdout + res.stderr)
     if verbose:
         print(res.stderr, file=sys.stderr)
+
+
+def _build_marshal(verbose: bool) -> None:
+    import torch
+
+    root = os.path.dirname(os.path.abspath(torch.__file__))
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
+    includes = [INCLUDE, os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    lib = os.path.join(root, "lib")
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{d}" for d in includes], MARSHAL_SRC, "-o", MARSHAL_PATH,
+           f"-L{lib}", f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    _run(cmd, "g++", verbose)
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
+    """Compile every csrc/*.cu into one shared library and csrc/marshal.cpp into the extension module; returns the library's path."""
+    headers = glob.glob(os.path.join(INCLUDE, "*.h"))
+    if force or _older(LIB_PATH, sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + headers):
+        cmd = [_nvcc(), *NVCC_FLAGS, "-I", INCLUDE, "-I", CSRC, "-o", LIB_PATH, *sources()]
+        if verbose:
+            cmd[1:1] = ["-Xptxas", "-v"]
+        _run(cmd, "nvcc", verbose)
+    if force or _older(MARSHAL_PATH, [MARSHAL_SRC] + headers):
+        _build_marshal(verbose)
     return LIB_PATH
 
 

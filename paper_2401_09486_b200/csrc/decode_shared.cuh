@@ -55,8 +55,10 @@ inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len
     p.m_tiles = (int)((rows + SHP_ROWS - 1) / SHP_ROWS);
     p.p_blocks = (prefix_len + SHP_KEYS - 1) / SHP_KEYS;
     int64_t w = std::max(1, SHP_CTAS / p.m_tiles);
-    // whole kv heads per worker, or whole workers per kv head, where that costs less than a segment more per worker would
-    if (w >= Hkv && w / Hkv * Hkv * 10 >= w * 9) w = w / Hkv * Hkv;
+    // shares that end inside a kv head make most workers change heads once, which costs about as much as six blocks (draining
+    // the products, storing a partial result, new query rows): whole workers per kv head where their longer shares cost less
+    const int64_t all = (int64_t)Hkv * p.p_blocks, whole = w / Hkv * Hkv;
+    if (whole > 0 && (all + whole - 1) / whole <= (all + w - 1) / w + 6) w = whole;
     p.p_workers = (int)std::min<int64_t>(w, (int64_t)Hkv * ((p.p_blocks + 1) / 2));   // two blocks each at least
     p.g_rows = cuda_cores ? (g < 3 ? (int)g : 4) : (g <= 8 ? (int)g : 16);
     p.g_tiles = (int)((g + p.g_rows - 1) / p.g_rows);
@@ -178,18 +180,14 @@ __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 #endif
 
-// Two kernels share an SM only while it is split between L1 and shared memory the same way: all three ask for the same split.
-template <typename K>
-cudaError_t prepare_kernel(K kernel, int smem) {
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-    if (e == cudaSuccess && smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    return e;
-}
+// Attributes of a kernel, set once per device: its dynamic shared memory, and the split of an SM between L1 and shared memory
+// (two kernels share an SM only while both are fine with its split: all three ask for the same one).
+cudaError_t prepare_kernel(const void* kernel, int smem);   // decode_shared.cu
 
 // Launch a kernel that may start while the one before it in the stream still runs.
 template <typename... P, typename... A>
 cudaError_t launch_behind(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, bool behind, A... args) {
-    cudaError_t e = prepare_kernel(kernel, smem);
+    cudaError_t e = prepare_kernel(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
