@@ -41,7 +41,7 @@ template <typename T, int D, int G>
 __global__ void __launch_bounds__(OWN_WARPS * 32)
 shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
     using V = Vec16<T>;
-    constexpr int N = V::N, LPK = D / N, KPL = 32 / LPK, NL = OWN_KEYS / KPL < 4 ? OWN_KEYS / KPL : 4;
+    constexpr int N = V::N, LPK = D / N, KPL = 32 / LPK, NL = OWN_KEYS / KPL < 8 ? OWN_KEYS / KPL : 8;
     __shared__ int64_t scan[SeqBlocks::MAX_GROUPS + 1];
     __shared__ int64_t wsum[OWN_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LPK, li = lane % LPK;
@@ -159,22 +159,23 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
 }
 
 // ------------------------------------------------------------------ prefix on CUDA cores (fp32, small pages, second opinion)
-// 32 query rows against 64 keys at a time, all in fp32 in shared memory: scores with 2 x 4 and outputs with 4 x (D / 32)
-// values per thread in registers.  Query row m of kv head h is head h g + m mod g of sequence m / g.
-constexpr int SIMT_R = 32, SIMT_K = SHP_KEYS, SIMT_THREADS = 256;
+// RT query rows against 64 keys at a time, all in fp32 in shared memory, with RT / 16 x 4 scores and RT / 8 x (D / 32) outputs
+// per thread in registers; the next keys are on their way from memory while these are worked on.  Bound by fp32 FMA for many
+// rows, by the latency of a block's steps for few.  Query row m of kv head h is head h g + m mod g of sequence m / g.
+constexpr int SIMT_K = SHP_KEYS, SIMT_THREADS = 256;
 
-template <typename T, int D>
+template <int D, int RT>
 struct SimtSmem {
-    static constexpr int Q = 0, K = Q + SIMT_R * (D + 4), V = K + SIMT_K * (D + 4), S = V + SIMT_K * D, ML = S + SIMT_R * (SIMT_K + 4),
-                         FLOATS = ML + 3 * SIMT_R;
+    static constexpr int Q = 0, K = Q + RT * (D + 4), V = K + SIMT_K * (D + 4), S = V + SIMT_K * D, ML = S + RT * (SIMT_K + 4),
+                         FLOATS = ML + 3 * RT;
 };
 
-template <typename T, int D>
-__global__ void __launch_bounds__(SIMT_THREADS)
+template <typename T, int D, int RT>
+__global__ void __launch_bounds__(SIMT_THREADS, RT == 64 ? 1 : 2)
 shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
     using V = Vec16<T>;
-    using SM = SimtSmem<T, D>;
-    constexpr int N = V::N, LPK = D / N, DC = D / 32;   // output features per thread: 4 rows x DC
+    using SM = SimtSmem<D, RT>;
+    constexpr int N = V::N, LPK = D / N, DC = D / 32, PASSES = SIMT_K * LPK / SIMT_THREADS, SR = RT / 16, OR = RT / 8;
     extern __shared__ __align__(16) float sm[];
     let_next_start();
     const int tid = threadIdx.x, rows = a.B * a.g;
@@ -183,18 +184,29 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
     const int64_t blocks = (int64_t)a.Hkv * p.p_blocks;
     int64_t t = first_block(worker, blocks, p.p_workers);
     const int64_t t_end = first_block(worker + 1, blocks, p.p_workers);
-    const int r_in = blockIdx.y * SIMT_R, row0 = mt * SHP_ROWS + r_in;   // 32 rows of the tile per blockIdx.y
-    if (row0 >= rows) return;
-    const int sr = (tid >> 4) * 2, sk = tid & 15;         // scores: rows sr, sr+1; keys sk + 16 u
-    const int orow = (tid >> 5) * 4, oc = tid & 31;       // outputs: rows orow .. +3 (a warp's own); features oc*DC ..
+    const int r_in = blockIdx.y * RT, row0 = mt * SHP_ROWS + r_in;   // RT rows of the tile per blockIdx.y
+    if (row0 >= rows || t >= t_end) return;
+    const int sr = (tid >> 4) * SR, sk = tid & 15;        // scores: rows sr ..; keys sk + 16 u
+    const int orow = (tid >> 5) * OR, oc = tid & 31;      // outputs: rows orow .. (a warp's own); features oc * DC ..
+    uint4 kv[2][PASSES];
+    auto load = [&](int h, int k0) {                      // all of the thread's loads at once
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int r = (tid + i * SIMT_THREADS) / LPK, c = (tid + i * SIMT_THREADS) % LPK;
+            const int64_t row = prefix_row(a, h, min(k0 + r, a.prefix_len - 1)) * D;   // keys past the end repeat the last one
+            kv[0][i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.k_prefix) + row) + c);
+            kv[1][i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.v_prefix) + row) + c);
+        }
+    };
+    load((int)(t / p.p_blocks), (int)(t % p.p_blocks) * SHP_KEYS);
     while (t < t_end) {                                   // segments of the CTA's share
         const int h = (int)(t / p.p_blocks), blk0 = (int)(t - (int64_t)h * p.p_blocks);
         const int blk1 = (int)min((int64_t)p.p_blocks, blk0 + (t_end - t));
-        t += blk1 - blk0;
         const int begin = blk0 * SHP_KEYS, end = min(a.prefix_len, blk1 * SHP_KEYS);
         const int64_t seg = (int64_t)(worker + h) * p.m_tiles + mt;
         __syncthreads();
-        for (int idx = tid; idx < SIMT_R * LPK; idx += SIMT_THREADS) {
+#pragma unroll 4
+        for (int idx = tid; idx < RT * LPK; idx += SIMT_THREADS) {
             const int r = idx / LPK, c = idx - r * LPK, m = min(row0 + r, rows - 1);
             const T* qp = static_cast<const T*>(a.q) + ((int64_t)(m / a.g) * a.Hq + h * a.g + m % a.g) * D;
             float f[N];
@@ -202,42 +214,56 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
 #pragma unroll
             for (int e = 0; e < N; ++e) sm[SM::Q + r * (D + 4) + c * N + e] = f[e] * scale_log2;
         }
-        if (tid < SIMT_R) { sm[SM::ML + tid] = -INFINITY; sm[SM::ML + SIMT_R + tid] = 0.f; }
-        float acc[4][DC];
+        if (tid < RT) { sm[SM::ML + tid] = -INFINITY; sm[SM::ML + RT + tid] = 0.f; }
+        uint64_t acc[OR][DC / 2];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < OR; ++u)
 #pragma unroll
-            for (int c = 0; c < DC; ++c) acc[u][c] = 0.f;
+            for (int c = 0; c < DC / 2; ++c) acc[u][c] = 0;
         for (int k0 = begin; k0 < end; k0 += SIMT_K) {
-            __syncthreads();
-            for (int idx = tid; idx < SIMT_K * LPK; idx += SIMT_THREADS) {
-                const int r = idx / LPK, c = idx - r * LPK;
-                const int64_t row = prefix_row(a, h, min(k0 + r, a.prefix_len - 1)) * D;   // keys past the end repeat the last one
+            if (k0 > begin) __syncthreads();              // the tiles have been read
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i) {
+                const int r = (tid + i * SIMT_THREADS) / LPK, c = (tid + i * SIMT_THREADS) % LPK;
                 float f[N];
-                V::unpack(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.k_prefix) + row) + c), f);
+                V::unpack(kv[0][i], f);
 #pragma unroll
-                for (int e = 0; e < N; ++e) sm[SM::K + r * (D + 4) + c * N + e] = f[e];
-                V::unpack(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.v_prefix) + row) + c), f);
+                for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(&sm[SM::K + r * (D + 4) + c * N + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+                V::unpack(kv[1][i], f);
 #pragma unroll
-                for (int e = 0; e < N; ++e) sm[SM::V + r * D + c * N + e] = f[e];
+                for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(&sm[SM::V + r * D + c * N + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
             }
+            if (++t < t_end) load((int)(t / p.p_blocks), (int)(t % p.p_blocks) * SHP_KEYS);
             __syncthreads();
-            float s[2][4] = {};
+            // two-wide FMA: sums over even and odd features side by side
+            uint64_t s2[SR][4];
+#pragma unroll
+            for (int u = 0; u < SR; ++u)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) s2[u][w] = 0;
 #pragma unroll 4
             for (int d = 0; d < D; d += 4) {
-                float4 qv[2], kv[4];
+                ulonglong2 qv[SR], kf[4];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) qv[u] = *reinterpret_cast<const float4*>(&sm[SM::Q + (sr + u) * (D + 4) + d]);
+                for (int u = 0; u < SR; ++u) qv[u] = *reinterpret_cast<const ulonglong2*>(&sm[SM::Q + (sr + u) * (D + 4) + d]);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) kv[u] = *reinterpret_cast<const float4*>(&sm[SM::K + (sk + 16 * u) * (D + 4) + d]);
+                for (int u = 0; u < 4; ++u) kf[u] = *reinterpret_cast<const ulonglong2*>(&sm[SM::K + (sk + 16 * u) * (D + 4) + d]);
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < SR; ++u)
 #pragma unroll
-                    for (int w = 0; w < 4; ++w)
-                        s[u][w] = fmaf(qv[u].x, kv[w].x, fmaf(qv[u].y, kv[w].y, fmaf(qv[u].z, kv[w].z, fmaf(qv[u].w, kv[w].w, s[u][w]))));
+                    for (int w = 0; w < 4; ++w) s2[u][w] = fma2(qv[u].y, kf[w].y, fma2(qv[u].x, kf[w].x, s2[u][w]));
             }
+            float s[SR][4];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {   // 16 lanes share a row
+            for (int u = 0; u < SR; ++u)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    float lo, hi;
+                    unpack2(s2[u][w], lo, hi);
+                    s[u][w] = lo + hi;
+                }
+#pragma unroll
+            for (int u = 0; u < SR; ++u) {   // 16 lanes share a row
                 float mx = -INFINITY;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -260,32 +286,33 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
                 if ((tid & 15) == 0) {
                     const float alpha = exp2f(m_old - ref);
                     sm[SM::ML + sr + u] = m_new;
-                    sm[SM::ML + SIMT_R + sr + u] = sm[SM::ML + SIMT_R + sr + u] * alpha + sum;
-                    sm[SM::ML + 2 * SIMT_R + sr + u] = alpha;
+                    sm[SM::ML + RT + sr + u] = sm[SM::ML + RT + sr + u] * alpha + sum;
+                    sm[SM::ML + 2 * RT + sr + u] = alpha;
                 }
             }
             __syncthreads();
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float alpha = sm[SM::ML + 2 * SIMT_R + orow + u];
+            for (int u = 0; u < OR; ++u) {
+                const float alpha = sm[SM::ML + 2 * RT + orow + u];
 #pragma unroll
-                for (int c = 0; c < DC; ++c) acc[u][c] *= alpha;
+                for (int c = 0; c < DC / 2; ++c) acc[u][c] = fma2(acc[u][c], pack2(alpha, alpha), 0);
             }
-#pragma unroll 4
+#pragma unroll 2
             for (int k = 0; k < SIMT_K; k += 4) {
-                float4 pv[4];
+                float4 pv[OR];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) pv[u] = *reinterpret_cast<const float4*>(&sm[SM::S + (orow + u) * (SIMT_K + 4) + k]);
+                for (int u = 0; u < OR; ++u) pv[u] = *reinterpret_cast<const float4*>(&sm[SM::S + (orow + u) * (SIMT_K + 4) + k]);
 #pragma unroll
                 for (int kk = 0; kk < 4; ++kk) {
-                    float vv[DC];
+                    uint64_t vv[DC / 2];
 #pragma unroll
-                    for (int c = 0; c < DC; ++c) vv[c] = sm[SM::V + (k + kk) * D + oc * DC + c];
+                    for (int c = 0; c < DC / 2; ++c) vv[c] = *reinterpret_cast<const uint64_t*>(&sm[SM::V + (k + kk) * D + oc * DC + 2 * c]);
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
+                    for (int u = 0; u < OR; ++u) {
                         const float pr = kk == 0 ? pv[u].x : kk == 1 ? pv[u].y : kk == 2 ? pv[u].z : pv[u].w;
+                        const uint64_t pr2 = pack2(pr, pr);
 #pragma unroll
-                        for (int c = 0; c < DC; ++c) acc[u][c] = fmaf(pr, vv[c], acc[u][c]);
+                        for (int c = 0; c < DC / 2; ++c) acc[u][c] = fma2(pr2, vv[c], acc[u][c]);
                     }
                 }
             }
@@ -293,27 +320,34 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
         __syncthreads();
         float* ws = static_cast<float*>(a.ws);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const float inv = 1.f / sm[SM::ML + SIMT_R + orow + u];
+        for (int u = 0; u < OR; ++u) {
+            const float inv = 1.f / sm[SM::ML + RT + orow + u];
+            if (row0 + orow + u < rows) {
 #pragma unroll
-            for (int c = 0; c < DC; ++c) {
-                const int d = oc * DC + c;
-                ws[p.p_o + seg * SHP_ROWS * D + ((int64_t)(d >> 2) * SHP_ROWS + r_in + orow + u) * 4 + (d & 3)] = acc[u][c] * inv;
+                for (int c = 0; c < DC / 2; ++c) {
+                    const int d = oc * DC + 2 * c;
+                    float lo, hi;
+                    unpack2(acc[u][c], lo, hi);
+                    *reinterpret_cast<float2*>(ws + p.p_o + seg * SHP_ROWS * D + ((int64_t)(d >> 2) * SHP_ROWS + r_in + orow + u) * 4 + (d & 3)) =
+                        make_float2(lo * inv, hi * inv);
+                }
             }
         }
-        if (tid < SIMT_R) ws[p.p_lse + seg * SHP_ROWS + r_in + tid] = sm[SM::ML + tid] + log2f(sm[SM::ML + SIMT_R + tid]);
+        if (tid < RT && row0 + tid < rows) ws[p.p_lse + seg * SHP_ROWS + r_in + tid] = sm[SM::ML + tid] + log2f(sm[SM::ML + RT + tid]);
     }
 }
 
 // ------------------------------------------------------------------ merge
-// CTA: 32 query rows of one kv head (lanes) x 8 groups of 4 features (warps).  The time is that of its chain of dependent
-// loads, so partial results are taken MERGE_AT_ONCE at a time, values and log2-sum-exps together, under a running maximum.
+// CTA: 32 query rows of one kv head (lanes) x 8 / WAYS groups of 4 features (warps) x WAYS shares of the partial results.  The
+// time is that of its chain of dependent loads, so partial results are taken MERGE_AT_ONCE at a time, values and
+// log2-sum-exps together, under a running maximum, and a long list of them is read by WAYS warps.
 constexpr int MERGE_THREADS = 256, MERGE_AT_ONCE = 8;
 
-template <typename T, int D>
+template <typename T, int D, int WAYS>
 __global__ void __launch_bounds__(MERGE_THREADS)
 shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
-    const int lane = threadIdx.x & 31, c4 = blockIdx.y * 8 + (threadIdx.x >> 5);
+    constexpr int GROUPS = 8 / WAYS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, way = warp / GROUPS, c4 = blockIdx.y * GROUPS + warp % GROUPS;
     const int h = blockIdx.z, row = min((int)(blockIdx.x * 32 + lane), a.B * a.g - 1);   // rows past the last repeat it
     const int b = row / a.g, j = row - b * a.g;
     const int len = __ldg(a.cache_lens + b);
@@ -338,7 +372,7 @@ shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     // n partial results of this row and these features: log2-sum-exps at lse[s * lse_step], values at v[s * v_step]
     auto add = [&](int n, const float* lse, int64_t lse_step, const float* v, int64_t v_step) {
-        for (int s0 = 0; s0 < n; s0 += MERGE_AT_ONCE) {
+        for (int s0 = way * MERGE_AT_ONCE; s0 < n; s0 += WAYS * MERGE_AT_ONCE) {
             float e[MERGE_AT_ONCE];
             float4 y[MERGE_AT_ONCE];
 #pragma unroll
@@ -367,12 +401,36 @@ shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
     };
     add(n_prefix, ws + p.p_lse + p_first * SHP_ROWS + r, (int64_t)p.m_tiles * SHP_ROWS,
         ws + p.p_o + p_first * SHP_ROWS * D + ((int64_t)c4 * SHP_ROWS + r) * 4, (int64_t)p.m_tiles * SHP_ROWS * D);
-    if (len < 0) return;   // no request
+    const bool live = len >= 0 && blockIdx.x * 32 + lane < a.B * a.g;   // a request, and no repeated row
+    if (live) {
     const int64_t all = per_head * a.Hkv * p.g_tiles, W = own_workers(all, p.workers);
     const int64_t w0 = block_worker(hh * per_head + cum0, all, W), first = w0 + hh * a.B + b;
     const int n_own = (int)(block_worker(hh * per_head + cum1 - 1, all, W) - w0) + 1;
     add(n_own, ws + p.own_lse + first * p.g_rows + x, p.g_rows, ws + p.own_o + (first * p.g_rows + x) * D + c4 * 4, (int64_t)p.g_rows * D);
-    if (blockIdx.x * 32 + lane >= a.B * a.g) return;
+    }
+    if constexpr (WAYS > 1) {
+        __shared__ float s_m[WAYS][GROUPS][32], s_t[WAYS][GROUPS][32];
+        __shared__ float4 s_o[WAYS][GROUPS][32];
+        const int grp = warp % GROUPS;
+        s_m[way][grp][lane] = M;
+        s_t[way][grp][lane] = total;
+        s_o[way][grp][lane] = o;
+        __syncthreads();
+        if (way > 0) return;
+#pragma unroll
+        for (int y = 1; y < WAYS; ++y) M = fmaxf(M, s_m[y][grp][lane]);
+        total = 0.f;
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int y = 0; y < WAYS; ++y) {
+            const float my = s_m[y][grp][lane], f = my == -INFINITY ? 0.f : exp2f(my - M);
+            const float4 v = s_o[y][grp][lane];
+            if (f == 0.f) continue;
+            total += f * s_t[y][grp][lane];
+            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+        }
+    }
+    if (!live) return;
     const float inv = 1.f / total;
     const int64_t out = (int64_t)b * a.Hq + h * a.g + j;
     if constexpr (sizeof(T) == 2)
@@ -415,11 +473,17 @@ static cudaError_t own_stream(const SharedArgs& a, const SharedPlan& p, bool beh
     return launch_behind(kernel, dim3(STREAM_CTAS), OWN_WARPS * 32, 0, st, behind, a, p);
 }
 
+template <typename T, int D, int RT>
+static cudaError_t prefix_simt_rt(const SharedArgs& a, const SharedPlan& p, cudaStream_t st) {
+    constexpr int smem = SimtSmem<D, RT>::FLOATS * (int)sizeof(float);
+    const int rows = std::min(a.B * a.g, SHP_ROWS);
+    return launch_behind(shared_prefix_simt_kernel<T, D, RT>, dim3(p.p_workers * p.m_tiles, (rows + RT - 1) / RT), SIMT_THREADS, smem, st, false, a, p);
+}
+// the tallest row tile that the rows fill
 template <typename T, int D>
 static cudaError_t prefix_simt(const SharedArgs& a, const SharedPlan& p, cudaStream_t st) {
-    constexpr int smem = SimtSmem<T, D>::FLOATS * (int)sizeof(float);
     const int rows = a.B * a.g;
-    return launch_behind(shared_prefix_simt_kernel<T, D>, dim3(p.p_workers * p.m_tiles, std::min(SHP_ROWS / SIMT_R, (rows + SIMT_R - 1) / SIMT_R)), SIMT_THREADS, smem, st, false, a, p);
+    return rows <= 16 ? prefix_simt_rt<T, D, 16>(a, p, st) : rows <= 32 ? prefix_simt_rt<T, D, 32>(a, p, st) : prefix_simt_rt<T, D, 64>(a, p, st);
 }
 
 template <typename T, int D>
@@ -438,7 +502,10 @@ static cudaError_t shared_t(const SharedArgs& a, bool generic, cudaStream_t st) 
         e = own_stream<T, D>(a, p, prefix, st);
     }
     if (e != cudaSuccess) return e;
-    return launch_behind(shared_merge_kernel<T, D>, dim3((a.B * a.g + 31) / 32, D / 32, a.Hkv), MERGE_THREADS, 0, st, true, a, p);
+    // a long list of partial results per row: many workers to a kv head, or own shares of one block
+    if (p.p_workers / a.Hkv >= 2 * MERGE_AT_ONCE)
+        return launch_behind(shared_merge_kernel<T, D, 4>, dim3((a.B * a.g + 31) / 32, D / 8, a.Hkv), MERGE_THREADS, 0, st, true, a, p);
+    return launch_behind(shared_merge_kernel<T, D, 1>, dim3((a.B * a.g + 31) / 32, D / 32, a.Hkv), MERGE_THREADS, 0, st, true, a, p);
 }
 
 cudaError_t launch_decode_shared(const SharedArgs& a, int D, loma_dtype dt, bool generic, cudaStream_t st) {

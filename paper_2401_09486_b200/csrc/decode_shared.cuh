@@ -59,7 +59,7 @@ inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len
     // the products, storing a partial result, new query rows): whole workers per kv head where their longer shares cost less
     const int64_t all = (int64_t)Hkv * p.p_blocks, whole = w / Hkv * Hkv;
     if (whole > 0 && (all + whole - 1) / whole <= (all + w - 1) / w + 6) w = whole;
-    p.p_workers = (int)std::min<int64_t>(w, (int64_t)Hkv * ((p.p_blocks + 1) / 2));   // two blocks each at least
+    p.p_workers = (int)std::min<int64_t>(w, (int64_t)Hkv * p.p_blocks);
     p.g_rows = cuda_cores ? (g < 3 ? (int)g : 4) : (g <= 8 ? (int)g : 16);
     p.g_tiles = (int)((g + p.g_rows - 1) / p.g_rows);
     p.workers = (cuda_cores ? STREAM_CTAS : OWN_CTAS) * OWN_WARPS;

@@ -140,21 +140,8 @@ __device__ __forceinline__ float fast_ex2(float x) {
     return y;
 }
 
-// Packed pairs of fp32 (sm_100 has two-wide fp32 FMA and ADD) and the three-input maximum: the
-// softmax warps are bound by instruction issue, so fewer instructions per score matter.
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
+// Packed pairs of fp32 (sm_100 has two-wide fp32 FMA and ADD; pack2, unpack2 and fma2 are in loma_internal.cuh) and the
+// three-input maximum: the softmax warps are bound by instruction issue, so fewer instructions per score matter.
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
