@@ -16,8 +16,6 @@
 // an HBM-bound stream runs under a tensor-bound product; the merge waits for both.
 #include <math.h>
 
-#include <mutex>
-
 #include "decode_shared.cuh"
 
 namespace loma {
@@ -442,25 +440,6 @@ shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
 }
 
 // ------------------------------------------------------------------ host side
-cudaError_t prepare_kernel(const void* kernel, int smem) {
-    static std::mutex mu;
-    static struct { const void* kernel; uint64_t devices; } done[64];
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    std::lock_guard<std::mutex> lock(mu);
-    int i = 0;
-    while (i < 64 && done[i].kernel && done[i].kernel != kernel) ++i;
-    if (i < 64 && dev < 64 && done[i].kernel == kernel && (done[i].devices >> dev & 1)) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-    if (e == cudaSuccess && smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == cudaSuccess && i < 64 && dev < 64) {
-        done[i].kernel = kernel;
-        done[i].devices |= 1ull << dev;
-    }
-    return e;
-}
-
 size_t decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int prefix_len, int max_len) {
     (void)max_len;   // the lengths decide how the own part is cut, not into how many pieces
     const int64_t n = std::max(make_shared_plan(B, Hq, Hkv, D, prefix_len, false).total, make_shared_plan(B, Hq, Hkv, D, prefix_len, true).total);

@@ -180,10 +180,6 @@ __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 #endif
 
-// Attributes of a kernel, set once per device: its dynamic shared memory, and the split of an SM between L1 and shared memory
-// (two kernels share an SM only while both are fine with its split: all three ask for the same one).
-cudaError_t prepare_kernel(const void* kernel, int smem);   // decode_shared.cu
-
 // Launch a kernel that may start while the one before it in the stream still runs.
 template <typename... P, typename... A>
 cudaError_t launch_behind(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, bool behind, A... args) {

@@ -236,6 +236,11 @@ int check_device();
 int make_layout(int n_chunks, int c, int t, int tail_read, unsigned flags, Layout* L);
 int log2_exact(int x);   // log2 of a power of two, or -1
 
+// ---- kernel attributes, set once per device (serving_api.cu) ----
+// Dynamic shared memory, and the split of an SM between L1 and shared memory: two kernels share an SM only while both are
+// fine with its split, so all of them ask for the same one.
+cudaError_t prepare_kernel(const void* kernel, int smem);
+
 // ---- launch accounting -------------------------------------------------------
 void count_launches(int n);   // called by every launcher with the number of kernels it enqueued
 

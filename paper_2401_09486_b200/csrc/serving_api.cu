@@ -4,8 +4,32 @@
 #include <math.h>
 
 #include <algorithm>
+#include <mutex>
 
 #include "decode_shared.cuh"
+
+namespace loma {
+
+cudaError_t prepare_kernel(const void* kernel, int smem) {
+    static std::mutex mu;
+    static struct { const void* kernel; uint64_t devices; } done[64];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> lock(mu);
+    int i = 0;
+    while (i < 64 && done[i].kernel && done[i].kernel != kernel) ++i;
+    if (i < 64 && dev < 64 && done[i].kernel == kernel && (done[i].devices >> dev & 1)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    if (e == cudaSuccess && smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess && i < 64 && dev < 64) {
+        done[i].kernel = kernel;
+        done[i].devices |= 1ull << dev;
+    }
+    return e;
+}
+
+}  // namespace loma
 
 using namespace loma;
 
