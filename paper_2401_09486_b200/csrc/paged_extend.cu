@@ -9,10 +9,11 @@
 // its dependent steps (lengths -> sums -> pages -> slots) when the batch is small and by the three row outputs when
 // many prompts arrive at once.
 //
-// Up to FUSED_MAX_B sequences one launch does everything: every CTA scans all sequences for itself in shared memory
-// (12 bytes a sequence out of L2, two or three microseconds at 4096) and then writes its own slab of rows and its own
-// share of the sequences, so nothing waits for another CTA.  Longer batches, and calls that update `held` or `taken`
-// in place (where one CTA's write would be another CTA's input), scan in one CTA and write rows in a second launch.
+// Up to FUSED_MAX_B sequences one launch does everything: every CTA scans all sequences for itself in shared memory (12
+// bytes a sequence out of L2) and then writes its own slab of rows and its own share of the sequences, so nothing waits for
+// another CTA.  What a single-token step needs after the sums -- the page of each sequence's next entry and the head of the
+// free list -- is fetched before them.  Longer batches, and calls that update `held` or `taken` in place (where one CTA's
+// write would be another CTA's input), scan in one CTA and write rows in a second launch.
 #include <limits.h>
 
 #include <algorithm>
@@ -55,19 +56,20 @@ __host__ __device__ inline int pages_got(const ExtendArgs& a, int first, int fre
     return left < fresh ? left : fresh;
 }
 
-// slot and position of entry len + i of sequence b; h, first: its pages before the call, its first fresh page
-__host__ __device__ inline void row_values(const ExtendArgs& a, int b, int i, int len, int h, int first, int& slot, int& pos) {
-    const int64_t e = (int64_t)len + i;
-    const int64_t p = (a.pos0 ? (int64_t)a.pos0[b] : (int64_t)len) + i;
-    pos = saturate(p);
-    slot = -1;
-    if (e < ((int64_t)a.max_pages << a.log2_ps)) {
-        const int block = (int)(e >> a.log2_ps);
-        const int page = block < h ? a.block_table[(int64_t)b * a.max_pages + block] : free_page(a, (int64_t)first + block - h);
-        const int mask = (1 << a.log2_ps) - 1;
-        if (page >= 0 && page <= ((INT_MAX - mask) >> a.log2_ps)) slot = (page << a.log2_ps) + (int)(e & mask);
-    }
+// slot of entry e of a sequence from its page, or -1
+__host__ __device__ inline int slot_of(const ExtendArgs& a, int page, int64_t e) {
+    const int mask = (1 << a.log2_ps) - 1;
+    return page >= 0 && page <= ((INT_MAX - mask) >> a.log2_ps) ? (page << a.log2_ps) + (int)(e & mask) : -1;
 }
+
+// slot of entry len + i of sequence b; h, first: its pages before the call, its first fresh page
+__host__ __device__ inline int row_slot(const ExtendArgs& a, int b, int i, int len, int h, int first) {
+    const int64_t e = (int64_t)len + i;
+    if (e >= ((int64_t)a.max_pages << a.log2_ps)) return -1;
+    const int block = (int)(e >> a.log2_ps);
+    return slot_of(a, block < h ? a.block_table[(int64_t)b * a.max_pages + block] : free_page(a, (int64_t)first + block - h), e);
+}
+__host__ __device__ inline int first_pos(const ExtendArgs& a, int b, int len) { return a.pos0 ? a.pos0[b] : len; }
 
 // ------------------------------------------------------------------ host form
 void host_paged_extend(const ExtendArgs& a) {
@@ -79,8 +81,9 @@ void host_paged_extend(const ExtendArgs& a) {
         a.page_start[b] = first;
         for (int i = 0; i < s.n && rows + i < a.max_rows; ++i) {
             const int64_t r = rows + i;
-            row_values(a, b, i, s.len, s.h, first, a.slots[r], a.row_pos[r]);
+            a.slots[r] = row_slot(a, b, i, s.len, s.h, first);
             a.row_seq[r] = b;
+            a.row_pos[r] = saturate((int64_t)first_pos(a, b, s.len) + i);
         }
         for (int i = 0; i < s.fresh; ++i)
             a.block_table[(int64_t)b * a.max_pages + s.h + i] = free_page(a, (int64_t)first + i);
@@ -99,7 +102,7 @@ void host_paged_extend(const ExtendArgs& a) {
 
 // ------------------------------------------------------------------ device form
 constexpr int EXT_THREADS = 512;
-constexpr int FUSED_MAX_B = 4096;    // two int32 sums per sequence in shared memory: 32 KB
+constexpr int FUSED_MAX_B = 2048;    // five numbers per sequence in shared memory: 40 KB
 constexpr int ROWS_PER_THREAD = 4;   // consecutive rows: one search, 16-byte stores
 
 // Exclusive sums over the block of one (rows, pages) pair per thread; every thread gets the block's totals too.
@@ -138,31 +141,22 @@ __device__ __forceinline__ int find_seq(const int* start, int lo, int hi, int r)
     return lo;
 }
 
-// Rows r0 .. r0+3 of the packed batch.  start / first: row_start and page_start (B + 1 values, shared or global memory).
-// h_from_out: `held` is being updated in place, so a sequence's pages before the call are what it holds now less what it got.
-__device__ __forceinline__ void write_rows(const ExtendArgs& a, const int* start, const int* first, int r0, bool vec, bool h_from_out) {
+// Rows r0 .. r0+3 of the packed batch; start: row_start (B + 1 values).  enter(b) makes b the current sequence, slot(i) and
+// pos(i) are those of its i-th new entry.
+template <typename Enter, typename Slot, typename Pos>
+__device__ __forceinline__ void write_rows(const ExtendArgs& a, const int* start, int r0, bool vec, Enter&& enter, Slot&& slot_at, Pos&& pos_at) {
     int slot[ROWS_PER_THREAD], seq[ROWS_PER_THREAD], pos[ROWS_PER_THREAD];
     const int total = start[a.B];
-    int b = r0 < total ? find_seq(start, 0, a.B, r0) : a.B;
-    int len = 0, h = 0, have = -1;
+    int b = r0 < total ? find_seq(start, 0, a.B, r0) : a.B, have = -1;
 #pragma unroll
     for (int u = 0; u < ROWS_PER_THREAD; ++u) {
         const int r = r0 + u;
         slot[u] = -1; seq[u] = -1; pos[u] = 0;
         if (r >= total || r < 0) continue;
         while (start[b + 1] <= r) ++b;
-        if (b != have) {
-            if (h_from_out) {
-                const int room = a.max_pages << a.log2_ps;
-                len = clampi(a.cache_lens[b], 0, room);
-                h = a.held_out[b] - pages_got(a, first[b], first[b + 1] - first[b]);
-            } else {
-                const SeqNeed s = seq_need(a, b);
-                len = s.len; h = s.h;
-            }
-            have = b;
-        }
-        row_values(a, b, r - start[b], len, h, first[b], slot[u], pos[u]);
+        if (b != have) { enter(b); have = b; }
+        slot[u] = slot_at(r - start[b]);
+        pos[u] = pos_at(r - start[b]);
         seq[u] = b;
     }
     if (vec && r0 + ROWS_PER_THREAD <= a.max_rows) {
@@ -182,15 +176,23 @@ __device__ __forceinline__ void write_rows(const ExtendArgs& a, const int* start
 
 __global__ void __launch_bounds__(EXT_THREADS)
 paged_extend_fused_kernel(const ExtendArgs a, int vec) {
-    __shared__ int s_row[FUSED_MAX_B + 1], s_page[FUSED_MAX_B + 1];
-    for (int b = threadIdx.x; b < a.B; b += EXT_THREADS) {
+    __shared__ int s_row[FUSED_MAX_B + 1], s_page[FUSED_MAX_B + 1], s_len[FUSED_MAX_B], s_h[FUSED_MAX_B], s_pos[FUSED_MAX_B];
+    __shared__ int s_next[EXT_THREADS], s_free[EXT_THREADS];   // page of sequence b's entry len (b < EXT_THREADS); head of the free list
+    const int tid = threadIdx.x, room = a.max_pages << a.log2_ps;
+    int head = -1, next = -1;
+    if (tid < a.n_free) head = __ldg(a.free_pages + tid);
+    for (int b = tid; b < a.B; b += EXT_THREADS) {
         const SeqNeed s = seq_need(a, b);
         s_row[b] = s.n;
         s_page[b] = s.fresh;
+        s_len[b] = s.len;
+        s_h[b] = s.h;
+        s_pos[b] = first_pos(a, b, s.len);
+        if (b < EXT_THREADS && s.len < room && (s.len >> a.log2_ps) < s.h) next = a.block_table[(int64_t)b * a.max_pages + (s.len >> a.log2_ps)];
     }
     __syncthreads();
     const int per = (a.B + EXT_THREADS - 1) / EXT_THREADS;
-    const int b0 = min(a.B, (int)threadIdx.x * per), b1 = min(a.B, b0 + per);
+    const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
     int64_t rows = 0, pages = 0, tr, tp;
     for (int b = b0; b < b1; ++b) { rows += s_row[b]; pages += s_page[b]; }
     block_scan2(rows, pages, tr, tp);
@@ -201,27 +203,42 @@ paged_extend_fused_kernel(const ExtendArgs a, int vec) {
         rows += n;
         pages += f;
     }
-    if (threadIdx.x == 0) { s_row[a.B] = saturate(tr); s_page[a.B] = saturate(tp); }
+    if (tid == 0) { s_row[a.B] = saturate(tr); s_page[a.B] = saturate(tp); }
+    s_next[tid] = next;
+    s_free[tid] = head;
     __syncthreads();
+    auto free_at = [&](int64_t idx) { return idx < EXT_THREADS ? s_free[idx] : free_page(a, idx); };
 
-    // this CTA's share of the sequences: sums, held pages, fresh table entries (a warp per sequence)
-    for (int b = blockIdx.x * EXT_THREADS + threadIdx.x; b <= a.B; b += gridDim.x * EXT_THREADS) {
+    // this CTA's share of the sequences: sums and held pages, then the fresh table entries (a warp per sequence)
+    for (int b = blockIdx.x * EXT_THREADS + tid; b <= a.B; b += gridDim.x * EXT_THREADS) {
         a.row_start[b] = s_row[b];
         a.page_start[b] = s_page[b];
-        if (b < a.B) {
-            const SeqNeed s = seq_need(a, b);
-            a.held_out[b] = s.h + pages_got(a, s_page[b], s.fresh);
-        }
-    }
-    const int lane = threadIdx.x & 31;
-    for (int b = blockIdx.x * (EXT_THREADS / 32) + (threadIdx.x >> 5); b < a.B; b += gridDim.x * (EXT_THREADS / 32)) {
-        const SeqNeed s = seq_need(a, b);
-        for (int i = lane; i < s.fresh; i += 32)
-            a.block_table[(int64_t)b * a.max_pages + s.h + i] = free_page(a, (int64_t)s_page[b] + i);
+        if (b < a.B) a.held_out[b] = s_h[b] + pages_got(a, s_page[b], s_page[b + 1] - s_page[b]);
     }
     const int64_t step = (int64_t)gridDim.x * EXT_THREADS * ROWS_PER_THREAD;
-    for (int64_t r = ((int64_t)blockIdx.x * EXT_THREADS + threadIdx.x) * ROWS_PER_THREAD; r < a.max_rows; r += step)
-        write_rows(a, s_row, s_page, (int)r, vec, false);
+    for (int64_t r = ((int64_t)blockIdx.x * EXT_THREADS + tid) * ROWS_PER_THREAD; r < a.max_rows; r += step) {
+        int cur = 0, len = 0, h = 0, first = 0, pos = 0, block = -1, page = -1;
+        write_rows(a, s_row, (int)r, vec,
+                   [&](int b) { cur = b; len = s_len[b]; h = s_h[b]; first = s_page[b]; pos = s_pos[b]; block = -1; },
+                   [&](int i) {
+                       const int64_t e = (int64_t)len + i;
+                       if (e >= room) return -1;
+                       const int blk = (int)(e >> a.log2_ps);
+                       if (blk != block) {   // rows of one page look it up once
+                           block = blk;
+                           if (blk >= h) page = free_at((int64_t)first + blk - h);
+                           else if (cur < EXT_THREADS && blk == len >> a.log2_ps) page = s_next[cur];
+                           else page = a.block_table[(int64_t)cur * a.max_pages + blk];
+                       }
+                       return slot_of(a, page, e);
+                   },
+                   [&](int i) { return saturate((int64_t)pos + i); });
+    }
+    const int lane = tid & 31;
+    for (int b = blockIdx.x * (EXT_THREADS / 32) + (tid >> 5); b < a.B; b += gridDim.x * (EXT_THREADS / 32)) {
+        const int fresh = s_page[b + 1] - s_page[b];
+        for (int i = lane; i < fresh; i += 32) a.block_table[(int64_t)b * a.max_pages + s_h[b] + i] = free_at((int64_t)s_page[b] + i);
+    }
 }
 
 // One CTA: the sums, held pages and the free list's new start.  Every value a thread reads of `held` it reads before it
@@ -267,7 +284,18 @@ paged_extend_rows_kernel(const ExtendArgs a, int vec) {
     }
     const int64_t step = (int64_t)gridDim.x * EXT_THREADS * ROWS_PER_THREAD;
     for (int64_t r = ((int64_t)blockIdx.x * EXT_THREADS + threadIdx.x) * ROWS_PER_THREAD; r < a.max_rows; r += step)
-        write_rows(a, a.row_start, a.page_start, (int)r, vec, true);
+    {
+        int cur = 0, len = 0, h = 0, first = 0;
+        write_rows(a, a.row_start, (int)r, vec,
+                   [&](int b) {   // `held` may have been updated in place: a sequence's pages before the call are what it holds now less what it got
+                       cur = b;
+                       len = clampi(a.cache_lens[b], 0, a.max_pages << a.log2_ps);
+                       first = a.page_start[b];
+                       h = a.held_out[b] - pages_got(a, first, a.page_start[b + 1] - first);
+                   },
+                   [&](int i) { return row_slot(a, cur, i, len, h, first); },
+                   [&](int i) { return saturate((int64_t)first_pos(a, cur, len) + i); });
+    }
 }
 
 cudaError_t launch_paged_extend(const ExtendArgs& a, cudaStream_t st) {

@@ -310,95 +310,157 @@ cudaError_t launch_qk_norm_rope(const HeadsView& q, const HeadsView& k, int B, i
 }
 
 // ------------------------------------------------------------------ serving form
-// One packed row (token) per blockIdx.x; its Hq + 2 Hk heads are dealt to the warps of gridDim.y CTAs.  A lane's first
-// AT_ONCE heads are all in flight while the angles are computed.
-constexpr int APP_WARPS = 4, AT_ONCE = 4;
+// A warp takes a packed row (token), or one of `parts` shares of its heads where there are few tokens: RPW heads at a time out
+// of the row's list [q heads | k heads | v heads], fetched ahead across the borders between rows.  The D / 2 angles of a row are
+// computed once, two per lane, and reach the other lanes through shared memory of the warp's own; no barrier.  Bound by
+// instruction issue as much as by HBM, so what does not change from row to row (theta, gains) is kept.
+constexpr int APP_STAGES = 6, APP_RING = APP_STAGES * 2 * QKN_WARPS * 32 * 16;   // 48 KB a CTA
 
 template <typename T, int D>
-__global__ void __launch_bounds__(APP_WARPS * 32)
-qk_norm_rope_append_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(QKN_WARPS * 32, 3)
+qk_norm_rope_append_kernel(const AppendArgs a, int parts) {
     using V = Vec16<T>;
-    constexpr int N = V::N, HALF = D / 2, LPR = HALF / N, HPW = 32 / LPR;   // heads per warp access
-    __shared__ float s_cs[HALF], s_sn[HALF];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d0 = (lane % LPR) * N;
-    const int64_t row = blockIdx.x;
-    const int total = a.Hq + 2 * a.Hk, step = gridDim.y * APP_WARPS * HPW;
-    const int slot = __ldg(a.slots + row);
-    const bool stored = slot >= 0 && slot < (int64_t)a.n_pages * a.page_size;
-    auto source = [&](int it) -> const T* {
-        if (it < a.Hq) return static_cast<const T*>(a.q) + row * a.q_row + it * a.q_head + d0;
-        if (it < a.Hq + a.Hk) return static_cast<const T*>(a.k) + row * a.k_row + (it - a.Hq) * a.k_head + d0;
-        return static_cast<const T*>(a.v) + row * a.v_row + (it - a.Hq - a.Hk) * a.v_head + d0;
+    constexpr int N = V::N, HALF = D / 2, LPR = HALF / N, RPW = 32 / LPR, AP = HALF / 32;   // AP: angles a lane computes
+    constexpr uint32_t CHUNK = QKN_WARPS * 32 * 16, STAGE = 2 * CHUNK;
+    extern __shared__ __align__(16) uint8_t qkn_ring[];
+    __shared__ __align__(16) float s_gain[2][D];                    // wq, wk
+    __shared__ __align__(16) float s_ang[QKN_WARPS][2][HALF];       // cos, sin of the warp's row
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = lane / LPR, d0 = (lane % LPR) * N;
+    const int total = a.Hq + 2 * a.Hk, steps = (total + RPW - 1) / RPW;       // heads of a row; steps of RPW heads
+    const int64_t items = (int64_t)a.T * parts, stride = (int64_t)gridDim.x * QKN_WARPS;
+    int64_t item = (int64_t)warp * gridDim.x + blockIdx.x;                     // neighbours on different SMs
+    // the fetch runs ahead: its own row and step
+    int64_t item_f = item;
+    int row_f = 0, step_f = 0, last_f = 0;
+    auto enter = [&](int64_t it, int& row, int& first, int& last) {
+        row = parts == 1 ? (int)it : (int)(it / parts);
+        const int part = parts == 1 ? 0 : (int)(it - (int64_t)row * parts);
+        first = steps * part / parts;
+        last = steps * (part + 1) / parts;
     };
-    // the heads this lane works on, AT_ONCE of them in flight at a time
-    const int first = (blockIdx.y * APP_WARPS + warp) * HPW;
-    uint4 xl[AT_ONCE], xh[AT_ONCE];
-    auto load = [&](int base) {
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            const T* src = source(min(base + u * step + lane / LPR, total - 1));
-            if (base + u * step < total) {
-                xl[u] = __ldcs(reinterpret_cast<const uint4*>(src));
-                xh[u] = __ldcs(reinterpret_cast<const uint4*>(src + HALF));
+    if (item < items) enter(item_f, row_f, step_f, last_f);
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(qkn_ring) + threadIdx.x * 16;
+    uint32_t slot_f = ring;
+    auto fetch = [&]() {
+        if (item_f < items) {
+            const int it = min(step_f * RPW + group, total - 1);               // past the last head: it again
+            const T* src;
+            if (it < a.Hq) src = static_cast<const T*>(a.q) + row_f * a.q_row + it * a.q_head;
+            else if (it < a.Hq + a.Hk) src = static_cast<const T*>(a.k) + row_f * a.k_row + (it - a.Hq) * a.k_head;
+            else src = static_cast<const T*>(a.v) + row_f * a.v_row + (it - a.Hq - a.Hk) * a.v_head;
+            cp_async16(slot_f, src + d0);
+            cp_async16(slot_f + CHUNK, src + d0 + HALF);
+            if (++step_f == last_f) {
+                item_f += stride;
+                if (item_f < items) enter(item_f, row_f, step_f, last_f);
             }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        slot_f = slot_f == ring + (APP_STAGES - 1) * STAGE ? ring : slot_f + STAGE;
     };
-    load(first);
-    const int pos = __ldg(a.positions + row);
-    for (int d = threadIdx.x; d < HALF; d += APP_WARPS * 32) angle_cos_sin(pos, exp2(-a.log2_base * (2.0 * d / D)), s_cs[d], s_sn[d]);
+#pragma unroll
+    for (int u = 0; u < APP_STAGES - 1; ++u) fetch();
+    uint32_t slot_at = ring;
+    int row = 0, step = 0, last = 0, pos = 0, cell = 0;
+    if (item < items) {
+        enter(item, row, step, last);
+        pos = __ldg(a.positions + row);
+        cell = __ldg(a.slots + row);
+    }
+    // under the first loads: what all rows share
+    for (int d = threadIdx.x; d < 2 * D; d += QKN_WARPS * 32) {
+        const T* w = static_cast<const T*>(d < D ? a.wq : a.wk);
+        s_gain[d / D][d % D] = w ? (float)w[d % D] : 1.f;
+    }
+    double theta[AP];
+#pragma unroll
+    for (int u = 0; u < AP; ++u) theta[u] = exp2(-a.log2_base * (2.0 * (lane + 32 * u) / D));
     __syncthreads();
-    float cs[N], sn[N];
+
+    if (item >= items) return;
+    for (;;) {
+        // this row's angles; the next row's position and slot are on their way
+        const int64_t next = item + stride;
+        int row_n = row, step_n = 0, last_n = 0, pos_n = 0, cell_n = 0;
+        if (next < items) {
+            enter(next, row_n, step_n, last_n);
+            pos_n = __ldg(a.positions + row_n);
+            cell_n = __ldg(a.slots + row_n);
+        }
+        __syncwarp();
 #pragma unroll
-    for (int u = 0; u < N; ++u) { cs[u] = s_cs[d0 + u]; sn[u] = s_sn[d0 + u]; }
-    const int page = stored ? slot / a.page_size : 0, in_page = stored ? slot - page * a.page_size : 0;
-    for (int base = first; base < total; base += AT_ONCE * step) {
-        if (base > first) load(base);
+        for (int u = 0; u < AP; ++u) angle_cos_sin(pos, theta[u], s_ang[warp][0][lane + 32 * u], s_ang[warp][1][lane + 32 * u]);
+        __syncwarp();
+        float cs[N], sn[N];
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            if (base + u * step >= total) break;
-            const int it = base + u * step + lane / LPR;
+        for (int u = 0; u < N; u += 4) {
+            const float4 c4 = *reinterpret_cast<const float4*>(&s_ang[warp][0][d0 + u]), s4 = *reinterpret_cast<const float4*>(&s_ang[warp][1][d0 + u]);
+            cs[u] = c4.x; cs[u + 1] = c4.y; cs[u + 2] = c4.z; cs[u + 3] = c4.w;
+            sn[u] = s4.x; sn[u + 1] = s4.y; sn[u + 2] = s4.z; sn[u + 3] = s4.w;
+        }
+        const bool stored = cell >= 0 && cell < (int64_t)a.n_pages * a.page_size;
+        const int page = stored ? cell / a.page_size : 0, in_page = stored ? cell - page * a.page_size : 0;
+        T* q_row = static_cast<T*>(a.q_out) + (int64_t)row * a.Hq * D + d0;
+        const int64_t kv_row = ((int64_t)page * a.Hk * a.page_size + in_page) * D + d0, kv_head = (int64_t)a.page_size * D;
+#pragma unroll 1
+        for (; step < last; ++step) {
+            fetch();
+            asm volatile("cp.async.wait_group %0;" ::"n"(APP_STAGES - 1) : "memory");
+            uint4 xl, xh;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(xl.x), "=r"(xl.y), "=r"(xl.z), "=r"(xl.w) : "r"(slot_at) : "memory");
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(xh.x), "=r"(xh.y), "=r"(xh.z), "=r"(xh.w) : "r"(slot_at + CHUNK) : "memory");
+            slot_at = slot_at == ring + (APP_STAGES - 1) * STAGE ? ring : slot_at + STAGE;
+            const int it = step * RPW + group;
             const bool is_q = it < a.Hq, is_v = it >= a.Hq + a.Hk;
-            float x[N], y[N], wl[N], wh[N];
-            V::unpack(xl[u], x);
-            V::unpack(xh[u], y);
-            load_gain(static_cast<const T*>(is_q ? a.wq : a.wk), d0, wl, wh, HALF);
-            float ssq = 0.f;
+            if (step * RPW < a.Hq + a.Hk) {   // some head of the step is not a value
+                float x[N], y[N];
+                V::unpack(xl, x);
+                V::unpack(xh, y);
+                float ssq = 0.f;
 #pragma unroll
-            for (int e = 0; e < N; ++e) ssq = fmaf(x[e], x[e], fmaf(y[e], y[e], ssq));
-            const float r = rsqrtf(row_sum<LPR>(ssq) * (1.f / D) + a.eps);
-            if (!is_v) {
+                for (int e = 0; e < N; ++e) ssq = fmaf(x[e], x[e], fmaf(y[e], y[e], ssq));
+                const float r = rsqrtf(row_sum<LPR>(ssq) * (1.f / D) + a.eps);
+                const float* gain = s_gain[is_q ? 0 : 1] + d0;
                 float ra[N], rc[N];
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float ya = x[e] * r * wl[e], yc = y[e] * r * wh[e];
-                    ra[e] = ya * cs[e] - yc * sn[e];
-                    rc[e] = yc * cs[e] + ya * sn[e];
+                for (int u = 0; u < N; u += 4) {
+                    const float4 wl = *reinterpret_cast<const float4*>(gain + u), wh = *reinterpret_cast<const float4*>(gain + HALF + u);
+                    const float l[4] = {wl.x, wl.y, wl.z, wl.w}, g[4] = {wh.x, wh.y, wh.z, wh.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float ya = x[u + e] * r * l[e], yc = y[u + e] * r * g[e];
+                        ra[u + e] = ya * cs[u + e] - yc * sn[u + e];
+                        rc[u + e] = yc * cs[u + e] + ya * sn[u + e];
+                    }
                 }
-                xl[u] = V::pack(ra);
-                xh[u] = V::pack(rc);
+                if (!is_v) {
+                    xl = V::pack(ra);
+                    xh = V::pack(rc);
+                }
             }
             if (it < total && (is_q || stored)) {
-                T* dst;
-                if (is_q) {
-                    dst = static_cast<T*>(a.q_out) + (row * a.Hq + it) * D;
-                } else {
-                    const int h = is_v ? it - a.Hq - a.Hk : it - a.Hq;
-                    dst = static_cast<T*>(is_v ? a.v_pool : a.k_pool) + (((int64_t)page * a.Hk + h) * a.page_size + in_page) * D;
-                }
-                *reinterpret_cast<uint4*>(dst + d0) = xl[u];
-                *reinterpret_cast<uint4*>(dst + d0 + HALF) = xh[u];
+                T* dst = is_q ? q_row + it * D : static_cast<T*>(is_v ? a.v_pool : a.k_pool) + kv_row + (is_v ? it - a.Hq - a.Hk : it - a.Hq) * kv_head;
+                *reinterpret_cast<uint4*>(dst) = xl;
+                *reinterpret_cast<uint4*>(dst + HALF) = xh;
             }
         }
+        if (next >= items) break;
+        item = next;
+        row = row_n; step = step_n; last = last_n; pos = pos_n; cell = cell_n;
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 template <typename T, int D>
 static cudaError_t append_t(const AppendArgs& a, cudaStream_t st) {
-    constexpr int HPW = 32 / ((D / 2) / Vec16<T>::N);
-    const int most = (a.Hq + 2 * a.Hk + APP_WARPS * HPW - 1) / (APP_WARPS * HPW);
-    int split = 1;   // few tokens: their heads over several CTAs
-    while (split < most && (int64_t)a.T * split < 148 * 4) ++split;
-    qk_norm_rope_append_kernel<T, D><<<dim3(a.T, split), APP_WARPS * 32, 0, st>>>(a);
+    constexpr int RPW = 32 / ((D / 2) / Vec16<T>::N);
+    const cudaError_t e = prepare_kernel(reinterpret_cast<const void*>(qk_norm_rope_append_kernel<T, D>), APP_RING);
+    if (e != cudaSuccess) return e;
+    // few tokens: their heads over several warps, until every SM has eight of them or a warp has one step
+    const int steps = (a.Hq + 2 * a.Hk + RPW - 1) / RPW;
+    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(steps, 148 * QKN_WARPS / a.T));
+    const int64_t ctas = ((int64_t)a.T * parts + QKN_WARPS - 1) / QKN_WARPS;
+    qk_norm_rope_append_kernel<T, D><<<(unsigned)std::min<int64_t>(ctas, 148 * 3), QKN_WARPS * 32, APP_RING, st>>>(a, parts);
     count_launches(1);
     return cudaGetLastError();
 }
