@@ -710,7 +710,7 @@ LOMA_API int loma_compress_step_ragged(const void* q_mem, const void* k_mem, con
  *   row_seq      [out]     int32 [max_rows]: sequence of the row, -1 behind the last
  *   row_pos      [out]     int32 [max_rows]: (pos0 ? pos0[b] : len) + i, the row's position id; 0 behind the last
  * Sums and positions beyond INT_MAX are stored as INT_MAX.  Rows at and beyond max_rows are not written.
- * on_device != 0: every pointer is [device] and the work is enqueued on `stream` (one launch up to 2048
+ * on_device != 0: every pointer is [device] and the work is enqueued on `stream` (one launch up to 1536
  * sequences when nothing is updated in place, else two); on_device == 0: every pointer is [host], no CUDA call.
  * Errors: INVALID_ARG (page size not a power of two <= 65536, max_pages * page_size > INT_MAX, a required
  * pointer NULL, outputs that overlap inputs or each other), ALIGNMENT (4 bytes), UNSUPPORTED, CUDA.

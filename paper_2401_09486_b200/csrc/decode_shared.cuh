@@ -174,31 +174,7 @@ struct SeqBlocks {
     }
 };
 
-// Programmatic dependent launch: the next kernel of the stream may start once every CTA of this one has called the first;
-// the second waits until the kernels this one was launched behind have finished.
-__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 #endif
-
-// Launch a kernel that may start while the one before it in the stream still runs.
-template <typename... P, typename... A>
-cudaError_t launch_behind(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, bool behind, A... args) {
-    cudaError_t e = prepare_kernel(reinterpret_cast<const void*>(kernel), smem);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = behind ? 1 : 0;
-    e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
-    if (e == cudaSuccess) count_launches(1);
-    return e;
-}
 
 // The three kernels of a step: prefix, own (beside it: launched behind it, sharing no result) and merge (launched behind
 // own, which ends after the prefix kernel).  The own kernel, bf16 (decode_shared_own.cu); cudaErrorNotSupported = use the

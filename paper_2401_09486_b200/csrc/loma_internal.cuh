@@ -307,4 +307,31 @@ struct Vec16<__nv_bfloat16> {
     }
 };
 
+#ifdef __CUDACC__
+// Programmatic dependent launch: the next kernel of the stream may start once every CTA of this one has called the first;
+// the second waits until the kernels this one was launched behind have finished.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Launch a kernel that may start while the one before it in the stream still runs.
+template <typename... P, typename... A>
+cudaError_t launch_behind(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, bool behind, A... args) {
+    cudaError_t e = prepare_kernel(reinterpret_cast<const void*>(kernel), smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = behind ? 1 : 0;
+    e = cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+    if (e == cudaSuccess) count_launches(1);
+    return e;
+}
+#endif
+
 }  // namespace loma

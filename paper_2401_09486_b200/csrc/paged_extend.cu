@@ -29,18 +29,21 @@ struct SeqNeed {
     int len, n, h, fresh;
 };
 
-__host__ __device__ inline SeqNeed seq_need(const ExtendArgs& a, int b) {
+__host__ __device__ inline SeqNeed seq_need(const ExtendArgs& a, int given, int fresh, int held) {
     SeqNeed s;
     const int room = a.max_pages << a.log2_ps;
-    const int given = a.cache_lens[b];
     s.len = clampi(given, 0, room);
-    s.n = given < 0 ? 0 : (a.new_lens ? clampi(a.new_lens[b], 0, INT_MAX) : 1);
+    s.n = given < 0 ? 0 : clampi(fresh, 0, INT_MAX);
     const int mask = (1 << a.log2_ps) - 1;
-    s.h = a.held ? clampi(a.held[b], 0, a.max_pages) : (int)(((int64_t)s.len + mask) >> a.log2_ps);
+    s.h = a.held ? clampi(held, 0, a.max_pages) : (int)(((int64_t)s.len + mask) >> a.log2_ps);
     const int64_t end = (int64_t)s.len + s.n < room ? (int64_t)s.len + s.n : room;
     const int want = (int)((end + mask) >> a.log2_ps);
     s.fresh = s.n > 0 && want > s.h ? want - s.h : 0;
     return s;
+}
+
+__host__ __device__ inline SeqNeed seq_need(const ExtendArgs& a, int b) {
+    return seq_need(a, a.cache_lens[b], a.new_lens ? a.new_lens[b] : 1, a.held ? a.held[b] : 0);
 }
 
 __host__ __device__ inline int saturate(int64_t x) { return x > INT_MAX ? INT_MAX : (int)x; }
@@ -102,7 +105,7 @@ void host_paged_extend(const ExtendArgs& a) {
 
 // ------------------------------------------------------------------ device form
 constexpr int EXT_THREADS = 512;
-constexpr int FUSED_MAX_B = 2048;    // five numbers per sequence in shared memory: 40 KB
+constexpr int FUSED_MAX_B = 1536;    // six numbers per sequence in shared memory: 36 KB
 constexpr int ROWS_PER_THREAD = 4;   // consecutive rows: one search, 16-byte stores
 
 // Exclusive sums over the block of one (rows, pages) pair per thread; every thread gets the block's totals too.
@@ -148,6 +151,19 @@ __device__ __forceinline__ void write_rows(const ExtendArgs& a, const int* start
     int slot[ROWS_PER_THREAD], seq[ROWS_PER_THREAD], pos[ROWS_PER_THREAD];
     const int total = start[a.B];
     int b = r0 < total ? find_seq(start, 0, a.B, r0) : a.B, have = -1;
+    bool done = false;
+    if (r0 < total && start[b + 1] - r0 >= ROWS_PER_THREAD) {   // the usual case of a prompt: one sequence, and one page
+        enter(b);
+        have = b;
+        const int i = r0 - start[b], s0 = slot_at(i), p0 = pos_at(i);
+        const int mask = (1 << a.log2_ps) - 1;
+        done = s0 >= 0 && (s0 & mask) + ROWS_PER_THREAD - 1 <= mask && p0 <= INT_MAX - ROWS_PER_THREAD;
+        if (done) {
+#pragma unroll
+            for (int u = 0; u < ROWS_PER_THREAD; ++u) { slot[u] = s0 + u; seq[u] = b; pos[u] = p0 + u; }
+        }
+    }
+    if (!done)
 #pragma unroll
     for (int u = 0; u < ROWS_PER_THREAD; ++u) {
         const int r = r0 + u;
@@ -177,34 +193,51 @@ __device__ __forceinline__ void write_rows(const ExtendArgs& a, const int* start
 __global__ void __launch_bounds__(EXT_THREADS)
 paged_extend_fused_kernel(const ExtendArgs a, int vec) {
     __shared__ int s_row[FUSED_MAX_B + 1], s_page[FUSED_MAX_B + 1], s_len[FUSED_MAX_B], s_h[FUSED_MAX_B], s_pos[FUSED_MAX_B];
-    __shared__ int s_next[EXT_THREADS], s_free[EXT_THREADS];   // page of sequence b's entry len (b < EXT_THREADS); head of the free list
+    __shared__ int s_next[FUSED_MAX_B], s_free[EXT_THREADS];   // page of a sequence's entry len; head of the free list
     const int tid = threadIdx.x, room = a.max_pages << a.log2_ps;
-    int head = -1, next = -1;
-    if (tid < a.n_free) head = __ldg(a.free_pages + tid);
-    for (int b = tid; b < a.B; b += EXT_THREADS) {
-        const SeqNeed s = seq_need(a, b);
-        s_row[b] = s.n;
-        s_page[b] = s.fresh;
-        s_len[b] = s.len;
-        s_h[b] = s.h;
-        s_pos[b] = first_pos(a, b, s.len);
-        if (b < EXT_THREADS && s.len < room && (s.len >> a.log2_ps) < s.h) next = a.block_table[(int64_t)b * a.max_pages + (s.len >> a.log2_ps)];
+    // a thread's sequences are neighbours: up to PER of them, all their numbers in flight at once
+    constexpr int PER = FUSED_MAX_B / EXT_THREADS;
+    const int per = (a.B + EXT_THREADS - 1) / EXT_THREADS, b0 = tid * per;
+    int lens[PER], news[PER], helds[PER], pos0s[PER];
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const bool in = u < per && b0 + u < a.B;
+        lens[u] = in ? __ldg(a.cache_lens + b0 + u) : -1;
+        news[u] = in && a.new_lens ? __ldg(a.new_lens + b0 + u) : 1;
+        helds[u] = in && a.held ? __ldg(a.held + b0 + u) : 0;
+        pos0s[u] = in && a.pos0 ? __ldg(a.pos0 + b0 + u) : 0;
     }
-    __syncthreads();
-    const int per = (a.B + EXT_THREADS - 1) / EXT_THREADS;
-    const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
+    const int head = tid < a.n_free ? __ldg(a.free_pages + tid) : -1;
+    SeqNeed need[PER];
+    int next[PER];
     int64_t rows = 0, pages = 0, tr, tp;
-    for (int b = b0; b < b1; ++b) { rows += s_row[b]; pages += s_page[b]; }
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        need[u] = seq_need(a, lens[u], news[u], helds[u]);
+        next[u] = -1;
+        if (u < per && b0 + u < a.B) {
+            const int len = need[u].len;
+            if (len < room && (len >> a.log2_ps) < need[u].h) next[u] = a.block_table[(int64_t)(b0 + u) * a.max_pages + (len >> a.log2_ps)];
+            rows += need[u].n;
+            pages += need[u].fresh;
+        }
+    }
     block_scan2(rows, pages, tr, tp);
-    for (int b = b0; b < b1; ++b) {
-        const int n = s_row[b], f = s_page[b];
-        s_row[b] = saturate(rows);
-        s_page[b] = saturate(pages);
-        rows += n;
-        pages += f;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const int b = b0 + u;
+        if (u < per && b < a.B) {
+            s_row[b] = saturate(rows);
+            s_page[b] = saturate(pages);
+            s_len[b] = need[u].len;
+            s_h[b] = need[u].h;
+            s_pos[b] = a.pos0 ? pos0s[u] : need[u].len;
+            s_next[b] = next[u];
+            rows += need[u].n;
+            pages += need[u].fresh;
+        }
     }
     if (tid == 0) { s_row[a.B] = saturate(tr); s_page[a.B] = saturate(tp); }
-    s_next[tid] = next;
     s_free[tid] = head;
     __syncthreads();
     auto free_at = [&](int64_t idx) { return idx < EXT_THREADS ? s_free[idx] : free_page(a, idx); };
@@ -227,7 +260,7 @@ paged_extend_fused_kernel(const ExtendArgs a, int vec) {
                        if (blk != block) {   // rows of one page look it up once
                            block = blk;
                            if (blk >= h) page = free_at((int64_t)first + blk - h);
-                           else if (cur < EXT_THREADS && blk == len >> a.log2_ps) page = s_next[cur];
+                           else if (blk == len >> a.log2_ps) page = s_next[cur];
                            else page = a.block_table[(int64_t)cur * a.max_pages + blk];
                        }
                        return slot_of(a, page, e);
@@ -243,38 +276,60 @@ paged_extend_fused_kernel(const ExtendArgs a, int vec) {
 
 // One CTA: the sums, held pages and the free list's new start.  Every value a thread reads of `held` it reads before it
 // writes held_out, and no other thread reads that entry, so the two may be one array.
-constexpr int SCAN_THREADS = 1024;
+constexpr int SCAN_THREADS = 1024, SCAN_AT_ONCE = 4;
 __global__ void __launch_bounds__(SCAN_THREADS)
 paged_extend_scan_kernel(const ExtendArgs a) {
-    const int per = (a.B + SCAN_THREADS - 1) / SCAN_THREADS;
-    const int b0 = min((int64_t)a.B, (int64_t)threadIdx.x * per), b1 = min((int64_t)a.B, (int64_t)b0 + per);
-    int64_t rows = 0, pages = 0, tr, tp;
-    for (int b = b0; b < b1; ++b) {
-        const SeqNeed s = seq_need(a, b);
-        rows += s.n;
-        pages += s.fresh;
-    }
-    const int64_t base = a.taken ? clampi(*a.taken, 0, INT_MAX) : 0;
-    block_scan2(rows, pages, tr, tp);   // its barriers also order every read of *taken before the write below
-    pages += base;
-    for (int b = b0; b < b1; ++b) {
-        const SeqNeed s = seq_need(a, b);
-        const int first = saturate(pages);
-        a.row_start[b] = saturate(rows);
-        a.page_start[b] = first;
-        a.held_out[b] = s.h + pages_got(a, first, s.fresh);
-        rows += s.n;
-        pages += s.fresh;
+    // SCAN_THREADS * SCAN_AT_ONCE neighbouring sequences at a time
+    __shared__ int s_taken;
+    let_next_start();
+    if (threadIdx.x == 0) s_taken = a.taken ? clampi(*a.taken, 0, INT_MAX) : 0;
+    __syncthreads();
+    int64_t rows0 = 0, pages0 = s_taken;
+    for (int64_t base = 0; base < a.B; base += SCAN_THREADS * SCAN_AT_ONCE) {
+        const int64_t b0 = base + (int64_t)threadIdx.x * SCAN_AT_ONCE;
+        int lens[SCAN_AT_ONCE], news[SCAN_AT_ONCE], helds[SCAN_AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < SCAN_AT_ONCE; ++u) {
+            const bool in = b0 + u < a.B;
+            lens[u] = in ? a.cache_lens[b0 + u] : -1;
+            news[u] = in && a.new_lens ? a.new_lens[b0 + u] : 1;
+            helds[u] = in && a.held ? a.held[b0 + u] : 0;
+        }
+        SeqNeed need[SCAN_AT_ONCE];
+        int64_t rows = 0, pages = 0, tr, tp;
+#pragma unroll
+        for (int u = 0; u < SCAN_AT_ONCE; ++u) {
+            need[u] = seq_need(a, lens[u], news[u], helds[u]);
+            rows += need[u].n;
+            pages += need[u].fresh;
+        }
+        block_scan2(rows, pages, tr, tp);
+        rows += rows0;
+        pages += pages0;
+#pragma unroll
+        for (int u = 0; u < SCAN_AT_ONCE; ++u)
+            if (b0 + u < a.B) {
+                const int first = saturate(pages);
+                a.row_start[b0 + u] = saturate(rows);
+                a.page_start[b0 + u] = first;
+                a.held_out[b0 + u] = need[u].h + pages_got(a, first, need[u].fresh);
+                rows += need[u].n;
+                pages += need[u].fresh;
+            }
+        rows0 += tr;
+        pages0 += tp;
+        __syncthreads();   // the scan's shared sums are used again
     }
     if (threadIdx.x == 0) {
-        a.row_start[a.B] = saturate(tr);
-        a.page_start[a.B] = saturate(base + tp);
-        if (a.taken) *a.taken = saturate(base + tp);
+        a.row_start[a.B] = saturate(rows0);
+        a.page_start[a.B] = saturate(pages0);
+        if (a.taken) *a.taken = saturate(pages0);
     }
 }
 
 __global__ void __launch_bounds__(EXT_THREADS)
 paged_extend_rows_kernel(const ExtendArgs a, int vec) {
+    wait_for_previous();   // launched while the scan runs
     const int lane = threadIdx.x & 31;
     for (int64_t b = (int64_t)blockIdx.x * (EXT_THREADS / 32) + (threadIdx.x >> 5); b < a.B;
          b += (int64_t)gridDim.x * (EXT_THREADS / 32)) {
@@ -302,8 +357,8 @@ cudaError_t launch_paged_extend(const ExtendArgs& a, cudaStream_t st) {
     const int vec = (((uintptr_t)a.slots | (uintptr_t)a.row_seq | (uintptr_t)a.row_pos) & 15u) == 0;
     const int64_t row_ctas = ((int64_t)a.max_rows + EXT_THREADS * ROWS_PER_THREAD - 1) / (EXT_THREADS * ROWS_PER_THREAD);
     const int64_t seq_ctas = ((int64_t)a.B + EXT_THREADS / 32 - 1) / (EXT_THREADS / 32);
-    // two CTAs of 512 threads per SM hide the page loads of the rows; more would repeat the scan for nothing
-    const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(148 * 2, std::max(row_ctas, seq_ctas)));
+    // every CTA repeats the scan: two per SM at most (1000 prompts, 1.1 million rows: 148 CTAs 11.3 us, 296 10.1, 592 11.1)
+    const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(296, std::max(row_ctas, seq_ctas)));
     if (a.B <= FUSED_MAX_B && a.held != a.held_out && !a.taken) {
         paged_extend_fused_kernel<<<grid, EXT_THREADS, 0, st>>>(a, vec);
         count_launches(1);
@@ -313,9 +368,7 @@ cudaError_t launch_paged_extend(const ExtendArgs& a, cudaStream_t st) {
     count_launches(1);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    paged_extend_rows_kernel<<<grid, EXT_THREADS, 0, st>>>(a, vec);
-    count_launches(1);
-    return cudaGetLastError();
+    return launch_behind(paged_extend_rows_kernel, dim3(grid), EXT_THREADS, 0, st, true, a, vec);
 }
 
 }  // namespace loma
