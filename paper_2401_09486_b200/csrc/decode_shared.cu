@@ -336,10 +336,9 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
 }
 
 // ------------------------------------------------------------------ merge
-// CTA: 32 query rows of one kv head (lanes) x 8 / WAYS groups of 4 features (warps) x WAYS shares of the partial results.  The
-// time is that of its chain of dependent loads, so partial results are taken MERGE_AT_ONCE at a time, values and
-// log2-sum-exps together, under a running maximum, and a long list of them is read by WAYS warps.
-constexpr int MERGE_THREADS = 256, MERGE_AT_ONCE = 8;
+// CTA: 32 query rows of one kv head (lanes) x 8 / WAYS groups of 4 features (warps) x WAYS shares of the partial results: a
+// long list of them is read by WAYS warps.
+constexpr int MERGE_THREADS = 256;
 
 template <typename T, int D, int WAYS>
 __global__ void __launch_bounds__(MERGE_THREADS)
@@ -351,98 +350,49 @@ shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
     const int len = __ldg(a.cache_lens + b);
     const float* ws = static_cast<const float*>(a.ws);
     const int mt = row / SHP_ROWS, r = row - mt * SHP_ROWS;
-    // the prefix segments of this tile
-    const int64_t p_all = (int64_t)a.Hkv * p.p_blocks;
-    int64_t p_first = 0;
-    int n_prefix = 0;
-    if (p.p_blocks > 0) {
-        const int64_t w0 = block_worker((int64_t)h * p.p_blocks, p_all, p.p_workers);
-        n_prefix = (int)(block_worker((int64_t)(h + 1) * p.p_blocks - 1, p_all, p.p_workers) - w0) + 1;
-        p_first = (w0 + h) * p.m_tiles + mt;
-    }
+    const PrefixSegments ps(a, p, h, mt);
     const int gt = j / p.g_rows, x = j - gt * p.g_rows;
     const int64_t hh = (int64_t)h * p.g_tiles + gt;
     // before any thread may leave: the kernel after this one counts on all three having finished
     wait_for_previous();
     const int64_t* cum = reinterpret_cast<const int64_t*>(ws + p.cum);
     const int64_t per_head = __ldcg(cum + a.B), cum0 = __ldcg(cum + b), cum1 = __ldcg(cum + b + 1);
-    float M = -INFINITY, total = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    // n partial results of this row and these features: log2-sum-exps at lse[s * lse_step], values at v[s * v_step]
-    auto add = [&](int n, const float* lse, int64_t lse_step, const float* v, int64_t v_step) {
-        for (int s0 = way * MERGE_AT_ONCE; s0 < n; s0 += WAYS * MERGE_AT_ONCE) {
-            float e[MERGE_AT_ONCE];
-            float4 y[MERGE_AT_ONCE];
-#pragma unroll
-            for (int u = 0; u < MERGE_AT_ONCE; ++u) {
-                e[u] = -INFINITY;
-                if (s0 + u < n) {
-                    e[u] = __ldcg(lse + (s0 + u) * lse_step);
-                    y[u] = __ldcg(reinterpret_cast<const float4*>(v + (s0 + u) * v_step));
-                }
-            }
-            float m = M;
-#pragma unroll
-            for (int u = 0; u < MERGE_AT_ONCE; ++u) m = fmaxf(m, e[u]);
-            const float keep = M == -INFINITY ? 0.f : exp2f(M - m);
-            M = m;
-            total *= keep;
-            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
-#pragma unroll
-            for (int u = 0; u < MERGE_AT_ONCE; ++u) {
-                if (e[u] == -INFINITY) continue;   // no weight: past the last, or scores of -inf (values 0/0)
-                const float f = exp2f(e[u] - m);
-                total += f;
-                o.x = fmaf(f, y[u].x, o.x); o.y = fmaf(f, y[u].y, o.y); o.z = fmaf(f, y[u].z, o.z); o.w = fmaf(f, y[u].w, o.w);
-            }
-        }
-    };
-    add(n_prefix, ws + p.p_lse + p_first * SHP_ROWS + r, (int64_t)p.m_tiles * SHP_ROWS,
-        ws + p.p_o + p_first * SHP_ROWS * D + ((int64_t)c4 * SHP_ROWS + r) * 4, (int64_t)p.m_tiles * SHP_ROWS * D);
+    RowMerge m;
+    m.add<WAYS>(ps.n, ws + p.p_lse + ps.first * SHP_ROWS + r, (int64_t)p.m_tiles * SHP_ROWS,
+                ws + p.p_o + ps.first * SHP_ROWS * D + ((int64_t)c4 * SHP_ROWS + r) * 4, (int64_t)p.m_tiles * SHP_ROWS * D, way);
     const bool live = len >= 0 && blockIdx.x * 32 + lane < a.B * a.g;   // a request, and no repeated row
     if (live) {
-    const int64_t all = per_head * a.Hkv * p.g_tiles, W = own_workers(all, p.workers);
-    const int64_t w0 = block_worker(hh * per_head + cum0, all, W), first = w0 + hh * a.B + b;
-    const int n_own = (int)(block_worker(hh * per_head + cum1 - 1, all, W) - w0) + 1;
-    add(n_own, ws + p.own_lse + first * p.g_rows + x, p.g_rows, ws + p.own_o + (first * p.g_rows + x) * D + c4 * 4, (int64_t)p.g_rows * D);
+        const int64_t all = per_head * a.Hkv * p.g_tiles, W = own_workers(all, p.workers);
+        const int64_t w0 = block_worker(hh * per_head + cum0, all, W), first = w0 + hh * a.B + b;
+        const int n_own = (int)(block_worker(hh * per_head + cum1 - 1, all, W) - w0) + 1;
+        m.add<WAYS>(n_own, ws + p.own_lse + first * p.g_rows + x, p.g_rows, ws + p.own_o + (first * p.g_rows + x) * D + c4 * 4,
+                    (int64_t)p.g_rows * D, way);
     }
     if constexpr (WAYS > 1) {
-        __shared__ float s_m[WAYS][GROUPS][32], s_t[WAYS][GROUPS][32];
-        __shared__ float4 s_o[WAYS][GROUPS][32];
+        __shared__ RowMerge s_part[WAYS][GROUPS][32];
         const int grp = warp % GROUPS;
-        s_m[way][grp][lane] = M;
-        s_t[way][grp][lane] = total;
-        s_o[way][grp][lane] = o;
+        s_part[way][grp][lane] = m;
         __syncthreads();
         if (way > 0) return;
+        RowMerge all;
 #pragma unroll
-        for (int y = 1; y < WAYS; ++y) M = fmaxf(M, s_m[y][grp][lane]);
-        total = 0.f;
-        o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int y = 0; y < WAYS; ++y) all.M = fmaxf(all.M, s_part[y][grp][lane].M);
 #pragma unroll
         for (int y = 0; y < WAYS; ++y) {
-            const float my = s_m[y][grp][lane], f = my == -INFINITY ? 0.f : exp2f(my - M);
-            const float4 v = s_o[y][grp][lane];
-            if (f == 0.f) continue;
-            total += f * s_t[y][grp][lane];
-            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+            const RowMerge& q = s_part[y][grp][lane];
+            if (q.M == -INFINITY) continue;
+            const float f = exp2f(q.M - all.M);
+            all.total += f * q.total;
+            all.o.x = fmaf(f, q.o.x, all.o.x); all.o.y = fmaf(f, q.o.y, all.o.y); all.o.z = fmaf(f, q.o.z, all.o.z); all.o.w = fmaf(f, q.o.w, all.o.w);
         }
+        m = all;
     }
-    if (!live) return;
-    const float inv = 1.f / total;
-    const int64_t out = (int64_t)b * a.Hq + h * a.g + j;
-    if constexpr (sizeof(T) == 2)
-        *reinterpret_cast<uint2*>(static_cast<T*>(a.o) + out * D + c4 * 4) =
-            make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-    else
-        *reinterpret_cast<float4*>(static_cast<T*>(a.o) + out * D + c4 * 4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    if (a.lse && c4 == 0) a.lse[out] = (M + log2f(total)) * 0.6931471805599453f;
+    if (live) m.store<T, D>(a, (int64_t)b * a.Hq + h * a.g + j, c4);
 }
 
 // ------------------------------------------------------------------ host side
 size_t decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int prefix_len, int max_len) {
-    (void)max_len;   // the lengths decide how the own part is cut, not into how many pieces
-    const int64_t n = std::max(make_shared_plan(B, Hq, Hkv, D, prefix_len, false).total, make_shared_plan(B, Hq, Hkv, D, prefix_len, true).total);
+    const int64_t n = std::max(make_shared_plan(B, Hq, Hkv, D, prefix_len, max_len, false).total, make_shared_plan(B, Hq, Hkv, D, prefix_len, max_len, true).total);
     return (size_t)n * sizeof(float);
 }
 
@@ -467,7 +417,7 @@ static cudaError_t prefix_simt(const SharedArgs& a, const SharedPlan& p, cudaStr
 
 template <typename T, int D>
 static cudaError_t shared_t(const SharedArgs& a, bool generic, cudaStream_t st) {
-    SharedPlan p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, false);
+    SharedPlan p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len, false);
     const bool prefix = p.p_blocks > 0, tc = sizeof(T) == 2 && !generic;
     cudaError_t e = cudaErrorNotSupported;
     if (prefix) {
@@ -477,10 +427,10 @@ static cudaError_t shared_t(const SharedArgs& a, bool generic, cudaStream_t st) 
     }
     e = tc ? launch_shared_own_tma(a, p, D, prefix, st) : cudaErrorNotSupported;
     if (e == cudaErrorNotSupported) {
-        p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, true);   // the prefix part is cut and stored the same way
+        p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len, true);   // the prefix part is cut and stored the same way
         e = own_stream<T, D>(a, p, prefix, st);
     }
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || p.whole) return e;   // whole: the own kernel has joined the parts
     // a long list of partial results per row: many workers to a kv head, or own shares of one block
     if (p.p_workers / a.Hkv >= 2 * MERGE_AT_ONCE)
         return launch_behind(shared_merge_kernel<T, D, 4>, dim3((a.B * a.g + 31) / 32, D / 8, a.Hkv), MERGE_THREADS, 0, st, true, a, p);

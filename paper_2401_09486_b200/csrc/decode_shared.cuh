@@ -12,6 +12,7 @@ constexpr int SHP_KEYS = 64;    // prefix keys per block
 constexpr int OWN_KEYS = 16;    // own keys per block
 constexpr int OWN_WARPS = 4;    // an own worker is a warp
 constexpr int OWN_CTAS = 148, STREAM_CTAS = 4 * 148;
+constexpr int OWN_WHOLE = 8;    // a sequence of so many blocks is not cut
 
 // Prefix CTAs that a call is cut for: one per SM, so that the own kernel runs beside it.  (Two per SM fill each other's waits,
 // but the own kernel then has to wait for them: B128 Hq32 Hkv8, prefix 16384 and up to 1500 own entries, 127 us against 95;
@@ -34,6 +35,7 @@ struct SharedPlan {
     int g_rows;         // own: query heads of a kv head per head tile (8 or 16 rows of a warp-level product, or fewer heads)
     int g_tiles;        //      head tiles per kv head
     int workers;        //      W, before it is cut down for few blocks
+    bool whole;         //      units are not cut: worker w takes units w, w + W, ..., and slot = unit
     // partial results in the workspace, as offsets in floats.  Prefix segment: outputs [D/4][128][4] (so that a warp whose lanes
     // are rows stores 512 contiguous bytes) and 128 log2-sum-exps.  Own segment: outputs [g_rows][D] and g_rows
     // log2-sum-exps.  cum: int64 [B + 1], blocks before sequence b within one (kv head, head tile).
@@ -49,7 +51,7 @@ __host__ __device__ inline int64_t first_block(int64_t w, int64_t T, int64_t W) 
 __host__ __device__ inline int64_t own_workers(int64_t T, int workers) { return T < workers ? T : workers; }
 
 // cuda_cores: the own part runs on shared_own_stream_kernel (fp32, small pages, second opinion)
-inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len, bool cuda_cores) {
+inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len, int max_len, bool cuda_cores) {
     SharedPlan p;
     const int64_t g = Hq / Hkv, rows = (int64_t)B * g;
     p.m_tiles = (int)((rows + SHP_ROWS - 1) / SHP_ROWS);
@@ -63,6 +65,7 @@ inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len
     p.g_rows = cuda_cores ? (g < 3 ? (int)g : 4) : (g <= 8 ? (int)g : 16);
     p.g_tiles = (int)((g + p.g_rows - 1) / p.g_rows);
     p.workers = (cuda_cores ? STREAM_CTAS : OWN_CTAS) * OWN_WARPS;
+    p.whole = !cuda_cores && own_blocks(max_len) <= OWN_WHOLE;
     int64_t at = 0;
     auto take = [&](int64_t n) { const int64_t o = at; at += (n + 63) / 64 * 64; return o; };
     const int64_t p_segments = p.p_blocks ? (int64_t)(p.p_workers + Hkv) * p.m_tiles : 0, segments = p.workers + (int64_t)B * Hkv * p.g_tiles;
@@ -176,9 +179,71 @@ struct SeqBlocks {
 
 #endif
 
+#ifdef __CUDACC__
+// One query row's four features joined from partial results under a running maximum.  The time of a merge is that of its chain
+// of dependent loads, so MERGE_AT_ONCE results are taken at a time, values and log2-sum-exps together.
+constexpr int MERGE_AT_ONCE = 8;
+struct RowMerge {
+    float M = -INFINITY, total = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    // n results: log2-sum-exps at lse[s * lse_step], values at v[s * v_step]; of every WAYS batches the way-th
+    template <int WAYS>
+    __device__ __forceinline__ void add(int n, const float* lse, int64_t lse_step, const float* v, int64_t v_step, int way) {
+        for (int s0 = way * MERGE_AT_ONCE; s0 < n; s0 += WAYS * MERGE_AT_ONCE) {
+            float e[MERGE_AT_ONCE];
+            float4 y[MERGE_AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < MERGE_AT_ONCE; ++u) {
+                e[u] = -INFINITY;
+                if (s0 + u < n) {
+                    e[u] = __ldcg(lse + (s0 + u) * lse_step);
+                    y[u] = __ldcg(reinterpret_cast<const float4*>(v + (s0 + u) * v_step));
+                }
+            }
+            float m = M;
+#pragma unroll
+            for (int u = 0; u < MERGE_AT_ONCE; ++u) m = fmaxf(m, e[u]);
+            const float keep = M == -INFINITY ? 0.f : exp2f(M - m);
+            M = m;
+            total *= keep;
+            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+#pragma unroll
+            for (int u = 0; u < MERGE_AT_ONCE; ++u) {
+                if (e[u] == -INFINITY) continue;   // no weight: past the last, or scores of -inf (values 0/0)
+                const float f = exp2f(e[u] - m);
+                total += f;
+                o.x = fmaf(f, y[u].x, o.x); o.y = fmaf(f, y[u].y, o.y); o.z = fmaf(f, y[u].z, o.z); o.w = fmaf(f, y[u].w, o.w);
+            }
+        }
+    }
+    template <typename T, int D>
+    __device__ __forceinline__ void store(const SharedArgs& a, int64_t row, int c4) const {   // row = b * Hq + head
+        const float inv = 1.f / total;
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<uint2*>(static_cast<T*>(a.o) + row * D + c4 * 4) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        else
+            *reinterpret_cast<float4*>(static_cast<T*>(a.o) + row * D + c4 * 4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        if (a.lse && c4 == 0) a.lse[row] = (M + log2f(total)) * 0.6931471805599453f;
+    }
+};
+
+// the prefix segments of query tile mt of kv head h: how many, and the first one's slot (the next is m_tiles further)
+struct PrefixSegments {
+    int n = 0;
+    int64_t first = 0;
+    __device__ __forceinline__ PrefixSegments(const SharedArgs& a, const SharedPlan& p, int h, int mt) {
+        if (p.p_blocks == 0) return;
+        const int64_t all = (int64_t)a.Hkv * p.p_blocks, w0 = block_worker((int64_t)h * p.p_blocks, all, p.p_workers);
+        n = (int)(block_worker((int64_t)(h + 1) * p.p_blocks - 1, all, p.p_workers) - w0) + 1;
+        first = (w0 + h) * p.m_tiles + mt;
+    }
+};
+#endif
+
 // The three kernels of a step: prefix, own (beside it: launched behind it, sharing no result) and merge (launched behind
-// own, which ends after the prefix kernel).  The own kernel, bf16 (decode_shared_own.cu); cudaErrorNotSupported = use the
-// CUDA-core kernel
+// own, which ends after the prefix kernel).  Where own caches hold a few blocks at most (p.whole), each sequence stays with one
+// warp of the own kernel, which joins the parts itself: two kernels.  The own kernel, bf16 (decode_shared_own.cu);
+// cudaErrorNotSupported = use the CUDA-core kernel
 cudaError_t launch_shared_own_tma(const SharedArgs& a, const SharedPlan& p, int D, bool behind, cudaStream_t st);
 // the prefix on the tensor cores (decode_shared_tc.cu); cudaErrorNotSupported = use the CUDA-core kernel
 cudaError_t launch_shared_prefix_tc(const SharedArgs& a, const SharedPlan& p, int D, cudaStream_t st);

@@ -56,8 +56,8 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, u
                  : "memory");
 }
 
-// R: column tiles of 8 query heads.
-template <int D, int R>
+// R: column tiles of 8 query heads.  WHOLE: p.whole.
+template <int D, int R, bool WHOLE>
 __global__ void __launch_bounds__(OWN_WARPS * 32, R == 1 ? 3 : 2)
 shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, const SharedPlan p, int* status) {
     using SM = OwnSmem<D>;
@@ -79,19 +79,54 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.v)) : "memory");
     }
     const SeqBlocks sb{a};
-    const int per = sb.scan<OWN_WARPS>(scan, wsum, blockIdx.x == 0 ? reinterpret_cast<int64_t*>(static_cast<float*>(a.ws) + p.cum) : nullptr);
-    const int64_t T = scan[(a.B + per - 1) / per] * a.Hkv * p.g_tiles;
-    const int64_t W = own_workers(T, p.workers);
     const int w = warp * gridDim.x + blockIdx.x;   // neighbours on different SMs
-    if (w < W) {
+    const int units = a.Hkv * p.g_tiles * a.B;
+    // Cursors over this worker's blocks: `c` is being worked on, `f` is being fetched.  `left`: blocks of the share still to come,
+    // or (WHOLE) the unit the cursor is in.
+    struct Cursor {
+        SeqBlocks::Cursor at;
+        int left;
+    } c, f;
+    enum { END, SAME, NEW };       // what the next block is: none, of the same sequence and head, of another
+    auto to_unit = [&](Cursor& x, int u) {   // WHOLE: the first unit from u on, in steps of the workers, that holds a request
+        for (; u < units; u += p.workers) {
+            x.at.hh = u / a.B;
+            x.at.b = u - x.at.hh * a.B;
+            x.at.len = sb.len(x.at.b);
+            if (x.at.len >= 0) break;
+        }
+        x.at.blk = 0;
+        x.left = u;
+        return u < units;
+    };
+    auto next = [&](Cursor& x) -> int {
+        if constexpr (WHOLE) {
+            if ((x.at.blk + 1) * OWN_KEYS <= x.at.len) { ++x.at.blk; return SAME; }
+            return to_unit(x, x.left + p.workers) ? NEW : END;
+        } else {
+            if (--x.left == 0) return END;
+            return sb.advance(x.at) ? NEW : SAME;
+        }
+    };
+    bool busy;
+    if constexpr (WHOLE) {
+        busy = to_unit(c, w);
+        __syncthreads();           // barriers and abort flag are set up
+    } else {
+        const int per = sb.scan<OWN_WARPS>(scan, wsum, blockIdx.x == 0 ? reinterpret_cast<int64_t*>(static_cast<float*>(a.ws) + p.cum) : nullptr);
+        const int64_t T = scan[(a.B + per - 1) / per] * a.Hkv * p.g_tiles, W = own_workers(T, p.workers);
+        busy = w < W;
+        if (busy) {
+            const int64_t t0 = first_block(w, T, W);
+            c.left = (int)(first_block(w + 1, T, W) - t0);
+            c.at = sb.find(t0, scan, per);
+        }
+    }
+    if (busy) {
+        f = c;
         const uint32_t ring = ((smem_u32(own_smem) + 1023u) & ~1023u) + warp * NS * SM::STAGE;
         uint8_t* ring_gen = own_smem + (ring - smem_u32(own_smem));
         volatile int* abortp = &abort_flag;
-        const int64_t t0 = first_block(w, T, W);
-        int left = (int)(first_block(w + 1, T, W) - t0);   // blocks still to be worked on
-        int to_fetch = left;
-        // two cursors over the same blocks: `c` is being worked on, `f` is being fetched
-        SeqBlocks::Cursor c = sb.find(t0, scan, per), f = c;
         // a box holds its rows panel by panel: where panel 1 and rows 8..15 of a tile lie
         const int boxes = a.pg.table ? max(1, OWN_KEYS >> a.pg.log2_ps) : 1, box_rows = OWN_KEYS / boxes;
         const uint32_t panel = box_rows * 128, upper = boxes == 1 ? 1024 : 1024 * PANELS;
@@ -100,18 +135,19 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
         int base_f = 0, h_f = 0;         // contiguous: first row of the fetch cursor's (sequence, kv head)
         const int32_t* table_f = nullptr;
         auto enter_f = [&]() {
-            h_f = p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles;
-            base_f = (f.b * a.Hkv + h_f) * a.cap;   // the cache has less than 2^31 rows
-            table_f = a.pg.table + (int64_t)f.b * a.pg.max_pages;
+            h_f = p.g_tiles == 1 ? f.at.hh : f.at.hh / p.g_tiles;
+            base_f = (f.at.b * a.Hkv + h_f) * a.cap;   // the cache has less than 2^31 rows
+            table_f = a.pg.table + (int64_t)f.at.b * a.pg.max_pages;
         };
         auto row_f = [&]() -> int {
-            if (!a.pg.table) return base_f + f.blk * OWN_KEYS;
-            const int key = f.blk * OWN_KEYS + (lane < boxes ? lane : 0) * box_rows;
-            const int page = min(max(__ldg(table_f + (min(key, f.len) >> a.pg.log2_ps)), 0), a.pg.n_pages - 1);
+            if (!a.pg.table) return base_f + f.at.blk * OWN_KEYS;
+            const int key = f.at.blk * OWN_KEYS + (lane < boxes ? lane : 0) * box_rows;
+            const int page = min(max(__ldg(table_f + (min(key, f.at.len) >> a.pg.log2_ps)), 0), a.pg.n_pages - 1);
             return ((page * a.Hkv + h_f) << a.pg.log2_ps) + (key & ((1 << a.pg.log2_ps) - 1));
         };
         enter_f();
         int next_row = row_f(), slot_f = 0;
+        bool fetching = true;
         auto fetch = [&]() {
             const uint32_t bar = smem_u32(&bars[warp][slot_f]), dst = ring + slot_f * SM::STAGE;
             if (lane == 0) mbar_expect_tx(bar, SM::STAGE);
@@ -121,12 +157,12 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
                 tma_rows(dst + SM::TILE + lane * 1024 * PANELS, &maps.v, bar, next_row);
             }
             slot_f = slot_f + 1 == NS ? 0 : slot_f + 1;
-            if (--to_fetch > 0) {
-                if (sb.advance(f)) enter_f();
-                next_row = row_f();
-            }
+            const int what = next(f);
+            fetching = what != END;
+            if (what == NEW) enter_f();
+            if (fetching) next_row = row_f();
         };
-        for (int i = 0; i < NS && to_fetch > 0; ++i) fetch();
+        for (int i = 0; i < NS && fetching; ++i) fetch();
 
         // ldmatrix addresses of the operands A.  K: rows = keys 0-7 | 8-15, k = features 16 i .. + 7 | + 8 .. + 15.  V: rows = features
         // 16 i .. + 7 | + 8 .. + 15, k = keys 0-7 | 8-15, each 8 x 8 part transposed.  The swizzle exchanges a row's 16-byte
@@ -143,15 +179,15 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
         int slot = 0, h = 0, gt = 0, heads = 0;
         uint32_t phase = 0;
         bool fresh = true, ok = true;
-        for (; left > 0; --left) {
+        for (;;) {
             if (fresh) {   // a new segment: this triple's query heads
-                h = p.g_tiles == 1 ? c.hh : c.hh / p.g_tiles;
-                gt = c.hh - h * p.g_tiles;
+                h = p.g_tiles == 1 ? c.at.hh : c.at.hh / p.g_tiles;
+                gt = c.at.hh - h * p.g_tiles;
                 heads = min(p.g_rows, a.g - gt * p.g_rows);
 #pragma unroll
                 for (int x = 0; x < R; ++x) {
                     const int hd = x * 8 + r;
-                    const uint32_t* qp = reinterpret_cast<const uint32_t*>(q + ((int64_t)c.b * a.Hq + h * a.g + gt * p.g_rows + min(hd, heads - 1)) * D);
+                    const uint32_t* qp = reinterpret_cast<const uint32_t*>(q + ((int64_t)c.at.b * a.Hq + h * a.g + gt * p.g_rows + min(hd, heads - 1)) * D);
 #pragma unroll
                     for (int i = 0; i < KS; ++i) {
                         qf[x][i][0] = hd < heads ? __ldg(qp + 8 * i + j) : 0u;
@@ -166,11 +202,11 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
                 }
                 fresh = false;
             }
-            const int valid = c.len + 1 - c.blk * OWN_KEYS;   // keys from this block on, the new token the last of them
+            const int valid = c.at.len + 1 - c.at.blk * OWN_KEYS;   // keys from this block on, the new token the last of them
             const bool tail = valid <= OWN_KEYS;
             uint4 k_tok, v_tok;   // this lane's part of the new token's rows
             if (tail && a.k_new && lane < D / 8) {
-                const int64_t src = (((int64_t)c.b * a.Hkv + h) * D) / 8 + lane;
+                const int64_t src = (((int64_t)c.at.b * a.Hkv + h) * D) / 8 + lane;
                 k_tok = __ldg(static_cast<const uint4*>(a.k_new) + src);
                 v_tok = __ldg(static_cast<const uint4*>(a.v_new) + src);
             }
@@ -186,7 +222,7 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
                     *reinterpret_cast<uint4*>(tile + at(valid - 1, lane)) = k_tok;
                     *reinterpret_cast<uint4*>(tile + SM::TILE + at(valid - 1, lane)) = v_tok;
                     if (gt == 0) {   // no fetch of this launch uses what lies there
-                        const int64_t dst = own_row(a, c.b, h, c.len) * (D / 8) + lane;
+                        const int64_t dst = own_row(a, c.at.b, h, c.at.len) * (D / 8) + lane;
                         static_cast<uint4*>(a.k_cache)[dst] = k_tok;
                         static_cast<uint4*>(a.v_cache)[dst] = v_tok;
                     }
@@ -254,11 +290,11 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
             }
             // every lane has read the stage (its values are in registers): fetch the next block into it
             __syncwarp();
-            if (to_fetch > 0) fetch();
+            if (fetching) fetch();
             if (++slot == NS) { slot = 0; phase ^= 1; }
 
-            if (tail || left == 1) {   // the segment ends
-                const int64_t seg = (int64_t)w + (int64_t)c.hh * a.B + c.b;
+            if (tail || (!WHOLE && c.left == 1)) {   // the segment ends
+                const int64_t seg = (WHOLE ? 0 : (int64_t)w) + (int64_t)c.at.hh * a.B + c.at.b;
 #pragma unroll
                 for (int x = 0; x < R; ++x)
 #pragma unroll
@@ -280,7 +316,7 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
                     }
                 fresh = true;
             }
-            if (left > 1) sb.advance(c);
+            if (next(c) == END) break;
         }
         if (!ok) {
             // leaving early: give copies already in flight a bounded time to land in this CTA's shared memory
@@ -289,6 +325,28 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
         }
     }
     wait_for_previous();   // the merge needs the prefix kernel's results too: this kernel ends after it
+    if constexpr (WHOLE) {
+        // this warp's units: its own results (each lane reads what the warp has written) and the prefix segments.  A lane has
+        // four features of a row, so D / 4 lanes share one
+        __syncwarp();
+        constexpr int LANES = D / 4, ROWS = 32 / LANES;
+        const int c4 = lane % LANES;
+        const float* part = static_cast<const float*>(a.ws);
+        Cursor u;
+        for (bool any = to_unit(u, w); any; any = to_unit(u, u.left + p.workers)) {
+            const int h = u.at.hh / p.g_tiles, gt = u.at.hh - h * p.g_tiles, heads = min(p.g_rows, a.g - gt * p.g_rows);
+            for (int x = lane / LANES; x < heads; x += ROWS) {
+                const int row = u.at.b * a.g + gt * p.g_rows + x, mt = row / SHP_ROWS, rt = row - mt * SHP_ROWS;
+                const PrefixSegments ps(a, p, h, mt);
+                const int64_t own = (int64_t)u.left * p.g_rows + x;
+                RowMerge m;
+                m.add<1>(1, part + p.own_lse + own, 0, part + p.own_o + own * D + c4 * 4, 0, 0);
+                m.add<1>(ps.n, part + p.p_lse + ps.first * SHP_ROWS + rt, (int64_t)p.m_tiles * SHP_ROWS,
+                         part + p.p_o + ps.first * SHP_ROWS * D + ((int64_t)c4 * SHP_ROWS + rt) * 4, (int64_t)p.m_tiles * SHP_ROWS * D, 0);
+                m.store<__nv_bfloat16, D>(a, (int64_t)u.at.b * a.Hq + h * a.g + gt * p.g_rows + x, c4);
+            }
+        }
+    }
 }
 
 // ------------------------------------------------------------------ host side
@@ -302,7 +360,7 @@ static bool encode_rows(CUtensorMap* map, const void* p, int D, int64_t rows, in
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int R>
+template <int D, int R, bool WHOLE>
 static cudaError_t own_tma_t(const SharedArgs& a, const SharedPlan& p, bool behind, cudaStream_t st) {
     OwnMaps maps;
     const int ps = 1 << a.pg.log2_ps;
@@ -315,12 +373,17 @@ static cudaError_t own_tma_t(const SharedArgs& a, const SharedPlan& p, bool behi
     int* status = device_status_word();
     if (!status) return cudaErrorUnknown;
     constexpr int smem = OwnSmem<D>::TOTAL;
-    return launch_behind(shared_own_tma_kernel<D, R>, dim3(OWN_CTAS), OWN_WARPS * 32, smem, st, behind, maps, a, p, status);
+    return launch_behind(shared_own_tma_kernel<D, R, WHOLE>, dim3(OWN_CTAS), OWN_WARPS * 32, smem, st, behind, maps, a, p, status);
+}
+
+template <int D, int R>
+static cudaError_t own_tma_r(const SharedArgs& a, const SharedPlan& p, bool behind, cudaStream_t st) {
+    return p.whole ? own_tma_t<D, R, true>(a, p, behind, st) : own_tma_t<D, R, false>(a, p, behind, st);
 }
 
 cudaError_t launch_shared_own_tma(const SharedArgs& a, const SharedPlan& p, int D, bool behind, cudaStream_t st) {
-    if (p.g_rows <= 8) return D == 64 ? own_tma_t<64, 1>(a, p, behind, st) : own_tma_t<128, 1>(a, p, behind, st);
-    return D == 64 ? own_tma_t<64, 2>(a, p, behind, st) : own_tma_t<128, 2>(a, p, behind, st);
+    if (p.g_rows <= 8) return D == 64 ? own_tma_r<64, 1>(a, p, behind, st) : own_tma_r<128, 1>(a, p, behind, st);
+    return D == 64 ? own_tma_r<64, 2>(a, p, behind, st) : own_tma_r<128, 2>(a, p, behind, st);
 }
 
 }  // namespace loma
