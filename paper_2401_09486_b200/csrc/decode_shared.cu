@@ -12,7 +12,7 @@
 //            shared_own_stream_kernel on CUDA cores
 //   merge    one thread per query row and four features adds the parts in a fixed order (results repeat bit for bit)
 //
-// The prefix and the own kernel share no result, so the second starts beside the first (programmatic dependent launch) and
+// The own and the prefix kernel share no result, so the second starts beside the first (programmatic dependent launch) and
 // an HBM-bound stream runs under a tensor-bound product; the merge waits for both.
 #include <math.h>
 
@@ -153,7 +153,7 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
             if (t + 1 < t_end) sb.advance(c);
         }
     }
-    wait_for_previous();   // this kernel ends after the prefix kernel
+    if (blockIdx.x == 0) wait_for_previous();   // this kernel ends after the prefix kernel where it is launched behind it
 }
 
 // ------------------------------------------------------------------ prefix on CUDA cores (fp32, small pages, second opinion)
@@ -183,7 +183,7 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
     int64_t t = first_block(worker, blocks, p.p_workers);
     const int64_t t_end = first_block(worker + 1, blocks, p.p_workers);
     const int r_in = blockIdx.y * RT, row0 = mt * SHP_ROWS + r_in;   // RT rows of the tile per blockIdx.y
-    if (row0 >= rows || t >= t_end) return;
+    if (row0 >= rows) t = t_end;
     const int sr = (tid >> 4) * SR, sk = tid & 15;        // scores: rows sr ..; keys sk + 16 u
     const int orow = (tid >> 5) * OR, oc = tid & 31;      // outputs: rows orow .. (a warp's own); features oc * DC ..
     uint4 kv[2][PASSES];
@@ -196,7 +196,7 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
             kv[1][i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.v_prefix) + row) + c);
         }
     };
-    load((int)(t / p.p_blocks), (int)(t % p.p_blocks) * SHP_KEYS);
+    if (t < t_end) load((int)(t / p.p_blocks), (int)(t % p.p_blocks) * SHP_KEYS);
     while (t < t_end) {                                   // segments of the CTA's share
         const int h = (int)(t / p.p_blocks), blk0 = (int)(t - (int64_t)h * p.p_blocks);
         const int blk1 = (int)min((int64_t)p.p_blocks, blk0 + (t_end - t));
@@ -338,11 +338,14 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
 // ------------------------------------------------------------------ merge
 // CTA: 32 query rows of one kv head (lanes) x 8 / WAYS groups of 4 features (warps) x WAYS shares of the partial results: a
 // long list of them is read by WAYS warps.
+// Many rows have one warp each and take four results at a time: registers for four CTAs per SM, so that 592 of them are one wave
+// (4096 rows, 5 prefix segments: 6.5 us after the last result with eight at a time and two CTAs per SM).
 constexpr int MERGE_THREADS = 256;
 
 template <typename T, int D, int WAYS>
-__global__ void __launch_bounds__(MERGE_THREADS)
+__global__ void __launch_bounds__(MERGE_THREADS, WAYS == 1 ? 4 : 2)
 shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
+    constexpr int AT_ONCE = WAYS == 1 ? 4 : 8;
     constexpr int GROUPS = 8 / WAYS;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, way = warp / GROUPS, c4 = blockIdx.y * GROUPS + warp % GROUPS;
     const int h = blockIdx.z, row = min((int)(blockIdx.x * 32 + lane), a.B * a.g - 1);   // rows past the last repeat it
@@ -358,15 +361,15 @@ shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
     const int64_t* cum = reinterpret_cast<const int64_t*>(ws + p.cum);
     const int64_t per_head = __ldcg(cum + a.B), cum0 = __ldcg(cum + b), cum1 = __ldcg(cum + b + 1);
     RowMerge m;
-    m.add<WAYS>(ps.n, ws + p.p_lse + ps.first * SHP_ROWS + r, (int64_t)p.m_tiles * SHP_ROWS,
+    m.add<WAYS, AT_ONCE>(ps.n, ws + p.p_lse + ps.first * SHP_ROWS + r, (int64_t)p.m_tiles * SHP_ROWS,
                 ws + p.p_o + ps.first * SHP_ROWS * D + ((int64_t)c4 * SHP_ROWS + r) * 4, (int64_t)p.m_tiles * SHP_ROWS * D, way);
     const bool live = len >= 0 && blockIdx.x * 32 + lane < a.B * a.g;   // a request, and no repeated row
     if (live) {
         const int64_t all = per_head * a.Hkv * p.g_tiles, W = own_workers(all, p.workers);
         const int64_t w0 = block_worker(hh * per_head + cum0, all, W), first = w0 + hh * a.B + b;
         const int n_own = (int)(block_worker(hh * per_head + cum1 - 1, all, W) - w0) + 1;
-        m.add<WAYS>(n_own, ws + p.own_lse + first * p.g_rows + x, p.g_rows, ws + p.own_o + (first * p.g_rows + x) * D + c4 * 4,
-                    (int64_t)p.g_rows * D, way);
+        m.add<WAYS, AT_ONCE>(n_own, ws + p.own_lse + first * p.g_rows + x, p.g_rows, ws + p.own_o + (first * p.g_rows + x) * D + c4 * 4,
+                    (int64_t)p.g_rows * D, WAYS - 1 - way);   // the last way begins here, beside the first one's prefix results
     }
     if constexpr (WAYS > 1) {
         __shared__ RowMerge s_part[WAYS][GROUPS][32];
@@ -403,38 +406,51 @@ static cudaError_t own_stream(const SharedArgs& a, const SharedPlan& p, bool beh
 }
 
 template <typename T, int D, int RT>
-static cudaError_t prefix_simt_rt(const SharedArgs& a, const SharedPlan& p, cudaStream_t st) {
+static cudaError_t prefix_simt_rt(const SharedArgs& a, const SharedPlan& p, bool behind, cudaStream_t st) {
     constexpr int smem = SimtSmem<D, RT>::FLOATS * (int)sizeof(float);
     const int rows = std::min(a.B * a.g, SHP_ROWS);
-    return launch_behind(shared_prefix_simt_kernel<T, D, RT>, dim3(p.p_workers * p.m_tiles, (rows + RT - 1) / RT), SIMT_THREADS, smem, st, false, a, p);
+    return launch_behind(shared_prefix_simt_kernel<T, D, RT>, dim3(p.p_workers * p.m_tiles, (rows + RT - 1) / RT), SIMT_THREADS, smem, st, behind, a, p);
 }
 // the tallest row tile that the rows fill
 template <typename T, int D>
-static cudaError_t prefix_simt(const SharedArgs& a, const SharedPlan& p, cudaStream_t st) {
+static cudaError_t prefix_simt(const SharedArgs& a, const SharedPlan& p, bool behind, cudaStream_t st) {
     const int rows = a.B * a.g;
-    return rows <= 16 ? prefix_simt_rt<T, D, 16>(a, p, st) : rows <= 32 ? prefix_simt_rt<T, D, 32>(a, p, st) : prefix_simt_rt<T, D, 64>(a, p, st);
+    return rows <= 16 ? prefix_simt_rt<T, D, 16>(a, p, behind, st) : rows <= 32 ? prefix_simt_rt<T, D, 32>(a, p, behind, st)
+                                                                                 : prefix_simt_rt<T, D, 64>(a, p, behind, st);
 }
 
 template <typename T, int D>
 static cudaError_t shared_t(const SharedArgs& a, bool generic, cudaStream_t st) {
-    SharedPlan p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len, false);
-    const bool prefix = p.p_blocks > 0, tc = sizeof(T) == 2 && !generic;
+    const bool tc = sizeof(T) == 2 && !generic;
+    SharedPlan p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len, !tc);
+    auto prefix = [&](bool behind) {
+        if (p.p_blocks == 0) return cudaSuccess;
+        const cudaError_t e = tc ? launch_shared_prefix_tc(a, p, D, behind, st) : cudaErrorNotSupported;
+        return e == cudaErrorNotSupported ? prefix_simt<T, D>(a, p, behind, st) : e;
+    };
     cudaError_t e = cudaErrorNotSupported;
-    if (prefix) {
-        if (tc) e = launch_shared_prefix_tc(a, p, D, st);
-        if (e == cudaErrorNotSupported) e = prefix_simt<T, D>(a, p, st);
-        if (e != cudaSuccess) return e;
+    if (p.whole && shared_own_tma_fits(a, D)) {
+        e = prefix(false);
+        return e == cudaSuccess ? launch_shared_own_tma(a, p, D, p.p_blocks > 0, st) : e;
     }
-    e = tc ? launch_shared_own_tma(a, p, D, prefix, st) : cudaErrorNotSupported;
-    if (e == cudaErrorNotSupported) {
+    p.whole = false;
+    if (tc) e = launch_shared_own_tma(a, p, D, false, st);
+    if (e == cudaSuccess) {
+        e = prefix(true);
+    } else if (e == cudaErrorNotSupported) {
+        // CUDA cores: neither kernel leaves room for the other, and the longer one goes first
         p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len, true);   // the prefix part is cut and stored the same way
-        e = own_stream<T, D>(a, p, prefix, st);
+        e = prefix(false);
+        if (e == cudaSuccess) e = own_stream<T, D>(a, p, p.p_blocks > 0, st);
     }
-    if (e != cudaSuccess || p.whole) return e;   // whole: the own kernel has joined the parts
-    // a long list of partial results per row: many workers to a kv head, or own shares of one block
-    if (p.p_workers / a.Hkv >= 2 * MERGE_AT_ONCE)
-        return launch_behind(shared_merge_kernel<T, D, 4>, dim3((a.B * a.g + 31) / 32, D / 8, a.Hkv), MERGE_THREADS, 0, st, true, a, p);
-    return launch_behind(shared_merge_kernel<T, D, 1>, dim3((a.B * a.g + 31) / 32, D / 32, a.Hkv), MERGE_THREADS, 0, st, true, a, p);
+    if (e != cudaSuccess) return e;
+    // as many warps to a row's partial results as there is room for in one wave
+    const dim3 grid((a.B * a.g + 31) / 32, D / 32, a.Hkv);
+    const int64_t ctas = (int64_t)grid.x * grid.y * grid.z;
+    auto merge = [&](auto* kernel, int ways) { return launch_behind(kernel, dim3(grid.x, grid.y * ways, grid.z), MERGE_THREADS, 0, st, true, a, p); };
+    if (ctas * 4 <= 296) return merge(shared_merge_kernel<T, D, 4>, 4);
+    if (ctas * 2 <= 296) return merge(shared_merge_kernel<T, D, 2>, 2);
+    return merge(shared_merge_kernel<T, D, 1>, 1);
 }
 
 cudaError_t launch_decode_shared(const SharedArgs& a, int D, loma_dtype dt, bool generic, cudaStream_t st) {

@@ -12,12 +12,14 @@ constexpr int SHP_KEYS = 64;    // prefix keys per block
 constexpr int OWN_KEYS = 16;    // own keys per block
 constexpr int OWN_WARPS = 4;    // an own worker is a warp
 constexpr int OWN_CTAS = 148, STREAM_CTAS = 4 * 148;
-constexpr int OWN_WHOLE = 8;    // a sequence of so many blocks is not cut
+// sequences of so many blocks are not cut, while there are so few query rows that the workers join their parts quickly and
+// so few prefix blocks that it does not matter which kernel starts first
+constexpr int OWN_WHOLE = 8, OWN_WHOLE_ROWS = 2 * OWN_CTAS * OWN_WARPS;
 
-// Prefix CTAs that a call is cut for: one per SM, so that the own kernel runs beside it.  (Two per SM fill each other's waits,
-// but the own kernel then has to wait for them: B128 Hq32 Hkv8, prefix 16384 and up to 1500 own entries, 127 us against 95;
-// without own entries 49 against 52 us, and an HBM-bound prefix, B32 H32 prefix 8192, 39 against 36 us.)
-constexpr int SHP_CTAS = 148;
+// Prefix CTAs that a call is cut for: two per SM, which fill each other's waits (B128 Hq32 Hkv8, prefix 16384: 33-35 us alone
+// against 45-48 with one; B32 H32, the HBM-bound one: 40-43 against 48-51).  While an SM also holds a CTA of the own kernel it
+// has room for one of them, and the second comes when the other is done.
+constexpr int SHP_CTAS = 296;
 
 // The cut of a call.  Depends on the sizes alone, so results repeat and the workspace can be sized before the call.
 //
@@ -65,7 +67,8 @@ inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len
     p.g_rows = cuda_cores ? (g < 3 ? (int)g : 4) : (g <= 8 ? (int)g : 16);
     p.g_tiles = (int)((g + p.g_rows - 1) / p.g_rows);
     p.workers = (cuda_cores ? STREAM_CTAS : OWN_CTAS) * OWN_WARPS;
-    p.whole = !cuda_cores && own_blocks(max_len) <= OWN_WHOLE;
+    p.whole = !cuda_cores && own_blocks(max_len) <= OWN_WHOLE && (int64_t)B * Hq <= OWN_WHOLE_ROWS &&
+              (int64_t)Hkv * p.p_blocks * p.m_tiles <= SHP_CTAS;
     int64_t at = 0;
     auto take = [&](int64_t n) { const int64_t o = at; at += (n + 63) / 64 * 64; return o; };
     const int64_t p_segments = p.p_blocks ? (int64_t)(p.p_workers + Hkv) * p.m_tiles : 0, segments = p.workers + (int64_t)B * Hkv * p.g_tiles;
@@ -181,19 +184,18 @@ struct SeqBlocks {
 
 #ifdef __CUDACC__
 // One query row's four features joined from partial results under a running maximum.  The time of a merge is that of its chain
-// of dependent loads, so MERGE_AT_ONCE results are taken at a time, values and log2-sum-exps together.
-constexpr int MERGE_AT_ONCE = 8;
+// of dependent loads, so AT_ONCE results are taken at a time, values and log2-sum-exps together.
 struct RowMerge {
     float M = -INFINITY, total = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     // n results: log2-sum-exps at lse[s * lse_step], values at v[s * v_step]; of every WAYS batches the way-th
-    template <int WAYS>
+    template <int WAYS, int AT_ONCE>
     __device__ __forceinline__ void add(int n, const float* lse, int64_t lse_step, const float* v, int64_t v_step, int way) {
-        for (int s0 = way * MERGE_AT_ONCE; s0 < n; s0 += WAYS * MERGE_AT_ONCE) {
-            float e[MERGE_AT_ONCE];
-            float4 y[MERGE_AT_ONCE];
+        for (int s0 = way * AT_ONCE; s0 < n; s0 += WAYS * AT_ONCE) {
+            float e[AT_ONCE];
+            float4 y[AT_ONCE];
 #pragma unroll
-            for (int u = 0; u < MERGE_AT_ONCE; ++u) {
+            for (int u = 0; u < AT_ONCE; ++u) {
                 e[u] = -INFINITY;
                 if (s0 + u < n) {
                     e[u] = __ldcg(lse + (s0 + u) * lse_step);
@@ -202,13 +204,13 @@ struct RowMerge {
             }
             float m = M;
 #pragma unroll
-            for (int u = 0; u < MERGE_AT_ONCE; ++u) m = fmaxf(m, e[u]);
+            for (int u = 0; u < AT_ONCE; ++u) m = fmaxf(m, e[u]);
             const float keep = M == -INFINITY ? 0.f : exp2f(M - m);
             M = m;
             total *= keep;
             o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
 #pragma unroll
-            for (int u = 0; u < MERGE_AT_ONCE; ++u) {
+            for (int u = 0; u < AT_ONCE; ++u) {
                 if (e[u] == -INFINITY) continue;   // no weight: past the last, or scores of -inf (values 0/0)
                 const float f = exp2f(e[u] - m);
                 total += f;
@@ -240,12 +242,13 @@ struct PrefixSegments {
 };
 #endif
 
-// The three kernels of a step: prefix, own (beside it: launched behind it, sharing no result) and merge (launched behind
-// own, which ends after the prefix kernel).  Where own caches hold a few blocks at most (p.whole), each sequence stays with one
-// warp of the own kernel, which joins the parts itself: two kernels.  The own kernel, bf16 (decode_shared_own.cu);
-// cudaErrorNotSupported = use the CUDA-core kernel
+// The three kernels of a step: own, prefix (launched behind it, sharing no result, so that it starts beside it) and merge
+// (launched behind the prefix kernel, which ends after the own kernel).  Where own caches hold a few blocks at most and the
+// prefix is short (p.whole), the prefix kernel comes first, each sequence stays with one warp of the own kernel, and that joins
+// the parts itself: two kernels.  On CUDA cores: prefix, own, merge.  The own kernel, bf16 (decode_shared_own.cu); cudaErrorNotSupported = use the CUDA-core kernel
+bool shared_own_tma_fits(const SharedArgs& a, int D);
 cudaError_t launch_shared_own_tma(const SharedArgs& a, const SharedPlan& p, int D, bool behind, cudaStream_t st);
 // the prefix on the tensor cores (decode_shared_tc.cu); cudaErrorNotSupported = use the CUDA-core kernel
-cudaError_t launch_shared_prefix_tc(const SharedArgs& a, const SharedPlan& p, int D, cudaStream_t st);
+cudaError_t launch_shared_prefix_tc(const SharedArgs& a, const SharedPlan& p, int D, bool behind, cudaStream_t st);
 
 }  // namespace loma

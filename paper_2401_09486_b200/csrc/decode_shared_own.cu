@@ -138,6 +138,13 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
             h_f = p.g_tiles == 1 ? f.at.hh : f.at.hh / p.g_tiles;
             base_f = (f.at.b * a.Hkv + h_f) * a.cap;   // the cache has less than 2^31 rows
             table_f = a.pg.table + (int64_t)f.at.b * a.pg.max_pages;
+            // the segment's query heads and new token, wanted when its blocks have arrived
+            const int gt_f = f.at.hh - h_f * p.g_tiles, lines = min(p.g_rows, a.g - gt_f * p.g_rows) * PANELS;   // of 128 bytes
+            const __nv_bfloat16* line = nullptr;
+            if (lane < lines) line = static_cast<const __nv_bfloat16*>(a.q) + ((int64_t)f.at.b * a.Hq + h_f * a.g + gt_f * p.g_rows) * D + lane * 64;
+            else if (lane >= 32 - 2 * PANELS && a.k_new)
+                line = static_cast<const __nv_bfloat16*>(lane >= 32 - PANELS ? a.k_new : a.v_new) + ((int64_t)f.at.b * a.Hkv + h_f) * D + (lane & (PANELS - 1)) * 64;
+            if (line) asm volatile("prefetch.global.L2 [%0];" ::"l"(line));
         };
         auto row_f = [&]() -> int {
             if (!a.pg.table) return base_f + f.at.blk * OWN_KEYS;
@@ -324,8 +331,9 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
             while (clock64() - t_off < 2000000ll) {}
         }
     }
-    wait_for_previous();   // the merge needs the prefix kernel's results too: this kernel ends after it
     if constexpr (WHOLE) {
+        wait_for_previous();   // the prefix kernel's results
+
         // this warp's units: its own results (each lane reads what the warp has written) and the prefix segments.  A lane has
         // four features of a row, so D / 4 lanes share one
         __syncwarp();
@@ -340,8 +348,8 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
                 const PrefixSegments ps(a, p, h, mt);
                 const int64_t own = (int64_t)u.left * p.g_rows + x;
                 RowMerge m;
-                m.add<1>(1, part + p.own_lse + own, 0, part + p.own_o + own * D + c4 * 4, 0, 0);
-                m.add<1>(ps.n, part + p.p_lse + ps.first * SHP_ROWS + rt, (int64_t)p.m_tiles * SHP_ROWS,
+                m.add<1, 1>(1, part + p.own_lse + own, 0, part + p.own_o + own * D + c4 * 4, 0, 0);
+                m.add<1, 8>(ps.n, part + p.p_lse + ps.first * SHP_ROWS + rt, (int64_t)p.m_tiles * SHP_ROWS,
                          part + p.p_o + ps.first * SHP_ROWS * D + ((int64_t)c4 * SHP_ROWS + rt) * 4, (int64_t)p.m_tiles * SHP_ROWS * D, 0);
                 m.store<__nv_bfloat16, D>(a, (int64_t)u.at.b * a.Hq + h * a.g + gt * p.g_rows + x, c4);
             }
@@ -360,15 +368,25 @@ static bool encode_rows(CUtensorMap* map, const void* p, int D, int64_t rows, in
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// rows of the cache or pool as TMA sees it, and rows of a box
+static int64_t own_rows(const SharedArgs& a) {
+    return a.pg.table ? ((int64_t)a.pg.n_pages * a.Hkv << a.pg.log2_ps) : (int64_t)a.B * a.Hkv * a.cap;
+}
+static int own_box_rows(const SharedArgs& a) { return a.pg.table ? std::min(1 << a.pg.log2_ps, OWN_KEYS) : OWN_KEYS; }
+
+// a box of fewer than 8 rows would start inside a swizzle group, a tile has 16 rows at least, and a row's number is 32 bits
+bool shared_own_tma_fits(const SharedArgs& a, int D) {
+    (void)D;
+    const int64_t rows = own_rows(a);
+    return encode_fn() && own_box_rows(a) >= 8 && rows >= OWN_KEYS && rows <= INT_MAX;
+}
+
 template <int D, int R, bool WHOLE>
 static cudaError_t own_tma_t(const SharedArgs& a, const SharedPlan& p, bool behind, cudaStream_t st) {
     OwnMaps maps;
-    const int ps = 1 << a.pg.log2_ps;
-    const int64_t rows = a.pg.table ? ((int64_t)a.pg.n_pages * a.Hkv << a.pg.log2_ps) : (int64_t)a.B * a.Hkv * a.cap;
-    const int box_rows = a.pg.table ? std::min(ps, OWN_KEYS) : OWN_KEYS;
-    // a box of fewer than 8 rows would start inside a swizzle group; a tile has 16 rows at least
-    if (box_rows < 8 || rows < OWN_KEYS || rows > INT_MAX || !encode_rows(&maps.k, a.k_cache, D, rows, box_rows) ||
-        !encode_rows(&maps.v, a.v_cache, D, rows, box_rows))
+    const int64_t rows = own_rows(a);
+    const int box_rows = own_box_rows(a);
+    if (!shared_own_tma_fits(a, D) || !encode_rows(&maps.k, a.k_cache, D, rows, box_rows) || !encode_rows(&maps.v, a.v_cache, D, rows, box_rows))
         return cudaErrorNotSupported;
     int* status = device_status_word();
     if (!status) return cudaErrorUnknown;

@@ -9,6 +9,7 @@
 //   warps 0-3  query rows, softmax: thread = query row.  64 keys (an "event") at a time: scores out of TMEM, row maximum, probabilities
 //              2^(s scale - ref) as bf16 back over the scores.  The reference maximum only moves, and the accumulator in TMEM
 //              is only rescaled, when a row's maximum has grown by more than 2^8, which bounds a probability by 2^8
+//   warps 4-7  a warpgroup of their own, so that registers can be moved to the softmax; warps 6 and 7 do nothing
 //   warp 4     TMA: K and V in tiles of 64 keys through one ring of NS slots, in the order in which they are used
 //              K0 K1 V0 K2 V1 K3 V2 ...
 //   warp 5     MMA: S(e+2) is issued right after P V(e) into the score buffer that event e has left, so the tensor pipe works
@@ -31,7 +32,7 @@ __device__ __forceinline__ void tma_prefix(uint32_t dst, const CUtensorMap* map,
                  : "memory");
 }
 
-constexpr int SHT_THREADS = 192, SHT_TMEM = 256;
+constexpr int SHT_THREADS = 256, SHT_TMEM = 256;
 
 template <int D>
 struct ShtSmem {
@@ -109,7 +110,10 @@ shared_prefix_tc_kernel(const __grid_constant__ SharedMaps maps, const ShtParams
 
     // Items (tiles of 64 keys) and events are numbered through over all segments: item n lies in ring slot n mod NS, event e uses
     // score buffer e & 1.
+    // registers: launched with 128 a thread (two CTAs fill an SM's, and each of its four schedulers has the same share), of which
+    // warps 4-7 leave most to the softmax
     if (warp == 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;" ::: "memory");
         // ------------------------------------------------------------ TMA producer
         bool ok = true;
         // a box of a whole tile's 64 rows takes all panels; smaller ones (short pages, a short prefix) go panel by panel, since the
@@ -150,6 +154,7 @@ shared_prefix_tc_kernel(const __grid_constant__ SharedMaps maps, const ShtParams
             while (clock64() - t0 < 2000000ll) {}
         }
     } else if (warp == 5) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;" ::: "memory");
         // ------------------------------------------------------------ MMA issuer: uniform control flow, one elected lane issues
         // instruction descriptors: fp32 accumulate, bf16 x bf16, M = 128; N = 64 keys, or N = D with V as the MN-major operand
         constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
@@ -203,7 +208,10 @@ shared_prefix_tc_kernel(const __grid_constant__ SharedMaps maps, const ShtParams
             }
             e0 += E;
         }
+    } else if (warp >= 6) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;" ::: "memory");
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;" ::: "memory");
         // ------------------------------------------------------------ query rows, softmax and partial results
         const int rr = threadIdx.x, rows = p.B * p.g;
         const uint32_t lane_addr = tmem + ((uint32_t)(warp * 32) << 16), o_addr = lane_addr + 128;
@@ -355,6 +363,8 @@ shared_prefix_tc_kernel(const __grid_constant__ SharedMaps maps, const ShtParams
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(SHT_TMEM) : "memory");
     }
+    // the merge needs the own kernel's results too: this kernel ends after it.  One CTA waits; the others leave their places
+    if (blockIdx.x == 0) wait_for_previous();
 }
 
 // ------------------------------------------------------------------ host side
@@ -371,7 +381,7 @@ static bool encode_prefix(CUtensorMap* map, const void* p, int D, int64_t rows, 
 }
 
 template <int D>
-static cudaError_t prefix_tc_t(const SharedArgs& a, const SharedPlan& p, cudaStream_t st) {
+static cudaError_t prefix_tc_t(const SharedArgs& a, const SharedPlan& p, bool behind, cudaStream_t st) {
     ShtParams t;
     SharedMaps maps;
     const int ps = 1 << a.pg.log2_ps;
@@ -398,11 +408,11 @@ static cudaError_t prefix_tc_t(const SharedArgs& a, const SharedPlan& p, cudaStr
     t.log2_ps = a.pg.log2_ps; t.n_pages = a.pg.n_pages;
     t.scale_log2 = a.scale * 1.4426950408889634f;
     constexpr int smem = ShtSmem<D>::TOTAL;
-    return launch_behind(shared_prefix_tc_kernel<D>, dim3(p.p_workers * p.m_tiles), SHT_THREADS, smem, st, false, maps, t);
+    return launch_behind(shared_prefix_tc_kernel<D>, dim3(p.p_workers * p.m_tiles), SHT_THREADS, smem, st, behind, maps, t);
 }
 
-cudaError_t launch_shared_prefix_tc(const SharedArgs& a, const SharedPlan& p, int D, cudaStream_t st) {
-    return D == 64 ? prefix_tc_t<64>(a, p, st) : prefix_tc_t<128>(a, p, st);
+cudaError_t launch_shared_prefix_tc(const SharedArgs& a, const SharedPlan& p, int D, bool behind, cudaStream_t st) {
+    return D == 64 ? prefix_tc_t<64>(a, p, behind, st) : prefix_tc_t<128>(a, p, behind, st);
 }
 
 }  // namespace loma
