@@ -157,10 +157,10 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
 }
 
 // ------------------------------------------------------------------ prefix on CUDA cores (fp32, small pages, second opinion)
-// RT query rows against 64 keys at a time, all in fp32 in shared memory, with RT / 16 x 4 scores and RT / 8 x (D / 32) outputs
+// RT query rows against 32 keys at a time, all in fp32 in shared memory, with RT / 16 x 2 scores and RT / 8 x (D / 32) outputs
 // per thread in registers; the next keys are on their way from memory while these are worked on.  Bound by fp32 FMA for many
 // rows, by the latency of a block's steps for few.  Query row m of kv head h is head h g + m mod g of sequence m / g.
-constexpr int SIMT_K = SHP_KEYS, SIMT_THREADS = 256;
+constexpr int SIMT_THREADS = 256;
 
 template <int D, int RT>
 struct SimtSmem {
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(SIMT_THREADS, RT == 64 ? 1 : 2)
 shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
     using V = Vec16<T>;
     using SM = SimtSmem<D, RT>;
-    constexpr int N = V::N, LPK = D / N, DC = D / 32, PASSES = SIMT_K * LPK / SIMT_THREADS, SR = RT / 16, OR = RT / 8;
+    constexpr int N = V::N, LPK = D / N, DC = D / 32, PASSES = SIMT_K * LPK / SIMT_THREADS, SR = RT / 16, KU = SIMT_K / 16, OR = RT / 8;
     extern __shared__ __align__(16) float sm[];
     let_next_start();
     const int tid = threadIdx.x, rows = a.B * a.g;
@@ -196,11 +196,11 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
             kv[1][i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.v_prefix) + row) + c);
         }
     };
-    if (t < t_end) load((int)(t / p.p_blocks), (int)(t % p.p_blocks) * SHP_KEYS);
+    if (t < t_end) load((int)(t / p.p_blocks), (int)(t % p.p_blocks) * SIMT_K);
     while (t < t_end) {                                   // segments of the CTA's share
         const int h = (int)(t / p.p_blocks), blk0 = (int)(t - (int64_t)h * p.p_blocks);
         const int blk1 = (int)min((int64_t)p.p_blocks, blk0 + (t_end - t));
-        const int begin = blk0 * SHP_KEYS, end = min(a.prefix_len, blk1 * SHP_KEYS);
+        const int begin = blk0 * SIMT_K, end = min(a.prefix_len, blk1 * SIMT_K);
         const int64_t seg = (int64_t)(worker + h) * p.m_tiles + mt;
         __syncthreads();
 #pragma unroll 4
@@ -231,31 +231,31 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
 #pragma unroll
                 for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(&sm[SM::V + r * D + c * N + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
             }
-            if (++t < t_end) load((int)(t / p.p_blocks), (int)(t % p.p_blocks) * SHP_KEYS);
+            if (++t < t_end) load((int)(t / p.p_blocks), (int)(t % p.p_blocks) * SIMT_K);
             __syncthreads();
             // two-wide FMA: sums over even and odd features side by side
-            uint64_t s2[SR][4];
+            uint64_t s2[SR][KU];
 #pragma unroll
             for (int u = 0; u < SR; ++u)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) s2[u][w] = 0;
+                for (int w = 0; w < KU; ++w) s2[u][w] = 0;
 #pragma unroll 4
             for (int d = 0; d < D; d += 4) {
-                ulonglong2 qv[SR], kf[4];
+                ulonglong2 qv[SR], kf[KU];
 #pragma unroll
                 for (int u = 0; u < SR; ++u) qv[u] = *reinterpret_cast<const ulonglong2*>(&sm[SM::Q + (sr + u) * (D + 4) + d]);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) kf[u] = *reinterpret_cast<const ulonglong2*>(&sm[SM::K + (sk + 16 * u) * (D + 4) + d]);
+                for (int u = 0; u < KU; ++u) kf[u] = *reinterpret_cast<const ulonglong2*>(&sm[SM::K + (sk + 16 * u) * (D + 4) + d]);
 #pragma unroll
                 for (int u = 0; u < SR; ++u)
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) s2[u][w] = fma2(qv[u].y, kf[w].y, fma2(qv[u].x, kf[w].x, s2[u][w]));
+                    for (int w = 0; w < KU; ++w) s2[u][w] = fma2(qv[u].y, kf[w].y, fma2(qv[u].x, kf[w].x, s2[u][w]));
             }
-            float s[SR][4];
+            float s[SR][KU];
 #pragma unroll
             for (int u = 0; u < SR; ++u)
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
+                for (int w = 0; w < KU; ++w) {
                     float lo, hi;
                     unpack2(s2[u][w], lo, hi);
                     s[u][w] = lo + hi;
@@ -264,7 +264,7 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
             for (int u = 0; u < SR; ++u) {   // 16 lanes share a row
                 float mx = -INFINITY;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
+                for (int w = 0; w < KU; ++w) {
                     if (k0 + sk + 16 * w >= end) s[u][w] = -INFINITY;
                     mx = fmaxf(mx, s[u][w]);
                 }
@@ -273,7 +273,7 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
                 const float m_old = sm[SM::ML + sr + u], m_new = fmaxf(m_old, mx), ref = m_new == -INFINITY ? 0.f : m_new;
                 float sum = 0.f;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
+                for (int w = 0; w < KU; ++w) {
                     const float e = exp2f(s[u][w] - ref);
                     sum += e;
                     sm[SM::S + (sr + u) * (SIMT_K + 4) + sk + 16 * w] = e;

@@ -8,7 +8,8 @@
 namespace loma {
 
 constexpr int SHP_ROWS = 128;   // query rows of a prefix tile
-constexpr int SHP_KEYS = 64;    // prefix keys per block
+constexpr int SHP_KEYS = 64;    // prefix keys per block on the tensor cores
+constexpr int SIMT_K = 32;      // and on CUDA cores, where a block takes a few microseconds: finer shares
 constexpr int OWN_KEYS = 16;    // own keys per block
 constexpr int OWN_WARPS = 4;    // an own worker is a warp
 constexpr int OWN_CTAS = 148, STREAM_CTAS = 4 * 148;
@@ -24,7 +25,7 @@ constexpr int SHP_CTAS = 296;
 // The cut of a call.  Depends on the sizes alone, so results repeat and the workspace can be sized before the call.
 //
 // Both parts are cut into equal shares whatever their shape.  The blocks of all units of work are numbered through -- prefix:
-// unit = kv head, SHP_KEYS keys a block; own: unit = (kv head, head tile, sequence), OWN_KEYS keys a block -- and worker w of
+// unit = kv head, p_keys keys a block; own: unit = (kv head, head tile, sequence), OWN_KEYS keys a block -- and worker w of
 // W takes blocks [T w / W, T (w + 1) / W).  A worker's stay in one unit is a segment with a partial result in slot w + unit:
 // along the numbering either the worker or the unit moves on, so no two segments share a slot, and the segments of one unit
 // lie behind one another.  Own lengths are known on the device only, so T is found there.
@@ -32,6 +33,7 @@ constexpr int SHP_CTAS = 296;
 // come out of HBM once and reach the other tiles through L2 while the own kernel streams through it.
 struct SharedPlan {
     int m_tiles;        // prefix: tiles of SHP_ROWS query rows per kv head
+    int p_keys;         //         keys per block
     int p_blocks;       //         blocks per kv head (0: no prefix)
     int p_workers;      //         W: m_tiles CTAs each
     int g_rows;         // own: query heads of a kv head per head tile (8 or 16 rows of a warp-level product, or fewer heads)
@@ -57,8 +59,9 @@ inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len
     SharedPlan p;
     const int64_t g = Hq / Hkv, rows = (int64_t)B * g;
     p.m_tiles = (int)((rows + SHP_ROWS - 1) / SHP_ROWS);
-    p.p_blocks = (prefix_len + SHP_KEYS - 1) / SHP_KEYS;
-    int64_t w = std::max(1, SHP_CTAS / p.m_tiles);
+    p.p_keys = cuda_cores ? SIMT_K : SHP_KEYS;
+    p.p_blocks = (prefix_len + p.p_keys - 1) / p.p_keys;
+    int64_t w = std::max(1, (cuda_cores ? SHP_CTAS / 2 : SHP_CTAS) / p.m_tiles);   // CUDA cores: one CTA fills an SM
     // shares that end inside a kv head make most workers change heads once, which costs about as much as six blocks (draining
     // the products, storing a partial result, new query rows): whole workers per kv head where their longer shares cost less
     const int64_t all = (int64_t)Hkv * p.p_blocks, whole = w / Hkv * Hkv;
