@@ -5,11 +5,11 @@
 // with weights 2^(lse_i - max), so the parts are computed where they are cheap and joined at the end:
 //
 //   prefix   all B g query rows of a kv head against the same K and V: a matrix product, 128 rows at a time, that reads
-//            the prefix once for the batch instead of once per sequence (bf16: tcgen05, decode_shared_tc.cu; fp32 and
-//            page sizes below 8: shared_prefix_simt_kernel)
+//            the prefix once for the batch instead of once per sequence (bf16: tcgen05, decode_shared_tc.cu; fp32, page
+//            sizes below 8 and own caches of fewer than 16 rows in all: shared_prefix_simt_kernel)
 //   own      one query row per head of a group against rows nobody else reads: a stream bound by HBM, cut into equal
-//            shares of keys whatever the lengths (SharedPlan).  bf16: decode_shared_own.cu; fp32 and page sizes below 8:
-//            shared_own_stream_kernel on CUDA cores
+//            shares of keys whatever the lengths (SharedPlan).  bf16: decode_shared_own.cu; else, and wherever the
+//            prefix stays off the tensor cores: shared_own_stream_kernel
 //   merge    one thread per query row and four features adds the parts in a fixed order (results repeat bit for bit)
 //
 // The own and the prefix kernel share no result, so the second starts beside the first (programmatic dependent launch) and
@@ -414,6 +414,7 @@ static cudaError_t prefix_simt_rt(const SharedArgs& a, const SharedPlan& p, bool
 // the tallest row tile that the rows fill
 template <typename T, int D>
 static cudaError_t prefix_simt(const SharedArgs& a, const SharedPlan& p, bool behind, cudaStream_t st) {
+    if (p.p_keys != SIMT_K) return cudaErrorInvalidValue;
     const int rows = a.B * a.g;
     return rows <= 16 ? prefix_simt_rt<T, D, 16>(a, p, behind, st) : rows <= 32 ? prefix_simt_rt<T, D, 32>(a, p, behind, st)
                                                                                  : prefix_simt_rt<T, D, 64>(a, p, behind, st);
@@ -421,25 +422,21 @@ static cudaError_t prefix_simt(const SharedArgs& a, const SharedPlan& p, bool be
 
 template <typename T, int D>
 static cudaError_t shared_t(const SharedArgs& a, bool generic, cudaStream_t st) {
-    const bool tc = sizeof(T) == 2 && !generic;
-    SharedPlan p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len, !tc);
+    // both parts on the tensor cores or both on CUDA cores: a cut and the kernels that follow it belong together
+    const bool tc = sizeof(T) == 2 && !generic && shared_own_tma_fits(a) && (a.prefix_len == 0 || shared_prefix_tc_fits(a));
+    const SharedPlan p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len, !tc);
     auto prefix = [&](bool behind) {
-        if (p.p_blocks == 0) return cudaSuccess;
-        const cudaError_t e = tc ? launch_shared_prefix_tc(a, p, D, behind, st) : cudaErrorNotSupported;
-        return e == cudaErrorNotSupported ? prefix_simt<T, D>(a, p, behind, st) : e;
+        return p.p_blocks == 0 ? cudaSuccess : tc ? launch_shared_prefix_tc(a, p, D, behind, st) : prefix_simt<T, D>(a, p, behind, st);
     };
-    cudaError_t e = cudaErrorNotSupported;
-    if (p.whole && shared_own_tma_fits(a, D)) {
+    cudaError_t e;
+    if (p.whole) {
         e = prefix(false);
         return e == cudaSuccess ? launch_shared_own_tma(a, p, D, p.p_blocks > 0, st) : e;
     }
-    p.whole = false;
-    if (tc) e = launch_shared_own_tma(a, p, D, false, st);
-    if (e == cudaSuccess) {
-        e = prefix(true);
-    } else if (e == cudaErrorNotSupported) {
-        // CUDA cores: neither kernel leaves room for the other, and the longer one goes first
-        p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len, true);   // the prefix part is cut and stored the same way
+    if (tc) {
+        e = launch_shared_own_tma(a, p, D, false, st);
+        if (e == cudaSuccess) e = prefix(true);
+    } else {   // neither kernel leaves room for the other, and the longer one goes first
         e = prefix(false);
         if (e == cudaSuccess) e = own_stream<T, D>(a, p, p.p_blocks > 0, st);
     }

@@ -54,7 +54,7 @@ __host__ __device__ inline int64_t first_block(int64_t w, int64_t T, int64_t W) 
 
 __host__ __device__ inline int64_t own_workers(int64_t T, int workers) { return T < workers ? T : workers; }
 
-// cuda_cores: the own part runs on shared_own_stream_kernel (fp32, small pages, second opinion)
+// cuda_cores: both parts run on CUDA cores (fp32, pages of fewer than 8, own caches of fewer than 16 rows in all, second opinion)
 inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len, int max_len, bool cuda_cores) {
     SharedPlan p;
     const int64_t g = Hq / Hkv, rows = (int64_t)B * g;
@@ -248,10 +248,12 @@ struct PrefixSegments {
 // The three kernels of a step: own, prefix (launched behind it, sharing no result, so that it starts beside it) and merge
 // (launched behind the prefix kernel, which ends after the own kernel).  Where own caches hold a few blocks at most and the
 // prefix is short (p.whole), the prefix kernel comes first, each sequence stays with one warp of the own kernel, and that joins
-// the parts itself: two kernels.  On CUDA cores: prefix, own, merge.  The own kernel, bf16 (decode_shared_own.cu); cudaErrorNotSupported = use the CUDA-core kernel
-bool shared_own_tma_fits(const SharedArgs& a, int D);
+// the parts itself: two kernels.  On CUDA cores: prefix, own, merge.
+// bf16 own caches (decode_shared_own.cu), and whether TMA can address them
+bool shared_own_tma_fits(const SharedArgs& a);
 cudaError_t launch_shared_own_tma(const SharedArgs& a, const SharedPlan& p, int D, bool behind, cudaStream_t st);
-// the prefix on the tensor cores (decode_shared_tc.cu); cudaErrorNotSupported = use the CUDA-core kernel
+// the prefix on the tensor cores (decode_shared_tc.cu), and whether TMA can address it
+bool shared_prefix_tc_fits(const SharedArgs& a);
 cudaError_t launch_shared_prefix_tc(const SharedArgs& a, const SharedPlan& p, int D, bool behind, cudaStream_t st);
 
 }  // namespace loma

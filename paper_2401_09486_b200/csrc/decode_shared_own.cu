@@ -375,8 +375,7 @@ static int64_t own_rows(const SharedArgs& a) {
 static int own_box_rows(const SharedArgs& a) { return a.pg.table ? std::min(1 << a.pg.log2_ps, OWN_KEYS) : OWN_KEYS; }
 
 // a box of fewer than 8 rows would start inside a swizzle group, a tile has 16 rows at least, and a row's number is 32 bits
-bool shared_own_tma_fits(const SharedArgs& a, int D) {
-    (void)D;
+bool shared_own_tma_fits(const SharedArgs& a) {
     const int64_t rows = own_rows(a);
     return encode_fn() && own_box_rows(a) >= 8 && rows >= OWN_KEYS && rows <= INT_MAX;
 }
@@ -386,8 +385,7 @@ static cudaError_t own_tma_t(const SharedArgs& a, const SharedPlan& p, bool behi
     OwnMaps maps;
     const int64_t rows = own_rows(a);
     const int box_rows = own_box_rows(a);
-    if (!shared_own_tma_fits(a, D) || !encode_rows(&maps.k, a.k_cache, D, rows, box_rows) || !encode_rows(&maps.v, a.v_cache, D, rows, box_rows))
-        return cudaErrorNotSupported;
+    if (!encode_rows(&maps.k, a.k_cache, D, rows, box_rows) || !encode_rows(&maps.v, a.v_cache, D, rows, box_rows)) return cudaErrorInvalidValue;
     int* status = device_status_word();
     if (!status) return cudaErrorUnknown;
     constexpr int smem = OwnSmem<D>::TOTAL;

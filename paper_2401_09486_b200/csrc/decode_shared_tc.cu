@@ -380,23 +380,23 @@ static bool encode_prefix(CUtensorMap* map, const void* p, int D, int64_t rows, 
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+static int64_t prefix_outer(const SharedArgs& a) { return a.prefix_table ? (int64_t)a.pg.n_pages * a.Hkv : a.Hkv; }
+
+// a box of fewer than 8 rows of a page would start inside a swizzle group, and a coordinate is 32 bits
+bool shared_prefix_tc_fits(const SharedArgs& a) {
+    return encode_fn() && (!a.prefix_table || a.pg.log2_ps >= 3) && prefix_outer(a) <= INT_MAX;
+}
+
 template <int D>
 static cudaError_t prefix_tc_t(const SharedArgs& a, const SharedPlan& p, bool behind, cudaStream_t st) {
     ShtParams t;
     SharedMaps maps;
     const int ps = 1 << a.pg.log2_ps;
-    int64_t rows, step, outer;
-    if (a.prefix_table) {
-        if (ps < 8) return cudaErrorNotSupported;   // a box would start inside an 8-row swizzle group
-        t.box_rows = std::min(ps, SHP_KEYS);
-        rows = ps; step = ps; outer = (int64_t)a.pg.n_pages * a.Hkv;
-    } else {
-        t.box_rows = std::min(a.prefix_len, SHP_KEYS);
-        rows = a.prefix_len; step = a.prefix_cap; outer = a.Hkv;
-    }
-    if (outer > INT_MAX || !encode_prefix(&maps.k, a.k_prefix, D, rows, step, outer, t.box_rows) ||
+    const int64_t rows = a.prefix_table ? ps : a.prefix_len, step = a.prefix_table ? ps : a.prefix_cap, outer = prefix_outer(a);
+    t.box_rows = (int)std::min<int64_t>(rows, SHP_KEYS);
+    if (p.p_keys != SHP_KEYS || !encode_prefix(&maps.k, a.k_prefix, D, rows, step, outer, t.box_rows) ||
         !encode_prefix(&maps.v, a.v_prefix, D, rows, step, outer, t.box_rows))
-        return cudaErrorNotSupported;
+        return cudaErrorInvalidValue;
     float* ws = static_cast<float*>(a.ws);
     t.q = static_cast<const __nv_bfloat16*>(a.q);
     t.prefix_table = a.prefix_table;

@@ -15,7 +15,7 @@ from oracle import serving_oracle as S
 from paper_2401_09486_b200 import autograd as A
 from paper_2401_09486_b200 import binding as L
 from paper_2401_09486_b200 import build, synthetic
-from tests.test_serving_host import check_extend, extend_case, run_extend
+from tests.test_serving_host import check_extend, extend_case, huge_extend_case, run_extend
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -81,6 +81,44 @@ def test_extend_one_long_prompt_among_idle_slots_and_unaligned_outputs():
     torch.cuda.synchronize()
     check_extend([tb, *out, *rows, None], want)
     assert (buf[:, 0] == -77).all()
+
+
+@pytest.mark.parametrize("in_place", [False, True])       # one launch, and two
+def test_extend_saturates(in_place):
+    case = huge_extend_case()
+    got = run_extend(*case[:5], None, case[5], 4, 50, device=DEV, in_place=in_place)
+    torch.cuda.synchronize()
+    check_extend(got, S.paged_extend(*case[:5], None, case[5], 4, 50))
+
+
+def test_extend_replayed_steps_keep_their_state_on_the_device():
+    """A captured step that updates held and taken in place hands out every entry once, over replays."""
+    B, M, ps = 700, 8, 4
+    i32 = dict(dtype=torch.int32, device=DEV)
+    lens, held, taken = torch.zeros(B, **i32), torch.zeros(B, **i32), torch.zeros(1, **i32)
+    table, free = torch.full((B, M), -1, **i32), torch.randperm(B * M, device=DEV).to(torch.int32)
+    rs, pg, sl, sq, po = (torch.empty(n, **i32) for n in (B + 1, B + 1, B, B, B))
+
+    def step():
+        L.loma_paged_extend(lens, None, held, None, free, taken, table, ps, rs, pg, held, sl, sq, po)
+        lens.add_(1)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    seen = [sl.clone()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(9):
+        graph.replay()
+        seen.append(sl.clone())
+    torch.cuda.synchronize()
+    every = torch.cat(seen)
+    assert (every >= 0).all() and every.unique().numel() == 10 * B
+    assert int(taken) == 3 * B and (held == 3).all() and torch.equal(free[: 3 * B].sort().values, table[:, :3].flatten().sort().values)
 
 
 # ------------------------------------------------------------------------------------------------ norm + rotation
@@ -371,7 +409,12 @@ SHARED = [
     (3, 4, 2, 128, 45, [6, 1, 9], 1),                             # pages of fewer than 8 rows
     (3, 4, 2, 64, 45, [6, 1, 9], 4),
     (2, 4, 2, 128, 0, [100, 5], 16),
+    (1500, 1, 1, 64, 20, [13 * i % 61 - 1 for i in range(1500)], 0),         # several sequences to a group of the own scan
+    (9, 16, 8, 128, 100, [2000, 1999, 0, -1, 777, 1500, 16, 15, 2000], 0),   # shares that hold parts of several sequences
+    (6, 8, 4, 64, 300, [900, 3, -1, 500, 0, 899], 8),
+    (40, 64, 4, 64, 500, [i % 20 for i in range(40)], 16),                   # 640 query rows per kv head, groups of 16
 ]
+WIDE = (130, 100, 100, 64, 1300, [i % 5 for i in range(130)], 0)             # prefix shares that end inside a kv head, two row tiles
 
 
 @pytest.mark.parametrize("dtype,flags", [(torch.float32, 0), (torch.bfloat16, 0), (torch.bfloat16, L.LOMA_FLAG_FORCE_GENERIC)])
@@ -387,6 +430,56 @@ def test_shared_decode(case, dtype, flags):
     call_shared(s, flags, lse=False)                              # the appended row is written again: bit for bit the same
     torch.cuda.synchronize()
     assert torch.equal(first, s["o"])
+
+
+@pytest.mark.parametrize("case", [(1, 1, 1, 64, 100, [0], 0), (1, 1, 1, 128, 1000, [0], 0), (1, 8, 2, 128, 300, [2], 0), (2, 4, 1, 64, 70, [-1, 3], 0),
+                                  (1, 2, 2, 64, 333, [4], 0)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_shared_decode_caches_of_a_few_rows(case, dtype):
+    """Own caches around 16 rows in all, below which a tile of them is no tile: prefix and own part take one path together."""
+    s = shared_case(*case, dtype, seed=7)
+    before = s["kc"].clone(), s["vc"].clone()
+    call_shared(s)
+    torch.cuda.synchronize()
+    check_shared(s)
+    caches_after(s, before)
+
+
+def test_shared_decode_prefix_shares_across_heads():
+    s = shared_case(*WIDE, torch.bfloat16, seed=77)
+    call_shared(s)
+    torch.cuda.synchronize()
+    check_shared(s)
+
+
+@pytest.mark.parametrize("ps", [0, 16])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_shared_decode_replayed_with_new_inputs(ps, dtype):
+    """Captured once, replayed with other queries, tokens and lengths (fewer and more than at capture): the eager call's bits."""
+    first = shared_case(12, 8, 2, 128, 900, [300, 20, -1, 0] * 3, ps, dtype, seed=31)
+    other = shared_case(12, 8, 2, 128, 900, [17, -1, 300, 255] * 3, ps, dtype, seed=32)
+    call_shared(other)
+    torch.cuda.synchronize()
+    want = other["o"].clone(), other["lse"].clone()
+    check_shared(other)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call_shared(first)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call_shared(first)
+    graph.replay()
+    torch.cuda.synchronize()
+    check_shared(first)
+    for k, v in other.items():
+        if isinstance(v, torch.Tensor) and k != "ws":
+            first[k].copy_(v)
+    first["o"].fill_(9.0), first["lse"].fill_(9.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(first["o"], want[0]) and torch.equal(first["lse"], want[1])
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])

@@ -84,6 +84,21 @@ def test_host_extend_defaults_and_steps_in_place(lib):
     assert int(taken) == int((table >= 0).sum()) and held.tolist() == [2, 3, 4]
 
 
+def huge_extend_case():
+    """Sums and positions far beyond 32 bits, entries beyond the table, page numbers whose slots do not fit."""
+    big = 2**31 - 1
+    lens, new = [5, big, 0, -2**31, 3], [big, big, -2**31, big, 4]
+    table = [[7, -1, -1], [1, 2, 3], [-1, -1, -1], [9, 9, 9], [big, 4, -1]]
+    return lens, new, [1, 3, 0, big, 2], [10, big, 0, 0, big - 1], [40, 41], table
+
+
+def test_host_extend_saturates(lib):
+    case = huge_extend_case()
+    got = run_extend(*case[:5], None, case[5], 4, 50)
+    check_extend(got, S.paged_extend(*case[:5], None, case[5], 4, 50))
+    assert got[1].tolist() == [0] + [2**31 - 1] * 5          # row_start
+
+
 def test_extend_refusals(lib):
     def call(B=2, ps=4, M=3, rows=4, n_free=2, dev=0, swap=None):
         p = {n: 0x10000 + 0x1000 * i for i, n in enumerate("lens new held pos free taken table rs pg ho sl sq po".split())}
