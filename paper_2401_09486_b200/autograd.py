@@ -108,5 +108,7 @@ class _QkNormRope(torch.autograd.Function):
 def loma_qk_norm_rope(q, k, wq, wk, n_chunks: int, c: int, t: int, tail_read: int = 0, flags: int = 0, eps: float = 0.0,
                       theta_base: float = 0.0, position_type: int = 0):
     """Per-head RMS norm of q [B, Hq, S, D] and k [B, Hk, S, D] with gains wq, wk ([D] or None) and the rotary embedding at the
-    layout's position ids as one differentiable torch op; returns (q_out, k_out).  Gradients flow to q, k, wq and wk."""
+    layout's position ids as one differentiable torch op; returns (q_out, k_out).  Gradients flow to q, k, wq and wk, once (no
+    double backward).  To capture a step into a CUDA graph, first drop every eager graph of the same leaves: torch ties a leaf's
+    gradient to the stream of its first use, and a capture may not wait for a stream outside it."""
     return _QkNormRope.apply(q, k, wq, wk, n_chunks, c, t, tail_read, flags, eps, theta_base, position_type)

@@ -413,6 +413,8 @@ SHARED = [
     (9, 16, 8, 128, 100, [2000, 1999, 0, -1, 777, 1500, 16, 15, 2000], 0),   # shares that hold parts of several sequences
     (6, 8, 4, 64, 300, [900, 3, -1, 500, 0, 899], 8),
     (40, 64, 4, 64, 500, [i % 20 for i in range(40)], 16),                   # 640 query rows per kv head, groups of 16
+    (3, 40, 2, 128, 200, [100, -1, 3], 0),                                   # groups of 20, short own caches
+    (3, 4, 2, 64, 90, [-1, -1, -1], 0),                                      # nothing but idle slots
 ]
 WIDE = (130, 100, 100, 64, 1300, [i % 5 for i in range(130)], 0)             # prefix shares that end inside a kv head, two row tiles
 
@@ -438,6 +440,32 @@ def test_shared_decode(case, dtype, flags):
 def test_shared_decode_caches_of_a_few_rows(case, dtype):
     """Own caches around 16 rows in all, below which a tile of them is no tile: prefix and own part take one path together."""
     s = shared_case(*case, dtype, seed=7)
+    before = s["kc"].clone(), s["vc"].clone()
+    call_shared(s)
+    torch.cuda.synchronize()
+    check_shared(s)
+    caches_after(s, before)
+
+
+@pytest.mark.parametrize("ps", [0, 16])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_shared_decode_all_idle_under_a_high_bound(ps, dtype):
+    s = shared_case(3, 4, 2, 64, 90, [300, 20, 4], ps, dtype, seed=9)
+    s["lens"].fill_(-1)
+    before = s["kc"].clone(), s["vc"].clone()
+    call_shared(s)
+    torch.cuda.synchronize()
+    assert (s["o"] == 9.0).all() and (s["lse"] == 9.0).all() and L.loma_device_status() == 0
+    caches_after(s, before)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_shared_decode_pool_of_one_page(dtype):
+    """A pool of 8 rows in all, fewer than a tile has, that holds the sequence's entries and no prefix."""
+    s = shared_case(1, 2, 1, 64, 0, [5], 8, dtype, seed=21)
+    page = int(s["table"][0, 0])
+    s["kc"], s["vc"] = s["kc"][page:page + 1].clone(), s["vc"][page:page + 1].clone()
+    s["table"].zero_()
     before = s["kc"].clone(), s["vc"].clone()
     call_shared(s)
     torch.cuda.synchronize()
