@@ -32,14 +32,39 @@ __device__ __forceinline__ int64_t prefix_row(const SharedArgs& a, int h, int j)
     return ((((int64_t)page * a.Hkv + h) << a.pg.log2_ps) + (j & ((1 << a.pg.log2_ps) - 1)));
 }
 
+// Sums over the lanes that differ in bit O, each keeping one half of the M values
+template <int M, int O>
+__device__ __forceinline__ void halve(float* s, int lane) {
+    const bool up = lane & O;
+#pragma unroll
+    for (int i = 0; i < M / 2; ++i) {
+        const float lo = s[i], hi = s[i + M / 2];
+        s[i] = (up ? hi : lo) + __shfl_xor_sync(0xffffffffu, up ? lo : hi, O);
+    }
+}
+
+// ... over the lanes that differ in any bit of 2 O - 1: value li * M / (2 O) + v of the M, or each value in 2 O / M lanes
+template <int M, int O>
+__device__ __forceinline__ void spread_sum(float* s, int lane) {
+    if constexpr (M > 1) halve<M, O>(s, lane);
+    else s[0] += __shfl_xor_sync(0xffffffffu, s[0], O);
+    if constexpr (O > 1) spread_sum<(M > 1 ? M / 2 : 1), O / 2>(s, lane);
+}
+
 // ------------------------------------------------------------------ own cache on CUDA cores (fp32, second opinion)
 // A worker is a warp, as in shared_own_tma_kernel.  The lanes that share a row hold 16 bytes of it each; G heads of the
-// group at a time, so a row is loaded once for them.
+// group at a time, so a row is loaded once for them.  The G x NL partial scores of a lane are added up over those lanes with
+// the results spread over them (16 shuffles for 16 scores instead of 80), so a lane keeps the maximum and the sum of one head
+// and takes one exponential where it would take 16; probabilities go back to all lanes through the warp's shared memory.
+// Loads in flight come from 16 warps per SM.
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(OWN_WARPS * 32)
+__global__ void __launch_bounds__(OWN_WARPS * 32, 4)
 shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
     using V = Vec16<T>;
-    constexpr int N = V::N, LPK = D / N, KPL = 32 / LPK, NL = OWN_KEYS / KPL < 8 ? OWN_KEYS / KPL : 8;
+    constexpr int N = V::N, LPK = D / N, KPL = 32 / LPK, NL_MOST = G == 4 ? 4 : 8, NL = OWN_KEYS / KPL < NL_MOST ? OWN_KEYS / KPL : NL_MOST;
+    // scores of a lane's keys and heads; how many a lane keeps, in how many lanes each is; lanes of a head
+    constexpr int M = G * NL, KEEP = M > LPK ? M / LPK : 1, DUP = LPK > M ? LPK / M : 1, LH = LPK / G;
+    __shared__ __align__(16) float s_prob[OWN_WARPS][KPL][M];
     __shared__ int64_t scan[SeqBlocks::MAX_GROUPS + 1];
     __shared__ int64_t wsum[OWN_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LPK, li = lane % LPK;
@@ -54,7 +79,7 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
         const int64_t t_end = first_block(w + 1, total, W);
         SeqBlocks::Cursor c = sb.find(t, scan, per);
         const float scale_log2 = a.scale * 1.4426950408889634f;
-        float q[G][N], acc[G][N], m[G], l[G];
+        float q[G][N], acc[G][N], m = -INFINITY, l = 0.f;   // m, l: of head li / LH, this lane's share of its keys
         bool fresh = true;
         for (; t < t_end; ++t) {
             const int h = c.hh / p.g_tiles, gt = c.hh - h * p.g_tiles, heads = min(G, a.g - gt * G), len = c.len;
@@ -67,9 +92,9 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
                     V::unpack(__ldg(reinterpret_cast<const uint4*>(qp) + li), q[x]);
 #pragma unroll
                     for (int e = 0; e < N; ++e) { q[x][e] *= scale_log2; acc[x][e] = 0.f; }
-                    m[x] = -INFINITY;
-                    l[x] = 0.f;
                 }
+                m = -INFINITY;
+                l = 0.f;
                 fresh = false;
             }
 #pragma unroll 1
@@ -82,41 +107,65 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
                     kr[i] = ld_stream16((key == len && kn ? kn : static_cast<const T*>(a.k_cache) + row) + li * N);
                     vr[i] = ld_stream16((key == len && vn ? vn : static_cast<const T*>(a.v_cache) + row) + li * N);
                 }
+                float s[M];
 #pragma unroll
-                for (int x = 0; x < G; ++x) {
-                    float s[NL], mb = -INFINITY;
+                for (int i = 0; i < NL; ++i) {
+                    float kf[N];
+                    V::unpack(kr[i], kf);
 #pragma unroll
-                    for (int i = 0; i < NL; ++i) {
-                        float kf[N];
-                        V::unpack(kr[i], kf);
-                        s[i] = 0.f;
+                    for (int x = 0; x < G; ++x) {
+                        s[x * NL + i] = 0.f;
 #pragma unroll
-                        for (int e = 0; e < N; ++e) s[i] = fmaf(q[x][e], kf[e], s[i]);
+                        for (int e = 0; e < N; ++e) s[x * NL + i] = fmaf(q[x][e], kf[e], s[x * NL + i]);
                     }
+                }
+                spread_sum<M, LPK / 2>(s, lane);
+                float top = -INFINITY;
 #pragma unroll
-                    for (int o = LPK / 2; o > 0; o >>= 1)
+                for (int v = 0; v < KEEP; ++v) {
+                    if (j0 + (li % LH / DUP * KEEP + v) * KPL + sub > len) s[v] = -INFINITY;
+                    top = fmaxf(top, s[v]);
+                }
 #pragma unroll
-                        for (int i = 0; i < NL; ++i) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+                for (int o = DUP; o < LH; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
 #pragma unroll
-                    for (int i = 0; i < NL; ++i) {
-                        s[i] = j0 + i * KPL + sub <= len ? s[i] : -INFINITY;
-                        mb = fmaxf(mb, s[i]);
+                for (int o = LPK; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                // the reference moves only when a head's maximum has grown by more than 2^8 (probabilities stay below 2^8)
+                if (__any_sync(0xffffffffu, top > m + 8.f)) {
+                    const float m_new = fmaxf(m, top), alpha = m_new == -INFINITY ? 1.f : exp2f(m - m_new);
+                    m = m_new;
+                    l *= alpha;
+#pragma unroll
+                    for (int x = 0; x < G; ++x) {
+                        const float f = __shfl_sync(0xffffffffu, alpha, x * LH);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) acc[x][e] *= f;
                     }
+                }
+                const float ref = m == -INFINITY ? 0.f : m;
+                __syncwarp();   // the last round's probabilities have been read
 #pragma unroll
-                    for (int o = 16; o >= LPK; o >>= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, o));
-                    const float m_new = fmaxf(m[x], mb), ref = m_new == -INFINITY ? 0.f : m_new, alpha = exp2f(m[x] - ref);
-                    m[x] = m_new;
-                    l[x] *= alpha;
+                for (int v = 0; v < KEEP; ++v) {
+                    const float pr = exp2f(s[v] - ref);
+                    l += pr;
+                    if (li % DUP == 0) s_prob[warp][sub][li / DUP * KEEP + v] = pr;
+                }
+                __syncwarp();
 #pragma unroll
-                    for (int e = 0; e < N; ++e) acc[x][e] *= alpha;
+                for (int i = 0; i < NL; i += 4) {
+                    float4 pr[G];
 #pragma unroll
-                    for (int i = 0; i < NL; ++i) {
-                        const float pr = exp2f(s[i] - ref);
+                    for (int x = 0; x < G; ++x) pr[x] = *reinterpret_cast<const float4*>(&s_prob[warp][sub][x * NL + i]);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
                         float vf[N];
-                        V::unpack(vr[i], vf);
-                        l[x] += pr;
+                        V::unpack(vr[i + y], vf);
 #pragma unroll
-                        for (int e = 0; e < N; ++e) acc[x][e] = fmaf(pr, vf[e], acc[x][e]);
+                        for (int x = 0; x < G; ++x) {
+                            const float f = y == 0 ? pr[x].x : y == 1 ? pr[x].y : y == 2 ? pr[x].z : pr[x].w;
+#pragma unroll
+                            for (int e = 0; e < N; ++e) acc[x][e] = fmaf(f, vf[e], acc[x][e]);
+                        }
                     }
                 }
             }
@@ -124,22 +173,22 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
             if (tail || t + 1 == t_end) {
                 const int64_t seg = w + (int64_t)c.hh * a.B + c.b;
 #pragma unroll
+                for (int o = DUP; o < LH; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+#pragma unroll
+                for (int o = LPK; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+                const int mine = li / LH;
+                if (lane < LPK && li % LH == 0 && mine < heads) ws[p.own_lse + seg * p.g_rows + mine] = m + log2f(l);
+#pragma unroll
                 for (int x = 0; x < G; ++x) {
-                    float lt = l[x], ot[N];
+                    const float inv = 1.f / __shfl_sync(0xffffffffu, l, x * LH);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) ot[e] = acc[x][e];
+                    for (int e = 0; e < N; ++e)
 #pragma unroll
-                    for (int o = 16; o >= LPK; o >>= 1) {
-                        lt += __shfl_xor_sync(0xffffffffu, lt, o);
-#pragma unroll
-                        for (int e = 0; e < N; ++e) ot[e] += __shfl_xor_sync(0xffffffffu, ot[e], o);
-                    }
+                        for (int o = 16; o >= LPK; o >>= 1) acc[x][e] += __shfl_xor_sync(0xffffffffu, acc[x][e], o);
                     if (x < heads && lane < LPK) {
-                        const float inv = 1.f / lt;
                         float4* o = reinterpret_cast<float4*>(ws + p.own_o + (seg * p.g_rows + x) * D + li * N);
 #pragma unroll
-                        for (int e = 0; e < N; e += 4) o[e / 4] = make_float4(ot[e] * inv, ot[e + 1] * inv, ot[e + 2] * inv, ot[e + 3] * inv);
-                        if (lane == 0) ws[p.own_lse + seg * p.g_rows + x] = m[x] + log2f(lt);
+                        for (int e = 0; e < N; e += 4) o[e / 4] = make_float4(acc[x][e] * inv, acc[x][e + 1] * inv, acc[x][e + 2] * inv, acc[x][e + 3] * inv);
                     }
                 }
                 // the new token's K and V go to entry len (read by nobody in this launch)
@@ -157,26 +206,35 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
 }
 
 // ------------------------------------------------------------------ prefix on CUDA cores (fp32, small pages, second opinion)
-// RT query rows against 32 keys at a time, all in fp32 in shared memory, with RT / 16 x 2 scores and RT / 8 x (D / 32) outputs
-// per thread in registers; the next keys are on their way from memory while these are worked on.  Bound by fp32 FMA for many
-// rows, by the latency of a block's steps for few.  Query row m of kv head h is head h g + m mod g of sequence m / g.
+// RT query rows against 32 keys at a time, all in fp32, RT / 8 rows to a warp from the scores to the outputs: between two
+// barriers (one per block, K and V are double buffered) a warp waits for nobody.
+//   scores   a lane has 4 keys x up to 4 rows and every 2nd or 4th group of 4 features; the lanes that share a tile then halve
+//            it between them while they add their sums.  That takes 12 shared-memory wavefronts for 32 two-wide FMAs a lane,
+//            fewer than the FMAs take; a tile of 2 keys x 4 rows needed twice as many.
+//   outputs  a lane has D / 32 features of all of the warp's rows; probabilities come through the warp's own shared memory.
+// Bound by fp32 FMA for many rows, by the latency of a block's steps for few.  Query row m of kv head h is head h g + m mod g of
+// sequence m / g.
 constexpr int SIMT_THREADS = 256;
 
 template <int D, int RT>
-struct SimtSmem {
-    static constexpr int Q = 0, K = Q + RT * (D + 4), V = K + SIMT_K * (D + 4), S = V + SIMT_K * D, ML = S + RT * (SIMT_K + 4),
-                         FLOATS = ML + 3 * RT;
+struct SimtSmem {   // in floats
+    static constexpr int K_TILE = SIMT_K * (D + 4), TILE = K_TILE + SIMT_K * D;   // K rows padded: lanes read 8 rows at a time
+    static constexpr int Q = 0, KV = Q + RT * (D + 4), P = KV + 2 * TILE, A = P + RT * SIMT_K, FLOATS = A + RT;
 };
 
 template <typename T, int D, int RT>
-__global__ void __launch_bounds__(SIMT_THREADS, RT == 64 ? 1 : 2)
+__global__ void __launch_bounds__(SIMT_THREADS, 2)
 shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
     using V = Vec16<T>;
     using SM = SimtSmem<D, RT>;
-    constexpr int N = V::N, LPK = D / N, DC = D / 32, PASSES = SIMT_K * LPK / SIMT_THREADS, SR = RT / 16, KU = SIMT_K / 16, OR = RT / 8;
+    static_assert(SIMT_K == 32, "8 lanes x 4 keys");
+    constexpr int N = V::N, LPK = D / N, DC = D / 32, PASSES = SIMT_K * LPK / SIMT_THREADS;
+    constexpr int WR = RT / 8, TR = WR < 4 ? WR : 4, RL = WR / TR, DL = 4 / RL;   // rows of a warp and a lane; lanes over rows, features
+    constexpr int M = TR * 4 / DL, KR = M < 4 ? 1 : M / 4, KK = M < 4 ? M : 4;    // scores a lane keeps: KR rows x KK keys
+    constexpr bool ASYNC = sizeof(T) == 4;                                        // bf16 is widened on its way, through registers
     extern __shared__ __align__(16) float sm[];
     let_next_start();
-    const int tid = threadIdx.x, rows = a.B * a.g;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rows = a.B * a.g;
     const float scale_log2 = a.scale * 1.4426950408889634f;
     const int worker = blockIdx.x / p.m_tiles, mt = blockIdx.x - worker * p.m_tiles;
     const int64_t blocks = (int64_t)a.Hkv * p.p_blocks;
@@ -184,23 +242,47 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
     const int64_t t_end = first_block(worker + 1, blocks, p.p_workers);
     const int r_in = blockIdx.y * RT, row0 = mt * SHP_ROWS + r_in;   // RT rows of the tile per blockIdx.y
     if (row0 >= rows) t = t_end;
-    const int sr = (tid >> 4) * SR, sk = tid & 15;        // scores: rows sr ..; keys sk + 16 u
-    const int orow = (tid >> 5) * OR, oc = tid & 31;      // outputs: rows orow .. (a warp's own); features oc * DC ..
-    uint4 kv[2][PASSES];
-    auto load = [&](int h, int k0) {                      // all of the thread's loads at once
+    const int kl = lane & 7, rl = (lane >> 3) % RL, dl = (lane >> 3) / RL;        // scores: keys kl + 8 w, rows rl * TR + u
+    const int base = DL == 2 ? dl * M : (dl >> 1) * 2 * M + (dl & 1) * M;         // the first (row, key) that the lane keeps
+    const int row_k = warp * WR + rl * TR + base / 4, col_k = base % 4;
+    const float* q_at = sm + SM::Q + (warp * WR + rl * TR) * (D + 4) + 4 * dl;
+    float* p_warp = sm + SM::P + warp * WR * SIMT_K;
+
+    // the fetch is a block ahead, and the rows' places (a table entry away) are known another block earlier
+    int h_f = 0, blk_f = 0;
+    int64_t row_f[PASSES];
+    uint4 kv[ASYNC ? 1 : 2][ASYNC ? 1 : PASSES];
+    auto find_rows = [&]() {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i)   // keys past the end repeat the last one
+            row_f[i] = prefix_row(a, h_f, min(blk_f * SIMT_K + (tid + i * SIMT_THREADS) / LPK, a.prefix_len - 1)) * D;
+    };
+    auto fetch = [&](int buf, bool more) {
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
             const int r = (tid + i * SIMT_THREADS) / LPK, c = (tid + i * SIMT_THREADS) % LPK;
-            const int64_t row = prefix_row(a, h, min(k0 + r, a.prefix_len - 1)) * D;   // keys past the end repeat the last one
-            kv[0][i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.k_prefix) + row) + c);
-            kv[1][i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.v_prefix) + row) + c);
+            const T* kp = static_cast<const T*>(a.k_prefix) + row_f[i] + c * N;
+            const T* vp = static_cast<const T*>(a.v_prefix) + row_f[i] + c * N;
+            if constexpr (ASYNC) {
+                float* tile = sm + SM::KV + buf * SM::TILE;
+                cp_async16((uint32_t)__cvta_generic_to_shared(tile + r * (D + 4) + c * N), kp);
+                cp_async16((uint32_t)__cvta_generic_to_shared(tile + SM::K_TILE + r * D + c * N), vp);
+            } else {
+                kv[0][i] = __ldg(reinterpret_cast<const uint4*>(kp));
+                kv[1][i] = __ldg(reinterpret_cast<const uint4*>(vp));
+            }
         }
+        if (++blk_f == p.p_blocks) { blk_f = 0; ++h_f; }
+        if (more) find_rows();
     };
-    if (t < t_end) load((int)(t / p.p_blocks), (int)(t % p.p_blocks) * SIMT_K);
+    int buf = 0, h = 0, blk = 0;
+    if (t < t_end) {
+        h = h_f = (int)(t / p.p_blocks);
+        blk = blk_f = (int)(t - (int64_t)h * p.p_blocks);
+        find_rows();
+        fetch(0, t + 1 < t_end);
+    }
     while (t < t_end) {                                   // segments of the CTA's share
-        const int h = (int)(t / p.p_blocks), blk0 = (int)(t - (int64_t)h * p.p_blocks);
-        const int blk1 = (int)min((int64_t)p.p_blocks, blk0 + (t_end - t));
-        const int begin = blk0 * SIMT_K, end = min(a.prefix_len, blk1 * SIMT_K);
         const int64_t seg = (int64_t)(worker + h) * p.m_tiles + mt;
         __syncthreads();
 #pragma unroll 4
@@ -212,102 +294,127 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
 #pragma unroll
             for (int e = 0; e < N; ++e) sm[SM::Q + r * (D + 4) + c * N + e] = f[e] * scale_log2;
         }
-        if (tid < RT) { sm[SM::ML + tid] = -INFINITY; sm[SM::ML + RT + tid] = 0.f; }
-        uint64_t acc[OR][DC / 2];
+        uint64_t acc[WR][DC / 2];
+        float mx[KR], l[KR];
 #pragma unroll
-        for (int u = 0; u < OR; ++u)
+        for (int u = 0; u < WR; ++u)
 #pragma unroll
             for (int c = 0; c < DC / 2; ++c) acc[u][c] = 0;
-        for (int k0 = begin; k0 < end; k0 += SIMT_K) {
-            if (k0 > begin) __syncthreads();              // the tiles have been read
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int r = (tid + i * SIMT_THREADS) / LPK, c = (tid + i * SIMT_THREADS) % LPK;
-                float f[N];
-                V::unpack(kv[0][i], f);
+        for (int u = 0; u < KR; ++u) { mx[u] = -INFINITY; l[u] = 0.f; }
+        for (; blk < p.p_blocks && t < t_end; ++blk, buf ^= 1) {
+            float* k_tile = sm + SM::KV + buf * SM::TILE;
+            float* v_tile = k_tile + SM::K_TILE;
+            if constexpr (ASYNC) {
+                asm volatile("cp.async.wait_all;" ::: "memory");
+            } else {
 #pragma unroll
-                for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(&sm[SM::K + r * (D + 4) + c * N + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
-                V::unpack(kv[1][i], f);
+                for (int i = 0; i < PASSES; ++i) {
+                    const int r = (tid + i * SIMT_THREADS) / LPK, c = (tid + i * SIMT_THREADS) % LPK;
+                    float f[N];
+                    V::unpack(kv[0][i], f);
 #pragma unroll
-                for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(&sm[SM::V + r * D + c * N + e]) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+                    for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(k_tile + r * (D + 4) + c * N + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+                    V::unpack(kv[1][i], f);
+#pragma unroll
+                    for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(v_tile + r * D + c * N + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+                }
             }
-            if (++t < t_end) load((int)(t / p.p_blocks), (int)(t % p.p_blocks) * SIMT_K);
-            __syncthreads();
-            // two-wide FMA: sums over even and odd features side by side
-            uint64_t s2[SR][KU];
+            __syncthreads();                              // the tile is there, and the other one has been read
+            if (++t < t_end) fetch(buf ^ 1, t + 1 < t_end);
+            uint64_t s2[TR][4];                           // two-wide FMA: sums over even and odd features side by side
 #pragma unroll
-            for (int u = 0; u < SR; ++u)
+            for (int u = 0; u < TR; ++u)
 #pragma unroll
-                for (int w = 0; w < KU; ++w) s2[u][w] = 0;
-#pragma unroll 4
-            for (int d = 0; d < D; d += 4) {
-                ulonglong2 qv[SR], kf[KU];
+                for (int w = 0; w < 4; ++w) s2[u][w] = 0;
+            const float* k_at = k_tile + kl * (D + 4) + 4 * dl;
+#pragma unroll 2
+            for (int d = 0; d < D; d += 4 * DL) {
+                ulonglong2 qv[TR];
 #pragma unroll
-                for (int u = 0; u < SR; ++u) qv[u] = *reinterpret_cast<const ulonglong2*>(&sm[SM::Q + (sr + u) * (D + 4) + d]);
+                for (int u = 0; u < TR; ++u) qv[u] = *reinterpret_cast<const ulonglong2*>(q_at + u * (D + 4) + d);
 #pragma unroll
-                for (int u = 0; u < KU; ++u) kf[u] = *reinterpret_cast<const ulonglong2*>(&sm[SM::K + (sk + 16 * u) * (D + 4) + d]);
+                for (int w = 0; w < 4; ++w) {
+                    const ulonglong2 kf = *reinterpret_cast<const ulonglong2*>(k_at + 8 * w * (D + 4) + d);
 #pragma unroll
-                for (int u = 0; u < SR; ++u)
-#pragma unroll
-                    for (int w = 0; w < KU; ++w) s2[u][w] = fma2(qv[u].y, kf[w].y, fma2(qv[u].x, kf[w].x, s2[u][w]));
+                    for (int u = 0; u < TR; ++u) s2[u][w] = fma2(qv[u].y, kf.y, fma2(qv[u].x, kf.x, s2[u][w]));
+                }
             }
-            float s[SR][KU];
+            float s[TR * 4];
 #pragma unroll
-            for (int u = 0; u < SR; ++u)
+            for (int u = 0; u < TR; ++u)
 #pragma unroll
-                for (int w = 0; w < KU; ++w) {
+                for (int w = 0; w < 4; ++w) {
                     float lo, hi;
                     unpack2(s2[u][w], lo, hi);
-                    s[u][w] = lo + hi;
+                    s[4 * u + w] = lo + hi;
+                }
+            halve<TR * 4, 16>(s, lane);
+            if constexpr (DL == 4) halve<TR * 2, 8>(s, lane);
+            // the reference moves only when a row's maximum has grown by more than 2^8 (probabilities stay below 2^8)
+            float top[KR];
+            bool grown = false;
+#pragma unroll
+            for (int u = 0; u < KR; ++u) {
+                top[u] = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < KK; ++w) {
+                    float& x = s[u * KK + w];
+                    if (blk * SIMT_K + kl + 8 * (col_k + w) >= a.prefix_len) x = -INFINITY;
+                    top[u] = fmaxf(top[u], x);
                 }
 #pragma unroll
-            for (int u = 0; u < SR; ++u) {   // 16 lanes share a row
-                float mx = -INFINITY;
+                for (int o = 1; o < (KK < 4 ? 16 : 8); o <<= 1) top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], o));
+                grown |= top[u] > mx[u] + 8.f;
+            }
+            if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
-                for (int w = 0; w < KU; ++w) {
-                    if (k0 + sk + 16 * w >= end) s[u][w] = -INFINITY;
-                    mx = fmaxf(mx, s[u][w]);
+                for (int u = 0; u < KR; ++u) {
+                    const float m_new = fmaxf(mx[u], top[u]), alpha = m_new == -INFINITY ? 1.f : exp2f(mx[u] - m_new);
+                    mx[u] = m_new;
+                    l[u] *= alpha;
+                    if (kl == 0 && col_k == 0) sm[SM::A + row_k + u] = alpha;
                 }
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                const float m_old = sm[SM::ML + sr + u], m_new = fmaxf(m_old, mx), ref = m_new == -INFINITY ? 0.f : m_new;
-                float sum = 0.f;
-#pragma unroll
-                for (int w = 0; w < KU; ++w) {
-                    const float e = exp2f(s[u][w] - ref);
-                    sum += e;
-                    sm[SM::S + (sr + u) * (SIMT_K + 4) + sk + 16 * w] = e;
-                }
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                 __syncwarp();
-                if ((tid & 15) == 0) {
-                    const float alpha = exp2f(m_old - ref);
-                    sm[SM::ML + sr + u] = m_new;
-                    sm[SM::ML + RT + sr + u] = sm[SM::ML + RT + sr + u] * alpha + sum;
-                    sm[SM::ML + 2 * RT + sr + u] = alpha;
+#pragma unroll
+                for (int u = 0; u < WR; ++u) {
+                    const float alpha = sm[SM::A + warp * WR + u];
+#pragma unroll
+                    for (int c = 0; c < DC / 2; ++c) acc[u][c] = fma2(acc[u][c], pack2(alpha, alpha), 0);
                 }
             }
-            __syncthreads();
 #pragma unroll
-            for (int u = 0; u < OR; ++u) {
-                const float alpha = sm[SM::ML + 2 * RT + orow + u];
+            for (int u = 0; u < KR; ++u) {
+                const float ref = mx[u] == -INFINITY ? 0.f : mx[u];
 #pragma unroll
-                for (int c = 0; c < DC / 2; ++c) acc[u][c] = fma2(acc[u][c], pack2(alpha, alpha), 0);
+                for (int w = 0; w < KK; ++w) {
+                    s[u * KK + w] = exp2f(s[u * KK + w] - ref);
+                    l[u] += s[u * KK + w];
+                }
+                float* dst = sm + SM::P + (row_k + u) * SIMT_K + kl * 4 + col_k;      // column 4 kl + w: key kl + 8 w
+                if constexpr (KK == 4) *reinterpret_cast<float4*>(dst) = make_float4(s[u * 4], s[u * 4 + 1], s[u * 4 + 2], s[u * 4 + 3]);
+                else *reinterpret_cast<float2*>(dst) = make_float2(s[u * KK], s[u * KK + 1]);
             }
+            __syncwarp();
 #pragma unroll 2
-            for (int k = 0; k < SIMT_K; k += 4) {
-                float4 pv[OR];
+            for (int k = 0; k < 8; ++k) {
+                float4 pv[WR];
 #pragma unroll
-                for (int u = 0; u < OR; ++u) pv[u] = *reinterpret_cast<const float4*>(&sm[SM::S + (orow + u) * (SIMT_K + 4) + k]);
+                for (int u = 0; u < WR; ++u) pv[u] = *reinterpret_cast<const float4*>(p_warp + u * SIMT_K + 4 * k);
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
+                for (int w = 0; w < 4; ++w) {
+                    const float* vp = v_tile + (k + 8 * w) * D + lane * DC;
                     uint64_t vv[DC / 2];
+                    if constexpr (DC == 4) {
+                        const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(vp);
+                        vv[0] = x.x;
+                        vv[DC / 2 - 1] = x.y;
+                    } else {
+                        vv[0] = *reinterpret_cast<const uint64_t*>(vp);
+                    }
 #pragma unroll
-                    for (int c = 0; c < DC / 2; ++c) vv[c] = *reinterpret_cast<const uint64_t*>(&sm[SM::V + (k + kk) * D + oc * DC + 2 * c]);
-#pragma unroll
-                    for (int u = 0; u < OR; ++u) {
-                        const float pr = kk == 0 ? pv[u].x : kk == 1 ? pv[u].y : kk == 2 ? pv[u].z : pv[u].w;
+                    for (int u = 0; u < WR; ++u) {
+                        const float pr = w == 0 ? pv[u].x : w == 1 ? pv[u].y : w == 2 ? pv[u].z : pv[u].w;
                         const uint64_t pr2 = pack2(pr, pr);
 #pragma unroll
                         for (int c = 0; c < DC / 2; ++c) acc[u][c] = fma2(pr2, vv[c], acc[u][c]);
@@ -315,23 +422,34 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
                 }
             }
         }
-        __syncthreads();
+        // the segment ends: sums over the lanes of a row, outputs divided by them
         float* ws = static_cast<float*>(a.ws);
+        __syncwarp();
 #pragma unroll
-        for (int u = 0; u < OR; ++u) {
-            const float inv = 1.f / sm[SM::ML + RT + orow + u];
-            if (row0 + orow + u < rows) {
+        for (int u = 0; u < KR; ++u) {
+#pragma unroll
+            for (int o = 1; o < (KK < 4 ? 16 : 8); o <<= 1) l[u] += __shfl_xor_sync(0xffffffffu, l[u], o);
+            if (kl == 0 && col_k == 0) {
+                sm[SM::A + row_k + u] = 1.f / l[u];
+                if (row0 + row_k + u < rows) ws[p.p_lse + seg * SHP_ROWS + r_in + row_k + u] = mx[u] + log2f(l[u]);
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < WR; ++u) {
+            const float inv = sm[SM::A + warp * WR + u];
+            if (row0 + warp * WR + u < rows) {
 #pragma unroll
                 for (int c = 0; c < DC / 2; ++c) {
-                    const int d = oc * DC + 2 * c;
+                    const int d = lane * DC + 2 * c;
                     float lo, hi;
                     unpack2(acc[u][c], lo, hi);
-                    *reinterpret_cast<float2*>(ws + p.p_o + seg * SHP_ROWS * D + ((int64_t)(d >> 2) * SHP_ROWS + r_in + orow + u) * 4 + (d & 3)) =
+                    *reinterpret_cast<float2*>(ws + p.p_o + seg * SHP_ROWS * D + ((int64_t)(d >> 2) * SHP_ROWS + r_in + warp * WR + u) * 4 + (d & 3)) =
                         make_float2(lo * inv, hi * inv);
                 }
             }
         }
-        if (tid < RT && row0 + tid < rows) ws[p.p_lse + seg * SHP_ROWS + r_in + tid] = sm[SM::ML + tid] + log2f(sm[SM::ML + RT + tid]);
+        if (blk == p.p_blocks) { blk = 0; ++h; }
     }
 }
 

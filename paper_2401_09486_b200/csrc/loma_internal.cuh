@@ -307,6 +307,10 @@ struct Vec16<__nv_bfloat16> {
     }
 };
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
 #ifdef __CUDACC__
 // Programmatic dependent launch: the next kernel of the stream may start once every CTA of this one has called the first;
 // the second waits until the kernels this one was launched behind have finished.

@@ -51,10 +51,6 @@ __device__ __forceinline__ float row_sum(float x) {
     return x;
 }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-
 // Pairs (batch, head) of one tensor that this lane walks: first, first + step, ... below p1.  `stages` fetches are in flight.
 // BWD: v.grad is read too, acc[0..N) / acc[N..2N) collect the lane's share of dw.
 template <typename T, int D, bool BWD, int STAGES>
