@@ -529,13 +529,14 @@ static cudaError_t prefix_simt_rt(const SharedArgs& a, const SharedPlan& p, bool
     const int rows = std::min(a.B * a.g, SHP_ROWS);
     return launch_behind(shared_prefix_simt_kernel<T, D, RT>, dim3(p.p_workers * p.m_tiles, (rows + RT - 1) / RT), SIMT_THREADS, smem, st, behind, a, p);
 }
-// the tallest row tile that the rows fill
+// Row tiles of 64 where that leaves two CTAs for an SM, which fill each other's waits, or else of 32 (B12 Hq16 Hkv4, prefix
+// 2500: 30.4 us with 64, 28.5 with 32); 16 for up to 16 rows only (28 rows: 41.7 us in one tile of 32, 53.7 in two of 16).
 template <typename T, int D>
 static cudaError_t prefix_simt(const SharedArgs& a, const SharedPlan& p, bool behind, cudaStream_t st) {
     if (p.p_keys != SIMT_K) return cudaErrorInvalidValue;
-    const int rows = a.B * a.g;
-    return rows <= 16 ? prefix_simt_rt<T, D, 16>(a, p, behind, st) : rows <= 32 ? prefix_simt_rt<T, D, 32>(a, p, behind, st)
-                                                                                 : prefix_simt_rt<T, D, 64>(a, p, behind, st);
+    const int rows = std::min(a.B * a.g, SHP_ROWS), share = p.p_workers * p.m_tiles;
+    if (rows > 32 && share * ((rows + 63) / 64) > 148) return prefix_simt_rt<T, D, 64>(a, p, behind, st);
+    return rows > 16 ? prefix_simt_rt<T, D, 32>(a, p, behind, st) : prefix_simt_rt<T, D, 16>(a, p, behind, st);
 }
 
 template <typename T, int D>
@@ -554,7 +555,7 @@ static cudaError_t shared_t(const SharedArgs& a, bool generic, cudaStream_t st) 
     if (tc) {
         e = launch_shared_own_tma(a, p, D, false, st);
         if (e == cudaSuccess) e = prefix(true);
-    } else {   // neither kernel leaves room for the other, and the longer one goes first
+    } else {   // the longer one goes first; the other's CTAs take the room it leaves
         e = prefix(false);
         if (e == cudaSuccess) e = own_stream<T, D>(a, p, p.p_blocks > 0, st);
     }

@@ -61,7 +61,7 @@ inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len
     p.m_tiles = (int)((rows + SHP_ROWS - 1) / SHP_ROWS);
     p.p_keys = cuda_cores ? SIMT_K : SHP_KEYS;
     p.p_blocks = (prefix_len + p.p_keys - 1) / p.p_keys;
-    int64_t w = std::max(1, (cuda_cores ? SHP_CTAS / 2 : SHP_CTAS) / p.m_tiles);   // CUDA cores: one CTA fills an SM
+    int64_t w = std::max(1, (cuda_cores ? SHP_CTAS / 2 : SHP_CTAS) / p.m_tiles);   // CUDA cores: B60 Hq16 Hkv2 prefix 4000 84 us cut for 148, 96 for 296
     // shares that end inside a kv head make most workers change heads once, which costs about as much as six blocks (draining
     // the products, storing a partial result, new query rows): whole workers per kv head where their longer shares cost less
     const int64_t all = (int64_t)Hkv * p.p_blocks, whole = w / Hkv * Hkv;

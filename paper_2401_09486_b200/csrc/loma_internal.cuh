@@ -319,12 +319,12 @@ __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontr
 
 // Launch a kernel that may start while the one before it in the stream still runs.
 template <typename... P, typename... A>
-cudaError_t launch_behind(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, bool behind, A... args) {
+cudaError_t launch_behind(void (*kernel)(P...), dim3 grid, dim3 threads, int smem, cudaStream_t st, bool behind, A... args) {
     cudaError_t e = prepare_kernel(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
+    cfg.blockDim = threads;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[1];

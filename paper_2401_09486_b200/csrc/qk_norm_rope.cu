@@ -210,6 +210,7 @@ qk_norm_rope_kernel(const HeadsView q, const HeadsView k, int B, Layout L, float
                 }
             }
             __syncthreads();
+            if (which == 1 || !k.dw) let_next_start();   // the sums of dw: here, so that their CTAs take no room from these
             if (threadIdx.x < D) {
                 float s = 0.f;
 #pragma unroll
@@ -228,6 +229,7 @@ __global__ void __launch_bounds__(1024)
 qk_norm_dw_kernel(const float* __restrict__ part, int n_cta, int D, T* __restrict__ dwq, T* __restrict__ dwk) {
     __shared__ double s[32][33];
     T* dw = blockIdx.y == 0 ? dwq : dwk;
+    wait_for_previous();   // launched while the last CTAs finish
     if (!dw) return;
     const int d = blockIdx.x * 32 + threadIdx.x;
     const float* p = part + (int64_t)blockIdx.y * n_cta * D + d;
@@ -290,10 +292,8 @@ static cudaError_t norm_t(const HeadsView& q, const HeadsView& k, int B, const L
     count_launches(1);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || (!q.dw && !k.dw)) return e;
-    qk_norm_dw_kernel<T><<<dim3(D / 32, 2), dim3(32, 32), 0, st>>>(static_cast<const float*>(ws), grid.x * grid.y, D,
-                                                                   static_cast<T*>(q.dw), static_cast<T*>(k.dw));
-    count_launches(1);
-    return cudaGetLastError();
+    return launch_behind(qk_norm_dw_kernel<T>, dim3(D / 32, 2), dim3(32, 32), 0, st, true, static_cast<const float*>(ws), (int)(grid.x * grid.y), D,
+                         static_cast<T*>(q.dw), static_cast<T*>(k.dw));
 }
 
 cudaError_t launch_qk_norm_rope(const HeadsView& q, const HeadsView& k, int B, int D, const Layout& L, loma_dtype dt, float eps,
