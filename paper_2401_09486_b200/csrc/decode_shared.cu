@@ -56,7 +56,8 @@ __device__ __forceinline__ void spread_sum(float* s, int lane) {
 // group at a time, so a row is loaded once for them.  The G x NL partial scores of a lane are added up over those lanes with
 // the results spread over them (16 shuffles for 16 scores instead of 80), so a lane keeps the maximum and the sum of one head
 // and takes one exponential where it would take 16; probabilities go back to all lanes through the warp's shared memory.
-// Loads in flight come from 16 warps per SM.
+// Loads in flight come from 16 warps per SM.  With the merge, fp32 B60 Hq16 Hkv2, lengths up to 300: 20.8 us (32.2 with every score
+// in every lane).
 template <typename T, int D, int G>
 __global__ void __launch_bounds__(OWN_WARPS * 32, 4)
 shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
@@ -212,8 +213,8 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
 //            it between them while they add their sums.  That takes 12 shared-memory wavefronts for 32 two-wide FMAs a lane,
 //            fewer than the FMAs take; a tile of 2 keys x 4 rows needed twice as many.
 //   outputs  a lane has D / 32 features of all of the warp's rows; probabilities come through the warp's own shared memory.
-// Bound by fp32 FMA for many rows, by the latency of a block's steps for few.  Query row m of kv head h is head h g + m mod g of
-// sequence m / g.
+// Bound by fp32 FMA for many rows, by the latency of a block's steps for few.  Measured: 480 query rows, 2 kv heads, D128, prefix 4000:
+// 67.8 us, FMA pipe active 53 % of the cycles, shared memory 57 %.  Query row m of kv head h is head h g + m mod g of sequence m / g.
 constexpr int SIMT_THREADS = 256;
 
 template <int D, int RT>

@@ -12,6 +12,7 @@
 // lane's heads are the same two in scores, maxima, sums and outputs.  A block takes about 150 instructions; four warps per
 // SM turn them over faster than HBM delivers (44 bytes per SM and nanosecond, 190 ns for the 8 KB of a block), and 96 KB
 // of rings leave room beside a CTA of the prefix kernel: the two run at the same time.
+// Measured alone: B128 Hq32 Hkv8 D128, lengths up to 1500, 397 MB: 67.7 us, 5.9 TB/s (0.91 of a copy).
 #include "decode_shared.cuh"
 #include "tcgen05_common.cuh"
 

@@ -16,6 +16,8 @@
 // fetches its next pairs into a ring of its own in shared memory (cp.async, nobody else reads it, so there is no barrier):
 // bytes in flight cost no registers, which w, cos / sin and the sums of dw need.  The rows that a warp takes together lie
 // behind one another in memory: consecutive rows of a head, or, in a projection's [B, S, H, D] output, heads of a row.
+// Measured, bf16, 4608 rows of B4, D128: forward of 32 + 32 heads 98.4 us (6.1 TB/s, 0.95 of a copy), backward of 32 + 8 heads 98.7 us
+// (5.7 TB/s, 0.89; issue slots 62 % taken).  A few hundred rows in fp32: 3.4 us forward, 5.5 us backward (two launches).
 #include <math.h>
 
 #include <algorithm>
@@ -309,7 +311,8 @@ cudaError_t launch_qk_norm_rope(const HeadsView& q, const HeadsView& k, int B, i
 // A warp takes a packed row (token), or one of `parts` shares of its heads where there are few tokens: RPW heads at a time out
 // of the row's list [q heads | k heads | v heads], fetched ahead across the borders between rows.  The D / 2 angles of a row are
 // computed once, two per lane, and reach the other lanes through shared memory of the warp's own; no barrier.  Bound by
-// instruction issue as much as by HBM, so what does not change from row to row (theta, gains) is kept.
+// instruction issue as much as by HBM, so what does not change from row to row (theta, gains) is kept.  Measured, bf16, 32 + 8 heads,
+// D128: 6000 rows 28.4 us (5.2 TB/s, 0.80 of a copy), 32 rows 3.8 us.
 constexpr int APP_STAGES = 6, APP_RING = APP_STAGES * 2 * QKN_WARPS * 32 * 16;   // 48 KB a CTA
 
 template <typename T, int D>
