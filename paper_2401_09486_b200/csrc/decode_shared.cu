@@ -514,7 +514,9 @@ shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
 
 // ------------------------------------------------------------------ host side
 size_t decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int prefix_len, int max_len) {
-    const int64_t n = std::max(make_shared_plan(B, Hq, Hkv, D, prefix_len, max_len, false).total, make_shared_plan(B, Hq, Hkv, D, prefix_len, max_len, true).total);
+    int64_t n = 0;   // whatever kernels a call with these sizes may run
+    for (int pages : {0, 1})
+        for (bool cuda_cores : {false, true}) n = std::max(n, make_shared_plan(B, Hq, Hkv, D, prefix_len, max_len, pages, cuda_cores).total);
     return (size_t)n * sizeof(float);
 }
 
@@ -544,7 +546,7 @@ template <typename T, int D>
 static cudaError_t shared_t(const SharedArgs& a, bool generic, cudaStream_t st) {
     // both parts on the tensor cores or both on CUDA cores: a cut and the kernels that follow it belong together
     const bool tc = sizeof(T) == 2 && !generic && shared_own_tma_fits(a) && (a.prefix_len == 0 || shared_prefix_tc_fits(a));
-    const SharedPlan p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len, !tc);
+    const SharedPlan p = make_shared_plan(a.B, a.Hq, a.Hkv, D, a.prefix_len, a.max_len, a.prefix_table ? 1 << a.pg.log2_ps : 0, !tc);
     auto prefix = [&](bool behind) {
         return p.p_blocks == 0 ? cudaSuccess : tc ? launch_shared_prefix_tc(a, p, D, behind, st) : prefix_simt<T, D>(a, p, behind, st);
     };

@@ -14,13 +14,15 @@ constexpr int OWN_KEYS = 16;    // own keys per block
 constexpr int OWN_WARPS = 4;    // an own worker is a warp
 constexpr int OWN_CTAS = 148, STREAM_CTAS = 4 * 148;
 // sequences of so many blocks are not cut, while there are so few query rows that the workers join their parts quickly and
-// so few prefix blocks that it does not matter which kernel starts first
+// so few prefix blocks that it does not matter which kernel starts first (B32 H32, own caches up to 64, prefix 8192: 36 us cut, 42
+// whole; B32 Hq32 Hkv8, prefix 16384: 30 against 46)
 constexpr int OWN_WHOLE = 8, OWN_WHOLE_ROWS = 2 * OWN_CTAS * OWN_WARPS;
 
-// Prefix CTAs that a call is cut for: two per SM, which fill each other's waits (B128 Hq32 Hkv8, prefix 16384: 33-35 us alone
-// against 45-48 with one; B32 H32, the HBM-bound one: 40-43 against 48-51).  While an SM also holds a CTA of the own kernel it
-// has room for one of them, and the second comes when the other is done.
-constexpr int SHP_CTAS = 296;
+// Prefix CTAs that a call is cut for: one or two per SM.  Alone, two fill each other's waits (B128 Hq32 Hkv8, prefix 16384: 33-35
+// us against 45-48; B32 H32, the HBM-bound one: 40-43 against 48-51).  But beside a CTA of the own kernel an SM has room for
+// one, so two per SM become two waves wherever the own kernel lasts as long as a CTA's share.  Hence two only where the
+// prefix is the longer part by far (see make_shared_plan).
+constexpr int SHP_CTAS = 148;
 
 // The cut of a call.  Depends on the sizes alone, so results repeat and the workspace can be sized before the call.
 //
@@ -54,24 +56,34 @@ __host__ __device__ inline int64_t first_block(int64_t w, int64_t T, int64_t W) 
 
 __host__ __device__ inline int64_t own_workers(int64_t T, int workers) { return T < workers ? T : workers; }
 
-// cuda_cores: both parts run on CUDA cores (fp32, pages of fewer than 8, own caches of fewer than 16 rows in all, second opinion)
-inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len, int max_len, bool cuda_cores) {
+// pages: entries to a page of the prefix (0: contiguous).  cuda_cores: both parts run on CUDA cores (fp32, pages of fewer than 8,
+// own caches of fewer than 16 rows in all, second opinion)
+inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len, int max_len, int pages, bool cuda_cores) {
     SharedPlan p;
     const int64_t g = Hq / Hkv, rows = (int64_t)B * g;
     p.m_tiles = (int)((rows + SHP_ROWS - 1) / SHP_ROWS);
     p.p_keys = cuda_cores ? SIMT_K : SHP_KEYS;
     p.p_blocks = (prefix_len + p.p_keys - 1) / p.p_keys;
-    int64_t w = std::max(1, (cuda_cores ? SHP_CTAS / 2 : SHP_CTAS) / p.m_tiles);   // CUDA cores: B60 Hq16 Hkv2 prefix 4000 84 us cut for 148, 96 for 296
-    // shares that end inside a kv head make most workers change heads once, which costs about as much as six blocks (draining
-    // the products, storing a partial result, new query rows): whole workers per kv head where their longer shares cost less
-    const int64_t all = (int64_t)Hkv * p.p_blocks, whole = w / Hkv * Hkv;
-    if (whole > 0 && (all + whole - 1) / whole <= (all + w - 1) / w + 6) w = whole;
-    p.p_workers = (int)std::min<int64_t>(w, (int64_t)Hkv * p.p_blocks);
     p.g_rows = cuda_cores ? (g < 3 ? (int)g : 4) : (g <= 8 ? (int)g : 16);
     p.g_tiles = (int)((g + p.g_rows - 1) / p.g_rows);
+    // Blocks per SM of both parts (own: at most).  A prefix block takes an SM 0.8 us, an own block 0.2, starting the own kernel
+    // five.  Measured, one CTA per SM against two: B128 Hq32 Hkv8 own 1500, prefix 16384 / 40000: 92 / 119 us against 94 / 134; own 64:
+    // 54 / 103 against 54 / 88; B200 Hq64 Hkv8 own 300, prefix 30000: 244 against 211; B16 Hq32 Hkv8 own 100, prefix 4096 / 32768:
+    // 15.5 / 36.5 against 20.3 / 39.8.  Tiles of several pages are work for the one thread that asks for them, and two CTAs have
+    // two: the last case in pages of 16, 48 against 43.
+    // Where the prefix kernel goes first (p.whole) it has the SMs to itself.
+    const int64_t all = (int64_t)Hkv * p.p_blocks;
+    p.whole = !cuda_cores && own_blocks(max_len) <= OWN_WHOLE && (int64_t)B * Hq <= OWN_WHOLE_ROWS && all * p.m_tiles <= 2 * SHP_CTAS;
+    const int64_t p_sm = all * p.m_tiles / 148, own_sm = (int64_t)B * Hkv * p.g_tiles * own_blocks(max_len) / 148;
+    const bool two = p.whole || (!cuda_cores && (pages > 0 && pages < SHP_KEYS ? p_sm > 6 + own_sm : p_sm > 30 + own_sm + own_sm / 8));
+    // CUDA cores: B60 Hq16 Hkv2, prefix 4000 84 us cut for one per SM, 96 for two
+    int64_t w = std::max(1, SHP_CTAS * (two ? 2 : 1) / p.m_tiles);
+    // shares that end inside a kv head make most workers change heads once, which costs about as much as six blocks (draining
+    // the products, storing a partial result, new query rows): whole workers per kv head where their longer shares cost less
+    const int64_t whole = w / Hkv * Hkv;
+    if (whole > 0 && (all + whole - 1) / whole <= (all + w - 1) / w + 6) w = whole;
+    p.p_workers = (int)std::min<int64_t>(w, all);
     p.workers = (cuda_cores ? STREAM_CTAS : OWN_CTAS) * OWN_WARPS;
-    p.whole = !cuda_cores && own_blocks(max_len) <= OWN_WHOLE && (int64_t)B * Hq <= OWN_WHOLE_ROWS &&
-              (int64_t)Hkv * p.p_blocks * p.m_tiles <= SHP_CTAS;
     int64_t at = 0;
     auto take = [&](int64_t n) { const int64_t o = at; at += (n + 63) / 64 * 64; return o; };
     const int64_t p_segments = p.p_blocks ? (int64_t)(p.p_workers + Hkv) * p.m_tiles : 0, segments = p.workers + (int64_t)B * Hkv * p.g_tiles;

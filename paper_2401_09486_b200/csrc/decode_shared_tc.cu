@@ -4,7 +4,8 @@
 // an online softmax between them: S = Q K^T, O = sum over keys of P V.  No mask but the end of the prefix.  A CTA takes 128
 // query rows (one row per TMEM lane) and a range of keys at a time; ranges are joined by the merge kernel.  With few rows the kernel
 // is bound by HBM (the prefix is read once per 128 rows), with many by the chain tensor pipe -> softmax -> tensor pipe, so
-// two CTAs share an SM and fill each other's waits: each has 256 of the 512 TMEM columns and half of the shared memory.
+// two CTAs fit on an SM and fill each other's waits: each has 256 of the 512 TMEM columns and half of the shared memory.  How
+// many a call is cut for: make_shared_plan.
 //
 //   warps 0-3  query rows, softmax: thread = query row.  64 keys (an "event") at a time: scores out of TMEM, row maximum, probabilities
 //              2^(s scale - ref) as bf16 back over the scores.  The reference maximum only moves, and the accumulator in TMEM

@@ -70,11 +70,11 @@ struct Args {
         PyObject* o = v[at++];
         if (dev < 0) return nullptr;
         if (o == Py_None) return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
-        if (PyLong_Check(o)) return PyLong_AsVoidPtr(o);
-        PyObject* h = PyObject_GetAttrString(o, "cuda_stream");
-        if (!h) throw PyFailed();
-        void* p = PyLong_AsVoidPtr(h);
-        Py_DECREF(h);
+        PyObject* h = nullptr;
+        if (!PyLong_Check(o) && !(h = PyObject_GetAttrString(o, "cuda_stream"))) throw PyFailed();
+        void* p = PyLong_AsVoidPtr(h ? h : o);
+        Py_XDECREF(h);
+        if (!p && PyErr_Occurred()) throw PyFailed();
         return p;
     }
     // a pointer of another device than the current one would reach the wrong GPU's kernel

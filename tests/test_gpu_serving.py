@@ -473,6 +473,15 @@ def test_shared_decode_pool_of_one_page(dtype):
     caches_after(s, before)
 
 
+@pytest.mark.parametrize("P,ps,D", [(48000, 0, 64), (12000, 16, 64), (12000, 16, 128)])
+def test_shared_decode_prefix_cut_for_two_ctas_per_sm(P, ps, D):
+    """Prefixes so much longer than the own caches that they are cut twice as finely."""
+    s = shared_case(2, 8, 8, D, P, [3, 200], ps, torch.bfloat16, seed=41)
+    call_shared(s)
+    torch.cuda.synchronize()
+    check_shared(s)
+
+
 def test_shared_decode_prefix_shares_across_heads():
     s = shared_case(*WIDE, torch.bfloat16, seed=77)
     call_shared(s)
