@@ -804,7 +804,7 @@ LOMA_API int loma_qk_norm_rope_append(const void* q, const void* k_new, const vo
  * paged: pools [n_pages, Hkv, page_size, D] hold prefix and own entries; prefix_table int32 [prefix_pages] and block_table
  * int32 [B, max_pages] name the pages (clamped to the pool on the device); prefix_len <= prefix_pages * page_size,
  * max_cache_len < max_pages * page_size.  No page may be both a prefix page and a page a new token is written to.
- * bf16 over a prefix in pages of fewer than 8 rows, and fp32, run the prefix on CUDA cores.
+ * fp32, pages of fewer than 8 rows and own caches of fewer than 16 rows in all run on CUDA cores.
  * Errors: INVALID_ARG (Hq not a multiple of Hkv, ...), UNSUPPORTED, ALIGNMENT, CAPACITY, WORKSPACE, CUDA.  B*Hq == 0 is a no-op.
  * ------------------------------------------------------------------------- */
 LOMA_API int loma_decode_attn_shared(const void* q, const void* k_new, const void* v_new, const void* k_prefix,
