@@ -699,7 +699,9 @@ LOMA_API int loma_compress_step_ragged(const void* q_mem, const void* k_mem, con
  *   cache_lens, new_lens, held, pos0 [in]   int32 [B]; all but cache_lens may be NULL
  *   free_pages   [in]      int32 [n_free] page numbers
  *   taken        [in/out]  int32 [1]: pages of free_pages drawn by earlier calls; the call starts behind them and
- *                          stores page_start[B].  NULL: starts at 0
+ *                          adds those it drew: min(page_start[B], n_free), never less than before.  What a short
+ *                          list left unmet is not counted: a later call, with a list that has grown, goes on with
+ *                          the first page nobody got.  NULL: starts at 0
  *   block_table  [in/out]  int32 [B, max_pages]
  *   row_start    [out]     int32 [B+1]: exclusive sums of n (row_start[B] = rows of the packed batch)
  *   page_start   [out]     int32 [B+1]: taken + exclusive sums of fresh; page_start[B] > n_free: the free list

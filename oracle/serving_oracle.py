@@ -13,7 +13,8 @@ INT_MAX = 2**31 - 1
 
 def paged_extend(cache_lens, new_lens, held, pos0, free_pages, taken, block_table, page_size, max_rows):
     """Returns (block_table, row_start, page_start, held_out, slots, row_seq, row_pos, taken) as an allocator that takes the
-    sequences one after the other would leave them."""
+    sequences one after the other would leave them.  taken: pages of the list that are in use now, where the call was given such
+    a count; without one the list's start is not kept and this is page_start[B]."""
     table = np.array(block_table, dtype=np.int64)
     B, M = table.shape
     ps = page_size
@@ -45,7 +46,8 @@ def paged_extend(cache_lens, new_lens, held, pos0, free_pages, taken, block_tabl
         held_out.append(h + got)
     rows += [(-1, -1, 0)] * (max_rows - len(rows))
     cols = [np.array([r[i] for r in rows], dtype=np.int64) for i in range(3)]
-    return (table, np.array(row_start), np.array(page_start), np.array(held_out, dtype=np.int64), *cols, page_start[-1])
+    after = page_start[-1] if taken is None else max(page_start[0], min(page_start[-1], len(free_pages)))
+    return (table, np.array(row_start), np.array(page_start), np.array(held_out, dtype=np.int64), *cols, after)
 
 
 def rms_norm(x, w=None, eps=1e-6):

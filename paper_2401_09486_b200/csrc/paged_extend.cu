@@ -60,6 +60,13 @@ __host__ __device__ inline int pages_got(const ExtendArgs& a, int first, int fre
     return left < fresh ? left : fresh;
 }
 
+// the free list's new start: pages handed out are behind it, pages asked for past the list's end are not (the sequences ask
+// again, and a longer list begins where this one ended)
+__host__ __device__ inline int taken_after(const ExtendArgs& a, int before, int64_t end) {
+    const int64_t drawn = end < a.n_free ? end : a.n_free;
+    return drawn > before ? (int)drawn : before;
+}
+
 // slot of entry e of a sequence from its page, or -1
 __host__ __device__ inline int slot_of(const ExtendArgs& a, int page, int64_t e) {
     const int mask = (1 << a.log2_ps) - 1;
@@ -77,7 +84,8 @@ __host__ __device__ inline int first_pos(const ExtendArgs& a, int b, int len) { 
 
 // ------------------------------------------------------------------ host form
 void host_paged_extend(const ExtendArgs& a) {
-    int64_t rows = 0, pages = a.taken ? clampi(*a.taken, 0, INT_MAX) : 0;
+    const int before = a.taken ? clampi(*a.taken, 0, INT_MAX) : 0;
+    int64_t rows = 0, pages = before;
     for (int b = 0; b < a.B; ++b) {
         const SeqNeed s = seq_need(a, b);
         const int first = saturate(pages), got = pages_got(a, first, s.fresh);
@@ -97,7 +105,7 @@ void host_paged_extend(const ExtendArgs& a) {
     }
     a.row_start[a.B] = saturate(rows);
     a.page_start[a.B] = saturate(pages);
-    if (a.taken) *a.taken = saturate(pages);
+    if (a.taken) *a.taken = taken_after(a, before, pages);
     for (int64_t r = rows; r < a.max_rows; ++r) {
         a.slots[r] = a.row_seq[r] = -1;
         a.row_pos[r] = 0;
@@ -324,7 +332,7 @@ paged_extend_scan_kernel(const ExtendArgs a) {
     if (threadIdx.x == 0) {
         a.row_start[a.B] = saturate(rows0);
         a.page_start[a.B] = saturate(pages0);
-        if (a.taken) *a.taken = saturate(pages0);
+        if (a.taken) *a.taken = taken_after(a, s_taken, pages0);
     }
 }
 

@@ -15,7 +15,7 @@ from oracle import serving_oracle as S
 from paper_2401_09486_b200 import autograd as A
 from paper_2401_09486_b200 import binding as L
 from paper_2401_09486_b200 import build, synthetic
-from tests.test_serving_host import check_extend, extend_case, huge_extend_case, run_extend
+from tests.test_serving_host import check_extend, exhaust_and_refill, extend_case, huge_extend_case, run_extend
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -679,3 +679,10 @@ def test_serving_step_eager_and_captured():
         assert torch.equal(state["o"], outs[i])
     for k in ("table", "held", "taken", "kp", "vp", "lens"):
         assert torch.equal(state[k], eager[k])
+
+
+# ------------------------------------------------------------------------------------------------ short free lists
+@pytest.mark.parametrize("B,n_first", [(5, 3), (3000, 700)])
+def test_extend_counts_only_the_pages_it_hands_out(B, n_first):
+    table, free = exhaust_and_refill(DEV, B=B, n_first=n_first)
+    assert torch.equal(table[:, 0], free[:B]) and (table[:, 1:] == -1).all()

@@ -216,3 +216,33 @@ def test_binding_refuses_mismatched_tensors():
     with pytest.raises(ValueError):
         L.loma_decode_attn_shared(torch.zeros(2, 2, 1, 64), None, None, torch.zeros(1, 5, 64), torch.zeros(1, 5, 64), 5, torch.zeros(2, 1, 4, 64),
                                   torch.zeros(2, 1, 5, 64), torch.zeros(2, 2, 1, 64), None, i32([0, 0]), 3)
+
+
+def exhaust_and_refill(device, B=5, ps=2, n_first=3):
+    """Steps of one token each over a list that runs short, is tried again twice and then grows: every page goes to one
+    sequence, none is passed over.  Returns the table and the pages held."""
+    t = dict(dtype=torch.int32, device=device)
+    lens, held, taken, table = torch.zeros(B, **t), torch.zeros(B, **t), torch.zeros(1, **t), torch.full((B, 4), -1, **t)
+    free = torch.arange(40, 40 + 2 * B, **t)
+    rs, pg, sl, sq, po = (torch.empty(n, **t) for n in (B + 1, B + 1, B, B, B))
+    for n in (n_first, n_first, n_first, n_first + 1, 2 * B, 2 * B):
+        before, had = int(taken), held.clone()
+        L.loma_paged_extend(lens, None, held, None, free[:n], taken, table, ps, rs, pg, held, sl, sq, po)
+        drawn = int((held - had).sum())
+        assert int(taken) == before + drawn <= n                             # what was handed out, no more
+        assert int(pg[-1]) == before + int((had == 0).sum())                 # what was asked for: the shortage can be read
+    assert int(taken) == B and held.tolist() == [1] * B
+    return table, free
+
+
+def test_host_extend_counts_only_the_pages_it_hands_out(lib):
+    table, free = exhaust_and_refill("cpu")
+    assert table[:, 0].tolist() == free[:5].tolist() and (table[:, 1:] == -1).all()
+
+
+def test_host_extend_list_shorter_than_what_was_taken(lib):
+    """A list that has been cut below the count keeps the count; the oracle agrees."""
+    case = ([0, 3], None, [0, 1], None, [5, 6], 4, [[-1, -1], [9, -1]])
+    got = run_extend(*case[:6], case[6], 2, 2)
+    check_extend(got, S.paged_extend(*case[:6], case[6], 2, 2))
+    assert int(got[-1]) == 4 and got[3].tolist() == [0, 1]
