@@ -804,8 +804,9 @@ LOMA_API int loma_qk_norm_rope_append(const void* q, const void* k_new, const vo
  *   workspace      [device]          loma_decode_shared_workspace_bytes(...) bytes, 16-byte aligned; contents need not
  *                                    be kept.  Calls that may overlap need workspaces of their own
  * paged: pools [n_pages, Hkv, page_size, D] hold prefix and own entries; prefix_table int32 [prefix_pages] and block_table
- * int32 [B, max_pages] name the pages (clamped to the pool on the device); prefix_len <= prefix_pages * page_size,
- * max_cache_len < max_pages * page_size.  No page may be both a prefix page and a page a new token is written to.
+ * int32 [B, max_pages] name the pages (numbers outside the pool are clamped to it where they are read; a new token whose page
+ * lies outside it, as where loma_paged_extend ran out of pages, is attended to but not stored); prefix_len <= prefix_pages *
+ * page_size, max_cache_len < max_pages * page_size.  No page may be both a prefix page and a page a new token is written to.
  * fp32, pages of fewer than 8 rows and own caches of fewer than 16 rows in all run on CUDA cores.
  * Errors: INVALID_ARG (Hq not a multiple of Hkv, ...), UNSUPPORTED, ALIGNMENT, CAPACITY, WORKSPACE, CUDA.  B*Hq == 0 is a no-op.
  * ------------------------------------------------------------------------- */

@@ -193,8 +193,9 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
                     }
                 }
                 // the new token's K and V go to entry len (read by nobody in this launch)
-                if (tail && kn && gt == 0 && lane < LPK) {
-                    const int64_t row = own_row(a, c.b, h, len) * D;
+                const int64_t cell = tail && kn && gt == 0 && lane < LPK ? token_row(a, c.b, h, len) : -1;
+                if (cell >= 0) {
+                    const int64_t row = cell * D;
                     reinterpret_cast<uint4*>(static_cast<T*>(a.k_cache) + row)[lane] = __ldg(reinterpret_cast<const uint4*>(kn) + lane);
                     reinterpret_cast<uint4*>(static_cast<T*>(a.v_cache) + row)[lane] = __ldg(reinterpret_cast<const uint4*>(vn) + lane);
                 }

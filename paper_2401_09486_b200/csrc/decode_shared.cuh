@@ -104,6 +104,16 @@ __device__ __forceinline__ int64_t own_row(const SharedArgs& a, int b, int h, in
     return ((((int64_t)page * a.Hkv + h) << a.pg.log2_ps) + (j & ((1 << a.pg.log2_ps) - 1)));
 }
 
+// the row that the new token of (b, h), entry j, is stored to, or -1: its sequence has no page for it (loma_paged_extend writes -1
+// into the table when the free list runs out), and the page that reads are clamped to is somebody else's
+__device__ __forceinline__ int64_t token_row(const SharedArgs& a, int b, int h, int j) {
+    if (a.pg.table) {
+        const int page = __ldg(a.pg.table + (int64_t)b * a.pg.max_pages + (j >> a.pg.log2_ps));
+        if (page < 0 || page >= a.pg.n_pages) return -1;
+    }
+    return own_row(a, b, h, j);
+}
+
 // The numbering of the own blocks, found again by every CTA from the lengths (B of them, out of L2 once per CTA).
 struct SeqBlocks {
     static constexpr int MAX_GROUPS = 512;

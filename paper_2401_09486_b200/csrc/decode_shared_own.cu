@@ -229,8 +229,9 @@ shared_own_tma_kernel(const __grid_constant__ OwnMaps maps, const SharedArgs a, 
                 if (a.k_new && lane < D / 8) {
                     *reinterpret_cast<uint4*>(tile + at(valid - 1, lane)) = k_tok;
                     *reinterpret_cast<uint4*>(tile + SM::TILE + at(valid - 1, lane)) = v_tok;
-                    if (gt == 0) {   // no fetch of this launch uses what lies there
-                        const int64_t dst = own_row(a, c.at.b, h, c.at.len) * (D / 8) + lane;
+                    const int64_t cell = gt == 0 ? token_row(a, c.at.b, h, c.at.len) : -1;
+                    if (cell >= 0) {   // no fetch of this launch uses what lies there
+                        const int64_t dst = cell * (D / 8) + lane;
                         static_cast<uint4*>(a.k_cache)[dst] = k_tok;
                         static_cast<uint4*>(a.v_cache)[dst] = v_tok;
                     }

@@ -686,3 +686,38 @@ def test_serving_step_eager_and_captured():
 def test_extend_counts_only_the_pages_it_hands_out(B, n_first):
     table, free = exhaust_and_refill(DEV, B=B, n_first=n_first)
     assert torch.equal(table[:, 0], free[:B]) and (table[:, 1:] == -1).all()
+
+
+# ------------------------------------------------------------------------------------------------ tokens without a page
+@pytest.mark.parametrize("dtype,flags", [(torch.float32, 0), (torch.bfloat16, 0), (torch.bfloat16, L.LOMA_FLAG_FORCE_GENERIC)])
+@pytest.mark.parametrize("missing", [-1, -2**31, 10**6])
+@pytest.mark.parametrize("mx", [20, 300])                       # sequences that stay whole, and ones that are cut
+def test_shared_decode_token_without_a_page_is_not_stored(mx, missing, dtype, flags):
+    """The page of sequence 0's new token is not in the pool: the token is attended to, and no page changes for it."""
+    s = shared_case(3, 4, 2, 64, 30, [16, 5, mx], 16, dtype, seed=5, poison=0.0)
+    s["table"][0, 1] = missing
+    before = s["kc"].clone(), s["vc"].clone()
+    call_shared(s, flags)
+    torch.cuda.synchronize()
+    check_shared(s)
+    s["lens"][0] = -1                                           # nothing stored for it
+    caches_after(s, before)
+
+
+def test_extend_out_of_pages_then_decode_keeps_the_other_requests():
+    """A free list that ends one page short, and the token stored by the attention: page 0 belongs to another request."""
+    B, Hq, Hkv, D, ps, dtype = 2, 4, 2, 64, 8, torch.bfloat16
+    i32 = dict(dtype=torch.int32, device=DEV)
+    kp, vp = (normal((3, Hkv, ps, D), s, dtype) for s in (1, 2))
+    table, lens = torch.tensor([[0, -1], [1, -1]], **i32), torch.tensor([8, 8], **i32)
+    rs, pg, held, sl, sq, po = (torch.empty(n, **i32) for n in (3, 3, 2, 2, 2, 2))
+    L.loma_paged_extend(lens, None, None, None, torch.tensor([2], **i32), None, table, ps, rs, pg, held, sl, sq, po)
+    assert table.tolist() == [[0, 2], [1, -1]] and sl.tolist() == [16, -1] and int(pg[2]) == 2
+    kn, vn = (normal((B, Hkv, 1, D), s, dtype) for s in (3, 4))
+    want = [x.clone() for x in (kp, vp)]
+    want[0][2, :, 0], want[1][2, :, 0] = kn[0, :, 0], vn[0, :, 0]
+    o = torch.empty(B, Hq, 1, D, dtype=dtype, device=DEV)
+    ws = torch.empty(L.loma_decode_shared_workspace_bytes(B, Hq, Hkv, D, 0, 15), dtype=torch.uint8, device=DEV)
+    L.loma_decode_attn_shared_paged(normal((B, Hq, 1, D), 5, dtype), kn, vn, kp, vp, None, 0, table, o, None, lens, 15, workspace=ws)
+    torch.cuda.synchronize()
+    assert torch.equal(kp, want[0]) and torch.equal(vp, want[1]) and torch.isfinite(o.float()).all()
