@@ -497,13 +497,15 @@ shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
         s_part[way][grp][lane] = m;
         __syncthreads();
         if (way > 0) return;
+        // a share that took no result, or only ones without weight, has a total of 0.  One whose log-sum-exps were all NaN has a maximum
+        // of -inf too, but its total is NaN and goes on into the row
         RowMerge all;
 #pragma unroll
         for (int y = 0; y < WAYS; ++y) all.M = fmaxf(all.M, s_part[y][grp][lane].M);
 #pragma unroll
         for (int y = 0; y < WAYS; ++y) {
             const RowMerge& q = s_part[y][grp][lane];
-            if (q.M == -INFINITY) continue;
+            if (q.total == 0.f) continue;
             const float f = exp2f(q.M - all.M);
             all.total += f * q.total;
             all.o.x = fmaf(f, q.o.x, all.o.x); all.o.y = fmaf(f, q.o.y, all.o.y); all.o.z = fmaf(f, q.o.z, all.o.z); all.o.w = fmaf(f, q.o.w, all.o.w);

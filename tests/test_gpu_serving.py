@@ -721,3 +721,57 @@ def test_extend_out_of_pages_then_decode_keeps_the_other_requests():
     L.loma_decode_attn_shared_paged(normal((B, Hq, 1, D), 5, dtype), kn, vn, kp, vp, None, 0, table, o, None, lens, 15, workspace=ws)
     torch.cuda.synchronize()
     assert torch.equal(kp, want[0]) and torch.equal(vp, want[1]) and torch.isfinite(o.float()).all()
+
+
+# ------------------------------------------------------------------------------------------------ NaN
+@pytest.mark.parametrize("dtype,flags", [(torch.float32, 0), (torch.bfloat16, 0), (torch.bfloat16, L.LOMA_FLAG_FORCE_GENERIC)])
+@pytest.mark.parametrize("where", ["prefix", "own", "token", "query"])
+@pytest.mark.parametrize("case", [(1, 4, 2, 64, 20, [5], 0), (2, 4, 2, 128, 40, [300, 200], 0), (3, 8, 2, 128, 3000, [400, 3, 900], 16),
+                                  (40, 8, 2, 64, 640, [200] * 40, 0), (128, 8, 8, 64, 300, [170] * 128, 0), (3, 8, 2, 64, 33, [9, -1, 40], 16)])
+def test_shared_decode_nan_reaches_the_outputs(case, where, dtype, flags):
+    """One NaN key that a row sees makes the row NaN, whichever part of the keys it lies in and however the parts are joined;
+    rows that do not see it stay as they were."""
+    clean, s = shared_case(*case, dtype, seed=61), shared_case(*case, dtype, seed=61)
+    nan = float("nan")
+    if where == "prefix":
+        (s["kc"][int(s["ptable"][0])] if s["ps"] else s["kp"])[:, 3] = nan
+    elif where == "own":
+        (s["kc"][int(s["table"][0, 0])] if s["ps"] else s["kc"][0])[:, 1] = nan
+    else:
+        s["kn" if where == "token" else "q"][0] = nan
+    for x in (clean, s):
+        call_shared(x, flags)
+    torch.cuda.synchronize()
+    check_shared(clean)
+    live = [b for b, n in enumerate(case[5]) if n >= 0]
+    hit = live if where == "prefix" else [0]
+    rest = [b for b in range(case[0]) if b not in hit]
+    assert torch.isnan(s["o"][hit].float()).all() and torch.isnan(s["lse"][hit]).all()
+    assert torch.equal(s["o"][rest], clean["o"][rest]) and torch.equal(s["lse"][rest], clean["lse"][rest])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("where", ["prefix", "own"])
+@pytest.mark.parametrize("n", [20, 200])
+def test_shared_decode_a_whole_part_of_nan(n, where, dtype):
+    """Every score of one part is NaN, so no maximum of it is a number."""
+    s = shared_case(1, 4, 2, 64, 40, [n], 0, dtype, seed=62)
+    for x in [s["kp"]] if where == "prefix" else [s["kc"], s["kn"]]:
+        x.fill_(float("nan"))
+    call_shared(s)
+    torch.cuda.synchronize()
+    assert torch.isnan(s["o"].float()).all() and torch.isnan(s["lse"]).all()
+
+
+@pytest.mark.parametrize("dtype,flags", [(torch.float32, 0), (torch.bfloat16, 0), (torch.bfloat16, L.LOMA_FLAG_FORCE_GENERIC)])
+@pytest.mark.parametrize("n", [20, 200])
+def test_shared_decode_a_part_without_weight(n, dtype, flags):
+    """Prefix scores of -inf: the prefix has no weight."""
+    s = shared_case(2, 4, 2, 64, 100, [n, 3], 0, dtype, seed=63)
+    s["q"].fill_(1.0)
+    s["kp"][:, :100] = 0
+    s["kp"][:, :100, 0] = -float("inf")
+    s["pre"] = tuple(x[:, :0] for x in s["pre"])                # as if there were none
+    call_shared(s, flags)
+    torch.cuda.synchronize()
+    check_shared(s)
