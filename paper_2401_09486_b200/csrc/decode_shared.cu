@@ -152,6 +152,11 @@ shared_own_stream_kernel(const SharedArgs a, const SharedPlan p) {
                     if (li % DUP == 0) s_prob[warp][sub][li / DUP * KEEP + v] = pr;
                 }
                 __syncwarp();
+                if (j0 + NL * KPL > len + 1) {   // repeated keys have no weight, but 0 x inf is not 0
+#pragma unroll
+                    for (int i = 0; i < NL; ++i)
+                        if (j0 + i * KPL + sub > len) vr[i] = make_uint4(0, 0, 0, 0);
+                }
 #pragma unroll
                 for (int i = 0; i < NL; i += 4) {
                     float4 pr[G];
@@ -265,13 +270,14 @@ shared_prefix_simt_kernel(const SharedArgs a, const SharedPlan p) {
             const int r = (tid + i * SIMT_THREADS) / LPK, c = (tid + i * SIMT_THREADS) % LPK;
             const T* kp = static_cast<const T*>(a.k_prefix) + row_f[i] + c * N;
             const T* vp = static_cast<const T*>(a.v_prefix) + row_f[i] + c * N;
+            const bool in = blk_f * SIMT_K + r < a.prefix_len;   // a repeated key's values are zero: its weight is, and 0 x inf is not 0
             if constexpr (ASYNC) {
                 float* tile = sm + SM::KV + buf * SM::TILE;
                 cp_async16((uint32_t)__cvta_generic_to_shared(tile + r * (D + 4) + c * N), kp);
-                cp_async16((uint32_t)__cvta_generic_to_shared(tile + SM::K_TILE + r * D + c * N), vp);
+                cp_async16_or_zero((uint32_t)__cvta_generic_to_shared(tile + SM::K_TILE + r * D + c * N), vp, in);
             } else {
                 kv[0][i] = __ldg(reinterpret_cast<const uint4*>(kp));
-                kv[1][i] = __ldg(reinterpret_cast<const uint4*>(vp));
+                kv[1][i] = in ? __ldg(reinterpret_cast<const uint4*>(vp)) : make_uint4(0, 0, 0, 0);
             }
         }
         if (++blk_f == p.p_blocks) { blk_f = 0; ++h_f; }

@@ -311,6 +311,11 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
+// ... or 16 bytes of zero
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool copy) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(copy ? 16 : 0) : "memory");
+}
+
 #ifdef __CUDACC__
 // Programmatic dependent launch: the next kernel of the stream may start once every CTA of this one has called the first;
 // the second waits until the kernels this one was launched behind have finished.

@@ -775,3 +775,22 @@ def test_shared_decode_a_part_without_weight(n, dtype, flags):
     call_shared(s, flags)
     torch.cuda.synchronize()
     check_shared(s)
+
+
+@pytest.mark.parametrize("dtype,flags", [(torch.float32, 0), (torch.bfloat16, 0), (torch.bfloat16, L.LOMA_FLAG_FORCE_GENERIC)])
+@pytest.mark.parametrize("where", ["prefix", "token"])
+@pytest.mark.parametrize("P,n,ps,D", [(37, 5, 0, 64), (37, 20, 16, 128), (37, 5, 4, 64), (65, 200, 0, 128), (31, 16, 1, 64)])
+def test_shared_decode_infinite_value_at_the_end_of_a_tile(P, n, ps, D, where, dtype, flags):
+    """V of the last key of a partial tile is infinite: that feature is infinite, as the mean says, and the others are not NaN."""
+    s = shared_case(2, 4, 2, D, P, [n, n], ps, dtype, seed=8)
+    inf = float("inf")
+    if where == "token":
+        s["vn"][:, :, 0, 1] = inf
+    elif ps:
+        s["vc"][int(s["ptable"][(P - 1) // ps]), :, (P - 1) % ps, 1] = inf
+    else:
+        s["vp"][:, P - 1, 1] = inf
+    call_shared(s, flags)
+    torch.cuda.synchronize()
+    o = s["o"].float()
+    assert (o[..., 1] == inf).all() and torch.isfinite(o[..., 2:]).all() and torch.isfinite(o[..., 0]).all()
