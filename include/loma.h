@@ -800,9 +800,10 @@ LOMA_API int loma_qk_norm_rope_append(const void* q, const void* k_new, const vo
  *   cache_lens     [device, in]      int32 [B]: own entries before this token; values above max_cache_len count as
  *                                    max_cache_len; negative: a slot without a request, whose o, lse and cache are left
  *                                    as they are
- *   max_cache_len  [host]            an upper bound that sizes the launch and the workspace; max_cache_len < cap
+ *   max_cache_len  [host]            an upper bound that sizes the launch; max_cache_len < cap
  *   workspace      [device]          loma_decode_shared_workspace_bytes(...) bytes, 16-byte aligned; contents need not
- *                                    be kept.  Calls that may overlap need workspaces of their own
+ *                                    be kept.  The size grows with B, prefix_len and max_cache_len: one made for the
+ *                                    largest of each serves every smaller call of the same heads.  Calls that may overlap need workspaces of their own
  * paged: pools [n_pages, Hkv, page_size, D] hold prefix and own entries; prefix_table int32 [prefix_pages] and block_table
  * int32 [B, max_pages] name the pages (numbers outside the pool are clamped to it where they are read; a new token whose page
  * lies outside it, as where loma_paged_extend ran out of pages, is attended to but not stored); prefix_len <= prefix_pages *

@@ -522,10 +522,23 @@ shared_merge_kernel(const SharedArgs a, const SharedPlan p) {
 }
 
 // ------------------------------------------------------------------ host side
+// What the largest cut of a call takes, whatever kernels it runs, and of every smaller one: a buffer made for an engine's largest
+// batch, prefix and cache bound has to do for its other steps too.  A plan's own size does not grow with them (short own caches
+// are cut for twice the prefix CTAs: B32 Hq32 Hkv8, prefix 2048, 19 MB up to 127 own entries, 15 MB from 128 on), so each of its
+// arrays is bounded apart.
 size_t decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int prefix_len, int max_len) {
-    int64_t n = 0;   // whatever kernels a call with these sizes may run
-    for (int pages : {0, 1})
-        for (bool cuda_cores : {false, true}) n = std::max(n, make_shared_plan(B, Hq, Hkv, D, prefix_len, max_len, pages, cuda_cores).total);
+    int64_t own_rows = 0, m_tiles = 0;
+    for (bool cuda_cores : {false, true}) {
+        const SharedPlan p = make_shared_plan(B, Hq, Hkv, D, prefix_len, max_len, 0, cuda_cores);
+        m_tiles = p.m_tiles;
+        own_rows = std::max(own_rows, (p.workers + (int64_t)B * Hkv * p.g_tiles) * p.g_rows);
+    }
+    // a worker per block at most, and as many CTAs as two per SM, or one per query tile; a partial result more per kv head
+    const int64_t blocks = ((int64_t)prefix_len + SIMT_K - 1) / SIMT_K;
+    const int64_t p_segments = blocks ? std::min(std::max<int64_t>(2 * SHP_CTAS, m_tiles), Hkv * blocks * m_tiles) + Hkv * m_tiles : 0;
+    const int64_t floats[] = {p_segments * SHP_ROWS * D, p_segments * SHP_ROWS, own_rows * D, own_rows, 2 * ((int64_t)B + 1)};
+    int64_t n = 0;
+    for (int64_t x : floats) n += (x + 63) / 64 * 64;
     return (size_t)n * sizeof(float);
 }
 

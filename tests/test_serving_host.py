@@ -2,6 +2,8 @@
 loma_paged_extend against the oracle."""
 
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -246,3 +248,28 @@ def test_host_extend_list_shorter_than_what_was_taken(lib):
     got = run_extend(*case[:6], case[6], 2, 2)
     check_extend(got, S.paged_extend(*case[:6], case[6], 2, 2))
     assert int(got[-1]) == 4 and got[3].tolist() == [0, 1]
+
+
+def test_shared_workspace_grows_with_the_sizes(lib):
+    """A buffer made for the largest batch, prefix and cache bound serves every smaller call, across the bounds at which the
+    cut of a call changes."""
+    need = L.loma_decode_shared_workspace_bytes
+    assert need(32, 32, 8, 128, 2048, 128) >= need(32, 32, 8, 128, 2048, 127) and need(16, 32, 8, 128, 32768, 8000) >= need(16, 32, 8, 128, 32768, 100)
+    assert need(32, 32, 8, 128, 2400, 127) >= need(32, 32, 8, 128, 2304, 127)
+    lens = [0, 1, 15, 16, 100, 111, 112, 127, 128, 129, 300, 1500, 8000, 100000]
+    prefixes = [0, 1, 31, 32, 33, 64, 65, 200, 1000, 2304, 2400, 4096, 9000, 32768, 200000]
+    batches = [1, 2, 3, 5, 8, 16, 31, 32, 33, 37, 64, 65, 128, 200, 300, 1000]
+    for Hq, Hkv in ((1, 1), (8, 8), (32, 8), (64, 8), (40, 2), (100, 100), (9, 1)):
+        grid = np.array([[[need(B, Hq, Hkv, 64, P, n) for n in lens] for P in prefixes] for B in batches], dtype=np.int64)
+        assert all((np.diff(grid, axis=i) >= 0).all() for i in range(3)), (Hq, Hkv)
+
+
+def test_shared_plan_replayed(lib, tmp_path):
+    """Every cut of a shared-prefix call, replayed on the host: blocks and partial results (tests/c_abi/shared_plan_check.cu)."""
+    exe = str(tmp_path / "shared_plan_check")
+    root, libdir = build.ROOT, build.PKG_DIR
+    subprocess.run([build._nvcc(), "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", build.INCLUDE, "-I", build.CSRC,
+                    os.path.join(root, "tests", "c_abi", "shared_plan_check.cu"), "-o", exe, "-L", libdir, "-lloma", "-Xlinker", f"-rpath={libdir}"],
+                   check=True)
+    out = subprocess.run([exe], capture_output=True, text=True)
+    assert out.returncode == 0 and "shared plans ok" in out.stdout, out.stdout + out.stderr
