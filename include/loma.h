@@ -742,7 +742,8 @@ LOMA_API int loma_paged_extend(int B, int page_size, int max_pages, int max_rows
  *                               not overlap)
  *   n_chunks .. tail_read, flags, position_type (0 or 1), theta_base   as in loma_rope_apply
  *   eps          <= 0 selects 1e-6
- *   workspace    [device]       backward: loma_qk_norm_rope_bwd_workspace_bytes(...) bytes, 256-byte aligned
+ *   workspace    [device]       backward: loma_qk_norm_rope_bwd_workspace_bytes(...) bytes, 256-byte aligned.  The size
+ *                               grows with B, the heads and the rows: one made for the largest serves the others
  * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA.  No rows: a no-op (backward: dwq, dwk become 0).
  * ------------------------------------------------------------------------- */
 LOMA_API int loma_qk_norm_rope_fwd(const void* q, const void* k, const void* wq, const void* wk, void* q_out,

@@ -250,26 +250,30 @@ qk_norm_dw_kernel(const float* __restrict__ part, int n_cta, int D, T* __restric
 
 // Rows per CTA, and slices of the pairs.  Every slice computes its rows' angles again, so there are as many as it takes to give
 // every SM two CTAs, and up to six per SM (waves that even out) only while a slice keeps 16 pairs a lane.
-static void norm_grid(int B, int Hq, int Hk, int D, const Layout& L, int elt_bytes, bool by_heads, dim3* grid) {
+constexpr int NORM_CTAS = 148 * 6;
+struct NormGrid {
+    int rows, slices;
+    int64_t most;   // CTAs of this call at most, and of every smaller one: rows * slices does not grow with the rows
+};
+static NormGrid norm_grid(int B, int Hq, int Hk, int D, const Layout& L, int elt_bytes, bool by_heads) {
     const int rpw = 32 / ((D / 2) / (16 / elt_bytes));
-    const int rows = (L.S + QKN_WARPS * (by_heads ? 1 : rpw) - 1) / (QKN_WARPS * (by_heads ? 1 : rpw));
+    NormGrid g;
+    g.rows = (L.S + QKN_WARPS * (by_heads ? 1 : rpw) - 1) / (QKN_WARPS * (by_heads ? 1 : rpw));
     const int pairs = B * (Hq + Hk), lane_pairs = by_heads ? (pairs + rpw - 1) / rpw : pairs;
     int slices = 1;
     while (slices < lane_pairs &&
-           ((int64_t)rows * slices < 148 * 2 || ((int64_t)rows * slices < 148 * 6 && lane_pairs / slices >= 32)))
+           ((int64_t)g.rows * slices < 148 * 2 || ((int64_t)g.rows * slices < NORM_CTAS && lane_pairs / slices >= 32)))
         slices *= 2;
-    *grid = dim3(rows, std::min(slices, lane_pairs));
+    g.slices = std::min(slices, lane_pairs);
+    g.most = std::min<int64_t>(std::max(g.rows, 2 * NORM_CTAS), (int64_t)g.rows * lane_pairs);   // the last doubling began below NORM_CTAS
+    return g;
 }
 
 size_t qk_norm_rope_bwd_workspace_bytes(int B, int Hq, int Hk, int D, const Layout& L) {
-    size_t most = 0;
+    int64_t most = 0;
     for (int es = 2; es <= 4; es += 2)
-        for (int by = 0; by < 2; ++by) {
-            dim3 g;
-            norm_grid(B, Hq, Hk, D, L, es, by != 0, &g);
-            most = std::max(most, (size_t)2 * g.x * g.y * D * sizeof(float));
-        }
-    return most;
+        for (bool by_heads : {false, true}) most = std::max(most, norm_grid(B, Hq, Hk, D, L, es, by_heads).most);
+    return (size_t)2 * most * D * sizeof(float);
 }
 
 template <typename T, int D>
@@ -277,8 +281,8 @@ static cudaError_t norm_t(const HeadsView& q, const HeadsView& k, int B, const L
                           bool backward, void* ws, cudaStream_t st) {
     const HeadsView& lead = q.H > 0 ? q : k;
     const bool by_heads = lead.H > 1 && lead.sh < lead.ss;   // heads of a row behind one another: [B, S, H, D]
-    dim3 grid;
-    norm_grid(B, q.H, k.H, D, L, sizeof(T), by_heads, &grid);
+    const NormGrid ng = norm_grid(B, q.H, k.H, D, L, sizeof(T), by_heads);
+    const dim3 grid(ng.rows, ng.slices);
     if (!backward) {
         cudaError_t e = prepare_kernel(reinterpret_cast<const void*>(qk_norm_rope_kernel<T, D, false>), QknRing<false>::BYTES);
         if (e != cudaSuccess) return e;

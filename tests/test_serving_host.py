@@ -273,3 +273,13 @@ def test_shared_plan_replayed(lib, tmp_path):
                    check=True)
     out = subprocess.run([exe], capture_output=True, text=True)
     assert out.returncode == 0 and "shared plans ok" in out.stdout, out.stdout + out.stderr
+
+
+def test_norm_workspace_grows_with_the_sizes(lib):
+    """A buffer made for the longest layout and the largest batch serves every smaller call; a few sums of D numbers per CTA."""
+    need = L.loma_qk_norm_rope_bwd_workspace_bytes
+    rows, batches, heads = [1, 2, 7, 8, 9, *range(20, 9000, 61), 34816, 100000], [1, 2, 3, 4, 9, 64], [(1, 0), (1, 1), (2, 2), (5, 2), (8, 8), (32, 8), (32, 32)]
+    for D in (64, 128):
+        grid = np.array([[[need(B, hq, hk, D, 0, 4, 0, S) for S in rows] for B in batches] for hq, hk in heads], dtype=np.int64)
+        assert all((np.diff(grid, axis=i) >= 0).all() for i in range(3))
+        assert grid.max() <= 2 * D * 4 * (100000 // 8 + 1) + 256
