@@ -72,13 +72,20 @@ def loma_rope(q, k, n_chunks: int, c: int, t: int, tail_read: int = 0, flags: in
     return _Rope.apply(q, k, n_chunks, c, t, tail_read, flags, theta_base, position_type)
 
 
+def _dense16(x):
+    """x contiguous and at a 16-byte address.  A contiguous view of a larger tensor may start anywhere: a slice of a flat
+    parameter buffer, or the gradient that a concatenation hands back."""
+    x = x.contiguous()
+    return x if x.data_ptr() % 16 == 0 else x.clone()
+
+
 class _QkNormRope(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, wq, wk, n_chunks, c, t, tail_read, flags, eps, theta_base, position_type):
         if not (q.is_cuda and k.is_cuda):
             raise RuntimeError("loma_qk_norm_rope needs CUDA tensors (there is no CPU path)")
-        q, k = q.contiguous(), k.contiguous()
-        wq, wk = (None if w is None else w.contiguous() for w in (wq, wk))
+        q, k = _dense16(q), _dense16(k)
+        wq, wk = (None if w is None else _dense16(w) for w in (wq, wk))
         q_out, k_out = torch.empty_like(q), torch.empty_like(k)
         ctx.layout = (n_chunks, c, t, tail_read, flags)
         ctx.norm = (eps, theta_base, position_type)
@@ -93,7 +100,7 @@ class _QkNormRope(torch.autograd.Function):
         q, k, wq, wk = ctx.saved_tensors
         n_chunks, c, t, tail_read, flags = ctx.layout
         eps, theta_base, position_type = ctx.norm
-        d_q_out, d_k_out = d_q_out.contiguous(), d_k_out.contiguous()
+        d_q_out, d_k_out = _dense16(d_q_out), _dense16(d_k_out)
         dq, dk = torch.empty_like(q), torch.empty_like(k)
         dwq, dwk = (torch.empty_like(w) if w is not None and need else None
                     for w, need in ((wq, ctx.needs_input_grad[2]), (wk, ctx.needs_input_grad[3])))

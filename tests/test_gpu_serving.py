@@ -794,3 +794,28 @@ def test_shared_decode_infinite_value_at_the_end_of_a_tile(P, n, ps, D, where, d
     torch.cuda.synchronize()
     o = s["o"].float()
     assert (o[..., 1] == inf).all() and torch.isfinite(o[..., 2:]).all() and torch.isfinite(o[..., 0]).all()
+
+
+# ------------------------------------------------------------------------------------------------ views at any address
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_rope_autograd_takes_views_at_any_address(dtype):
+    """Inputs that are contiguous slices of one flat buffer, and outputs joined behind a single number, so that their gradients
+    are contiguous slices too: the results of the same call on tensors of their own."""
+    D, rows = 64, 7
+    shapes = [(1, 2, rows, D), (1, 1, rows, D), (D,), (D,)]
+    sizes = [int(np.prod(x)) for x in shapes]
+    coef = normal((1 + sum(sizes[:2]),), 9, dtype)
+
+    def run(leaves):
+        a, b = A.loma_qk_norm_rope(*leaves, 0, 4, 0, rows)
+        joined = torch.cat([torch.zeros(1, dtype=dtype, device=DEV), a.reshape(-1), b.reshape(-1)])
+        return [a, b, *torch.autograd.grad((joined * coef).sum(), leaves)]
+
+    flat = normal((1 + sum(sizes),), 1, dtype)
+    views, at = [], 1
+    for n, shape in zip(sizes, shapes):
+        views.append(flat[at:at + n].view(shape).requires_grad_())
+        at += n
+    assert all(x.data_ptr() % 16 for x in views)
+    got, want = run(views), run([x.detach().clone().requires_grad_() for x in views])
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
