@@ -681,6 +681,11 @@ def _native():
         except ImportError as e:
             raise RuntimeError(f"the extension module _marshal.so is missing or broken ({e}): build it with "
                                "`python -m paper_2401_09486_b200.build` (there is no fallback path)") from e
+        from .build import marshal_key
+
+        if module.built_for != marshal_key():
+            raise RuntimeError(f"the extension module _marshal.so was built for {module.built_for}, not for {marshal_key()}: build it again with "
+                               "`python -m paper_2401_09486_b200.build`")
         names = ("loma_paged_extend", "loma_qk_norm_rope_fwd", "loma_qk_norm_rope_bwd", "loma_qk_norm_rope_append",
                  "loma_decode_attn_shared", "loma_decode_attn_shared_paged")
         module.bind(*[ctypes.cast(getattr(handle, n), ctypes.c_void_p).value for n in names])

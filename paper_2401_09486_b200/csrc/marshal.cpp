@@ -421,4 +421,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling f
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module); }
+// built_for: the Python and torch this module was compiled against; binding.py refuses it under any other
+PyMODINIT_FUNC PyInit__marshal(void) {
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", LOMA_BUILT_FOR) != 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}

@@ -283,3 +283,27 @@ def test_norm_workspace_grows_with_the_sizes(lib):
         grid = np.array([[[need(B, hq, hk, D, 0, 4, 0, S) for S in rows] for B in batches] for hq, hk in heads], dtype=np.int64)
         assert all((np.diff(grid, axis=i) >= 0).all() for i in range(3))
         assert grid.max() <= 2 * D * 4 * (100000 // 8 + 1) + 256
+
+
+def test_build_keeps_the_library_without_the_extension(lib, monkeypatch, tmp_path):
+    """A C user's build does not depend on torch's headers or on g++: the library is there, and a warning says what is not."""
+    monkeypatch.setattr(build, "MARSHAL_PATH", str(tmp_path / "_marshal.so"))
+
+    def fails(cmd, what, verbose):
+        raise RuntimeError(f"{what} failed")
+
+    monkeypatch.setattr(build, "_run", fails)
+    with pytest.warns(UserWarning, match="g\\+\\+ failed"):
+        assert build.build_library() == build.LIB_PATH
+    monkeypatch.setattr(build, "marshal_key", lambda: __import__("no_such_torch"))
+    with pytest.warns(UserWarning, match="no_such_torch"):
+        assert build.build_library() == build.LIB_PATH
+
+
+def test_extension_is_built_again_for_another_torch(lib, monkeypatch):
+    assert not build._marshal_stale() and L._native().built_for == build.marshal_key()
+    monkeypatch.setattr(torch, "__version__", "2.99.0")
+    assert build._marshal_stale()
+    monkeypatch.setattr(L, "_marshal", None)
+    with pytest.raises(RuntimeError, match="was built for"):
+        L._native()
