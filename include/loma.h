@@ -712,6 +712,10 @@ LOMA_API int loma_compress_step_ragged(const void* q_mem, const void* k_mem, con
  *   row_seq      [out]     int32 [max_rows]: sequence of the row, -1 behind the last
  *   row_pos      [out]     int32 [max_rows]: (pos0 ? pos0[b] : len) + i, the row's position id; 0 behind the last
  * Sums and positions beyond INT_MAX are stored as INT_MAX.  Rows at and beyond max_rows are not written.
+ * After a call that ran out of pages (page_start[B] > n_free) sequences may have -1 in their table row for entries the
+ * step counts on.  loma_qk_norm_rope_append and loma_decode_attn_shared_paged store nothing there; every attention reads
+ * such entries from a page of the pool that is not theirs (the other paged entry points store to it, too: they want
+ * every page to be there): drop those sequences' outputs and run the step again with a longer list.
  * on_device != 0: every pointer is [device] and the work is enqueued on `stream` (one launch up to 1536
  * sequences when nothing is updated in place, else two); on_device == 0: every pointer is [host], no CUDA call.
  * Errors: INVALID_ARG (page size not a power of two <= 65536, max_pages * page_size > INT_MAX, a required
@@ -734,8 +738,9 @@ LOMA_API int loma_paged_extend(int B, int page_size, int max_pages, int max_rows
  *
  *   q, k         [device, in]   [B, Hq, S, D] and [B, Hk, S, D]; Hq, Hk may differ, and one may be 0 (its
  *                               pointers are then ignored)
- *   wq, wk       [device, in]   [D] each, shared by the heads; NULL: ones
- *   q_out, k_out [device, out]  shape and strides of q and k; q_out == q and k_out == k is allowed
+ *                               B*Hq and B*Hk up to 65535, as for loma_rope_apply
+ *   wq, wk       [device, in]   [D] each, of q's type, shared by the heads; NULL: ones
+ *   q_out, k_out [device, out]  shape and strides of q and k; q_out == q and k_out == k is allowed, no other overlap
  *   d_q_out, d_k_out [device, in], dq, dk [device, out]   shape and strides of q and k; outputs must not alias inputs
  *   dwq, dwk     [device, out]  [D] each, or NULL (not computed)
  *   q_strides, k_strides [host] int64 [3]: batch, head and row stride in elements (multiples of 16 bytes; rows must
@@ -773,7 +778,8 @@ LOMA_API size_t loma_qk_norm_rope_bwd_workspace_bytes(int B, int Hq, int Hk, int
  *   slots        [device, in]   int32 [T]: page * page_size + row (loma_paged_extend); a row whose slot lies outside
  *                               [0, n_pages * page_size) stores no key and value.  No two rows may name one slot
  *   positions    [device, in]   int32 [T]
- *   q_strides, k_strides, v_strides [host] int64 [2]: row and head stride in elements
+ *   q_strides, k_strides, v_strides [host] int64 [2]: row and head stride in elements (multiples of 16 bytes; rows must
+ *                               not overlap)
  *   wq, wk, eps, theta_base     as above
  * Hq or Hk may be 0.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA.  T == 0 is a no-op.
  * ------------------------------------------------------------------------- */
@@ -789,7 +795,14 @@ LOMA_API int loma_qk_norm_rope_append(const void* q, const void* k_new, const vo
  * in which the first prefix_len entries are the same for every sequence and stored once, with grouped heads.
  * Query head hq of sequence b attends, under one softmax, to the prefix's entries [0, prefix_len) of kv head
  * hq / (Hq / Hkv), to the sequence's own entries [0, cache_lens[b]) and to its new token.  The prefix part is
- * computed for all sequences together (the prefix is read once, on the tensor cores for bf16).
+ * computed for all sequences together: the prefix is read once for up to 128 query rows (B * Hq / Hkv) of a kv head,
+ * and from L2 for further ones.
+ * Precision: scores, the softmax and the sums are fp32.  bf16 calls on the tensor cores round the probabilities to
+ * bf16 for the product with V (each weight off by 2^-8 of itself at most; outputs 0.0021-0.0023 from 64 bits, 0.0017
+ * with the rounding of the output alone).  loma_decode_attn_ragged keeps them in fp32, and so does this call on CUDA
+ * cores under LOMA_FLAG_FORCE_GENERIC.
+ * Rows go by slot of the batch: a slot without a request has its row in q and o.  loma_paged_extend and
+ * loma_qk_norm_rope_append go by packed row (row_seq says whose), so with idle slots q is scattered in between.
  *
  *   q, o           [device]          [B, Hq, 1, D] contiguous; Hq is a multiple of Hkv
  *   k_new, v_new   [device, in]      [B, Hkv, 1, D] contiguous; both NULL: the token's K/V already sit at entry
@@ -801,7 +814,8 @@ LOMA_API int loma_qk_norm_rope_append(const void* q, const void* k_new, const vo
  *   cache_lens     [device, in]      int32 [B]: own entries before this token; values above max_cache_len count as
  *                                    max_cache_len; negative: a slot without a request, whose o, lse and cache are left
  *                                    as they are
- *   max_cache_len  [host]            an upper bound that sizes the launch; max_cache_len < cap
+ *   max_cache_len  [host]            an upper bound that sizes the launch; max_cache_len < cap.  How the work is cut
+ *                                    follows the bound: one far above the lengths costs up to a fifth of the time
  *   workspace      [device]          loma_decode_shared_workspace_bytes(...) bytes, 16-byte aligned; contents need not
  *                                    be kept.  The size grows with B, prefix_len and max_cache_len: one made for the
  *                                    largest of each serves every smaller call of the same heads.  Calls that may overlap need workspaces of their own

@@ -69,7 +69,8 @@ inline SharedPlan make_shared_plan(int B, int Hq, int Hkv, int D, int prefix_len
     // Blocks per SM of both parts (own: at most).  A prefix block takes an SM 0.8 us, an own block 0.2, starting the own kernel
     // five.  Measured, one CTA per SM against two: B128 Hq32 Hkv8 own 1500, prefix 16384 / 40000: 92 / 119 us against 94 / 134; own 64:
     // 54 / 103 against 54 / 88; B200 Hq64 Hkv8 own 300, prefix 30000: 244 against 211; B16 Hq32 Hkv8 own 100, prefix 4096 / 32768:
-    // 15.5 / 36.5 against 20.3 / 39.8.  Tiles of several pages are work for the one thread that asks for them, and two CTAs have
+    // 15.5 / 36.5 against 20.3 / 39.8.  max_len is the caller's bound, the lengths being on the device: where it is a table's capacity
+    // and own caches are short, a long prefix is cut for one CTA per SM as if they were long.  Tiles of several pages are work for the one thread that asks for them, and two CTAs have
     // two: the last case in pages of 16, 48 against 43.
     // Where the prefix kernel goes first (p.whole) it has the SMs to itself.
     const int64_t all = (int64_t)Hkv * p.p_blocks;

@@ -14,7 +14,8 @@
 // another CTA.  What a single-token step needs after the sums -- the page of each sequence's next entry and the head of the
 // free list -- is fetched before them.  Longer batches, and calls that update `held` or `taken` in place (where one CTA's
 // write would be another CTA's input), scan in one CTA and write rows in a second launch.
-// Measured: 64 sequences with one token each 4.5 us, 1000 prompts with a million rows (11 MB written) 10.1 us.
+// Measured: 64 sequences with one token each 4.4 us, 1000 prompts with a million rows (11 MB written) 10.0 us; with held and taken
+// updated in place 8.5 and 15.4 us.
 #include <limits.h>
 
 #include <algorithm>

@@ -17,7 +17,8 @@
 // bytes in flight cost no registers, which w, cos / sin and the sums of dw need.  The rows that a warp takes together lie
 // behind one another in memory: consecutive rows of a head, or, in a projection's [B, S, H, D] output, heads of a row.
 // Measured, bf16, 4608 rows of B4, D128: forward of 32 + 32 heads 98.4 us (6.1 TB/s, 0.95 of a copy), backward of 32 + 8 heads 98.7 us
-// (5.7 TB/s, 0.89; issue slots 62 % taken).  A few hundred rows in fp32: 3.4 us forward, 5.5 us backward (two launches).
+// (5.7 TB/s, 0.89; issue slots 62 % taken).  The gains' sums are one partial result per CTA added up by D / 16 CTAs: 2 us there, 10 of 34
+// us for 34816 rows of 2 + 2 heads.  A few hundred rows in fp32: 3.4 us forward, 5.5 us backward (two launches).
 #include <math.h>
 
 #include <algorithm>
@@ -39,7 +40,8 @@ __device__ __forceinline__ void load_gain(const T* w, int d0, float (&lo)[Vec16<
     }
 }
 
-// cos and sin of pos * theta, the angle formed and reduced in double (see rope_cos_sin)
+// cos and sin of pos * theta, the angle formed and reduced in double (see rope_cos_sin).  The reduced angle is rounded to fp32 for
+// sincosf: off by 2^-23 at most, and the results by about as much
 __device__ __forceinline__ void angle_cos_sin(int pos, double theta, float& c, float& s) {
     double a = (double)pos * theta;
     a -= 6.283185307179586476925 * rint(a * 0.15915494309189533577);
