@@ -6,6 +6,10 @@ autograd through them), the NumPy oracle where it is quick enough.
 Tolerances as in test_gpu_serving.py: one rounding of the output, 4e-6 of the rotated pair for fp32 work (angles, a norm of at
 most 128 features, a few products), and n 2^-24 of the sum of magnitudes for a sum of n terms."""
 
+import subprocess
+import sys
+from concurrent.futures import ThreadPoolExecutor
+
 import numpy as np
 import pytest
 import torch
@@ -13,7 +17,8 @@ import torch
 import oracle
 from oracle import serving_oracle as S
 from paper_2401_09486_b200 import binding as L
-from tests.test_gpu_serving import DEV, U32, _library, call_shared, check_shared, empty_like, half_step, normal, shared_case  # noqa: F401
+from paper_2401_09486_b200 import build
+from tests.test_gpu_serving import DEV, U32, _library, call_shared, caches_after, check_shared, empty_like, half_step, normal, shared_case  # noqa: F401
 from tests.test_serving_host import check_extend, extend_case, run_extend
 
 pytestmark = pytest.mark.gpu
@@ -251,3 +256,98 @@ def test_extend_table_beyond_32_bits():
         assert po.tolist() == [0, 1, M - 3, M - 2, M - 1, M, 0, 0]
         assert tab[0, :3].tolist() == [9, 20, 0] and tab[2, M - 6:].tolist() == [0, 11, 12, 13, 21, 22] and not tab[1].any() and not tab[2, : M - 5].any()
         del tab
+
+
+# ------------------------------------------------------------------------------------------------ how calls meet
+@pytest.mark.parametrize("ps", [0, 8, 16])
+def test_shared_decode_two_sequences_to_a_warp(ps):
+    """Short own caches of more (sequence, kv head) pairs than there are warps: each stays whole, and a warp takes two."""
+    s = shared_case(70, 16, 16, 128, 100, [(7 * i) % 100 - 1 for i in range(70)], ps, torch.bfloat16, seed=4)
+    before = s["kc"].clone(), s["vc"].clone()
+    call_shared(s)
+    torch.cuda.synchronize()
+    check_shared(s)
+    caches_after(s, before)
+
+
+def test_shared_decode_from_several_threads():
+    cases = [shared_case(4 + i, 8, 2, 128, 300 + i, [10 * j for j in range(4 + i)], 0, torch.bfloat16, seed=300 + i) for i in range(6)]
+    torch.cuda.synchronize()
+
+    def work(s):
+        torch.cuda.set_device(0)
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(100):
+                call_shared(s)
+        stream.synchronize()
+
+    with ThreadPoolExecutor(len(cases)) as pool:
+        list(pool.map(work, cases))
+    for s in cases:
+        check_shared(s)
+
+
+def test_a_step_run_again_after_the_list_ran_short():
+    """A step that ran out of pages is run again with a longer list: the outputs of a step that had enough from the start."""
+    B, Hq, Hkv, D, ps, M, P, dtype = 6, 8, 2, 64, 8, 3, 20, torch.bfloat16
+    i32 = dict(dtype=torch.int32, device=DEV)
+    lens, w = torch.tensor([8, 5, 16, 0, 15, 8], **i32), 1 + normal((D,), 1, dtype, 0.2)
+    qkv, pools = normal((B, Hq + 2 * Hkv, D), 2, dtype), [normal((40, Hkv, ps, D), s, dtype) for s in (3, 4)]
+    ptable, free = torch.arange(3, **i32), torch.arange(30, 40, **i32)
+
+    def run(list_lengths):
+        held, taken, table = ((lens + ps - 1) // ps).to(torch.int32), torch.zeros(1, **i32), torch.full((B, M), -1, **i32)
+        for b, n in enumerate(held.tolist()):
+            table[b, :n] = torch.arange(4 + 3 * b, 4 + 3 * b + n, **i32)
+        kp, vp = (x.clone() for x in pools)
+        rs, pg, sl, sq, po = (torch.empty(n, **i32) for n in (B + 1, B + 1, B, B, B))
+        q, o = torch.empty(B, Hq, D, dtype=dtype, device=DEV), torch.empty(B, Hq, 1, D, dtype=dtype, device=DEV)
+        ws = torch.empty(L.loma_decode_shared_workspace_bytes(B, Hq, Hkv, D, P, M * ps - 1), dtype=torch.uint8, device=DEV)
+        for n in list_lengths:
+            L.loma_paged_extend(lens, None, held, lens + P, free[:n], taken, table, ps, rs, pg, held, sl, sq, po)
+            L.loma_qk_norm_rope_append(qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], w, w, q, kp, vp, sl, po)
+            L.loma_decode_attn_shared_paged(q[:, :, None], None, None, kp, vp, ptable, P, table, o, None, lens, M * ps - 1, workspace=ws)
+            short = int(pg[-1]) > n
+        assert not short and (sl >= 0).all() and int(taken) == 4
+        return o, kp
+
+    (enough, _), (again, kp) = run([10]), run([2, 10])
+    assert torch.equal(enough, again)
+    assert torch.equal(kp[:4], pools[0][:4])                      # the prefix's pages and one nobody has
+
+
+FIRST_CALL = """
+import sys
+import torch
+from paper_2401_09486_b200 import binding as L
+d, bf, which = "cuda:0", torch.bfloat16, sys.argv[1]
+i = lambda *x: torch.tensor(x, dtype=torch.int32, device=d)
+n32 = lambda *x: torch.zeros(*x, dtype=torch.int32, device=d)
+q, kn, kp = torch.randn(2, 4, 1, 64, device=d).to(bf), torch.randn(2, 2, 1, 64, device=d).to(bf), torch.randn(2, 100, 64, device=d).to(bf)
+kc, vc, o = torch.zeros(2, 2, 64, 64, device=d, dtype=bf), torch.zeros(2, 2, 64, 64, device=d, dtype=bf), torch.zeros_like(q)
+x, y, z, dw = torch.randn(2, 4, 10, 64, device=d), torch.zeros(2, 4, 10, 64, device=d), torch.zeros(2, 4, 10, 64, device=d), torch.zeros(64, device=d)
+lens, table, sl, qo = i(3, 40), torch.full((2, 4), -1, dtype=torch.int32, device=d), n32(2), torch.zeros(2, 4, 64, device=d, dtype=bf)
+ws = torch.zeros(max(L.loma_decode_shared_workspace_bytes(2, 4, 2, 64, 100, 63), 1 << 20), dtype=torch.uint8, device=d)
+calls = {"shared": (o, lambda: L.loma_decode_attn_shared(q, kn, kn, kp, kp, 100, kc, vc, o, None, lens, 63, workspace=ws)),
+         "extend": (sl, lambda: L.loma_paged_extend(lens, None, None, None, i9, n32(1), table, 16, n32(3), n32(3), n32(2), sl, n32(2), n32(2))),
+         "norm": (y, lambda: L.loma_qk_norm_rope_fwd(x, x, None, None, y, z, 0, 4, 0, 10)),
+         "backward": (dw, lambda: L.loma_qk_norm_rope_bwd(x, x, None, None, x + 1, x, y, z, dw, None, 0, 4, 0, 10, 0, ws)),
+         "append": (qo, lambda: L.loma_qk_norm_rope_append(q[:, :, 0], kn[:, :, 0], kn[:, :, 0], None, None, qo, kc, vc, lens, lens))}
+i9 = torch.arange(5, 14, dtype=torch.int32, device=d)
+out, call = calls[which]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    call()
+graph.replay()
+torch.cuda.synchronize()
+assert out.ne(0).any()
+print("captured")
+"""
+
+
+@pytest.mark.parametrize("which", ["shared", "extend", "norm", "backward", "append"])
+def test_the_first_call_of_a_process_may_be_captured(which):
+    out = subprocess.run([sys.executable, "-c", FIRST_CALL, which], capture_output=True, text=True, timeout=300, cwd=build.ROOT)
+    assert out.returncode == 0 and "captured" in out.stdout, out.stderr[-2000:]
