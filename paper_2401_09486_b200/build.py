@@ -56,8 +56,7 @@ def marshal_key() -> str:
     """What _marshal.so has to have been built for: it uses torch's C++ classes, whose layout changes between versions."""
     import torch
 
-    return (f"python {sys.version_info[0]}.{sys.version_info[1]}, torch {torch.__version__} in "
-            f"{os.path.dirname(os.path.abspath(torch.__file__))}, C++ ABI {int(torch._C._GLIBCXX_USE_CXX11_ABI)}")
+    return f"python {sys.version_info[0]}.{sys.version_info[1]}, torch {torch.__version__}, C++ ABI {int(torch._C._GLIBCXX_USE_CXX11_ABI)}"
 
 
 def _marshal_stale() -> bool:
