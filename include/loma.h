@@ -28,6 +28,12 @@
  *                          per-head RMS norm of q and k with the rotary embedding (training
  *                          layout; packed new tokens into cache pages)
  *   loma_paged_extend      block tables and slot maps from request lengths
+ *   loma_paged_release, _fork, _compact, _copy
+ *                          pages back to the free list, shared by sequences that go on from one
+ *                          cache, moved to the pool's low numbers, and copied
+ *   loma_kv4_append, loma_kv4_load, loma_decode_attn_kv4
+ *                          memory entries held in 4 bits: stored, read back, and attended to
+ *                          together with the uncompressed tail
  *   loma_layout_index      row -> (chunk, zone, offset, source token, position id)
  *                          (Section 4.1; Section 4.5, Eq. 14)
  *   loma_generation_index  generated token -> cache slot / position / compress flag
@@ -838,6 +844,148 @@ LOMA_API int loma_decode_attn_shared_paged(const void* q, const void* k_new, con
                                            loma_dtype dtype, float softmax_scale, unsigned flags, void* workspace,
                                            size_t workspace_bytes, void* stream);
 LOMA_API size_t loma_decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int prefix_len, int max_cache_len);
+
+/* ---------------------------------------------------------------------------
+ * loma_paged_release, loma_paged_fork, loma_paged_compact, loma_paged_copy -- what happens to pages after
+ * loma_paged_extend handed them out (the paper keeps one cache per sequence; an engine that hands out cache memory
+ * page by page also takes it back: a compress step turns tc entries into t, requests end, answers branch).
+ *
+ * The state they share, all int32, with ps = page_size and M = max_pages:
+ *   block_table [B, M], held [B]   as in loma_paged_extend: row b names the pages of columns [0, held[b]), held clamped to [0, M]
+ *   free_pages [n_free], taken [1] the free pages are free_pages[taken .. n_free), taken clamped to [0, n_free]; n_free never
+ *                                  changes: pages that come back are put in front, in the places of pages drawn before, and
+ *                                  taken falls.  A list made with every page of the pool has room for all that come back
+ *   refs [n_pages]                 table entries beyond the first that name the page: 0 for a page of one sequence and for a
+ *                                  free one.  loma_paged_extend and the attention entry points need not know it
+ *   counts [4]  [out]              see below.  Counts beyond INT_MAX are stored as INT_MAX
+ * Table entries outside [0, n_pages) (loma_paged_extend writes -1 when its list is short) are passed over.
+ * on_device != 0: every pointer is [device] and the work is enqueued on `stream`; 0: every pointer is [host], no CUDA call.
+ * Each is one launch; a step of extend, append, attention, release and fork needs no host read and can be captured.
+ *
+ * release   row b keeps ceil(keep_lens[b] / ps) of its pages, or all it has if those are fewer; keep_lens[b] negative: the row is
+ *           left alone (0 lets go of everything).  The table entries of the others become -1, refs of their pages falls by one per
+ *           entry, and pages that no entry names any more go, in ascending order, in front of the free list.
+ *           held_out [B] [out]: pages kept; may be `held`.   counts = {0, pages freed, of them without room in the list, 0}
+ *           After loma_compress_step_*: keep_lens = mem_len + t for the sequences that compressed, -1 for the others.
+ *
+ * fork      row b becomes row parents[b] as it was before the call (beams, several answers to one prompt; parents[b] = b: goes on;
+ *           a number outside [0, B): the row becomes empty).  With len = cache_lens of the parent (clamped to [0, M ps]) and
+ *           fixed = fixed_lens of it (entries that nothing will write to again, clamped to [0, len]; NULL: len), its columns are
+ *             [0, fixed / ps)           named by every child: refs rises by one for each child but one
+ *             [fixed / ps, ceil(len/ps)) hold entries yet to be written or rewritten (the last page in part; LoMA's tail, which a
+ *                                       compress step overwrites: fixed = its memory entries)
+ *           and all of them but for the pages it holds.  One child, the parent itself or else the lowest, takes over all the parent's
+ *           pages.  The others get fresh pages for the second stretch, drawn from the free list in the order of row and column,
+ *           each with an entry in the copy list.  The pages of a row that nobody goes on from are let go of, as by release, before
+ *           pages are drawn.  Pages of the second stretch must have no other owner (refs 0), as they have when forks were told
+ *           the truth about fixed.
+ *           parents, cache_lens, fixed_lens, held, block_table [in] (fixed_lens and held may be NULL; held NULL: ceil(len / ps))
+ *           table_out [B, M] [out]: every entry is written, -1 behind a row's pages; lens_out [B]: cache_lens[parents[b]], -1 for an
+ *             empty row; held_out [B].  They must not overlap the inputs: the caller exchanges the two tables
+ *           copy_src, copy_dst [max_copies] [out]: page copy_src[i] is to be copied to copy_dst[i]; copy_src[i] = -1 where the
+ *             parent's entry names no page of the pool; both -1 behind the last.  B * (pages a tail can span) bounds their number
+ *           Where the free list or the copy list ends, the child's table gets -1 instead and held_out counts what it got.
+ *           counts = {copies listed, pages freed, of them without room in the list, pages that could not be had}
+ *           workspace: loma_paged_fork_workspace_bytes(B) bytes, [device] or [host] like the rest
+ *
+ * compact   of the pages that are named or free, the lowest become the named ones: named pages above move, in ascending order, to
+ *           free ones below, in ascending order (at most max_copies of them), in every table entry and with their refs.  The pages
+ *           above the highest named one then hold nothing, and the free list is in ascending order.  Pages that are neither named
+ *           by block_table nor in the free list (a shared prefix, another table's) stay where they are.
+ *           page_map [n_pages] [out]: the new number of every page (its own if it did not move), for tables kept elsewhere
+ *           copy_src, copy_dst [max_copies] as above.   counts = {moves, free pages, named pages, moves left for another call}
+ *
+ * copy      page copy_src[i] of every pool is copied to page copy_dst[i], i < n_copies[0] (clamped to [0, max_copies]).  pools, page_bytes
+ *           [host]: n_pools device pointers (K and V of every layer, say) and the bytes of a page of each (multiples of 16), n_pages
+ *           pages each.  n_copies [device]: counts of fork or compact.  Pairs with a number outside [0, n_pages) are passed over.
+ *           No page may be a source and a destination of one call, or a destination twice (the lists above have neither).
+ *           One launch for up to 64 pools.
+ * Errors: INVALID_ARG (negative sizes, page size not a power of two <= 65536, max_pages * page_size > INT_MAX, a required pointer
+ * NULL, outputs that overlap inputs or each other), ALIGNMENT (4 bytes; pools and page_bytes 16), WORKSPACE, UNSUPPORTED, CUDA.
+ * ------------------------------------------------------------------------- */
+LOMA_API int loma_paged_release(int B, int page_size, int max_pages, int n_pages, int n_free, const int32_t* keep_lens,
+                                const int32_t* held, int32_t* block_table, int32_t* held_out, int32_t* refs,
+                                int32_t* free_pages, int32_t* taken, int32_t* counts, int on_device, void* stream);
+LOMA_API int loma_paged_fork(int B, int page_size, int max_pages, int n_pages, int n_free, int max_copies,
+                             const int32_t* parents, const int32_t* cache_lens, const int32_t* fixed_lens,
+                             const int32_t* held, const int32_t* block_table, int32_t* table_out, int32_t* lens_out,
+                             int32_t* held_out, int32_t* refs, int32_t* free_pages, int32_t* taken, int32_t* copy_src,
+                             int32_t* copy_dst, int32_t* counts, void* workspace, size_t workspace_bytes, int on_device,
+                             void* stream);
+LOMA_API size_t loma_paged_fork_workspace_bytes(int B);
+LOMA_API int loma_paged_compact(int B, int max_pages, int n_pages, int n_free, int max_copies, const int32_t* held,
+                                int32_t* block_table, int32_t* refs, int32_t* free_pages, int32_t* taken,
+                                int32_t* page_map, int32_t* copy_src, int32_t* copy_dst, int32_t* counts, int on_device,
+                                void* stream);
+LOMA_API int loma_paged_copy(int n_pools, void* const* pools, const int64_t* page_bytes, int n_pages,
+                             const int32_t* copy_src, const int32_t* copy_dst, const int32_t* n_copies, int max_copies,
+                             void* stream);
+
+/* ---------------------------------------------------------------------------
+ * loma_kv4_append, loma_kv4_load, loma_decode_attn_kv4 -- memory entries held in 4 bits.  LoMA's cache is made of memory
+ * entries, which stay for the whole request and are what a long request's cache consists of, and of the uncompressed tail
+ * (Section 3.1).  Here the memory entries lie in a paged pool in 4 bits, the tail in a cache of the call's type:
+ *   a token      loma_decode_attn_kv4 over both, which appends it to the tail
+ *   a full tail  loma_compress_step_ragged over the tail alone (mem_lens 0, negative for sequences that do not compress), which
+ *                leaves the t memory keys and values in the tail's first rows; loma_kv4_append of those rows; tail length 0
+ *   a prompt     loma_kv4_append of its memory entries (loma_prefill_cache); a further piece: loma_kv4_load into a cache, then
+ *                loma_prefill_attn_ragged
+ * Pages are handed out, taken back, shared and moved by loma_paged_extend and the entry points above.
+ *
+ * Format.  32 consecutive features of a row share a step h, the bf16 nearest to fp32(max |x| / 15); h below 2^-126 counts as 0, and a
+ * group with a value that is no finite number gets h = NaN.  x is held as its sign and m, the number of k in 1 .. 7 with
+ * |x| >= 2 h k, and stands for (2 m + 1) h with that sign (NaN, or 0, throughout a group whose h is).  With h above 0 that is off
+ * by h at most, a sixteenth of the group's range; a zero becomes +h.
+ * A row of D features takes D / 2 + D / 16 bytes.  A pool is n_pages pages of loma_kv4_page_bytes(Hkv, D, page_size) bytes; the order
+ * of bytes inside a page is the library's own.  page_size: a power of two from 16 to 65536.
+ *
+ * append    rows i < n of sequence b, n = new_lens[b] (at most l; NULL: l), become entries mem_lens[b] + i.  mem_lens[b] negative: the
+ *           sequence stores nothing.  Entries past max_pages * page_size, and entries whose page number lies outside the pool, are
+ *           not stored.  No two rows of a call may name one entry.
+ *   k, v         [device, in]   [B, Hkv, l, D] with k_strides, v_strides [host] int64 [3]: batch, head and row stride in elements
+ *                               (multiples of 16 bytes; rows must not overlap): the first rows of a tail cache, for instance
+ *   kv_pool      [device, out]
+ *   block_table  [device, in]   int32 [B, max_pages]
+ *   mem_lens, new_lens [device, in] int32 [B]
+ *
+ * load      entries [0, mem_lens[b]) of sequence b, at most cap of them, as values of the call's type (rounded once) into rows of
+ *           k_cache, v_cache [device, out] [B, Hkv, cap, D] contiguous; other rows are left as they are.
+ *
+ * decode    query head hq of sequence b attends, under one softmax, to memory entries [0, mem_lens[b]) of kv head
+ *           hq / (Hq / Hkv), to the tail's entries [0, tail_lens[b]) and to its new token.
+ *   q, o           [device]           [B, Hq, 1, D] contiguous; Hq is a multiple of Hkv
+ *   k_new, v_new   [device, in]       [B, Hkv, 1, D] contiguous, stored to entry tail_lens[b] of the tail; both NULL: they sit there
+ *   k_tail, v_tail [device, in/out]   [B, Hkv, cap, D] contiguous
+ *   lse            [device, out]      fp32 [B, Hq] or NULL
+ *   tail_lens      [device, in]       int32 [B]; values above max_tail_len count as max_tail_len; negative: a slot without a request,
+ *                                     whose o, lse and tail are left as they are
+ *   mem_lens       [device, in]       int32 [B], clamped to [0, max_mem_len]
+ *   max_tail_len, max_mem_len [host]  upper bounds; max_tail_len < cap, max_mem_len <= max_pages * page_size.  With max_mem_len 0 there
+ *                                     need be no pool
+ *   workspace      [device]           loma_decode_kv4_workspace_bytes(...) bytes, 16-byte aligned; contents need not be kept.  The
+ *                                     size grows with B, max_mem_len and max_tail_len.  Calls that may overlap need workspaces of their own
+ * Page numbers outside the pool are clamped to it where they are read (load, decode).
+ * Precision: memory entries are what they stand for, (2 m + 1) h, without a further rounding; scores, the softmax and the sums are
+ * fp32.  bf16 calls run on the tensor cores and round each weight (times the step of the value's group) to bf16 for the product
+ * with V, off by 2^-8 of itself at most; fp32, and LOMA_FLAG_FORCE_GENERIC, keep it.  On the tensor cores queries up to 2^60 and
+ * values up to 2^40 in magnitude.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CAPACITY, WORKSPACE, CUDA.  B * Hkv * l == 0, B * Hkv * cap == 0, B * Hq == 0: a no-op.
+ * ------------------------------------------------------------------------- */
+LOMA_API size_t loma_kv4_page_bytes(int Hkv, int D, int page_size);
+LOMA_API int loma_kv4_append(const void* k, const void* v, void* kv_pool, const int32_t* block_table, const int32_t* mem_lens,
+                             const int32_t* new_lens, int B, int Hkv, int D, int l, int page_size, int max_pages,
+                             int n_pages, const int64_t* k_strides, const int64_t* v_strides, loma_dtype dtype,
+                             void* stream);
+LOMA_API int loma_kv4_load(const void* kv_pool, const int32_t* block_table, const int32_t* mem_lens, void* k_cache,
+                           void* v_cache, int B, int Hkv, int D, int cap, int page_size, int max_pages, int n_pages,
+                           loma_dtype dtype, void* stream);
+LOMA_API int loma_decode_attn_kv4(const void* q, const void* k_new, const void* v_new, void* k_tail, void* v_tail,
+                                  const void* kv_pool, const int32_t* block_table, void* o, float* lse, int B, int Hq,
+                                  int Hkv, int D, int cap, const int32_t* tail_lens, int max_tail_len, int page_size,
+                                  int max_pages, int n_pages, const int32_t* mem_lens, int max_mem_len, loma_dtype dtype,
+                                  float softmax_scale, unsigned flags, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+LOMA_API size_t loma_decode_kv4_workspace_bytes(int B, int Hq, int Hkv, int D, int max_mem_len, int max_tail_len);
 
 /* Synchronises `stream`, then returns the device status word of the current
  * device: LOMA_OK, or LOMA_ERR_TIMEOUT if a bounded wait inside a kernel has

@@ -83,6 +83,16 @@ SIGNATURES = {
     "loma_decode_attn_shared_paged": (_i, [_p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _i, _i, _i, _p, _i, _i, _f, _u,
                                            _p, _sz, _p]),
     "loma_decode_shared_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
+    "loma_paged_release": (_i, [_i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _p, _p, _i, _p]),
+    "loma_paged_fork": (_i, [_i, _i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _i, _p]),
+    "loma_paged_fork_workspace_bytes": (_sz, [_i]),
+    "loma_paged_compact": (_i, [_i, _i, _i, _i, _i, _p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _p]),
+    "loma_paged_copy": (_i, [_i, _p, _p, _i, _p, _p, _p, _i, _p]),
+    "loma_kv4_page_bytes": (_sz, [_i, _i, _i]),
+    "loma_kv4_append": (_i, [_p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _i, _p, _p, _i, _p]),
+    "loma_kv4_load": (_i, [_p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _i, _i, _p]),
+    "loma_decode_attn_kv4": (_i, [_p, _p, _p, _p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _p, _i, _i, _i, _i, _p, _i, _i, _f, _u, _p, _sz, _p]),
+    "loma_decode_kv4_workspace_bytes": (_sz, [_i, _i, _i, _i, _i, _i]),
     "loma_device_status": (_i, [_p]),
     "loma_selftest_bounded_wait": (_i, [_p]),
     "loma_launch_count": (ctypes.c_uint64, []),
@@ -687,7 +697,8 @@ def _native():
             raise RuntimeError(f"the extension module _marshal.so was built for {module.built_for}, not for {marshal_key()}: build it again with "
                                "`python -m paper_2401_09486_b200.build`")
         names = ("loma_paged_extend", "loma_qk_norm_rope_fwd", "loma_qk_norm_rope_bwd", "loma_qk_norm_rope_append",
-                 "loma_decode_attn_shared", "loma_decode_attn_shared_paged")
+                 "loma_decode_attn_shared", "loma_decode_attn_shared_paged", "loma_paged_release", "loma_paged_fork", "loma_paged_compact",
+                 "loma_paged_copy", "loma_kv4_page_bytes", "loma_kv4_append", "loma_kv4_load", "loma_decode_attn_kv4")
         module.bind(*[ctypes.cast(getattr(handle, n), ctypes.c_void_p).value for n in names])
         _marshal = module
     return _marshal
@@ -753,3 +764,69 @@ def loma_decode_attn_shared_paged(q, k_new, v_new, k_pool, v_pool, prefix_table,
     _check((_marshal or _native()).decode_attn_shared_paged(q, k_new, v_new, k_pool, v_pool, prefix_table, prefix_len, block_table, o, lse,
                                                             cache_lens, max_cache_len, workspace, flags, softmax_scale, stream),
            "loma_decode_attn_shared_paged")
+
+
+# ---- the life of cache pages, and memory entries in 4 bits ---------------------------------------------------------------
+
+
+def loma_paged_release(keep_lens, held, block_table, page_size: int, held_out, refs, free_pages, taken, counts, stream=None) -> None:
+    """Pages past keep_lens (negative: row left alone) back to the free list (see include/loma.h).  int32 tensors, all on the device
+    or all on the host: keep_lens, held [B], block_table [B, max_pages] (in/out), held_out [B] (may be `held`), refs [n_pages],
+    free_pages [n_free], taken [1] (in/out), counts [4]."""
+    _check((_marshal or _native()).paged_release(keep_lens, held, block_table, page_size, held_out, refs, free_pages, taken, counts, stream),
+           "loma_paged_release")
+
+
+def loma_paged_fork_workspace_bytes(B: int) -> int:
+    return int(lib().loma_paged_fork_workspace_bytes(B))
+
+
+def loma_paged_fork(parents, cache_lens, fixed_lens, held, block_table, page_size: int, table_out, lens_out, held_out, refs, free_pages,
+                    taken, copy_src, copy_dst, counts, workspace=None, stream=None) -> None:
+    """Every row goes on from row parents[b]: whole pages below fixed_lens shared, the others copied through the list copy_src,
+    copy_dst (loma_paged_copy).  int32 tensors, all on the device or all on the host: parents, cache_lens, fixed_lens, held [B]
+    (fixed_lens and held may be None), block_table [B, max_pages]; outputs table_out, lens_out, held_out, copy_src, copy_dst, counts [4];
+    in/out refs [n_pages], free_pages [n_free], taken [1]; workspace: loma_paged_fork_workspace_bytes(B) bytes."""
+    _check((_marshal or _native()).paged_fork(parents, cache_lens, fixed_lens, held, block_table, page_size, table_out, lens_out, held_out, refs,
+                                              free_pages, taken, copy_src, copy_dst, counts, workspace, stream), "loma_paged_fork")
+
+
+def loma_paged_compact(held, block_table, refs, free_pages, taken, page_map, copy_src, copy_dst, counts, stream=None) -> None:
+    """Named pages to the lowest numbers.  int32 tensors, all on the device or all on the host: held [B]; in/out block_table
+    [B, max_pages], refs [n_pages], free_pages [n_free], taken [1]; outputs page_map [n_pages], copy_src, copy_dst, counts [4]."""
+    _check((_marshal or _native()).paged_compact(held, block_table, refs, free_pages, taken, page_map, copy_src, copy_dst, counts, stream),
+           "loma_paged_compact")
+
+
+def loma_paged_copy(pools, copy_src, copy_dst, n_copies, stream=None) -> None:
+    """Page copy_src[i] to page copy_dst[i] in each of `pools` (contiguous tensors [n_pages, ...] of any type), i < n_copies[0] (an int32
+    tensor of one entry on the device: the first of a fork's or a compaction's counts)."""
+    _check((_marshal or _native()).paged_copy(pools, copy_src, copy_dst, n_copies, stream), "loma_paged_copy")
+
+
+def loma_kv4_page_bytes(Hkv: int, D: int, page_size: int) -> int:
+    return int(lib().loma_kv4_page_bytes(Hkv, D, page_size))
+
+
+def loma_kv4_append(k, v, kv_pool, block_table, page_size: int, mem_lens, new_lens=None, stream=None) -> None:
+    """Rows of k, v [B, Hkv, l, D] (any strides over rows of D) become memory entries mem_lens[b] + i in 4 bits, for i < new_lens[b] (None:
+    all l).  kv_pool: uint8 [n_pages, loma_kv4_page_bytes(Hkv, D, page_size)]; block_table int32 [B, max_pages]."""
+    _check((_marshal or _native()).kv4_append(k, v, kv_pool, block_table, page_size, mem_lens, new_lens, stream), "loma_kv4_append")
+
+
+def loma_kv4_load(kv_pool, block_table, page_size: int, mem_lens, k_cache, v_cache, stream=None) -> None:
+    """Memory entries [0, mem_lens[b]) as values into k_cache, v_cache [B, Hkv, cap, D]."""
+    _check((_marshal or _native()).kv4_load(kv_pool, block_table, page_size, mem_lens, k_cache, v_cache, stream), "loma_kv4_load")
+
+
+def loma_decode_kv4_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, max_mem_len: int, max_tail_len: int) -> int:
+    return int(lib().loma_decode_kv4_workspace_bytes(B, Hq, Hkv, D, int(max_mem_len), int(max_tail_len)))
+
+
+def loma_decode_attn_kv4(q, k_new, v_new, k_tail, v_tail, tail_lens, max_tail_len: int, kv_pool, block_table, page_size: int, mem_lens,
+                         max_mem_len: int, o, lse, workspace=None, flags: int = 0, softmax_scale: float = 0.0, stream=None) -> None:
+    """Decode step over memory entries in 4 bits and the uncompressed tail.  q, o: [B, Hq, 1, D]; k_new, v_new: [B, Hkv, 1, D] or None
+    (already stored); k_tail, v_tail: [B, Hkv, cap, D]; tail_lens, mem_lens: int32 [B], tail_lens negative = no request; kv_pool,
+    block_table as in loma_kv4_append (None where max_mem_len is 0); workspace: loma_decode_kv4_workspace_bytes(...) bytes."""
+    _check((_marshal or _native()).decode_attn_kv4(q, k_new, v_new, k_tail, v_tail, tail_lens, max_tail_len, kv_pool, block_table, page_size,
+                                                   mem_lens, max_mem_len, o, lse, workspace, flags, softmax_scale, stream), "loma_decode_attn_kv4")

@@ -1,0 +1,392 @@
+// Decode attention over memory entries held in 4 bits and an uncompressed tail (loma_decode_attn_kv4).
+//
+// Query head hq of sequence b sees the memory entries [0, mem_lens[b]) of kv head hq div g (g = Hq / Hkv), the tail's entries
+// [0, tail_lens[b]) and the new token, under one softmax.  One query row per head against rows that no other sequence reads: a
+// stream bound by HBM, 144 bytes of 4-bit tiles per memory entry (D = 128) where bf16 has 512.  So few bytes leave little time for
+// arithmetic: 23 bytes per SM and clock from HBM are a tile of 16 entries every 100 clocks, and turning its 4096 numbers into
+// operands alone takes a warp 128 instructions.
+//
+// Cut: units are (kv head, head tile, sequence); a unit's blocks of 16 entries -- tiles of memory first, then the tail with the new
+// token last -- are numbered through, and worker w of W (a warp) takes blocks [T w / W, T (w + 1) / W).  A worker's stay in
+// one unit is a segment with a partial result in slot w + unit; kv4_merge_kernel joins a unit's segments in a fixed order.  The
+// lengths are known on the device only, so every CTA finds the cut from them.
+//
+// bf16: kv4_decode_kernel, warp-level products.  fp32, and the second opinion: kv4_stream_kernel on CUDA cores.
+#include "kv4.cuh"
+#include "tcgen05_common.cuh"
+
+namespace loma {
+
+constexpr int KV4_WARPS = 4;
+
+struct Kv4Plan {
+    int g_rows, g_tiles;   // query heads of a kv head per head tile, head tiles per kv head
+    int ctas, workers;     // W, before it is cut down for few blocks
+    // in the workspace, in floats.  Segment: outputs [g_rows][D], g_rows log2-sum-exps.  cum: int64 [B + 1], blocks before sequence b within
+    // one (kv head, head tile)
+    int64_t o, lse, cum, total;
+};
+
+static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, bool cuda_cores) {
+    Kv4Plan p;
+    const int g = Hq / Hkv;
+    p.g_rows = cuda_cores ? (g < 3 ? g : 4) : (g <= 8 ? g : 16);
+    p.g_tiles = (g + p.g_rows - 1) / p.g_rows;
+    p.ctas = 148 * (cuda_cores || p.g_rows <= 8 ? 4 : 2);
+    p.workers = p.ctas * KV4_WARPS;
+    int64_t at = 0;
+    auto take = [&](int64_t n) { const int64_t o = at; at += (n + 63) / 64 * 64; return o; };
+    const int64_t segments = p.workers + (int64_t)B * Hkv * p.g_tiles;
+    p.o = take(segments * p.g_rows * D);
+    p.lse = take(segments * p.g_rows);
+    p.cum = take(2 * ((int64_t)B + 1));
+    p.total = at;
+    return p;
+}
+
+// the worker that block t of T belongs to, and the first block of worker w (W <= T)
+__device__ __forceinline__ int64_t kv4_worker(int64_t t, int64_t T, int64_t W) { return ((t + 1) * W - 1) / T; }
+__device__ __forceinline__ int64_t kv4_first(int64_t w, int64_t T, int64_t W) { return T / W * w + T % W * w / W; }
+
+// One sequence's part of a unit.
+struct Kv4Seq {
+    int mem, tail;   // memory entries; tail entries before the new token (negative: no request)
+    int nm, n;       // blocks of memory, and in all
+};
+__device__ __forceinline__ Kv4Seq kv4_seq(const Kv4DecodeArgs& a, int b) {
+    Kv4Seq s;
+    s.mem = min(max(__ldg(a.mem_lens + b), 0), a.max_mem);
+    s.tail = min(__ldg(a.tail_lens + b), a.max_tail);
+    s.nm = (int)(((int64_t)s.mem + KV4_ROWS - 1) / KV4_ROWS);
+    s.n = s.tail < 0 ? 0 : s.nm + s.tail / KV4_ROWS + 1;
+    return s;
+}
+
+// The numbering of the blocks, found again by every CTA.
+struct Kv4Blocks {
+    static constexpr int MAX_GROUPS = 512, THREADS = KV4_WARPS * 32, PER_THREAD = MAX_GROUPS / THREADS;
+    struct Cursor {
+        int hh, b, blk;   // kv head * g_tiles + head tile, sequence, block
+        Kv4Seq s;
+    };
+    const Kv4DecodeArgs& a;
+
+    // s[i]: blocks before sequence i * per of one (kv head, head tile), i = 0 .. groups; returns per.  out: all B + 1 sums, stored for
+    // the merge kernel (or NULL).  Ends with a barrier.
+    __device__ __forceinline__ int scan(int64_t* s, int64_t* wsum, int64_t* out) const {
+        const int per = (a.B + MAX_GROUPS - 1) / MAX_GROUPS, groups = (a.B + per - 1) / per;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        int64_t mine[PER_THREAD], sum = 0;
+#pragma unroll
+        for (int u = 0; u < PER_THREAD; ++u) {
+            const int i = threadIdx.x * PER_THREAD + u;
+            mine[u] = 0;
+            for (int b = i * per; b < min(a.B, (i + 1) * per); ++b) mine[u] += kv4_seq(a, b).n;
+            sum += mine[u];
+        }
+        int64_t incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += x;
+        }
+        if (lane == 31) wsum[warp] = incl;
+        __syncthreads();
+        int64_t at = incl - sum;
+        for (int x = 0; x < warp; ++x) at += wsum[x];
+#pragma unroll
+        for (int u = 0; u < PER_THREAD; ++u) {
+            const int i = threadIdx.x * PER_THREAD + u;
+            if (i <= groups) s[i] = at;
+            if (out) {
+                int64_t c = at;
+                for (int b = i * per; b < min(a.B, (i + 1) * per); ++b) {
+                    out[b] = c;
+                    c += kv4_seq(a, b).n;
+                }
+                if (i == groups - 1) out[a.B] = c;
+            }
+            at += mine[u];
+        }
+        if (threadIdx.x == THREADS - 1 && groups == MAX_GROUPS) s[MAX_GROUPS] = at;
+        __syncthreads();
+        return per;
+    }
+
+    __device__ __forceinline__ Cursor find(int64_t t, const int64_t* s, int per) const {
+        const int groups = (a.B + per - 1) / per;
+        Cursor c;
+        c.hh = (int)(t / s[groups]);
+        int64_t rem = t - c.hh * s[groups];
+        int lo = 0, hi = groups;   // s[lo] <= rem < s[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (s[mid] <= rem) lo = mid; else hi = mid;
+        }
+        rem -= s[lo];
+        for (c.b = lo * per;; ++c.b) {
+            c.s = kv4_seq(a, c.b);
+            if (rem < c.s.n) break;
+            rem -= c.s.n;
+        }
+        c.blk = (int)rem;
+        return c;
+    }
+
+    // the next unit that holds a request; there has to be one
+    __device__ __forceinline__ void next_unit(Cursor& c) const {
+        c.blk = 0;
+        do {
+            if (++c.b == a.B) { c.b = 0; ++c.hh; }
+            c.s = kv4_seq(a, c.b);
+        } while (c.s.n == 0);
+    }
+};
+
+__device__ __forceinline__ int kv4_page_read(const Kv4Pool& m, int b, int j) {   // numbers outside the pool are clamped to it
+    return min(max(__ldg(m.table + (int64_t)b * m.max_pages + (j >> m.log2_ps)), 0), m.n_pages - 1);
+}
+
+// ------------------------------------------------------------------ CUDA cores
+// Eight lanes share an entry (a chunk each, 16 or 8 of its features), so a warp takes four entries at a time, G heads of the group
+// together.  All arithmetic in fp32; the one rounding is that of the output.
+template <typename T, int D, int G>
+__global__ void __launch_bounds__(KV4_WARPS * 32)
+kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
+    using TL = Kv4Tile<D>;
+    constexpr int NG = TL::GROUPS, N = 4 * NG;   // groups; features of a lane: 32 g + 4 x + e at [4 g + e]
+    __shared__ int64_t scan[Kv4Blocks::MAX_GROUPS + 1];
+    __shared__ int64_t wsum[KV4_WARPS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, x = lane & 7, sub = lane >> 3;
+    float* ws = static_cast<float*>(a.ws);
+    let_next_start();
+    const Kv4Blocks kb{a};
+    const int per = kb.scan(scan, wsum, blockIdx.x == 0 ? reinterpret_cast<int64_t*>(ws + p.cum) : nullptr);
+    const int64_t total = scan[(a.B + per - 1) / per] * a.Hkv * p.g_tiles, W = min(total, (int64_t)p.workers);
+    const int64_t w = (int64_t)warp * gridDim.x + blockIdx.x;
+    if (w >= W) return;
+    int64_t t = kv4_first(w, total, W);
+    const int64_t t_end = kv4_first(w + 1, total, W);
+    Kv4Blocks::Cursor c = kb.find(t, scan, per);
+    const float scale_log2 = a.scale * 1.4426950408889634f;
+    float q[G][N], acc[G][N], m[G], l[G];   // m: of all entries seen; l, acc: of this lane's `sub`
+    bool fresh = true;
+    for (; t < t_end; ++t) {
+        const int h = c.hh / p.g_tiles, gt = c.hh - h * p.g_tiles, heads = min(G, a.g - gt * G);
+        if (fresh) {
+#pragma unroll
+            for (int y = 0; y < G; ++y) {
+                const T* qp = static_cast<const T*>(a.q) + ((int64_t)c.b * a.Hq + h * a.g + gt * G + min(y, heads - 1)) * D + 4 * x;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    q[y][i] = (float)qp[32 * (i / 4) + i % 4] * scale_log2;
+                    acc[y][i] = 0.f;
+                }
+                m[y] = -INFINITY;
+                l[y] = 0.f;
+            }
+            fresh = false;
+        }
+        const bool memory = c.blk < c.s.nm;
+        const int first = (memory ? c.blk : c.blk - c.s.nm) * KV4_ROWS;        // of the block, in memory or in the tail
+        const int end = min(memory ? c.s.mem : c.s.tail + 1, first + KV4_ROWS);
+        const uint8_t* tile = memory ? a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, c.b, first), h, first) : nullptr;
+#pragma unroll 1
+        for (int j0 = first; j0 < end; j0 += 4) {
+            const int j = min(j0 + sub, end - 1);   // no row of another sequence is ever read
+            const bool there = j0 + sub < end;
+            float k[N], v[N];
+            if (memory) {
+                const uint8_t* bits = tile + kv4_chunk<D>(j & 15, x);
+                const uint8_t* steps = tile + TL::K_STEPS + (j & 15) * TL::STEPS;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    const float hk = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(steps + 2 * g) << 16);
+                    const float hv = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(steps + TL::V_STEPS - TL::K_STEPS + 2 * g) << 16);
+                    const uint32_t yk = *reinterpret_cast<const uint16_t*>(bits + 2 * g), yv = *reinterpret_cast<const uint16_t*>(bits + TL::V + 2 * g);
+                    constexpr int at_m[4] = {0, 3, 8, 11}, at_s[4] = {14, 15, 6, 7};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float nk = (float)(2 * (yk >> at_m[e] & 7) + 1) * hk, nv = (float)(2 * (yv >> at_m[e] & 7) + 1) * hv;
+                        k[4 * g + e] = yk >> at_s[e] & 1 ? -nk : nk;
+                        v[4 * g + e] = yv >> at_s[e] & 1 ? -nv : nv;
+                    }
+                }
+            } else {
+                const bool token = j == c.s.tail && a.k_new;
+                const int64_t at = token ? ((int64_t)c.b * a.Hkv + h) * D : (((int64_t)c.b * a.Hkv + h) * a.cap + j) * D;
+                const T* kp = static_cast<const T*>(token ? a.k_new : a.k_tail) + at + 4 * x;
+                const T* vp = static_cast<const T*>(token ? a.v_new : a.v_tail) + at + 4 * x;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    k[i] = (float)kp[32 * (i / 4) + i % 4];
+                    v[i] = (float)vp[32 * (i / 4) + i % 4];
+                }
+                if (token && gt == 0 && there) {   // entry tail of the cache is read by nobody in this launch
+                    const int64_t cell = (((int64_t)c.b * a.Hkv + h) * a.cap + j) * D + 4 * x;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        static_cast<T*>(a.k_tail)[cell + 32 * (i / 4) + i % 4] = kp[32 * (i / 4) + i % 4];
+                        static_cast<T*>(a.v_tail)[cell + 32 * (i / 4) + i % 4] = vp[32 * (i / 4) + i % 4];
+                    }
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < G; ++y) {
+                float s = 0.f;
+#pragma unroll
+                for (int i = 0; i < N; ++i) s = fmaf(q[y][i], k[i], s);
+#pragma unroll
+                for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                if (!there) s = -INFINITY;
+                const float top = fmaxf(m[y], fmaxf(fmaxf(s, __shfl_xor_sync(0xffffffffu, s, 8)), fmaxf(__shfl_xor_sync(0xffffffffu, s, 16), __shfl_xor_sync(0xffffffffu, s, 24))));
+                const float keep = top == -INFINITY ? 1.f : exp2f(m[y] - top), pr = top == -INFINITY ? (s == s ? 0.f : s) : exp2f(s - top);
+                m[y] = top;
+                l[y] = l[y] * keep + pr;
+#pragma unroll
+                for (int i = 0; i < N; ++i) acc[y][i] = acc[y][i] * keep + (there ? pr * v[i] : 0.f);   // a repeated row has no weight, but 0 x inf is not 0
+            }
+        }
+        const bool last = c.blk == c.s.n - 1;
+        if (last || t + 1 == t_end) {
+            const int64_t seg = w + (int64_t)c.hh * a.B + c.b;
+#pragma unroll
+            for (int y = 0; y < G; ++y) {
+#pragma unroll
+                for (int o = 8; o < 32; o <<= 1) {
+                    l[y] += __shfl_xor_sync(0xffffffffu, l[y], o);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) acc[y][i] += __shfl_xor_sync(0xffffffffu, acc[y][i], o);
+                }
+                if (y < heads && sub == 0) {
+                    const float inv = 1.f / l[y];
+#pragma unroll
+                    for (int g = 0; g < NG; ++g)
+                        *reinterpret_cast<float4*>(ws + p.o + (seg * p.g_rows + y) * D + 32 * g + 4 * x) =
+                            make_float4(acc[y][4 * g] * inv, acc[y][4 * g + 1] * inv, acc[y][4 * g + 2] * inv, acc[y][4 * g + 3] * inv);
+                    if (x == 0) ws[p.lse + seg * p.g_rows + y] = m[y] + log2f(l[y]);
+                }
+            }
+            fresh = true;
+        }
+        if (t + 1 == t_end) break;
+        if (last) kb.next_unit(c); else ++c.blk;
+    }
+}
+
+// ------------------------------------------------------------------ merge
+// A row's D features are D / 4 lanes; WAYS sets of lanes share a row's partial results.
+constexpr int KV4_MERGE_THREADS = 128;
+
+template <typename T, int D, int WAYS>
+__global__ void __launch_bounds__(KV4_MERGE_THREADS)
+kv4_merge_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
+    constexpr int LANES = D / 4, ROWS = KV4_MERGE_THREADS / LANES / WAYS, AT_ONCE = 8;
+    const int c4 = threadIdx.x % LANES, set = threadIdx.x / LANES, way = set % WAYS;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + set / WAYS;
+    const bool there = row < (int64_t)a.B * a.Hq;
+    const int b = there ? (int)(row / a.Hq) : 0, hq = there ? (int)(row - (int64_t)b * a.Hq) : 0;
+    const int h = hq / a.g, j = hq - h * a.g, gt = j / p.g_rows, x = j - gt * p.g_rows;
+    const bool live = there && __ldg(a.tail_lens + b) >= 0;
+    const float* ws = static_cast<const float*>(a.ws);
+    wait_for_previous();
+    float M = -INFINITY, total = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (live) {
+        const int64_t* cum = reinterpret_cast<const int64_t*>(ws + p.cum);
+        const int64_t per_head = __ldcg(cum + a.B), hh = (int64_t)h * p.g_tiles + gt, T_all = per_head * a.Hkv * p.g_tiles;
+        const int64_t W = min(T_all, (int64_t)p.workers), t0 = hh * per_head + __ldcg(cum + b), t1 = hh * per_head + __ldcg(cum + b + 1);
+        const int64_t w0 = kv4_worker(t0, T_all, W), first = w0 + hh * a.B + b;
+        const int n = (int)(kv4_worker(t1 - 1, T_all, W) - w0) + 1;
+        const float *lse = ws + p.lse + first * p.g_rows + x, *v = ws + p.o + (first * p.g_rows + x) * D + c4 * 4;
+        for (int s0 = way * AT_ONCE; s0 < n; s0 += WAYS * AT_ONCE) {   // results are fetched several at a time: the chain of loads is what takes time
+            float e[AT_ONCE];
+            float4 y[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                e[u] = -INFINITY;
+                if (s0 + u < n) {
+                    e[u] = __ldcg(lse + (int64_t)(s0 + u) * p.g_rows);
+                    y[u] = __ldcg(reinterpret_cast<const float4*>(v + (int64_t)(s0 + u) * p.g_rows * D));
+                }
+            }
+            float top = M;
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) top = fmaxf(top, e[u]);
+            const float keep = M == -INFINITY ? 1.f : exp2f(M - top);   // no weight yet, or NaN, which stays
+            M = top;
+            total *= keep;
+            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                if (e[u] == -INFINITY) continue;   // no weight: past the last, or scores of -inf (values 0/0)
+                const float f = exp2f(e[u] - top);
+                total += f;
+                o.x = fmaf(f, y[u].x, o.x); o.y = fmaf(f, y[u].y, o.y); o.z = fmaf(f, y[u].z, o.z); o.w = fmaf(f, y[u].w, o.w);
+            }
+        }
+    }
+    if constexpr (WAYS > 1) {
+        __shared__ float s_m[KV4_MERGE_THREADS], s_t[KV4_MERGE_THREADS];
+        __shared__ float4 s_o[KV4_MERGE_THREADS];
+        s_m[threadIdx.x] = M;
+        s_t[threadIdx.x] = total;
+        s_o[threadIdx.x] = o;
+        __syncthreads();
+        if (way > 0) return;
+        for (int y = 1; y < WAYS; ++y) M = fmaxf(M, s_m[threadIdx.x + y * LANES]);
+        total = 0.f;
+        o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int y = 0; y < WAYS; ++y) {
+            const int at = threadIdx.x + y * LANES;
+            if (s_t[at] == 0.f) continue;   // took no result, or only ones without weight (one of NaN alone has a total of NaN)
+            const float f = exp2f(s_m[at] - M);
+            total += f * s_t[at];
+            o.x = fmaf(f, s_o[at].x, o.x); o.y = fmaf(f, s_o[at].y, o.y); o.z = fmaf(f, s_o[at].z, o.z); o.w = fmaf(f, s_o[at].w, o.w);
+        }
+    }
+    if (!live) return;
+    const float inv = 1.f / total;
+    T* out = static_cast<T*>(a.o) + row * D + c4 * 4;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    else *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (a.lse && c4 == 0) a.lse[row] = (M + log2f(total)) * 0.6931471805599453f;
+}
+
+// ------------------------------------------------------------------ host side
+// both kernels' cuts, array by array, so that a buffer made for the largest call serves the smaller ones
+size_t decode_kv4_workspace_bytes(int B, int Hq, int Hkv, int D, int max_mem, int max_tail) {
+    (void)max_mem; (void)max_tail;   // the cut goes by workers, not by lengths
+    int64_t rows = 0;
+    for (bool cuda_cores : {false, true}) {
+        const Kv4Plan p = make_kv4_plan(B, Hq, Hkv, D, cuda_cores);
+        rows = std::max(rows, (p.workers + (int64_t)B * Hkv * p.g_tiles) * p.g_rows);
+    }
+    int64_t n = 0;
+    for (int64_t x : {rows * D, rows, 2 * ((int64_t)B + 1)}) n += (x + 63) / 64 * 64;
+    return (size_t)n * sizeof(float);
+}
+
+template <typename T, int D>
+static cudaError_t merge(const Kv4DecodeArgs& a, const Kv4Plan& p, cudaStream_t st) {
+    const int64_t rows = (int64_t)a.B * a.Hq;
+    constexpr int SETS = KV4_MERGE_THREADS / (D / 4);
+    const unsigned grid = (unsigned)((rows * SETS + SETS - 1) / SETS);
+    return launch_behind(kv4_merge_kernel<T, D, SETS>, dim3(grid), KV4_MERGE_THREADS, 0, st, true, a, p);
+}
+
+template <typename T, int D>
+static cudaError_t stream(const Kv4DecodeArgs& a, cudaStream_t st) {
+    const Kv4Plan p = make_kv4_plan(a.B, a.Hq, a.Hkv, D, true);
+    auto* kernel = p.g_rows == 1 ? kv4_stream_kernel<T, D, 1> : p.g_rows == 2 ? kv4_stream_kernel<T, D, 2> : kv4_stream_kernel<T, D, 4>;
+    const cudaError_t e = launch_behind(kernel, dim3(p.ctas), KV4_WARPS * 32, 0, st, false, a, p);
+    return e == cudaSuccess ? merge<T, D>(a, p, st) : e;
+}
+
+cudaError_t launch_decode_kv4(const Kv4DecodeArgs& a, int D, loma_dtype dt, bool generic, cudaStream_t st) {
+    (void)generic;
+    if (dt == LOMA_F32) return D == 64 ? stream<float, 64>(a, st) : stream<float, 128>(a, st);
+    return D == 64 ? stream<__nv_bfloat16, 64>(a, st) : stream<__nv_bfloat16, 128>(a, st);
+}
+
+}  // namespace loma

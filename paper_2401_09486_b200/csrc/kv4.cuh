@@ -1,0 +1,107 @@
+// Memory entries held in 4 bits: the format, and what its kernels have in common.
+//
+// 32 consecutive features of a row share a step h = bf16(fp32(max |x| / 15)); a value is held as its sign and m = 0 .. 7, the number of
+// k in 1 .. 7 with |x| >= 2 h k, and stands for +-(2 m + 1) h: sixteen evenly spaced values around zero, the outermost of which
+// is the group's largest.  Thresholds 2 h k are exact in fp32, so is 2 m + 1 times h, and nothing is rounded but h.  A step below 2^-126
+// is stored as 0 (all values 0), one that is no number as NaN (all values NaN).
+//
+// A pool is [n_pages][Hkv][page_size / 16] tiles of 16 entries.  A tile holds, for its 16 rows, the keys' bits, the values' bits, the
+// keys' steps, the values' steps, one behind the other, so one copy fetches it: 2304 bytes for D = 128 (in bf16: 8192).
+//
+// A row's bits are laid out for warp-level m16n8k16 products.  Feature 32 g + 4 x + e (group g, x = 0 .. 7, e = 0 .. 3) lies in
+// chunk x, half-word g, a half-word's 16 bits being
+//     m0 m1 s2 s3 | m2 m3 s0 s1        (3 3 1 1 | 3 3 1 1 bits, lowest first; s: sign)
+// With the half-word itself (e = 1), doubled (e = 0), and the same with its bytes exchanged (e = 3, 2), sign and m stand where one
+// AND and one OR make them the bf16 pattern of +-(2 m + 1) 2^-133 (times 4 for odd e): a number below the normal range, which the
+// products take as it is, so turning 4 bits into operands takes two instructions a pair and adds no offset that would have to be
+// taken off again.  Powers of two bring the sums back (see decode_kv4.cu).
+// Chunk x of row k lies at x ^ (4 if k & 4), which spreads the reads of a tile in shared memory over its banks.
+#pragma once
+
+#include <algorithm>
+
+#include "loma_internal.cuh"
+
+namespace loma {
+
+constexpr int KV4_ROWS = 16;    // entries to a tile
+constexpr int KV4_GROUP = 32;   // features that share a step
+
+template <int D>
+struct Kv4Tile {
+    static constexpr int GROUPS = D / KV4_GROUP;
+    static constexpr int CHUNK = D / 16;                         // bytes: a half-word per group
+    static constexpr int ROW = D / 2, STEPS = GROUPS * 2;        // bytes of a row's bits and of its steps
+    static constexpr int V = KV4_ROWS * ROW, K_STEPS = 2 * V, V_STEPS = K_STEPS + KV4_ROWS * STEPS;   // where they begin
+    static constexpr int BYTES = V_STEPS + KV4_ROWS * STEPS;
+};
+
+inline int64_t kv4_tile_bytes(int D) { return D == 64 ? Kv4Tile<64>::BYTES : Kv4Tile<128>::BYTES; }
+
+// the 4-bit memory of a batch
+struct Kv4Pool {
+    uint8_t* pool = nullptr;
+    const int32_t* table = nullptr;   // [B, max_pages]
+    int max_pages = 0, log2_ps = 0, n_pages = 0;
+};
+
+struct Kv4AppendArgs {
+    Kv4Pool m;
+    const void *k = nullptr, *v = nullptr;
+    int64_t k_stride[3] = {0, 0, 0}, v_stride[3] = {0, 0, 0};   // batch, head, row, in elements
+    const int32_t *mem_lens = nullptr, *new_lens = nullptr;
+    int B = 0, Hkv = 0, l = 0;
+};
+struct Kv4LoadArgs {
+    Kv4Pool m;
+    void *k = nullptr, *v = nullptr;   // [B, Hkv, cap, D]
+    const int32_t* mem_lens = nullptr;
+    int B = 0, Hkv = 0, cap = 0;
+};
+cudaError_t launch_kv4_append(const Kv4AppendArgs& a, int D, loma_dtype dt, cudaStream_t st);   // kv4_store.cu
+cudaError_t launch_kv4_load(const Kv4LoadArgs& a, int D, loma_dtype dt, cudaStream_t st);
+
+struct Kv4DecodeArgs {
+    Kv4Pool m;
+    const void *q = nullptr, *k_new = nullptr, *v_new = nullptr;   // [B, Hq, D], [B, Hkv, D]; k_new, v_new may be NULL
+    void *k_tail = nullptr, *v_tail = nullptr;                     // [B, Hkv, cap, D]
+    void* o = nullptr;                                             // [B, Hq, D]
+    float* lse = nullptr;                                          // [B, Hq] or NULL
+    const int32_t *mem_lens = nullptr, *tail_lens = nullptr;       // [B]; tail_lens negative: no request, nothing is written
+    int B = 0, Hq = 0, Hkv = 0, g = 0;
+    int max_mem = 0, max_tail = 0, cap = 0;
+    float scale = 0.f;
+    void* ws = nullptr;
+};
+size_t decode_kv4_workspace_bytes(int B, int Hq, int Hkv, int D, int max_mem, int max_tail);   // decode_kv4.cu
+cudaError_t launch_decode_kv4(const Kv4DecodeArgs& a, int D, loma_dtype dt, bool generic, cudaStream_t st);
+
+#ifdef __CUDACC__
+// page of block `block` of sequence b, or -1 where the table names none in the pool
+__device__ __forceinline__ int kv4_page(const Kv4Pool& m, int b, int block) {
+    const int page = __ldg(m.table + (int64_t)b * m.max_pages + block);
+    return page >= 0 && page < m.n_pages ? page : -1;
+}
+// where the tile of entry j of (page, h) begins
+template <int D>
+__device__ __forceinline__ int64_t kv4_tile(const Kv4Pool& m, int Hkv, int page, int h, int j) {
+    const int tiles = 1 << (m.log2_ps - 4), t = (j & ((1 << m.log2_ps) - 1)) >> 4;
+    return (((int64_t)page * Hkv + h) * tiles + t) * Kv4Tile<D>::BYTES;
+}
+// byte offset of chunk x of row k among a tile's bits of keys (or of values)
+template <int D>
+__device__ __forceinline__ int kv4_chunk(int k, int x) { return k * Kv4Tile<D>::ROW + (x ^ (k & 4)) * Kv4Tile<D>::CHUNK; }
+
+// A and B: half-words of two chunks (two rows, or two chunks of a row), group by group.  Out: the pair's four elements e as bf16 pairs
+// (A low, B high), +-(2 m + 1) 2^-133, times 4 for odd e.  `hi`: the upper half-words of the words.
+template <bool HI>
+__device__ __forceinline__ void kv4_pairs(uint32_t a, uint32_t b, uint32_t (&p)[4]) {
+    const uint32_t u = __byte_perm(a, b, HI ? 0x7632 : 0x5410), w = __byte_perm(a, b, HI ? 0x6723 : 0x4501);
+    p[0] = ((u << 1) & 0x800E800Eu) | 0x00010001u;
+    p[1] = (u & 0x80388038u) | 0x00040004u;
+    p[2] = ((w << 1) & 0x800E800Eu) | 0x00010001u;
+    p[3] = (w & 0x80388038u) | 0x00040004u;
+}
+#endif
+
+}  // namespace loma

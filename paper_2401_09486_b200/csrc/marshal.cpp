@@ -12,6 +12,7 @@
 #include <cstdint>
 #include <stdexcept>
 #include <string>
+#include <vector>
 
 #include "loma.h"
 
@@ -23,6 +24,14 @@ decltype(&loma_qk_norm_rope_bwd) p_norm_bwd;
 decltype(&loma_qk_norm_rope_append) p_append;
 decltype(&loma_decode_attn_shared) p_shared;
 decltype(&loma_decode_attn_shared_paged) p_shared_paged;
+decltype(&loma_paged_release) p_release;
+decltype(&loma_paged_fork) p_fork;
+decltype(&loma_paged_compact) p_compact;
+decltype(&loma_paged_copy) p_copy;
+decltype(&loma_kv4_page_bytes) p_page_bytes;
+decltype(&loma_kv4_append) p_kv4_append;
+decltype(&loma_kv4_load) p_kv4_load;
+decltype(&loma_decode_attn_kv4) p_kv4_decode;
 
 struct Refused : std::runtime_error {   // becomes a ValueError
     using std::runtime_error::runtime_error;
@@ -384,14 +393,220 @@ PyObject* decode_attn_shared_paged(PyObject*, PyObject* const* args, Py_ssize_t 
     });
 }
 
-// Addresses of the six entry points, in the order of their declarations above.
+// What the page bookkeeping calls share: the free list and the table.
+struct PagesCall {
+    int64_t B, M;
+    int n_pages, n_free;
+    int32_t *refs, *free_pages, *taken, *counts;
+
+    PagesCall(Args& a, const at::Tensor& lead, const at::Tensor& table, const at::Tensor& r, const at::Tensor& fp, const at::Tensor& tk, const at::Tensor& ct) {
+        a.device_of(lead, true);
+        B = lead.numel();
+        if (table.dim() != 2 || table.size(0) != B) a.no("block_table must be [B, max_pages]");
+        M = table.size(1);
+        if (B >= INT32_MAX || M > INT32_MAX || r.numel() > INT32_MAX || fp.numel() > INT32_MAX) a.no("too many entries");
+        n_pages = (int)r.numel();
+        n_free = (int)fp.numel();
+        refs = a.words("refs", &r, -1);
+        free_pages = a.words("free_pages", &fp, -1);
+        taken = a.words("taken", &tk, 1);
+        counts = a.words("counts", &ct, 4);
+    }
+};
+
+PyObject* paged_release(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&] {
+        Args a("loma_paged_release", args, n, 10);
+        const at::Tensor &keep = *a.tensor("keep_lens"), &held = *a.tensor("held"), &table = *a.tensor("block_table");
+        const int page_size = a.i32();
+        const at::Tensor &held_out = *a.tensor("held_out"), &refs = *a.tensor("refs"), &fp = *a.tensor("free_pages"), &tk = *a.tensor("taken"),
+                         &ct = *a.tensor("counts");
+        const PagesCall f(a, keep, table, refs, fp, tk, ct);
+        int32_t *p0 = a.words("keep_lens", &keep, f.B), *p1 = a.words("held", &held, f.B), *p2 = a.words("block_table", &table, -1),
+                *p3 = a.words("held_out", &held_out, f.B);
+        void* stream = a.stream();
+        return unlocked([&] {
+            return p_release((int)f.B, page_size, (int)f.M, f.n_pages, f.n_free, p0, p1, p2, p3, f.refs, f.free_pages, f.taken, f.counts, a.dev >= 0, stream);
+        });
+    });
+}
+
+PyObject* paged_fork(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&] {
+        Args a("loma_paged_fork", args, n, 17);
+        const at::Tensor &parents = *a.tensor("parents"), &lens = *a.tensor("cache_lens"), *fixed = a.tensor("fixed_lens", true), *held = a.tensor("held", true),
+                         &table = *a.tensor("block_table");
+        const int page_size = a.i32();
+        const at::Tensor &table_out = *a.tensor("table_out"), &lens_out = *a.tensor("lens_out"), &held_out = *a.tensor("held_out"), &refs = *a.tensor("refs"),
+                         &fp = *a.tensor("free_pages"), &tk = *a.tensor("taken"), &src = *a.tensor("copy_src"), &dst = *a.tensor("copy_dst"),
+                         &ct = *a.tensor("counts"), *ws = a.tensor("workspace", true);
+        const PagesCall f(a, parents, table, refs, fp, tk, ct);
+        if (src.numel() > INT32_MAX) a.no("too many entries");
+        int32_t *p0 = a.words("parents", &parents, f.B), *p1 = a.words("cache_lens", &lens, f.B), *p2 = a.words("fixed_lens", fixed, f.B),
+                *p3 = a.words("held", held, f.B), *p4 = a.words("block_table", &table, -1), *p5 = a.words("table_out", &table_out, f.B * f.M),
+                *p6 = a.words("lens_out", &lens_out, f.B), *p7 = a.words("held_out", &held_out, f.B), *p8 = a.words("copy_src", &src, -1),
+                *p9 = a.words("copy_dst", &dst, src.numel());
+        size_t bytes;
+        void *pws = a.scratch(ws, &bytes), *stream = a.stream();
+        return unlocked([&] {
+            return p_fork((int)f.B, page_size, (int)f.M, f.n_pages, f.n_free, (int)src.numel(), p0, p1, p2, p3, p4, p5, p6, p7, f.refs, f.free_pages, f.taken,
+                          p8, p9, f.counts, pws, bytes, a.dev >= 0, stream);
+        });
+    });
+}
+
+PyObject* paged_compact(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&] {
+        Args a("loma_paged_compact", args, n, 10);
+        const at::Tensor &held = *a.tensor("held"), &table = *a.tensor("block_table"), &refs = *a.tensor("refs"), &fp = *a.tensor("free_pages"),
+                         &tk = *a.tensor("taken"), &map = *a.tensor("page_map"), &src = *a.tensor("copy_src"), &dst = *a.tensor("copy_dst"),
+                         &ct = *a.tensor("counts");
+        const PagesCall f(a, held, table, refs, fp, tk, ct);
+        if (src.numel() > INT32_MAX) a.no("too many entries");
+        int32_t *p0 = a.words("held", &held, f.B), *p1 = a.words("block_table", &table, -1), *p2 = a.words("page_map", &map, f.n_pages),
+                *p3 = a.words("copy_src", &src, -1), *p4 = a.words("copy_dst", &dst, src.numel());
+        void* stream = a.stream();
+        return unlocked([&] {
+            return p_compact((int)f.B, (int)f.M, f.n_pages, f.n_free, (int)src.numel(), p0, p1, f.refs, f.free_pages, f.taken, p2, p3, p4, f.counts,
+                             a.dev >= 0, stream);
+        });
+    });
+}
+
+PyObject* paged_copy(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&] {
+        Args a("loma_paged_copy", args, n, 5);
+        PyObject* list = a.v[a.at++];
+        if (!PyList_Check(list) && !PyTuple_Check(list)) a.no("pools must be a list of tensors");
+        const at::Tensor &src = *a.tensor("copy_src"), &dst = *a.tensor("copy_dst"), &count = *a.tensor("n_copies");
+        a.device_of(src);
+        std::vector<void*> pools;
+        std::vector<int64_t> bytes;
+        int64_t pages = 0;
+        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(list); ++i) {
+            PyObject* o = PySequence_Fast_GET_ITEM(list, i);
+            if (!THPVariable_Check(o)) a.no("pools must be a list of tensors");
+            const at::Tensor& t = THPVariable_Unpack(o);
+            a.here("a pool", t);
+            if (t.dim() < 1 || !t.is_contiguous()) a.no("pools must be contiguous tensors [n_pages, ...]");
+            if (i > 0 && t.size(0) != pages) a.no("pools must have the same number of pages");
+            pages = t.size(0);
+            if (pages == 0 || t.numel() == 0) continue;
+            pools.push_back(t.data_ptr());
+            bytes.push_back((int64_t)(t.nbytes() / pages));
+        }
+        if (pages > INT32_MAX || pools.size() > INT32_MAX || src.numel() > INT32_MAX) a.no("too many entries");
+        int32_t *p0 = a.words("copy_src", &src, -1), *p1 = a.words("copy_dst", &dst, src.numel()), *p2 = a.words("n_copies", &count, 1);
+        void* stream = a.stream();
+        return unlocked([&] { return p_copy((int)pools.size(), pools.data(), bytes.data(), (int)pages, p0, p1, p2, (int)src.numel(), stream); });
+    });
+}
+
+// A pool of memory entries in 4 bits and the table behind which it lies.
+struct Kv4Call {
+    int page_size, pages = 0, M = 0;
+    void* pool = nullptr;
+    int32_t* table = nullptr;
+
+    Kv4Call(const Args& a, const at::Tensor* p, const at::Tensor* t, int ps, int64_t B, int64_t Hkv, int64_t D) : page_size(ps) {
+        if (B > INT32_MAX || Hkv > INT32_MAX || D > INT32_MAX) a.no("tensors too large");
+        if (t) {
+            if (t->dim() != 2 || t->size(0) != B || t->size(1) > INT32_MAX) a.no("block_table must be [B, max_pages]");
+            M = (int)t->size(1);
+            table = a.words("block_table", t, -1);
+        }
+        if (p) {
+            const int64_t want = (int64_t)p_page_bytes((int)Hkv, (int)D, ps);
+            if (p->dim() != 2 || p->size(0) > INT32_MAX) a.no("kv_pool must be [n_pages, page_bytes]");
+            pages = (int)p->size(0);
+            pool = want > 0 ? a.dense("kv_pool", p, {pages, want}, at::kByte) : p->data_ptr();   // no size: the entry point refuses the call
+        }
+    }
+};
+
+PyObject* kv4_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&] {
+        Args a("loma_kv4_append", args, n, 8);
+        const at::Tensor &k = *a.tensor("k"), &v = *a.tensor("v"), &pool = *a.tensor("kv_pool"), &table = *a.tensor("block_table");
+        const int ps = a.i32();
+        const at::Tensor &lens = *a.tensor("mem_lens"), *fresh = a.tensor("new_lens", true);
+        if (k.dim() != 4 || v.dim() != 4 || k.sizes() != v.sizes() || k.scalar_type() != v.scalar_type()) a.no("k and v must be [B, Hkv, l, D] of one dtype");
+        if (k.numel() && (k.stride(3) != 1 || v.stride(3) != 1)) a.no("head dimension must be contiguous");
+        a.device_of(k);
+        a.here("v", v);
+        const loma_dtype dt = a.dtype(k);
+        const Kv4Call f(a, &pool, &table, ps, k.size(0), k.size(1), k.size(3));
+        if (k.size(2) > INT32_MAX) a.no("tensors too large");
+        int32_t *p0 = a.words("mem_lens", &lens, k.size(0)), *p1 = a.words("new_lens", fresh, k.size(0));
+        void* stream = a.stream();
+        int64_t ks[3], vs[3];
+        strides_of(k, 3, ks);
+        strides_of(v, 3, vs);
+        return unlocked([&] {
+            return p_kv4_append(k.data_ptr(), v.data_ptr(), f.pool, f.table, p0, p1, (int)k.size(0), (int)k.size(1), (int)k.size(3), (int)k.size(2), ps, f.M,
+                                f.pages, ks, vs, dt, stream);
+        });
+    });
+}
+
+PyObject* kv4_load(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&] {
+        Args a("loma_kv4_load", args, n, 7);
+        const at::Tensor &pool = *a.tensor("kv_pool"), &table = *a.tensor("block_table");
+        const int ps = a.i32();
+        const at::Tensor &lens = *a.tensor("mem_lens"), &k = *a.tensor("k_cache"), &v = *a.tensor("v_cache");
+        if (k.dim() != 4) a.no("k_cache must be [B, Hkv, cap, D]");
+        a.device_of(k);
+        const loma_dtype dt = a.dtype(k);
+        void *pk = a.dense("k_cache", &k, k.sizes(), k.scalar_type()), *pv = a.dense("v_cache", &v, k.sizes(), k.scalar_type());
+        const Kv4Call f(a, &pool, &table, ps, k.size(0), k.size(1), k.size(3));
+        if (k.size(2) > INT32_MAX) a.no("tensors too large");
+        int32_t* p0 = a.words("mem_lens", &lens, k.size(0));
+        void* stream = a.stream();
+        return unlocked([&] {
+            return p_kv4_load(f.pool, f.table, p0, pk, pv, (int)k.size(0), (int)k.size(1), (int)k.size(3), (int)k.size(2), ps, f.M, f.pages, dt, stream);
+        });
+    });
+}
+
+PyObject* decode_attn_kv4(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+    return guarded([&] {
+        Args a("loma_decode_attn_kv4", args, n_args, 18);
+        const at::Tensor &q = *a.tensor("q"), *kn = a.tensor("k_new", true), *vn = a.tensor("v_new", true), &kt = *a.tensor("k_tail"), &vt = *a.tensor("v_tail"),
+                         &tails = *a.tensor("tail_lens");
+        const int max_tail = a.i32();
+        const at::Tensor *pool = a.tensor("kv_pool", true), *table = a.tensor("block_table", true);
+        const int ps = a.i32();
+        const at::Tensor& lens = *a.tensor("mem_lens");
+        const int max_mem = a.i32();
+        const at::Tensor &o = *a.tensor("o"), *lse = a.tensor("lse", true), *ws = a.tensor("workspace", true);
+        const unsigned flags = (unsigned)a.integer();
+        const float scale = a.number();
+        if (kt.dim() != 4) a.no("k_tail must be [B, Hkv, cap, D]");
+        const SharedCall f(a, q, kn, vn, o, lse, tails, kt.size(1), ws);
+        if (kt.size(2) > INT32_MAX) a.no("tensors too large");
+        const auto ty = q.scalar_type();
+        void *pkt = a.dense("k_tail", &kt, {f.B, f.Hkv, kt.size(2), f.D}, ty), *pvt = a.dense("v_tail", &vt, {f.B, f.Hkv, kt.size(2), f.D}, ty);
+        const Kv4Call m(a, pool, table, ps, f.B, f.Hkv, f.D);
+        int32_t* plens = a.words("mem_lens", &lens, f.B);
+        a.device_of(q);
+        void* stream = a.stream();
+        return unlocked([&] {
+            return p_kv4_decode(q.data_ptr(), f.pkn, f.pvn, pkt, pvt, m.pool, m.table, f.po, f.plse, f.B, f.Hq, f.Hkv, f.D, (int)kt.size(2), f.plens, max_tail,
+                                ps, m.M, m.pages, plens, max_mem, f.dt, scale, flags, f.ws, f.ws_bytes, stream);
+        });
+    });
+}
+
+// Addresses of the entry points, in the order of their declarations above.
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    void* p[6];
-    if (n != 6) {
-        PyErr_SetString(PyExc_ValueError, "bind takes six addresses");
+    constexpr int N = 14;
+    void* p[N];
+    if (n != N) {
+        PyErr_SetString(PyExc_ValueError, "bind takes fourteen addresses");
         return nullptr;
     }
-    for (int i = 0; i < 6; ++i) {
+    for (int i = 0; i < N; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: an address is zero");
@@ -404,6 +619,14 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     p_append = reinterpret_cast<decltype(p_append)>(p[3]);
     p_shared = reinterpret_cast<decltype(p_shared)>(p[4]);
     p_shared_paged = reinterpret_cast<decltype(p_shared_paged)>(p[5]);
+    p_release = reinterpret_cast<decltype(p_release)>(p[6]);
+    p_fork = reinterpret_cast<decltype(p_fork)>(p[7]);
+    p_compact = reinterpret_cast<decltype(p_compact)>(p[8]);
+    p_copy = reinterpret_cast<decltype(p_copy)>(p[9]);
+    p_page_bytes = reinterpret_cast<decltype(p_page_bytes)>(p[10]);
+    p_kv4_append = reinterpret_cast<decltype(p_kv4_append)>(p[11]);
+    p_kv4_load = reinterpret_cast<decltype(p_kv4_load)>(p[12]);
+    p_kv4_decode = reinterpret_cast<decltype(p_kv4_decode)>(p[13]);
     Py_RETURN_NONE;
 }
 
@@ -415,6 +638,13 @@ PyMethodDef methods[] = {
     {"qk_norm_rope_append", (PyCFunction)(void (*)())qk_norm_rope_append, METH_FASTCALL, "loma_qk_norm_rope_append"},
     {"decode_attn_shared", (PyCFunction)(void (*)())decode_attn_shared, METH_FASTCALL, "loma_decode_attn_shared"},
     {"decode_attn_shared_paged", (PyCFunction)(void (*)())decode_attn_shared_paged, METH_FASTCALL, "loma_decode_attn_shared_paged"},
+    {"paged_release", (PyCFunction)(void (*)())paged_release, METH_FASTCALL, "loma_paged_release"},
+    {"paged_fork", (PyCFunction)(void (*)())paged_fork, METH_FASTCALL, "loma_paged_fork"},
+    {"paged_compact", (PyCFunction)(void (*)())paged_compact, METH_FASTCALL, "loma_paged_compact"},
+    {"paged_copy", (PyCFunction)(void (*)())paged_copy, METH_FASTCALL, "loma_paged_copy"},
+    {"kv4_append", (PyCFunction)(void (*)())kv4_append, METH_FASTCALL, "loma_kv4_append"},
+    {"kv4_load", (PyCFunction)(void (*)())kv4_load, METH_FASTCALL, "loma_kv4_load"},
+    {"decode_attn_kv4", (PyCFunction)(void (*)())decode_attn_kv4, METH_FASTCALL, "loma_decode_attn_kv4"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling for libloma", -1, methods, nullptr, nullptr, nullptr, nullptr};
