@@ -274,6 +274,399 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
     }
 }
 
+// ------------------------------------------------------------------ tensor cores
+// A worker streams its tiles through a ring of its own in shared memory: one bulk copy per tile, NS - 1 tiles ahead and across the
+// borders between sequences.  The g query heads of a kv head share every row: with 16 entries as the rows and 8 heads as the
+// columns of m16n8k16 products,
+//     S^T [entries x heads] = K Q^T          O^T [features x heads] += V^T P^T
+// A group's step is the same for all entries of a column of K Q^T only within a row, so each group's product (two k-steps) goes
+// to an accumulator of its own and into the scores times the row's step; for V the step goes into the weights, so P^T is
+// rounded once per group.  P^T changes from the accumulator's layout to the operand's with 8 x 8 transposes (movmatrix).
+//
+// Powers of two: a tile's numbers are n 2^-133 (n odd, up to 15; times 4 for odd e, see kv4.cuh).  Queries carry 2^64 (2^62 against
+// odd e), weights 2^80, so sums stay in the normal range: scores come out times 2^-69, outputs times 2^-53 (2^-51).  The factors
+// are exact and are taken off where memory ends and the tail begins (to_plain), or with the partial result.
+//
+// Row r of the scores is entry pi(r) = r ^ (r >> 1 & 1): with the chunks' places that spreads the four rows whose values a lane
+// needs over the banks of shared memory (D = 128: no conflict).
+constexpr float KV4_Q = 18446744073709551616.f;                    // 2^64
+constexpr float KV4_S = 590295810358705651712.f;                   // 2^69
+constexpr float KV4_O = 9007199254740992.f;                        // 2^53
+constexpr float KV4_P_LOG2 = 80.f, KV4_P_INV = 8.271806125530277e-25f;   // 2^-80
+
+template <int D>
+struct Kv4Ring {
+    static constexpr int NS = D == 128 ? 5 : 10, WARP = NS * Kv4Tile<D>::BYTES, TOTAL = KV4_WARPS * WARP;
+};
+
+__device__ __forceinline__ void mma_acc(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+// G half-words of eight or four bytes as floats (bf16 bits)
+template <int G>
+__device__ __forceinline__ void steps_of(const uint8_t* p, float (&h)[G]) {
+    if constexpr (G == 4) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        h[0] = bf16lo(u.x); h[1] = bf16hi(u.x); h[2] = bf16lo(u.y); h[3] = bf16hi(u.y);
+    } else {
+        const uint32_t u = *reinterpret_cast<const uint32_t*>(p);
+        h[0] = bf16lo(u); h[1] = bf16hi(u);
+    }
+}
+// the words of two neighbouring chunks: w[chunk][i] holds groups 2 i and 2 i + 1
+template <int G>
+__device__ __forceinline__ void chunk_pair(const uint8_t* p, uint32_t (&w)[2][G / 2]) {
+    if constexpr (G == 4) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        w[0][0] = u.x; w[0][1] = u.y; w[1][0] = u.z; w[1][1] = u.w;
+    } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        w[0][0] = u.x; w[1][0] = u.y;
+    }
+}
+template <int G>
+__device__ __forceinline__ void one_chunk(const uint8_t* p, uint32_t (&w)[G / 2]) {
+    if constexpr (G == 4) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        w[0] = u.x; w[1] = u.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+}
+__device__ __forceinline__ void group_pairs(int g, uint32_t a, uint32_t b, uint32_t (&p)[4]) {
+    if (g & 1) kv4_pairs<true>(a, b, p); else kv4_pairs<false>(a, b, p);
+}
+
+// R: column tiles of 8 query heads
+template <int D, int R>
+__global__ void __launch_bounds__(KV4_WARPS * 32, R == 1 ? 4 : 2)
+kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
+    using TL = Kv4Tile<D>;
+    constexpr int G = TL::GROUPS, NS = Kv4Ring<D>::NS;
+    extern __shared__ __align__(128) uint8_t kv4_smem[];
+    __shared__ __align__(8) uint64_t bars[KV4_WARPS][NS];
+    __shared__ int64_t scan[Kv4Blocks::MAX_GROUPS + 1];
+    __shared__ int64_t wsum[KV4_WARPS];
+    __shared__ int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
+    float* ws = static_cast<float*>(a.ws);
+    if (lane == 0)
+        for (int i = 0; i < NS; ++i) mbar_init(smem_u32(&bars[warp][i]), 1);
+    if (threadIdx.x == 0) abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    let_next_start();
+    const Kv4Blocks kb{a};
+    const int per = kb.scan(scan, wsum, blockIdx.x == 0 ? reinterpret_cast<int64_t*>(ws + p.cum) : nullptr);
+    const int64_t T = scan[(a.B + per - 1) / per] * a.Hkv * p.g_tiles, W = min(T, (int64_t)p.workers);
+    const int64_t w = (int64_t)warp * gridDim.x + blockIdx.x;   // neighbours on different SMs
+    if (w >= W) return;
+    int left = (int)(kv4_first(w + 1, T, W) - kv4_first(w, T, W)), left_f = left;   // blocks of the share still to come, and still to be fetched
+    Kv4Blocks::Cursor c = kb.find(kv4_first(w, T, W), scan, per), f = c;
+
+    // the fetch cursor stands on the next tile to fetch; the table entry of a tile is read one tile before it is used
+    const uint8_t* src = nullptr;
+    auto seek = [&]() {   // past tail blocks
+        while (left_f > 0 && f.blk >= f.s.nm) {
+            left_f -= f.s.n - f.blk;
+            if (left_f > 0) kb.next_unit(f);
+        }
+        if (left_f > 0) src = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, f.b, f.blk * KV4_ROWS), p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles, f.blk * KV4_ROWS);
+    };
+    uint8_t* ring = kv4_smem + warp * Kv4Ring<D>::WARP;
+    int slot_f = 0;
+    auto fetch = [&]() {
+        if (lane == 0) {
+            const uint32_t bar = smem_u32(&bars[warp][slot_f]);
+            mbar_expect_tx(bar, TL::BYTES);
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(ring + slot_f * TL::BYTES)),
+                         "l"(src), "r"(TL::BYTES), "r"(bar)
+                         : "memory");
+        }
+        slot_f = slot_f + 1 == NS ? 0 : slot_f + 1;
+        ++f.blk;
+        --left_f;
+        seek();
+    };
+    seek();
+    for (int i = 0; i < NS && left_f > 0; ++i) fetch();
+
+    const float sc_tail = a.scale * 1.4426950408889634f, sc_mem = sc_tail * KV4_S;
+    const int pr = r ^ (r >> 1 & 1), pv0 = 2 * j ^ (j & 1), pv1 = pv0 ^ 1;   // entries of this lane's rows of scores, and of its pairs of values
+    const int k_at = pr * TL::ROW + (j ^ ((r & 4) >> 1)) * 2 * TL::CHUNK, v_x = (r ^ (j & 2) << 1) * TL::CHUNK;
+    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
+    uint32_t qf[R][2 * G][2];                    // operand B: column = head x * 8 + r
+    float m[R][2], ref[R][2], l[R][2];           // heads x * 8 + 2j, + 1.  m: the reference as a raw product; ref: what exponents are taken off
+    float acc[R][2 * G][4];
+    int slot = 0, h = 0, gt = 0, heads = 0;
+    uint32_t phase = 0;
+    bool fresh = true, plain = false, ok = true;
+
+    auto load_q = [&](float even, float odd) {
+#pragma unroll
+        for (int x = 0; x < R; ++x) {
+            const int hd = x * 8 + r;
+            const __nv_bfloat16* row = q + ((int64_t)c.b * a.Hq + h * a.g + gt * p.g_rows + min(hd, heads - 1)) * D + 8 * j;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                uint4 u = __ldg(reinterpret_cast<const uint4*>(row + 32 * g));
+                if (hd >= heads) u = make_uint4(0, 0, 0, 0);
+                const uint32_t e0 = __byte_perm(u.x, u.z, 0x5410), e1 = __byte_perm(u.x, u.z, 0x7632), e2 = __byte_perm(u.y, u.w, 0x5410),
+                               e3 = __byte_perm(u.y, u.w, 0x7632);
+                qf[x][2 * g][0] = pack_bf16(bf16lo(e0) * even, bf16hi(e0) * even);
+                qf[x][2 * g][1] = pack_bf16(bf16lo(e1) * odd, bf16hi(e1) * odd);
+                qf[x][2 * g + 1][0] = pack_bf16(bf16lo(e2) * even, bf16hi(e2) * even);
+                qf[x][2 * g + 1][1] = pack_bf16(bf16lo(e3) * odd, bf16hi(e3) * odd);
+            }
+        }
+    };
+    auto to_plain = [&]() {
+#pragma unroll
+        for (int x = 0; x < R; ++x) {
+#pragma unroll
+            for (int i = 0; i < 2 * G; ++i) {
+                acc[x][i][0] *= KV4_O; acc[x][i][1] *= KV4_O;
+                acc[x][i][2] *= KV4_O / 4; acc[x][i][3] *= KV4_O / 4;
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                l[x][y] *= KV4_P_INV;
+                m[x][y] *= KV4_S;
+                ref[x][y] += KV4_P_LOG2;
+            }
+        }
+        plain = true;
+    };
+    // z: raw products of rows pr (0, 1) and pr + 8 (2, 3), heads 2j, 2j + 1 (-inf: no weight) -> weights 2^(z sc - ref)
+    auto weights = [&](int x, float (&z)[4], float sc, float off) {
+        float m0 = fmaxf(z[0], z[2]), m1 = fmaxf(z[1], z[3]);
+        const float grow = 8.f / sc;
+        // the reference moves only when a head's maximum has grown by more than 2^8 (weights stay below 2^8)
+        if (__any_sync(0xffffffffu, m0 > m[x][0] + grow || m1 > m[x][1] + grow)) {
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) {
+                m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
+                m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, o));
+            }
+            m0 = fmaxf(m0, m[x][0]);
+            m1 = fmaxf(m1, m[x][1]);
+            const float f0 = m0 == -INFINITY ? 1.f : fast_ex2((m[x][0] - m0) * sc), f1 = m1 == -INFINITY ? 1.f : fast_ex2((m[x][1] - m1) * sc);
+            m[x][0] = m0;
+            m[x][1] = m1;
+            ref[x][0] = (m0 == -INFINITY ? 0.f : m0 * sc) - off;
+            ref[x][1] = (m1 == -INFINITY ? 0.f : m1 * sc) - off;
+            l[x][0] *= f0;
+            l[x][1] *= f1;
+#pragma unroll
+            for (int i = 0; i < 2 * G; ++i) {
+                acc[x][i][0] *= f0; acc[x][i][1] *= f1;
+                acc[x][i][2] *= f0; acc[x][i][3] *= f1;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = fast_ex2(fmaf(z[e], sc, -ref[x][e & 1]));
+        l[x][0] += z[0] + z[2];
+        l[x][1] += z[1] + z[3];
+    };
+
+    for (;;) {
+        if (fresh) {   // a new segment
+            h = p.g_tiles == 1 ? c.hh : c.hh / p.g_tiles;
+            gt = c.hh - h * p.g_tiles;
+            heads = min(p.g_rows, a.g - gt * p.g_rows);
+            plain = c.blk >= c.s.nm;
+            load_q(plain ? 1.f : KV4_Q, plain ? 1.f : KV4_Q / 4);
+#pragma unroll
+            for (int x = 0; x < R; ++x) {
+                m[x][0] = m[x][1] = -INFINITY;
+                ref[x][0] = ref[x][1] = plain ? 0.f : -KV4_P_LOG2;
+                l[x][0] = l[x][1] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 2 * G; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[x][i][e] = 0.f;
+            }
+            fresh = false;
+        }
+        if (c.blk < c.s.nm) {
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars[warp][slot]), phase, &abort_flag, status));
+            if (!ok) break;
+            const uint8_t* st = ring + slot * TL::BYTES;
+            const int valid = c.s.mem - c.blk * KV4_ROWS;   // entries from this tile on
+            float s[R][4];
+            {
+                uint32_t k0[2][G / 2], k1[2][G / 2];
+                float h0[G], h1[G];
+                chunk_pair<G>(st + k_at, k0);
+                chunk_pair<G>(st + k_at + 8 * TL::ROW, k1);
+                steps_of<G>(st + TL::K_STEPS + pr * TL::STEPS, h0);
+                steps_of<G>(st + TL::K_STEPS + (pr + 8) * TL::STEPS, h1);
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    uint32_t e0[4], e1[4];
+                    group_pairs(g, k0[0][g / 2], k0[1][g / 2], e0);
+                    group_pairs(g, k1[0][g / 2], k1[1][g / 2], e1);
+#pragma unroll
+                    for (int x = 0; x < R; ++x) {
+                        float t[4];
+                        mma_new(t, e0[0], e1[0], e0[1], e1[1], qf[x][2 * g][0], qf[x][2 * g][1]);
+                        mma_acc(t, e0[2], e1[2], e0[3], e1[3], qf[x][2 * g + 1][0], qf[x][2 * g + 1][1]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[x][e] = g == 0 ? t[e] * (e < 2 ? h0[g] : h1[g]) : fmaf(t[e], e < 2 ? h0[g] : h1[g], s[x][e]);
+                    }
+                }
+            }
+            uint32_t v0[G / 2], v1[G / 2], v2[G / 2], v3[G / 2];
+            float h0[G], h1[G];
+            one_chunk<G>(st + TL::V + pv0 * TL::ROW + v_x, v0);
+            one_chunk<G>(st + TL::V + pv1 * TL::ROW + v_x, v1);
+            one_chunk<G>(st + TL::V + (pv0 + 8) * TL::ROW + v_x, v2);
+            one_chunk<G>(st + TL::V + (pv1 + 8) * TL::ROW + v_x, v3);
+            steps_of<G>(st + TL::V_STEPS + pr * TL::STEPS, h0);
+            steps_of<G>(st + TL::V_STEPS + (pr + 8) * TL::STEPS, h1);
+            if (valid < KV4_ROWS) {   // rows past the last entry may hold anything: no weight, and 0 x NaN is not 0
+#pragma unroll
+                for (int x = 0; x < R; ++x)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (pr + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    if (pr >= valid) h0[g] = 0.f;
+                    if (pr + 8 >= valid) h1[g] = 0.f;
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < R; ++x) weights(x, s[x], sc_mem, KV4_P_LOG2);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                uint32_t e0[4], e1[4];
+                group_pairs(g, v0[g / 2], v1[g / 2], e0);
+                group_pairs(g, v2[g / 2], v3[g / 2], e1);
+#pragma unroll
+                for (int x = 0; x < R; ++x) {
+                    // weight times step, rounded to bf16: off by 2^-8 of its value at most; the sums stay in fp32
+                    const uint32_t b0 = transposed(pack_bf16(s[x][0] * h0[g], s[x][1] * h0[g])), b1 = transposed(pack_bf16(s[x][2] * h1[g], s[x][3] * h1[g]));
+                    mma_acc(acc[x][2 * g], e0[0], e0[1], e1[0], e1[1], b0, b1);
+                    mma_acc(acc[x][2 * g + 1], e0[2], e0[3], e1[2], e1[3], b0, b1);
+                }
+            }
+            // every lane is done with the tile: fetch the next one into it
+            __syncwarp();
+            if (left_f > 0) fetch();
+            if (++slot == NS) { slot = 0; phase ^= 1; }
+        } else {   // 16 entries of the tail, straight from memory; the last one is the new token
+            if (!plain) {
+                to_plain();
+                load_q(1.f, 1.f);
+            }
+            const int base = (c.blk - c.s.nm) * KV4_ROWS, valid = c.s.tail + 1 - base;
+            const int64_t cell0 = ((int64_t)c.b * a.Hkv + h) * a.cap;
+            auto row_at = [&](const void* cache, const void* fresh_row, int i) {   // no row of another sequence is ever read
+                const int e = min(base + i, c.s.tail);
+                return e == c.s.tail && fresh_row ? static_cast<const __nv_bfloat16*>(fresh_row) + ((int64_t)c.b * a.Hkv + h) * D
+                                                  : static_cast<const __nv_bfloat16*>(cache) + (cell0 + e) * D;
+            };
+            float s[R][4];
+#pragma unroll
+            for (int x = 0; x < R; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[x][e] = 0.f;
+            {
+                const __nv_bfloat16 *k0 = row_at(a.k_tail, a.k_new, pr) + 8 * j, *k1 = row_at(a.k_tail, a.k_new, pr + 8) + 8 * j;
+                uint4 u0[G], u1[G];
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    u0[g] = *reinterpret_cast<const uint4*>(k0 + 32 * g);
+                    u1[g] = *reinterpret_cast<const uint4*>(k1 + 32 * g);
+                }
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int x = 0; x < R; ++x) {
+                        mma_acc(s[x], __byte_perm(u0[g].x, u0[g].z, 0x5410), __byte_perm(u1[g].x, u1[g].z, 0x5410), __byte_perm(u0[g].x, u0[g].z, 0x7632),
+                                __byte_perm(u1[g].x, u1[g].z, 0x7632), qf[x][2 * g][0], qf[x][2 * g][1]);
+                        mma_acc(s[x], __byte_perm(u0[g].y, u0[g].w, 0x5410), __byte_perm(u1[g].y, u1[g].w, 0x5410), __byte_perm(u0[g].y, u0[g].w, 0x7632),
+                                __byte_perm(u1[g].y, u1[g].w, 0x7632), qf[x][2 * g + 1][0], qf[x][2 * g + 1][1]);
+                    }
+            }
+            uint2 v[4][G];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = (i & 1 ? pv1 : pv0) + (i & 2) * 4;
+                const __nv_bfloat16* row = row_at(a.v_tail, a.v_new, e) + 4 * r;
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    v[i][g] = *reinterpret_cast<const uint2*>(row + 32 * g);
+                    if (e >= valid) v[i][g] = make_uint2(0, 0);   // repeated rows have no weight, but 0 x inf is not 0
+                }
+            }
+            if (valid <= KV4_ROWS && a.k_new && gt == 0 && lane < D / 8) {   // entry `tail` of the cache is read by nobody in this launch
+                const int64_t from = (((int64_t)c.b * a.Hkv + h) * D) / 8 + lane, to = (cell0 + c.s.tail) * (D / 8) + lane;
+                static_cast<uint4*>(a.k_tail)[to] = __ldg(static_cast<const uint4*>(a.k_new) + from);
+                static_cast<uint4*>(a.v_tail)[to] = __ldg(static_cast<const uint4*>(a.v_new) + from);
+            }
+#pragma unroll
+            for (int x = 0; x < R; ++x) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (pr + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
+                weights(x, s[x], sc_tail, 0.f);
+                const uint32_t b0 = transposed(pack_bf16(s[x][0], s[x][1])), b1 = transposed(pack_bf16(s[x][2], s[x][3]));
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    mma_acc(acc[x][2 * g], __byte_perm(v[0][g].x, v[1][g].x, 0x5410), __byte_perm(v[0][g].x, v[1][g].x, 0x7632),
+                            __byte_perm(v[2][g].x, v[3][g].x, 0x5410), __byte_perm(v[2][g].x, v[3][g].x, 0x7632), b0, b1);
+                    mma_acc(acc[x][2 * g + 1], __byte_perm(v[0][g].y, v[1][g].y, 0x5410), __byte_perm(v[0][g].y, v[1][g].y, 0x7632),
+                            __byte_perm(v[2][g].y, v[3][g].y, 0x5410), __byte_perm(v[2][g].y, v[3][g].y, 0x7632), b0, b1);
+                }
+            }
+        }
+        const bool last = c.blk == c.s.n - 1;
+        if (last || left == 1) {   // the segment ends
+            if (!plain) to_plain();
+            const int64_t seg = w + (int64_t)c.hh * a.B + c.b;
+#pragma unroll
+            for (int x = 0; x < R; ++x)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    float lt = l[x][y];
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) lt += __shfl_xor_sync(0xffffffffu, lt, o);
+                    const int hd = x * 8 + 2 * j + y;
+                    if (hd < heads) {
+                        const float inv = 1.f / lt;
+                        float* o = ws + p.o + (seg * p.g_rows + hd) * D + 4 * r;   // 8 lanes: 128 contiguous bytes
+#pragma unroll
+                        for (int g = 0; g < G; ++g)
+                            *reinterpret_cast<float4*>(o + 32 * g) = make_float4(acc[x][2 * g][y] * inv, acc[x][2 * g][2 + y] * inv,
+                                                                               acc[x][2 * g + 1][y] * inv, acc[x][2 * g + 1][2 + y] * inv);
+                        if (r == 0) ws[p.lse + seg * p.g_rows + hd] = ref[x][y] + log2f(lt);
+                    }
+                }
+            fresh = true;
+        }
+        if (--left == 0) break;
+        if (last) kb.next_unit(c); else ++c.blk;
+    }
+    if (!ok) {
+        // leaving early: give copies already in flight a bounded time to land in this CTA's shared memory
+        const long long t_off = clock64();
+        while (clock64() - t_off < 2000000ll) {}
+    }
+}
+
 // ------------------------------------------------------------------ merge
 // A row's D features are D / 4 lanes; WAYS sets of lanes share a row's partial results.
 constexpr int KV4_MERGE_THREADS = 128;
@@ -383,10 +776,20 @@ static cudaError_t stream(const Kv4DecodeArgs& a, cudaStream_t st) {
     return e == cudaSuccess ? merge<T, D>(a, p, st) : e;
 }
 
+template <int D>
+static cudaError_t tensor_cores(const Kv4DecodeArgs& a, cudaStream_t st) {
+    const Kv4Plan p = make_kv4_plan(a.B, a.Hq, a.Hkv, D, false);
+    int* status = device_status_word();
+    if (!status) return cudaErrorUnknown;
+    auto* kernel = p.g_rows <= 8 ? kv4_decode_kernel<D, 1> : kv4_decode_kernel<D, 2>;
+    const cudaError_t e = launch_behind(kernel, dim3(p.ctas), KV4_WARPS * 32, Kv4Ring<D>::TOTAL, st, false, a, p, status);
+    return e == cudaSuccess ? merge<__nv_bfloat16, D>(a, p, st) : e;
+}
+
 cudaError_t launch_decode_kv4(const Kv4DecodeArgs& a, int D, loma_dtype dt, bool generic, cudaStream_t st) {
-    (void)generic;
     if (dt == LOMA_F32) return D == 64 ? stream<float, 64>(a, st) : stream<float, 128>(a, st);
-    return D == 64 ? stream<__nv_bfloat16, 64>(a, st) : stream<__nv_bfloat16, 128>(a, st);
+    if (generic) return D == 64 ? stream<__nv_bfloat16, 64>(a, st) : stream<__nv_bfloat16, 128>(a, st);
+    return D == 64 ? tensor_cores<64>(a, st) : tensor_cores<128>(a, st);
 }
 
 }  // namespace loma
