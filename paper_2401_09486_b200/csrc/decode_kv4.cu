@@ -25,6 +25,7 @@ struct Kv4Plan {
     // in the workspace, in floats.  Segment: outputs [g_rows][D], g_rows log2-sum-exps.  cum: int64 [B + 1], blocks before sequence b within
     // one (kv head, head tile)
     int64_t o, lse, cum, total;
+    uint32_t ones;         // 0x00010001 (see kv4_pairs)
 };
 
 static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, bool cuda_cores) {
@@ -32,7 +33,7 @@ static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, bool cuda_cores) {
     const int g = Hq / Hkv;
     p.g_rows = cuda_cores ? (g < 3 ? g : 4) : (g <= 8 ? g : 16);
     p.g_tiles = (g + p.g_rows - 1) / p.g_rows;
-    p.ctas = 148 * (cuda_cores || p.g_rows <= 8 ? 4 : 2);
+    p.ctas = 148 * (cuda_cores ? 4 : p.g_rows <= 8 ? 3 : 2);
     p.workers = p.ctas * KV4_WARPS;
     int64_t at = 0;
     auto take = [&](int64_t n) { const int64_t o = at; at += (n + 63) / 64 * 64; return o; };
@@ -41,6 +42,7 @@ static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, bool cuda_cores) {
     p.lse = take(segments * p.g_rows);
     p.cum = take(2 * ((int64_t)B + 1));
     p.total = at;
+    p.ones = 0x00010001u;
     return p;
 }
 
@@ -296,7 +298,7 @@ constexpr float KV4_P_LOG2 = 80.f, KV4_P_INV = 8.271806125530277e-25f;   // 2^-8
 
 template <int D>
 struct Kv4Ring {
-    static constexpr int NS = D == 128 ? 5 : 10, WARP = NS * Kv4Tile<D>::BYTES, TOTAL = KV4_WARPS * WARP;
+    static constexpr int NS = D == 128 ? 7 : 14, WARP = NS * Kv4Tile<D>::BYTES, TOTAL = KV4_WARPS * WARP;
 };
 
 __device__ __forceinline__ void mma_acc(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -345,13 +347,13 @@ __device__ __forceinline__ void one_chunk(const uint8_t* p, uint32_t (&w)[G / 2]
         w[0] = *reinterpret_cast<const uint32_t*>(p);
     }
 }
-__device__ __forceinline__ void group_pairs(int g, uint32_t a, uint32_t b, uint32_t (&p)[4]) {
-    if (g & 1) kv4_pairs<true>(a, b, p); else kv4_pairs<false>(a, b, p);
+__device__ __forceinline__ void group_pairs(int g, uint32_t a, uint32_t b, uint32_t ones, uint32_t (&p)[4]) {
+    if (g & 1) kv4_pairs<true>(a, b, ones, p); else kv4_pairs<false>(a, b, ones, p);
 }
 
 // R: column tiles of 8 query heads
 template <int D, int R>
-__global__ void __launch_bounds__(KV4_WARPS * 32, R == 1 ? 4 : 2)
+__global__ void __launch_bounds__(KV4_WARPS * 32, R == 1 ? 3 : 2)
 kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     using TL = Kv4Tile<D>;
     constexpr int G = TL::GROUPS, NS = Kv4Ring<D>::NS;
@@ -375,33 +377,42 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     int left = (int)(kv4_first(w + 1, T, W) - kv4_first(w, T, W)), left_f = left;   // blocks of the share still to come, and still to be fetched
     Kv4Blocks::Cursor c = kb.find(kv4_first(w, T, W), scan, per), f = c;
 
-    // the fetch cursor stands on the next tile to fetch; the table entry of a tile is read one tile before it is used
+    // Fetching goes by runs of tiles that lie behind one another in a page.
+    const int page_tiles = 1 << (a.m.log2_ps - 4);
     const uint8_t* src = nullptr;
-    auto seek = [&]() {   // past tail blocks
-        while (left_f > 0 && f.blk >= f.s.nm) {
+    int run = 0, h_f = p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles;
+    auto next_run = [&]() {
+        while (left_f > 0 && f.blk >= f.s.nm) {   // past tail blocks
             left_f -= f.s.n - f.blk;
-            if (left_f > 0) kb.next_unit(f);
+            if (left_f > 0) {
+                kb.next_unit(f);
+                h_f = p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles;
+            }
         }
-        if (left_f > 0) src = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, f.b, f.blk * KV4_ROWS), p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles, f.blk * KV4_ROWS);
+        if (left_f <= 0) return;
+        src = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, f.b, f.blk * KV4_ROWS), h_f, f.blk * KV4_ROWS);
+        run = min(min(page_tiles - (f.blk & (page_tiles - 1)), f.s.nm - f.blk), left_f);
+        f.blk += run;
+        left_f -= run;
     };
-    uint8_t* ring = kv4_smem + warp * Kv4Ring<D>::WARP;
+    uint8_t* const ring = kv4_smem + warp * Kv4Ring<D>::WARP;
+    const uint32_t ring_s = smem_u32(ring), bars_s = smem_u32(&bars[warp][0]);
     int slot_f = 0;
     auto fetch = [&]() {
         if (lane == 0) {
-            const uint32_t bar = smem_u32(&bars[warp][slot_f]);
-            mbar_expect_tx(bar, TL::BYTES);
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(ring + slot_f * TL::BYTES)),
-                         "l"(src), "r"(TL::BYTES), "r"(bar)
+            mbar_expect_tx(bars_s + slot_f * 8, TL::BYTES);
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ring_s + slot_f * TL::BYTES),
+                         "l"(src), "r"(TL::BYTES), "r"(bars_s + slot_f * 8)
                          : "memory");
         }
         slot_f = slot_f + 1 == NS ? 0 : slot_f + 1;
-        ++f.blk;
-        --left_f;
-        seek();
+        src += TL::BYTES;
+        if (--run == 0) next_run();
     };
-    seek();
-    for (int i = 0; i < NS && left_f > 0; ++i) fetch();
+    next_run();
+    for (int i = 0; i < NS && run > 0; ++i) fetch();
 
+    const uint32_t ones = p.ones;
     const float sc_tail = a.scale * 1.4426950408889634f, sc_mem = sc_tail * KV4_S;
     const int pr = r ^ (r >> 1 & 1), pv0 = 2 * j ^ (j & 1), pv1 = pv0 ^ 1;   // entries of this lane's rows of scores, and of its pairs of values
     const int k_at = pr * TL::ROW + (j ^ ((r & 4) >> 1)) * 2 * TL::CHUNK, v_x = (r ^ (j & 2) << 1) * TL::CHUNK;
@@ -411,7 +422,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     float acc[R][2 * G][4];
     int slot = 0, h = 0, gt = 0, heads = 0;
     uint32_t phase = 0;
-    bool fresh = true, plain = false, ok = true;
+    bool ok = true;
 
     auto load_q = [&](float even, float odd) {
 #pragma unroll
@@ -446,12 +457,11 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 ref[x][y] += KV4_P_LOG2;
             }
         }
-        plain = true;
     };
     // z: raw products of rows pr (0, 1) and pr + 8 (2, 3), heads 2j, 2j + 1 (-inf: no weight) -> weights 2^(z sc - ref)
-    auto weights = [&](int x, float (&z)[4], float sc, float off) {
+    const float grow_mem = 8.f / sc_mem, grow_tail = 8.f / sc_tail;
+    auto weights = [&](int x, float (&z)[4], float sc, float grow, float off) {
         float m0 = fmaxf(z[0], z[2]), m1 = fmaxf(z[1], z[3]);
-        const float grow = 8.f / sc;
         // the reference moves only when a head's maximum has grown by more than 2^8 (weights stay below 2^8)
         if (__any_sync(0xffffffffu, m0 > m[x][0] + grow || m1 > m[x][1] + grow)) {
 #pragma unroll
@@ -480,30 +490,28 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
         l[x][1] += z[1] + z[3];
     };
 
-    for (;;) {
-        if (fresh) {   // a new segment
-            h = p.g_tiles == 1 ? c.hh : c.hh / p.g_tiles;
-            gt = c.hh - h * p.g_tiles;
-            heads = min(p.g_rows, a.g - gt * p.g_rows);
-            plain = c.blk >= c.s.nm;
-            load_q(plain ? 1.f : KV4_Q, plain ? 1.f : KV4_Q / 4);
+    for (;;) {   // a segment: tiles of memory, then blocks of the tail
+        h = p.g_tiles == 1 ? c.hh : c.hh / p.g_tiles;
+        gt = c.hh - h * p.g_tiles;
+        heads = min(p.g_rows, a.g - gt * p.g_rows);
+        const int tiles = min(max(c.s.nm - c.blk, 0), left), tails = min(c.s.n - c.blk - tiles, left - tiles);
+        load_q(tiles ? KV4_Q : 1.f, tiles ? KV4_Q / 4 : 1.f);
 #pragma unroll
-            for (int x = 0; x < R; ++x) {
-                m[x][0] = m[x][1] = -INFINITY;
-                ref[x][0] = ref[x][1] = plain ? 0.f : -KV4_P_LOG2;
-                l[x][0] = l[x][1] = 0.f;
+        for (int x = 0; x < R; ++x) {
+            m[x][0] = m[x][1] = -INFINITY;
+            ref[x][0] = ref[x][1] = tiles ? -KV4_P_LOG2 : 0.f;
+            l[x][0] = l[x][1] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 2 * G; ++i)
+            for (int i = 0; i < 2 * G; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[x][i][e] = 0.f;
-            }
-            fresh = false;
+                for (int e = 0; e < 4; ++e) acc[x][i][e] = 0.f;
         }
-        if (c.blk < c.s.nm) {
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars[warp][slot]), phase, &abort_flag, status));
+        int valid = c.s.mem - c.blk * KV4_ROWS;   // entries from the tile on
+#pragma unroll 1
+        for (int i = 0; i < tiles; ++i, valid -= KV4_ROWS) {
+            ok = __all_sync(0xffffffffu, mbar_wait(bars_s + slot * 8, phase, &abort_flag, status));
             if (!ok) break;
             const uint8_t* st = ring + slot * TL::BYTES;
-            const int valid = c.s.mem - c.blk * KV4_ROWS;   // entries from this tile on
             float s[R][4];
             {
                 uint32_t k0[2][G / 2], k1[2][G / 2];
@@ -515,8 +523,8 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     uint32_t e0[4], e1[4];
-                    group_pairs(g, k0[0][g / 2], k0[1][g / 2], e0);
-                    group_pairs(g, k1[0][g / 2], k1[1][g / 2], e1);
+                    group_pairs(g, k0[0][g / 2], k0[1][g / 2], ones, e0);
+                    group_pairs(g, k1[0][g / 2], k1[1][g / 2], ones, e1);
 #pragma unroll
                     for (int x = 0; x < R; ++x) {
                         float t[4];
@@ -548,12 +556,12 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 }
             }
 #pragma unroll
-            for (int x = 0; x < R; ++x) weights(x, s[x], sc_mem, KV4_P_LOG2);
+            for (int x = 0; x < R; ++x) weights(x, s[x], sc_mem, grow_mem, KV4_P_LOG2);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 uint32_t e0[4], e1[4];
-                group_pairs(g, v0[g / 2], v1[g / 2], e0);
-                group_pairs(g, v2[g / 2], v3[g / 2], e1);
+                group_pairs(g, v0[g / 2], v1[g / 2], ones, e0);
+                group_pairs(g, v2[g / 2], v3[g / 2], ones, e1);
 #pragma unroll
                 for (int x = 0; x < R; ++x) {
                     // weight times step, rounded to bf16: off by 2^-8 of its value at most; the sums stay in fp32
@@ -564,14 +572,17 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
             }
             // every lane is done with the tile: fetch the next one into it
             __syncwarp();
-            if (left_f > 0) fetch();
+            if (run > 0) fetch();
             if (++slot == NS) { slot = 0; phase ^= 1; }
-        } else {   // 16 entries of the tail, straight from memory; the last one is the new token
-            if (!plain) {
-                to_plain();
-                load_q(1.f, 1.f);
-            }
-            const int base = (c.blk - c.s.nm) * KV4_ROWS, valid = c.s.tail + 1 - base;
+        }
+        if (!ok) break;
+        if (tiles) {
+            to_plain();
+            if (tails) load_q(1.f, 1.f);
+        }
+#pragma unroll 1
+        for (int i = 0; i < tails; ++i) {   // 16 entries of the tail, straight from memory; the last one is the new token
+            const int base = (c.blk + tiles + i - c.s.nm) * KV4_ROWS, valid = c.s.tail + 1 - base;
             const int64_t cell0 = ((int64_t)c.b * a.Hkv + h) * a.cap;
             auto row_at = [&](const void* cache, const void* fresh_row, int i) {   // no row of another sequence is ever read
                 const int e = min(base + i, c.s.tail);
@@ -622,7 +633,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (pr + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
-                weights(x, s[x], sc_tail, 0.f);
+                weights(x, s[x], sc_tail, grow_tail, 0.f);
                 const uint32_t b0 = transposed(pack_bf16(s[x][0], s[x][1])), b1 = transposed(pack_bf16(s[x][2], s[x][3]));
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
@@ -633,32 +644,28 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 }
             }
         }
-        const bool last = c.blk == c.s.n - 1;
-        if (last || left == 1) {   // the segment ends
-            if (!plain) to_plain();
-            const int64_t seg = w + (int64_t)c.hh * a.B + c.b;
+        const int64_t seg = w + (int64_t)c.hh * a.B + c.b;
 #pragma unroll
-            for (int x = 0; x < R; ++x)
+        for (int x = 0; x < R; ++x)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    float lt = l[x][y];
+            for (int y = 0; y < 2; ++y) {
+                float lt = l[x][y];
 #pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) lt += __shfl_xor_sync(0xffffffffu, lt, o);
-                    const int hd = x * 8 + 2 * j + y;
-                    if (hd < heads) {
-                        const float inv = 1.f / lt;
-                        float* o = ws + p.o + (seg * p.g_rows + hd) * D + 4 * r;   // 8 lanes: 128 contiguous bytes
+                for (int o = 4; o < 32; o <<= 1) lt += __shfl_xor_sync(0xffffffffu, lt, o);
+                const int hd = x * 8 + 2 * j + y;
+                if (hd < heads) {
+                    const float inv = 1.f / lt;
+                    float* o = ws + p.o + (seg * p.g_rows + hd) * D + 4 * r;   // 8 lanes: 128 contiguous bytes
 #pragma unroll
-                        for (int g = 0; g < G; ++g)
-                            *reinterpret_cast<float4*>(o + 32 * g) = make_float4(acc[x][2 * g][y] * inv, acc[x][2 * g][2 + y] * inv,
-                                                                               acc[x][2 * g + 1][y] * inv, acc[x][2 * g + 1][2 + y] * inv);
-                        if (r == 0) ws[p.lse + seg * p.g_rows + hd] = ref[x][y] + log2f(lt);
-                    }
+                    for (int g = 0; g < G; ++g)
+                        *reinterpret_cast<float4*>(o + 32 * g) = make_float4(acc[x][2 * g][y] * inv, acc[x][2 * g][2 + y] * inv,
+                                                                           acc[x][2 * g + 1][y] * inv, acc[x][2 * g + 1][2 + y] * inv);
+                    if (r == 0) ws[p.lse + seg * p.g_rows + hd] = ref[x][y] + log2f(lt);
                 }
-            fresh = true;
-        }
-        if (--left == 0) break;
-        if (last) kb.next_unit(c); else ++c.blk;
+            }
+        left -= tiles + tails;
+        if (left == 0) break;
+        kb.next_unit(c);
     }
     if (!ok) {
         // leaving early: give copies already in flight a bounded time to land in this CTA's shared memory

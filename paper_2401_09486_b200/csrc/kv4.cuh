@@ -93,14 +93,16 @@ template <int D>
 __device__ __forceinline__ int kv4_chunk(int k, int x) { return k * Kv4Tile<D>::ROW + (x ^ (k & 4)) * Kv4Tile<D>::CHUNK; }
 
 // A and B: half-words of two chunks (two rows, or two chunks of a row), group by group.  Out: the pair's four elements e as bf16 pairs
-// (A low, B high), +-(2 m + 1) 2^-133, times 4 for odd e.  `hi`: the upper half-words of the words.
+// (A low, B high), +-(2 m + 1) 2^-133, times 4 for odd e.  HI: the upper half-words of the words.  ones: 0x00010001, from a kernel
+// parameter: an AND-OR takes one constant in the instruction, and the other one, where the compiler knows it, is moved to a register
+// before every use.
 template <bool HI>
-__device__ __forceinline__ void kv4_pairs(uint32_t a, uint32_t b, uint32_t (&p)[4]) {
+__device__ __forceinline__ void kv4_pairs(uint32_t a, uint32_t b, uint32_t ones, uint32_t (&p)[4]) {
     const uint32_t u = __byte_perm(a, b, HI ? 0x7632 : 0x5410), w = __byte_perm(a, b, HI ? 0x6723 : 0x4501);
-    p[0] = ((u << 1) & 0x800E800Eu) | 0x00010001u;
-    p[1] = (u & 0x80388038u) | 0x00040004u;
-    p[2] = ((w << 1) & 0x800E800Eu) | 0x00010001u;
-    p[3] = (w & 0x80388038u) | 0x00040004u;
+    p[0] = ((u << 1) & 0x800E800Eu) | ones;
+    p[1] = (u & 0x80388038u) | ones << 2;
+    p[2] = ((w << 1) & 0x800E800Eu) | ones;
+    p[3] = (w & 0x80388038u) | ones << 2;
 }
 #endif
 
