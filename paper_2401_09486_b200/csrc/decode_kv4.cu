@@ -6,7 +6,7 @@
 // arithmetic: 23 bytes per SM and clock from HBM are a tile of 16 entries every 100 clocks, and turning its 4096 numbers into
 // operands alone takes a warp 128 instructions.
 //
-// Cut: units are (kv head, head tile, sequence); a unit's blocks of 16 entries -- tiles of memory first, then the tail with the new
+// Cut: units are (kv head, head tile, sequence); a unit's blocks -- 32 entries of memory each first, then 16 of the tail with the new
 // token last -- are numbered through, and worker w of W (a warp) takes blocks [T w / W, T (w + 1) / W).  A worker's stay in
 // one unit is a segment with a partial result in slot w + unit; kv4_merge_kernel joins a unit's segments in a fixed order.  The
 // lengths are known on the device only, so every CTA finds the cut from them.
@@ -18,6 +18,7 @@
 namespace loma {
 
 constexpr int KV4_WARPS = 4;
+constexpr int KV4_STEP = 32;   // memory entries to a block: two tiles
 
 struct Kv4Plan {
     int g_rows, g_tiles;   // query heads of a kv head per head tile, head tiles per kv head
@@ -59,7 +60,7 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4DecodeArgs& a, int b) {
     Kv4Seq s;
     s.mem = min(max(__ldg(a.mem_lens + b), 0), a.max_mem);
     s.tail = min(__ldg(a.tail_lens + b), a.max_tail);
-    s.nm = (int)(((int64_t)s.mem + KV4_ROWS - 1) / KV4_ROWS);
+    s.nm = (s.mem + KV4_STEP - 1) / KV4_STEP;
     s.n = s.tail < 0 ? 0 : s.nm + s.tail / KV4_ROWS + 1;
     return s;
 }
@@ -190,11 +191,12 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
             fresh = false;
         }
         const bool memory = c.blk < c.s.nm;
-        const int first = (memory ? c.blk : c.blk - c.s.nm) * KV4_ROWS;        // of the block, in memory or in the tail
-        const int end = min(memory ? c.s.mem : c.s.tail + 1, first + KV4_ROWS);
-        const uint8_t* tile = memory ? a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, c.b, first), h, first) : nullptr;
+        const int first = memory ? c.blk * KV4_STEP : (c.blk - c.s.nm) * KV4_ROWS;        // of the block, in memory or in the tail
+        const int end = memory ? min(c.s.mem, first + KV4_STEP) : min(c.s.tail + 1, first + KV4_ROWS);
+        const uint8_t* tile = nullptr;
 #pragma unroll 1
         for (int j0 = first; j0 < end; j0 += 4) {
+            if (memory && j0 % KV4_ROWS == 0) tile = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, c.b, j0), h, j0);
             const int j = min(j0 + sub, end - 1);   // no row of another sequence is ever read
             const bool there = j0 + sub < end;
             float k[N], v[N];
@@ -277,8 +279,8 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
 }
 
 // ------------------------------------------------------------------ tensor cores
-// A worker streams its tiles through a ring of its own in shared memory: one bulk copy per tile, NS - 1 tiles ahead and across the
-// borders between sequences.  The g query heads of a kv head share every row: with 16 entries as the rows and 8 heads as the
+// A worker streams its blocks through a ring of its own in shared memory: one bulk copy per block of two tiles (two where pages hold one
+// tile), NS - 1 blocks ahead and across the borders between sequences.  The g query heads of a kv head share every row: with 16 entries as the rows and 8 heads as the
 // columns of m16n8k16 products,
 //     S^T [entries x heads] = K Q^T          O^T [features x heads] += V^T P^T
 // A group's step is the same for all entries of a column of K Q^T only within a row, so each group's product (two k-steps) goes
@@ -298,7 +300,7 @@ constexpr float KV4_P_LOG2 = 80.f, KV4_P_INV = 8.271806125530277e-25f;   // 2^-8
 
 template <int D>
 struct Kv4Ring {
-    static constexpr int NS = D == 128 ? 7 : 14, WARP = NS * Kv4Tile<D>::BYTES, TOTAL = KV4_WARPS * WARP;
+    static constexpr int NS = D == 128 ? 3 : 6, STAGE = 2 * Kv4Tile<D>::BYTES, WARP = NS * STAGE, TOTAL = KV4_WARPS * WARP;
 };
 
 __device__ __forceinline__ void mma_acc(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -377,10 +379,11 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     int left = (int)(kv4_first(w + 1, T, W) - kv4_first(w, T, W)), left_f = left;   // blocks of the share still to come, and still to be fetched
     Kv4Blocks::Cursor c = kb.find(kv4_first(w, T, W), scan, per), f = c;
 
-    // Fetching goes by runs of tiles that lie behind one another in a page.
-    const int page_tiles = 1 << (a.m.log2_ps - 4);
+    // Fetching goes by runs of blocks that lie behind one another in a page.  Where a page is one tile, lanes 0 and 1 fetch one each.
+    const bool small_pages = a.m.log2_ps == 4;
+    const int page_blocks = small_pages ? 1 : 1 << (a.m.log2_ps - 5);
     const uint8_t* src = nullptr;
-    int run = 0, h_f = p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles;
+    int run = 0, rest = 0, h_f = p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles;   // rest: entries of the sequence from the next block on
     auto next_run = [&]() {
         while (left_f > 0 && f.blk >= f.s.nm) {   // past tail blocks
             left_f -= f.s.n - f.blk;
@@ -390,8 +393,10 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
             }
         }
         if (left_f <= 0) return;
-        src = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, f.b, f.blk * KV4_ROWS), h_f, f.blk * KV4_ROWS);
-        run = min(min(page_tiles - (f.blk & (page_tiles - 1)), f.s.nm - f.blk), left_f);
+        rest = f.s.mem - f.blk * KV4_STEP;
+        const int entry = f.blk * KV4_STEP + (small_pages && lane == 1 && rest > KV4_ROWS ? KV4_ROWS : 0);
+        src = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, f.b, entry), h_f, entry);
+        run = min(min(page_blocks - (f.blk & (page_blocks - 1)), f.s.nm - f.blk), left_f);
         f.blk += run;
         left_f -= run;
     };
@@ -399,14 +404,16 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     const uint32_t ring_s = smem_u32(ring), bars_s = smem_u32(&bars[warp][0]);
     int slot_f = 0;
     auto fetch = [&]() {
-        if (lane == 0) {
-            mbar_expect_tx(bars_s + slot_f * 8, TL::BYTES);
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ring_s + slot_f * TL::BYTES),
-                         "l"(src), "r"(TL::BYTES), "r"(bars_s + slot_f * 8)
+        const int bytes = rest > KV4_ROWS ? 2 * TL::BYTES : TL::BYTES;
+        if (lane == 0) mbar_expect_tx(bars_s + slot_f * 8, bytes);
+        __syncwarp();
+        if (lane == 0 || (small_pages && lane == 1 && rest > KV4_ROWS))
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ring_s + slot_f * Kv4Ring<D>::STAGE + lane * TL::BYTES),
+                         "l"(src), "r"(small_pages ? TL::BYTES : bytes), "r"(bars_s + slot_f * 8)
                          : "memory");
-        }
         slot_f = slot_f + 1 == NS ? 0 : slot_f + 1;
-        src += TL::BYTES;
+        src += 2 * TL::BYTES;
+        rest -= KV4_STEP;
         if (--run == 0) next_run();
     };
     next_run();
@@ -458,10 +465,16 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
             }
         }
     };
-    // z: raw products of rows pr (0, 1) and pr + 8 (2, 3), heads 2j, 2j + 1 (-inf: no weight) -> weights 2^(z sc - ref)
+    // z: raw products of rows pr (0, 1) and pr + 8 (2, 3) of one or two tiles, heads 2j, 2j + 1 (-inf: no weight) -> weights
+    // 2^(z sc - ref)
     const float grow_mem = 8.f / sc_mem, grow_tail = 8.f / sc_tail;
-    auto weights = [&](int x, float (&z)[4], float sc, float grow, float off) {
+    auto weights = [&](int x, auto& z, float sc, float grow, float off) {
+        constexpr int N = sizeof(z) / sizeof(float);
         float m0 = fmaxf(z[0], z[2]), m1 = fmaxf(z[1], z[3]);
+        if constexpr (N > 4) {
+            m0 = fmaxf(m0, fmaxf(z[4], z[6]));
+            m1 = fmaxf(m1, fmaxf(z[5], z[7]));
+        }
         // the reference moves only when a head's maximum has grown by more than 2^8 (weights stay below 2^8)
         if (__any_sync(0xffffffffu, m0 > m[x][0] + grow || m1 > m[x][1] + grow)) {
 #pragma unroll
@@ -485,12 +498,15 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
             }
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = fast_ex2(fmaf(z[e], sc, -ref[x][e & 1]));
-        l[x][0] += z[0] + z[2];
-        l[x][1] += z[1] + z[3];
+        for (int e = 0; e < N; ++e) z[e] = fast_ex2(fmaf(z[e], sc, -ref[x][e & 1]));
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            l[x][0] += z[e] + z[e + 2];
+            l[x][1] += z[e + 1] + z[e + 3];
+        }
     };
 
-    for (;;) {   // a segment: tiles of memory, then blocks of the tail
+    for (;;) {   // a segment: blocks of memory, then of the tail
         h = p.g_tiles == 1 ? c.hh : c.hh / p.g_tiles;
         gt = c.hh - h * p.g_tiles;
         heads = min(p.g_rows, a.g - gt * p.g_rows);
@@ -506,20 +522,22 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[x][i][e] = 0.f;
         }
-        int valid = c.s.mem - c.blk * KV4_ROWS;   // entries from the tile on
+        int valid = c.s.mem - c.blk * KV4_STEP;   // entries from the block on
 #pragma unroll 1
-        for (int i = 0; i < tiles; ++i, valid -= KV4_ROWS) {
+        for (int i = 0; i < tiles; ++i, valid -= KV4_STEP) {
             ok = __all_sync(0xffffffffu, mbar_wait(bars_s + slot * 8, phase, &abort_flag, status));
             if (!ok) break;
-            const uint8_t* st = ring + slot * TL::BYTES;
-            float s[R][4];
-            {
+            const uint8_t* st = ring + slot * Kv4Ring<D>::STAGE;
+            float s[R][8];   // of the two tiles
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint8_t* tile = st + u * TL::BYTES;
                 uint32_t k0[2][G / 2], k1[2][G / 2];
                 float h0[G], h1[G];
-                chunk_pair<G>(st + k_at, k0);
-                chunk_pair<G>(st + k_at + 8 * TL::ROW, k1);
-                steps_of<G>(st + TL::K_STEPS + pr * TL::STEPS, h0);
-                steps_of<G>(st + TL::K_STEPS + (pr + 8) * TL::STEPS, h1);
+                chunk_pair<G>(tile + k_at, k0);
+                chunk_pair<G>(tile + k_at + 8 * TL::ROW, k1);
+                steps_of<G>(tile + TL::K_STEPS + pr * TL::STEPS, h0);
+                steps_of<G>(tile + TL::K_STEPS + (pr + 8) * TL::STEPS, h1);
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     uint32_t e0[4], e1[4];
@@ -531,46 +549,56 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                         mma_new(t, e0[0], e1[0], e0[1], e1[1], qf[x][2 * g][0], qf[x][2 * g][1]);
                         mma_acc(t, e0[2], e1[2], e0[3], e1[3], qf[x][2 * g + 1][0], qf[x][2 * g + 1][1]);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[x][e] = g == 0 ? t[e] * (e < 2 ? h0[g] : h1[g]) : fmaf(t[e], e < 2 ? h0[g] : h1[g], s[x][e]);
+                        for (int e = 0; e < 4; ++e) {
+                            const float hs = e < 2 ? h0[g] : h1[g];
+                            s[x][4 * u + e] = g == 0 ? t[e] * hs : fmaf(t[e], hs, s[x][4 * u + e]);
+                        }
                     }
                 }
             }
-            uint32_t v0[G / 2], v1[G / 2], v2[G / 2], v3[G / 2];
-            float h0[G], h1[G];
-            one_chunk<G>(st + TL::V + pv0 * TL::ROW + v_x, v0);
-            one_chunk<G>(st + TL::V + pv1 * TL::ROW + v_x, v1);
-            one_chunk<G>(st + TL::V + (pv0 + 8) * TL::ROW + v_x, v2);
-            one_chunk<G>(st + TL::V + (pv1 + 8) * TL::ROW + v_x, v3);
-            steps_of<G>(st + TL::V_STEPS + pr * TL::STEPS, h0);
-            steps_of<G>(st + TL::V_STEPS + (pr + 8) * TL::STEPS, h1);
-            if (valid < KV4_ROWS) {   // rows past the last entry may hold anything: no weight, and 0 x NaN is not 0
+            if (valid < KV4_STEP) {   // rows past the last entry may hold anything: no weight
 #pragma unroll
                 for (int x = 0; x < R; ++x)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                    for (int e = 0; e < 8; ++e)
                         if (pr + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    if (pr >= valid) h0[g] = 0.f;
-                    if (pr + 8 >= valid) h1[g] = 0.f;
-                }
             }
 #pragma unroll
             for (int x = 0; x < R; ++x) weights(x, s[x], sc_mem, grow_mem, KV4_P_LOG2);
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                uint32_t e0[4], e1[4];
-                group_pairs(g, v0[g / 2], v1[g / 2], ones, e0);
-                group_pairs(g, v2[g / 2], v3[g / 2], ones, e1);
+            for (int u = 0; u < 2; ++u) {
+                const uint8_t* tile = st + u * TL::BYTES;
+                uint32_t v0[G / 2], v1[G / 2], v2[G / 2], v3[G / 2];
+                float h0[G], h1[G];
+                one_chunk<G>(tile + TL::V + pv0 * TL::ROW + v_x, v0);
+                one_chunk<G>(tile + TL::V + pv1 * TL::ROW + v_x, v1);
+                one_chunk<G>(tile + TL::V + (pv0 + 8) * TL::ROW + v_x, v2);
+                one_chunk<G>(tile + TL::V + (pv1 + 8) * TL::ROW + v_x, v3);
+                steps_of<G>(tile + TL::V_STEPS + pr * TL::STEPS, h0);
+                steps_of<G>(tile + TL::V_STEPS + (pr + 8) * TL::STEPS, h1);
+                if (valid < KV4_STEP) {   // ... and 0 x NaN is not 0
 #pragma unroll
-                for (int x = 0; x < R; ++x) {
-                    // weight times step, rounded to bf16: off by 2^-8 of its value at most; the sums stay in fp32
-                    const uint32_t b0 = transposed(pack_bf16(s[x][0] * h0[g], s[x][1] * h0[g])), b1 = transposed(pack_bf16(s[x][2] * h1[g], s[x][3] * h1[g]));
-                    mma_acc(acc[x][2 * g], e0[0], e0[1], e1[0], e1[1], b0, b1);
-                    mma_acc(acc[x][2 * g + 1], e0[2], e0[3], e1[2], e1[3], b0, b1);
+                    for (int g = 0; g < G; ++g) {
+                        if (pr + 16 * u >= valid) h0[g] = 0.f;
+                        if (pr + 16 * u + 8 >= valid) h1[g] = 0.f;
+                    }
+                }
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    uint32_t e0[4], e1[4];
+                    group_pairs(g, v0[g / 2], v1[g / 2], ones, e0);
+                    group_pairs(g, v2[g / 2], v3[g / 2], ones, e1);
+#pragma unroll
+                    for (int x = 0; x < R; ++x) {
+                        // weight times step, rounded to bf16: off by 2^-8 of its value at most; the sums stay in fp32
+                        const float* z = s[x] + 4 * u;
+                        const uint32_t b0 = transposed(pack_bf16(z[0] * h0[g], z[1] * h0[g])), b1 = transposed(pack_bf16(z[2] * h1[g], z[3] * h1[g]));
+                        mma_acc(acc[x][2 * g], e0[0], e0[1], e1[0], e1[1], b0, b1);
+                        mma_acc(acc[x][2 * g + 1], e0[2], e0[3], e1[2], e1[3], b0, b1);
+                    }
                 }
             }
-            // every lane is done with the tile: fetch the next one into it
+            // every lane is done with the block: fetch the next one into its place
             __syncwarp();
             if (run > 0) fetch();
             if (++slot == NS) { slot = 0; phase ^= 1; }
