@@ -34,7 +34,7 @@ static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, bool cuda_cores) {
     const int g = Hq / Hkv;
     p.g_rows = cuda_cores ? (g < 3 ? g : 4) : (g <= 8 ? g : 16);
     p.g_tiles = (g + p.g_rows - 1) / p.g_rows;
-    p.ctas = 148 * (cuda_cores ? 4 : p.g_rows <= 8 ? 3 : 2);
+    p.ctas = 148 * (cuda_cores ? (p.g_rows == 4 ? 2 : 4) : p.g_rows <= 8 ? 3 : 2);
     p.workers = p.ctas * KV4_WARPS;
     int64_t at = 0;
     auto take = [&](int64_t n) { const int64_t o = at; at += (n + 63) / 64 * 64; return o; };
@@ -151,15 +151,45 @@ __device__ __forceinline__ int kv4_page_read(const Kv4Pool& m, int b, int j) {  
 }
 
 // ------------------------------------------------------------------ CUDA cores
-// Eight lanes share an entry (a chunk each, 16 or 8 of its features), so a warp takes four entries at a time, G heads of the group
-// together.  All arithmetic in fp32; the one rounding is that of the output.
+// Eight lanes share an entry (a chunk each, 16 or 8 of its features), so a warp takes a tile in four rounds of four entries, G heads
+// of the group together.  The 4 G partial scores of a lane are added up over those lanes with the results spread over them, so a lane
+// keeps the maximum and the sum of one head; weights go back to all lanes through the warp's shared memory.  All arithmetic in
+// fp32; the one rounding is that of the output.
+
+// sums over the lanes that differ in bit O and below, M values; lane x keeps value x * M / 8 + v (or each value lies in 8 / M lanes)
+template <int M, int O>
+__device__ __forceinline__ void spread_sum8(float* s, int lane) {
+    if constexpr (M > 1) {
+        const bool up = lane & O;
+#pragma unroll
+        for (int i = 0; i < M / 2; ++i) {
+            const float lo = s[i], hi = s[i + M / 2];
+            s[i] = (up ? hi : lo) + __shfl_xor_sync(0xffffffffu, up ? lo : hi, O);
+        }
+    } else {
+        s[0] += __shfl_xor_sync(0xffffffffu, s[0], O);
+    }
+    if constexpr (O > 1) spread_sum8<(M > 1 ? M / 2 : 1), O / 2>(s, lane);
+}
+
+// four features
+__device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
+    const float4 u = *reinterpret_cast<const float4*>(p);
+    x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&x)[4]) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    x[0] = bf16lo(u.x); x[1] = bf16hi(u.x); x[2] = bf16lo(u.y); x[3] = bf16hi(u.y);
+}
+
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(KV4_WARPS * 32)
+__global__ void __launch_bounds__(KV4_WARPS * 32, G == 4 ? 2 : 4)
 kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
     using TL = Kv4Tile<D>;
-    constexpr int NG = TL::GROUPS, N = 4 * NG;   // groups; features of a lane: 32 g + 4 x + e at [4 g + e]
+    constexpr int NG = TL::GROUPS, M = 4 * G, KEEP = M > 8 ? M / 8 : 1, DUP = M < 8 ? 8 / M : 1, LH = 8 / G;
     __shared__ int64_t scan[Kv4Blocks::MAX_GROUPS + 1];
     __shared__ int64_t wsum[KV4_WARPS];
+    __shared__ __align__(16) float s_weight[KV4_WARPS][4][M];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, x = lane & 7, sub = lane >> 3;
     float* ws = static_cast<float*>(a.ws);
     let_next_start();
@@ -168,113 +198,206 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
     const int64_t total = scan[(a.B + per - 1) / per] * a.Hkv * p.g_tiles, W = min(total, (int64_t)p.workers);
     const int64_t w = (int64_t)warp * gridDim.x + blockIdx.x;
     if (w >= W) return;
-    int64_t t = kv4_first(w, total, W);
-    const int64_t t_end = kv4_first(w + 1, total, W);
-    Kv4Blocks::Cursor c = kb.find(t, scan, per);
+    int left = (int)(kv4_first(w + 1, total, W) - kv4_first(w, total, W));
+    Kv4Blocks::Cursor c = kb.find(kv4_first(w, total, W), scan, per);
+    const uint32_t ones = p.ones;
     const float scale_log2 = a.scale * 1.4426950408889634f;
-    float q[G][N], acc[G][N], m[G], l[G];   // m: of all entries seen; l, acc: of this lane's `sub`
-    bool fresh = true;
-    for (; t < t_end; ++t) {
-        const int h = c.hh / p.g_tiles, gt = c.hh - h * p.g_tiles, heads = min(G, a.g - gt * G);
-        if (fresh) {
+    float q[G][NG][4], acc[G][NG][4], m, ref, l;   // m (a score in powers of two), ref (what exponents are taken off), l: of head x / LH
+    // s: scores of the lane's four entries (rows i * 4 + sub of a tile) for all heads; the weights of all heads come back in it
+    auto weights = [&](float (&s)[M], int valid, float factor, float off) {
+        spread_sum8<M, 4>(s, lane);
+        float top = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < KEEP; ++v) {
+            s[v] = (x * KEEP / DUP + v) % 4 * 4 + sub < valid ? s[v] * factor : -INFINITY;
+            top = fmaxf(top, s[v]);
+        }
+#pragma unroll
+        for (int o = DUP; o < LH; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+        // the reference moves only when a head's maximum has grown by more than 2^8 (weights stay below 2^8)
+        if (__any_sync(0xffffffffu, top > m + 8.f)) {
+            const float m_new = fmaxf(m, top), keep = m_new == -INFINITY ? 1.f : exp2f(m - m_new);
+            m = m_new;
+            ref = (m == -INFINITY ? 0.f : m) - off;
+            l *= keep;
 #pragma unroll
             for (int y = 0; y < G; ++y) {
-                const T* qp = static_cast<const T*>(a.q) + ((int64_t)c.b * a.Hq + h * a.g + gt * G + min(y, heads - 1)) * D + 4 * x;
+                const float f = __shfl_sync(0xffffffffu, keep, y * LH);
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    q[y][i] = (float)qp[32 * (i / 4) + i % 4] * scale_log2;
-                    acc[y][i] = 0.f;
-                }
-                m[y] = -INFINITY;
-                l[y] = 0.f;
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[y][g][e] *= f;
             }
-            fresh = false;
         }
-        const bool memory = c.blk < c.s.nm;
-        const int first = memory ? c.blk * KV4_STEP : (c.blk - c.s.nm) * KV4_ROWS;        // of the block, in memory or in the tail
-        const int end = memory ? min(c.s.mem, first + KV4_STEP) : min(c.s.tail + 1, first + KV4_ROWS);
-        const uint8_t* tile = nullptr;
-#pragma unroll 1
-        for (int j0 = first; j0 < end; j0 += 4) {
-            if (memory && j0 % KV4_ROWS == 0) tile = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, c.b, j0), h, j0);
-            const int j = min(j0 + sub, end - 1);   // no row of another sequence is ever read
-            const bool there = j0 + sub < end;
-            float k[N], v[N];
-            if (memory) {
-                const uint8_t* bits = tile + kv4_chunk<D>(j & 15, x);
-                const uint8_t* steps = tile + TL::K_STEPS + (j & 15) * TL::STEPS;
+        __syncwarp();   // the last tile's weights have been read
 #pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    const float hk = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(steps + 2 * g) << 16);
-                    const float hv = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(steps + TL::V_STEPS - TL::K_STEPS + 2 * g) << 16);
-                    const uint32_t yk = *reinterpret_cast<const uint16_t*>(bits + 2 * g), yv = *reinterpret_cast<const uint16_t*>(bits + TL::V + 2 * g);
-                    constexpr int at_m[4] = {0, 3, 8, 11}, at_s[4] = {14, 15, 6, 7};
+        for (int v = 0; v < KEEP; ++v) {
+            const float pr = exp2f(s[v] - ref);
+            l += pr;
+            if (x % DUP == 0) s_weight[warp][sub][x * KEEP / DUP + v] = pr;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int y = 0; y < M; y += 4) load4(&s_weight[warp][sub][y], *reinterpret_cast<float(*)[4]>(s + y));
+    };
+    for (;;) {   // a segment: blocks of memory, then of the tail
+        const int h = c.hh / p.g_tiles, gt = c.hh - h * p.g_tiles, heads = min(G, a.g - gt * G);
+        const int blocks = min(max(c.s.nm - c.blk, 0), left), tails = min(c.s.n - c.blk - blocks, left - blocks);
+#pragma unroll
+        for (int y = 0; y < G; ++y) {
+            const T* qp = static_cast<const T*>(a.q) + ((int64_t)c.b * a.Hq + h * a.g + gt * G + min(y, heads - 1)) * D + 4 * x;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                load4(qp + 32 * g, q[y][g]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (blocks) q[y][g][e] *= e & 1 ? KV4_Q / 4 : KV4_Q;
+                    acc[y][g][e] = 0.f;
+                }
+            }
+        }
+        m = -INFINITY;
+        ref = blocks ? -KV4_P_LOG2 : 0.f;
+        l = 0.f;
+        const int end = min(c.s.mem, (c.blk + blocks) * KV4_STEP);
+#pragma unroll 1
+        for (int j0 = c.blk * KV4_STEP; j0 < end; j0 += KV4_ROWS) {
+            const uint8_t* tile = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, c.b, j0), h, j0);
+            const int valid = end - j0;
+            uint32_t kw[4][NG / 2], vw[4][NG / 2], kh[4][NG / 2], vh[4][NG / 2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = i * 4 + sub;
+                halves<NG>(tile + kv4_chunk<D>(row, x), kw[i]);
+                halves<NG>(tile + TL::K_STEPS + row * TL::STEPS, kh[i]);
+                halves<NG>(tile + TL::V + kv4_chunk<D>(row, x), vw[i]);
+                halves<NG>(tile + TL::V_STEPS + row * TL::STEPS, vh[i]);
+            }
+            float s[M];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int g = 0; g < NG; g += 2) {
+                    uint32_t n[4];
+                    kv4_word(kw[i][g / 2], ones, n);
+#pragma unroll
+                    for (int y = 0; y < G; ++y) {
+                        float lo = 0.f, hi = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            lo = fmaf(q[y][g][e], bf16lo(n[e]), lo);
+                            hi = fmaf(q[y][g + 1][e], bf16hi(n[e]), hi);
+                        }
+                        s[y * 4 + i] = fmaf(hi, bf16hi(kh[i][g / 2]), fmaf(lo, bf16lo(kh[i][g / 2]), g ? s[y * 4 + i] : 0.f));
+                    }
+                }
+            weights(s, valid, scale_log2 * KV4_S, KV4_P_LOG2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool there = i * 4 + sub < valid;   // rows past the last entry may hold anything, and 0 x NaN is not 0
+#pragma unroll
+                for (int g = 0; g < NG; g += 2) {
+                    uint32_t n[4];
+                    kv4_word(vw[i][g / 2], ones, n);
+                    const float h0 = there ? bf16lo(vh[i][g / 2]) : 0.f, h1 = there ? bf16hi(vh[i][g / 2]) : 0.f;
+#pragma unroll
+                    for (int y = 0; y < G; ++y) {
+                        const float w0 = s[y * 4 + i] * h0, w1 = s[y * 4 + i] * h1;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            acc[y][g][e] = fmaf(w0, bf16lo(n[e]), acc[y][g][e]);
+                            acc[y][g + 1][e] = fmaf(w1, bf16hi(n[e]), acc[y][g + 1][e]);
+                        }
+                    }
+                }
+            }
+        }
+        if (blocks) {   // the powers of two are taken off
+#pragma unroll
+            for (int y = 0; y < G; ++y)
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float nk = (float)(2 * (yk >> at_m[e] & 7) + 1) * hk, nv = (float)(2 * (yv >> at_m[e] & 7) + 1) * hv;
-                        k[4 * g + e] = yk >> at_s[e] & 1 ? -nk : nk;
-                        v[4 * g + e] = yv >> at_s[e] & 1 ? -nv : nv;
+                        acc[y][g][e] *= e & 1 ? KV4_O / 4 : KV4_O;
+                        q[y][g][e] *= e & 1 ? 4 / KV4_Q : 1 / KV4_Q;
                     }
-                }
-            } else {
+            l *= KV4_P_INV;
+            ref += KV4_P_LOG2;
+        }
+#pragma unroll 1
+        for (int t = 0; t < tails; ++t) {   // 16 entries of the tail; the last one is the new token
+            const int base = (c.blk + blocks + t - c.s.nm) * KV4_ROWS, valid = c.s.tail + 1 - base;
+            const T* row[2][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = min(base + i * 4 + sub, c.s.tail);   // no row of another sequence is ever read
                 const bool token = j == c.s.tail && a.k_new;
-                const int64_t at = token ? ((int64_t)c.b * a.Hkv + h) * D : (((int64_t)c.b * a.Hkv + h) * a.cap + j) * D;
-                const T* kp = static_cast<const T*>(token ? a.k_new : a.k_tail) + at + 4 * x;
-                const T* vp = static_cast<const T*>(token ? a.v_new : a.v_tail) + at + 4 * x;
+                const int64_t at = (token ? (int64_t)c.b * a.Hkv + h : ((int64_t)c.b * a.Hkv + h) * a.cap + j) * D + 4 * x;
+                row[0][i] = static_cast<const T*>(token ? a.k_new : a.k_tail) + at;
+                row[1][i] = static_cast<const T*>(token ? a.v_new : a.v_tail) + at;
+            }
+            float s[M];
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    k[i] = (float)kp[32 * (i / 4) + i % 4];
-                    v[i] = (float)vp[32 * (i / 4) + i % 4];
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    float k[4];
+                    load4(row[0][i] + 32 * g, k);
+#pragma unroll
+                    for (int y = 0; y < G; ++y)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[y * 4 + i] = fmaf(q[y][g][e], k[e], g + e ? s[y * 4 + i] : 0.f);
                 }
-                if (token && gt == 0 && there) {   // entry tail of the cache is read by nobody in this launch
-                    const int64_t cell = (((int64_t)c.b * a.Hkv + h) * a.cap + j) * D + 4 * x;
+            weights(s, valid, scale_log2, 0.f);
 #pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        static_cast<T*>(a.k_tail)[cell + 32 * (i / 4) + i % 4] = kp[32 * (i / 4) + i % 4];
-                        static_cast<T*>(a.v_tail)[cell + 32 * (i / 4) + i % 4] = vp[32 * (i / 4) + i % 4];
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    float v[4];
+                    load4(row[1][i] + 32 * g, v);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (i * 4 + sub >= valid) v[e] = 0.f;   // a repeated row has no weight, but 0 x inf is not 0
+#pragma unroll
+                        for (int y = 0; y < G; ++y) acc[y][g][e] = fmaf(s[y * 4 + i], v[e], acc[y][g][e]);
                     }
                 }
-            }
-#pragma unroll
-            for (int y = 0; y < G; ++y) {
-                float s = 0.f;
-#pragma unroll
-                for (int i = 0; i < N; ++i) s = fmaf(q[y][i], k[i], s);
-#pragma unroll
-                for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (!there) s = -INFINITY;
-                const float top = fmaxf(m[y], fmaxf(fmaxf(s, __shfl_xor_sync(0xffffffffu, s, 8)), fmaxf(__shfl_xor_sync(0xffffffffu, s, 16), __shfl_xor_sync(0xffffffffu, s, 24))));
-                const float keep = top == -INFINITY ? 1.f : exp2f(m[y] - top), pr = top == -INFINITY ? (s == s ? 0.f : s) : exp2f(s - top);
-                m[y] = top;
-                l[y] = l[y] * keep + pr;
-#pragma unroll
-                for (int i = 0; i < N; ++i) acc[y][i] = acc[y][i] * keep + (there ? pr * v[i] : 0.f);   // a repeated row has no weight, but 0 x inf is not 0
-            }
-        }
-        const bool last = c.blk == c.s.n - 1;
-        if (last || t + 1 == t_end) {
-            const int64_t seg = w + (int64_t)c.hh * a.B + c.b;
-#pragma unroll
-            for (int y = 0; y < G; ++y) {
-#pragma unroll
-                for (int o = 8; o < 32; o <<= 1) {
-                    l[y] += __shfl_xor_sync(0xffffffffu, l[y], o);
-#pragma unroll
-                    for (int i = 0; i < N; ++i) acc[y][i] += __shfl_xor_sync(0xffffffffu, acc[y][i], o);
-                }
-                if (y < heads && sub == 0) {
-                    const float inv = 1.f / l[y];
-#pragma unroll
-                    for (int g = 0; g < NG; ++g)
-                        *reinterpret_cast<float4*>(ws + p.o + (seg * p.g_rows + y) * D + 32 * g + 4 * x) =
-                            make_float4(acc[y][4 * g] * inv, acc[y][4 * g + 1] * inv, acc[y][4 * g + 2] * inv, acc[y][4 * g + 3] * inv);
-                    if (x == 0) ws[p.lse + seg * p.g_rows + y] = m[y] + log2f(l[y]);
+            if (valid <= KV4_ROWS && a.k_new && gt == 0) {   // entry `tail` of the cache is read by nobody in this launch
+                constexpr int N = 16 / sizeof(T);
+                if (lane < D / N) {
+                    const int64_t from = ((int64_t)c.b * a.Hkv + h) * D / N + lane, to = (((int64_t)c.b * a.Hkv + h) * a.cap + c.s.tail) * D / N + lane;
+                    static_cast<uint4*>(a.k_tail)[to] = __ldg(static_cast<const uint4*>(a.k_new) + from);
+                    static_cast<uint4*>(a.v_tail)[to] = __ldg(static_cast<const uint4*>(a.v_new) + from);
                 }
             }
-            fresh = true;
         }
-        if (t + 1 == t_end) break;
-        if (last) kb.next_unit(c); else ++c.blk;
+        const int64_t seg = w + (int64_t)c.hh * a.B + c.b;
+#pragma unroll
+        for (int o = DUP; o < LH; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        l += __shfl_xor_sync(0xffffffffu, l, 8);
+        l += __shfl_xor_sync(0xffffffffu, l, 16);
+        if (sub == 0 && x % LH == 0 && x / LH < heads) ws[p.lse + seg * p.g_rows + x / LH] = ref + log2f(l);
+#pragma unroll
+        for (int y = 0; y < G; ++y) {
+            const float inv = 1.f / __shfl_sync(0xffffffffu, l, y * LH);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    acc[y][g][e] += __shfl_xor_sync(0xffffffffu, acc[y][g][e], 8);
+                    acc[y][g][e] += __shfl_xor_sync(0xffffffffu, acc[y][g][e], 16);
+                }
+                if (y < heads && sub == 0)
+                    *reinterpret_cast<float4*>(ws + p.o + (seg * p.g_rows + y) * D + 32 * g + 4 * x) =
+                        make_float4(acc[y][g][0] * inv, acc[y][g][1] * inv, acc[y][g][2] * inv, acc[y][g][3] * inv);
+            }
+        }
+        left -= blocks + tails;
+        if (left == 0) break;
+        kb.next_unit(c);
     }
 }
 
@@ -287,17 +410,11 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
 // to an accumulator of its own and into the scores times the row's step; for V the step goes into the weights, so P^T is
 // rounded once per group.  P^T changes from the accumulator's layout to the operand's with 8 x 8 transposes (movmatrix).
 //
-// Powers of two: a tile's numbers are n 2^-133 (n odd, up to 15; times 4 for odd e, see kv4.cuh).  Queries carry 2^64 (2^62 against
-// odd e), weights 2^80, so sums stay in the normal range: scores come out times 2^-69, outputs times 2^-53 (2^-51).  The factors
-// are exact and are taken off where memory ends and the tail begins (to_plain), or with the partial result.
+// A tile's numbers are n 2^-133 (n odd, up to 15; times 4 for odd e, see kv4.cuh); the powers of two that queries and weights carry are
+// exact and are taken off where memory ends and the tail begins (to_plain), or with the partial result.
 //
 // Row r of the scores is entry pi(r) = r ^ (r >> 1 & 1): with the chunks' places that spreads the four rows whose values a lane
 // needs over the banks of shared memory (D = 128: no conflict).
-constexpr float KV4_Q = 18446744073709551616.f;                    // 2^64
-constexpr float KV4_S = 590295810358705651712.f;                   // 2^69
-constexpr float KV4_O = 9007199254740992.f;                        // 2^53
-constexpr float KV4_P_LOG2 = 80.f, KV4_P_INV = 8.271806125530277e-25f;   // 2^-80
-
 template <int D>
 struct Kv4Ring {
     static constexpr int NS = D == 128 ? 3 : 6, STAGE = 2 * Kv4Tile<D>::BYTES, WARP = NS * STAGE, TOTAL = KV4_WARPS * WARP;
@@ -338,15 +455,6 @@ __device__ __forceinline__ void chunk_pair(const uint8_t* p, uint32_t (&w)[2][G 
     } else {
         const uint2 u = *reinterpret_cast<const uint2*>(p);
         w[0][0] = u.x; w[1][0] = u.y;
-    }
-}
-template <int G>
-__device__ __forceinline__ void one_chunk(const uint8_t* p, uint32_t (&w)[G / 2]) {
-    if constexpr (G == 4) {
-        const uint2 u = *reinterpret_cast<const uint2*>(p);
-        w[0] = u.x; w[1] = u.y;
-    } else {
-        w[0] = *reinterpret_cast<const uint32_t*>(p);
     }
 }
 __device__ __forceinline__ void group_pairs(int g, uint32_t a, uint32_t b, uint32_t ones, uint32_t (&p)[4]) {
@@ -570,10 +678,10 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 const uint8_t* tile = st + u * TL::BYTES;
                 uint32_t v0[G / 2], v1[G / 2], v2[G / 2], v3[G / 2];
                 float h0[G], h1[G];
-                one_chunk<G>(tile + TL::V + pv0 * TL::ROW + v_x, v0);
-                one_chunk<G>(tile + TL::V + pv1 * TL::ROW + v_x, v1);
-                one_chunk<G>(tile + TL::V + (pv0 + 8) * TL::ROW + v_x, v2);
-                one_chunk<G>(tile + TL::V + (pv1 + 8) * TL::ROW + v_x, v3);
+                halves<G>(tile + TL::V + pv0 * TL::ROW + v_x, v0);
+                halves<G>(tile + TL::V + pv1 * TL::ROW + v_x, v1);
+                halves<G>(tile + TL::V + (pv0 + 8) * TL::ROW + v_x, v2);
+                halves<G>(tile + TL::V + (pv1 + 8) * TL::ROW + v_x, v3);
                 steps_of<G>(tile + TL::V_STEPS + pr * TL::STEPS, h0);
                 steps_of<G>(tile + TL::V_STEPS + (pr + 8) * TL::STEPS, h1);
                 if (valid < KV4_STEP) {   // ... and 0 x NaN is not 0

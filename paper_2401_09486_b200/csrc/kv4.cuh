@@ -57,6 +57,7 @@ struct Kv4LoadArgs {
     void *k = nullptr, *v = nullptr;   // [B, Hkv, cap, D]
     const int32_t* mem_lens = nullptr;
     int B = 0, Hkv = 0, cap = 0;
+    uint32_t ones = 0x00010001u;       // see kv4_pairs
 };
 cudaError_t launch_kv4_append(const Kv4AppendArgs& a, int D, loma_dtype dt, cudaStream_t st);   // kv4_store.cu
 cudaError_t launch_kv4_load(const Kv4LoadArgs& a, int D, loma_dtype dt, cudaStream_t st);
@@ -103,6 +104,31 @@ __device__ __forceinline__ void kv4_pairs(uint32_t a, uint32_t b, uint32_t ones,
     p[1] = (u & 0x80388038u) | ones << 2;
     p[2] = ((w << 1) & 0x800E800Eu) | ones;
     p[3] = (w & 0x80388038u) | ones << 2;
+}
+// the same of one word: elements e of groups 2 i (low) and 2 i + 1 (high) of a chunk
+__device__ __forceinline__ void kv4_word(uint32_t u, uint32_t ones, uint32_t (&p)[4]) {
+    const uint32_t w = __byte_perm(u, 0, 0x2301);
+    p[0] = ((u << 1) & 0x800E800Eu) | ones;
+    p[1] = (u & 0x80388038u) | ones << 2;
+    p[2] = ((w << 1) & 0x800E800Eu) | ones;
+    p[3] = (w & 0x80388038u) | ones << 2;
+}
+// Powers of two that keep sums over these patterns in the normal range: queries carry 2^64 (2^62 against odd e), weights 2^80, so scores
+// come out times 2^-69 and outputs times 2^-53 (2^-51).
+constexpr float KV4_Q = 18446744073709551616.f;                    // 2^64
+constexpr float KV4_S = 590295810358705651712.f;                   // 2^69
+constexpr float KV4_O = 9007199254740992.f;                        // 2^53
+constexpr float KV4_P_LOG2 = 80.f, KV4_P_INV = 8.271806125530277e-25f;   // 2^-80
+
+// G half-words (a chunk's bytes, a row's steps) as words
+template <int G>
+__device__ __forceinline__ void halves(const uint8_t* p, uint32_t (&w)[G / 2]) {
+    if constexpr (G == 4) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        w[0] = u.x; w[1] = u.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
 }
 #endif
 

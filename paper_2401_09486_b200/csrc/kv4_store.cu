@@ -1,24 +1,16 @@
 // Memory entries into a 4-bit pool and back (loma_kv4_append, loma_kv4_load); format in kv4.cuh.
 //
-// Eight lanes share a row: lane x has features 32 g + 4 x .. + 3 of every group g, which are the four of a half-word, so a group's
-// maximum takes three shuffles and a lane writes one chunk of 8 (or 4) bytes.  Keys and values of an entry go together: eight
-// loads in flight per lane.  Both directions are bound by HBM: 256 bytes of bf16 against 72 for a row of 128 features.  The three
-// comparisons per value that make m (instead of a division) are exact and leave the arithmetic well below the time of the bytes.
+// Eight lanes share a row: lane x has features 32 g + 4 x .. + 3 of every group g, which are the four of a half-word, so a lane writes
+// one chunk of 8 (or 4) bytes.  Keys and values of an entry go together: eight loads in flight per lane, and the largest magnitudes of
+// the eight groups are found with results spread over the lanes (seven shuffles), so each lane works out one step.  Both directions are
+// bound by HBM (256 bytes of bf16 against 72 for a row of 128 features) as long as a value costs few instructions: m is the integer part
+// of |x| / (2 h), a product and an addition that rounds towards zero; see kv4_half for why that is exact.
 #include "kv4.cuh"
 
 namespace loma {
 
 constexpr int STORE_THREADS = 256, STORE_ROWS = STORE_THREADS / 8;   // rows a block takes at a time
 
-template <typename T>
-__device__ __forceinline__ float4 load4(const T* p);
-template <>
-__device__ __forceinline__ float4 load4(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
-template <>
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-    const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
-    return make_float4(bf16lo(u.x), bf16hi(u.x), bf16lo(u.y), bf16hi(u.y));
-}
 __device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 __device__ __forceinline__ void store4(__nv_bfloat16* p, float a, float b, float c, float d) {
     *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
@@ -29,49 +21,98 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // a NaN stays
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+__device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t sel) {   // selectors from 8 on: the byte's sign, eight times
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel));
+    return r;
+}
 
-// the step of a group whose largest magnitude is `top`, as bf16 bits
+// Four features as they were loaded; -0 becomes 0, which is held with a positive sign.
+template <typename T>
+struct Four;
+template <>
+struct Four<float> {
+    float x[4];
+    __device__ __forceinline__ void load(const float* p) {
+        const float4 u = __ldg(reinterpret_cast<const float4*>(p));
+        x[0] = u.x + 0.f; x[1] = u.y + 0.f; x[2] = u.z + 0.f; x[3] = u.w + 0.f;
+    }
+    __device__ __forceinline__ float top() const { return max_nan(max_nan(fabsf(x[0]), fabsf(x[1])), max_nan(fabsf(x[2]), fabsf(x[3]))); }
+    __device__ __forceinline__ float at(int i) const { return x[i]; }
+    // upper halves of features 2 i and 2 i + 1
+    __device__ __forceinline__ uint32_t signs(int i) const { return __byte_perm(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]), 0x7632); }
+};
+template <>
+struct Four<__nv_bfloat16> {
+    __nv_bfloat162 w[2];
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
+        const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+        w[0] = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&u.x), zero);
+        w[1] = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&u.y), zero);
+    }
+    __device__ __forceinline__ uint32_t signs(int i) const { return *reinterpret_cast<const uint32_t*>(&w[i]); }
+    __device__ __forceinline__ float top() const {
+        const __nv_bfloat162 m = __hmax2_nan(__habs2(w[0]), __habs2(w[1]));
+        const uint32_t u = *reinterpret_cast<const uint32_t*>(&m);
+        return max_nan(bf16lo(u), bf16hi(u));
+    }
+    __device__ __forceinline__ float at(int i) const { return i & 1 ? bf16hi(signs(i / 2)) : bf16lo(signs(i / 2)); }
+};
+
+// The step of a group whose largest magnitude is `top`, as bf16 bits.  For bf16 input the product with 1 / 15 will do: top has 8 bits, a
+// number half way between two bf16 has 9, so top / 15 misses it by 2^-13 of itself at least, and the product is off by 2^-23.
+template <typename T>
 __device__ __forceinline__ uint32_t kv4_step(float top) {
-    const __nv_bfloat16 h = __float2bfloat16_rn(__fdiv_rn(top, 15.f));
+    const __nv_bfloat16 h = __float2bfloat16_rn(sizeof(T) == 2 ? top * (1.f / 15.f) : __fdiv_rn(top, 15.f));
     const uint32_t bits = __bfloat16_as_ushort(h);
     return bits >= 0x7f80u ? 0x7fffu : bits < 0x0080u ? 0u : bits;
 }
 
-// sign and m of a value whose group has step h: |x| >= 8h, then 4h, then 2h; the differences are exact (the larger is at most
-// twice the smaller where they are taken, since |x| <= 15 h (1 + 2^-8) < 16 h)
-__device__ __forceinline__ uint32_t kv4_code(float x, float h) {
-    float a = fabsf(x);
-    uint32_t m = 0;
-    if (a >= 8.f * h) { m = 4; a -= 8.f * h; }
-    if (a >= 4.f * h) { m |= 2; a -= 4.f * h; }
-    if (a >= 2.f * h) m |= 1;
-    return h > 0.f ? m | (x < 0.f ? 8u : 0u) : 0u;
+// A half-word of four codes.  r is 1 / (2 h) and a little more (2^-20 of itself, the reciprocal and the product are off by 2^-22), so
+// t = |x| r is at least m, and its integer part is m, or m + 1 where |x| lies less than 2^-19 below 2 h (m + 1).  bf16 input does not
+// (8 bits against 11: the two differ by 2^-11 of themselves or not at all); for fp32 the sign of |x| - 2 h k, exact in one FMA, tells.
+// |x| <= 15 h (1 + 2^-8), so m <= 7.
+template <typename T>
+__device__ __forceinline__ uint32_t kv4_half(const Four<T>& f, float h) {
+    constexpr float BIG = 8388608.f;   // 2^23: sums with it have the integer part in their low bits
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(2.f * h));
+    r *= 1.f + 0x1p-20f;
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = fabsf(f.at(i)), t = __fadd_rz(__fmul_rn(a, r), BIG);
+        u[i] = __float_as_uint(t);
+        if constexpr (sizeof(T) == 4) u[i] -= __float_as_uint(fmaf(-2.f * h, t - BIG, a)) >> 31;
+    }
+    const uint32_t m = u[0] + 8 * u[1] + 256 * u[2] + 2048 * u[3];   // what is above the low 16 bits does not matter
+    // byte 0: signs of features 2 (bit 6) and 3 (bit 7), byte 1: of 0 and 1
+    const uint32_t lo = permute(f.signs(0), f.signs(1), 0x009d), hi = permute(f.signs(0), f.signs(1), 0x00bf);
+    return h > 0.f ? (m & 0x3f3fu) | (lo & 0x4040u) | (hi & 0x8080u) : 0u;
 }
-// a half-word of four codes
-__device__ __forceinline__ uint32_t kv4_half(const float4& x, float h) {
-    const uint32_t c0 = kv4_code(x.x, h), c1 = kv4_code(x.y, h), c2 = kv4_code(x.z, h), c3 = kv4_code(x.w, h);
-    return (c0 & 7) | (c1 & 7) << 3 | (c2 >> 3) << 6 | (c3 >> 3) << 7 | (c2 & 7) << 8 | (c3 & 7) << 11 | (c0 >> 3) << 14 | (c1 >> 3) << 15;
-}
-__device__ __forceinline__ float kv4_value(uint32_t m, uint32_t sign, float h) {
-    const float v = (float)(2 * m + 1) * h;
-    return sign ? -v : v;
+
+// maxima over eight lanes of M values each; lane x keeps value x * M / 8
+template <int M, int O>
+__device__ __forceinline__ void spread_max8(float* s, int x, unsigned lanes) {
+    if constexpr (M > 1) {
+        const bool up = x & O;
+#pragma unroll
+        for (int i = 0; i < M / 2; ++i) {
+            const float lo = s[i], hi = s[i + M / 2];
+            s[i] = max_nan(up ? hi : lo, __shfl_xor_sync(lanes, up ? lo : hi, O));
+        }
+    } else {
+        s[0] = max_nan(s[0], __shfl_xor_sync(lanes, s[0], O));
+    }
+    if constexpr (O > 1) spread_max8<(M > 1 ? M / 2 : 1), O / 2>(s, x, lanes);
 }
 
 // G half-words: a chunk's bytes, or a row's steps
 template <int G>
-__device__ __forceinline__ void put_halves(uint8_t* p, const uint32_t (&w)[G]) {
-    if constexpr (G == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
-    else *reinterpret_cast<uint32_t*>(p) = w[0] | w[1] << 16;
-}
-template <int G>
-__device__ __forceinline__ void get_halves(const uint8_t* p, uint32_t (&w)[G]) {
-    if constexpr (G == 4) {
-        const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
-        w[0] = u.x & 0xffff; w[1] = u.x >> 16; w[2] = u.y & 0xffff; w[3] = u.y >> 16;
-    } else {
-        const uint32_t u = __ldg(reinterpret_cast<const uint32_t*>(p));
-        w[0] = u & 0xffff; w[1] = u >> 16;
-    }
+__device__ __forceinline__ void put_halves(uint8_t* p, const uint32_t (&w)[G / 2]) {
+    if constexpr (G == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(p) = w[0];
 }
 
 template <typename T, int D>
@@ -92,28 +133,31 @@ __global__ void __launch_bounds__(STORE_THREADS) kv4_append_kernel(const Kv4Appe
         if (page < 0) continue;
         const T* k = static_cast<const T*>(a.k) + b * a.k_stride[0] + h * a.k_stride[1] + i * a.k_stride[2] + 4 * x;
         const T* v = static_cast<const T*>(a.v) + b * a.v_stride[0] + h * a.v_stride[1] + i * a.v_stride[2] + 4 * x;
-        float4 f[2][G];
+        Four<T> f[2][G];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            f[0][g] = load4(k + 32 * g);
-            f[1][g] = load4(v + 32 * g);
+            f[0][g].load(k + 32 * g);
+            f[1][g].load(v + 32 * g);
         }
         uint8_t* tile = a.m.pool + kv4_tile<D>(a.m, a.Hkv, page, h, (int)j);
         const int row = (int)j & 15;
+        float top[2 * G];
+#pragma unroll
+        for (int i = 0; i < 2 * G; ++i) top[i] = f[i / G][i % G].top();
+        spread_max8<2 * G, 4>(top, x, mine);   // lane x: of group x G / 4 (keys' groups, then values')
+        const uint32_t bits = kv4_step<T>(top[0]), other = __shfl_xor_sync(mine, bits, 4 / G);
+        const uint32_t two = x & (4 / G) ? other | bits << 16 : bits | other << 16;
+        uint32_t step[2][G / 2];
+#pragma unroll
+        for (int i = 0; i < G; ++i) step[i / (G / 2)][i % (G / 2)] = __shfl_sync(mine, two, i * (8 / G), 8);
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-            uint32_t half[G], step[G];
+            uint32_t half[G / 2];
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const float4& y = f[w][g];
-                float top = max_nan(max_nan(fabsf(y.x), fabsf(y.y)), max_nan(fabsf(y.z), fabsf(y.w)));
-#pragma unroll
-                for (int o = 1; o < 8; o <<= 1) top = max_nan(top, __shfl_xor_sync(mine, top, o));
-                step[g] = kv4_step(top);
-                half[g] = kv4_half(y, __uint_as_float(step[g] << 16));
-            }
+            for (int i = 0; i < G / 2; ++i)
+                half[i] = kv4_half(f[w][2 * i], bf16lo(step[w][i])) | kv4_half(f[w][2 * i + 1], bf16hi(step[w][i])) << 16;
             put_halves<G>(tile + w * TL::V + kv4_chunk<D>(row, x), half);
-            if (x == 0) put_halves<G>(tile + TL::K_STEPS + w * (TL::V_STEPS - TL::K_STEPS) + row * TL::STEPS, step);
+            if (x == w) put_halves<G>(tile + TL::K_STEPS + w * (TL::V_STEPS - TL::K_STEPS) + row * TL::STEPS, step[w]);
         }
     }
 }
@@ -132,21 +176,24 @@ __global__ void __launch_bounds__(STORE_THREADS) kv4_load_kernel(const Kv4LoadAr
         const int page = min(max(__ldg(a.m.table + (int64_t)b * a.m.max_pages + (j >> a.m.log2_ps)), 0), a.m.n_pages - 1);
         const uint8_t* tile = a.m.pool + kv4_tile<D>(a.m, a.Hkv, page, h, j);
         const int row = j & 15;
-        uint32_t half[2][G], step[2][G];
+        uint32_t half[2][G / 2], step[2][G / 2];
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-            get_halves<G>(tile + w * TL::V + kv4_chunk<D>(row, x), half[w]);
-            get_halves<G>(tile + TL::K_STEPS + w * (TL::V_STEPS - TL::K_STEPS) + row * TL::STEPS, step[w]);
+            halves<G>(tile + w * TL::V + kv4_chunk<D>(row, x), half[w]);
+            halves<G>(tile + TL::K_STEPS + w * (TL::V_STEPS - TL::K_STEPS) + row * TL::STEPS, step[w]);
         }
+        // n 2^-133 times 2^127, the step and 2^6 (2^4 for odd e): exact in this order, whatever the step
+        constexpr float UP = 1.7014118346046923e38f;   // 2^127
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
             T* out = static_cast<T*>(w ? a.v : a.k) + (bh * a.cap + j) * D + 4 * x;
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const uint32_t y = half[w][g];
-                const float s = __uint_as_float(step[w][g] << 16);
-                store4(out + 32 * g, kv4_value(y & 7, y >> 14 & 1, s), kv4_value(y >> 3 & 7, y >> 15 & 1, s), kv4_value(y >> 8 & 7, y >> 6 & 1, s),
-                       kv4_value(y >> 11 & 7, y >> 7 & 1, s));
+            for (int g = 0; g < G; g += 2) {
+                uint32_t n[4];
+                kv4_word(half[w][g / 2], a.ones, n);
+                const float h0 = bf16lo(step[w][g / 2]), h1 = bf16hi(step[w][g / 2]);
+                store4(out + 32 * g, bf16lo(n[0]) * UP * h0 * 64.f, bf16lo(n[1]) * UP * h0 * 16.f, bf16lo(n[2]) * UP * h0 * 64.f, bf16lo(n[3]) * UP * h0 * 16.f);
+                store4(out + 32 * g + 32, bf16hi(n[0]) * UP * h1 * 64.f, bf16hi(n[1]) * UP * h1 * 16.f, bf16hi(n[2]) * UP * h1 * 64.f, bf16hi(n[3]) * UP * h1 * 16.f);
             }
         }
     }
