@@ -188,103 +188,169 @@ void host_paged_compact(const CompactArgs& a) {
 }
 
 // ------------------------------------------------------------------ device forms
-constexpr int PG_CTAS = 8, PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32, PG_ALL = PG_CTAS * PG_THREADS;
+constexpr int PG_CTAS = 8, PG_THREADS = 1024, PG_WARPS = PG_THREADS / 32, PG_ALL = PG_CTAS * PG_THREADS, PG_ALL_WARPS = PG_CTAS * PG_WARPS;
 
-// A CTA's part [lo, hi) of n things
+// A CTA's part [lo, hi) of n things, in units of `unit`
 struct Part {
     int64_t lo, hi;
-    __device__ __forceinline__ Part(int64_t n, int rank) {
-        const int64_t per = (n + PG_CTAS - 1) / PG_CTAS;
+    __device__ __forceinline__ Part(int64_t n, int unit, int rank) {
+        const int64_t per = ((n + unit - 1) / unit + PG_CTAS - 1) / PG_CTAS * unit;
         lo = min(per * rank, n);
         hi = min(lo + per, n);
     }
 };
 
-// Exclusive sums over the block of one number per thread, and the block's total.  Ends with a barrier before the next use.
-__device__ __forceinline__ int64_t block_sums(int64_t x, int64_t* total) {
-    __shared__ int64_t s_warp[PG_WARPS];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__device__ __forceinline__ int64_t warp_exclusive(int64_t x, int64_t* total) {
+    const int lane = threadIdx.x & 31;
     int64_t incl = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += u;
     }
+    *total = __shfl_sync(0xffffffffu, incl, 31);
+    return incl - x;
+}
+
+// Exclusive sums over the warps of a block of one number per warp (the same in all its lanes), and the total.
+__device__ __forceinline__ int64_t block_sums(int64_t of_warp, int64_t* total) {
+    __shared__ int64_t s_warp[PG_WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __syncthreads();
-    if (lane == 31) s_warp[warp] = incl;
+    if (lane == 0) s_warp[warp] = of_warp;
     __syncthreads();
-    int64_t before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < PG_WARPS; ++w) {
-        const int64_t s = s_warp[w];
-        before += w < warp ? s : 0;
-        all += s;
+    const int64_t before = warp_exclusive(s_warp[lane], total);   // one per lane: PG_WARPS is 32
+    return __shfl_sync(0xffffffffu, before, warp);
+}
+
+// Two numbers of each CTA to every CTA, and a barrier of the cluster; then the sums of the lower ranks' and of everyone's.
+// slot: in shared memory, one set per exchange.
+struct Exchange {
+    int64_t slot[2][PG_CTAS];
+    __device__ __forceinline__ void put(cg::cluster_group& cl, int64_t x, int64_t y) {
+        const int rank = cl.block_rank();
+        if (threadIdx.x < 2 * PG_CTAS) {
+            const int i = threadIdx.x / PG_CTAS, to = threadIdx.x % PG_CTAS;
+            *cl.map_shared_rank(&slot[i][rank], to) = i ? y : x;
+        }
+        cl.sync();
     }
-    *total = all;
-    return before + incl - x;
-}
-
-// Each CTA's number to every CTA; returns the sum of the lower ranks' and, in *all, of everyone's.  slot: PG_CTAS int64 in shared
-// memory, one set per exchange.  A barrier of the cluster.
-__device__ __forceinline__ int64_t exchange(cg::cluster_group& cl, int64_t* slot, int64_t mine, int64_t* all) {
-    const int rank = cl.block_rank();
-    if (threadIdx.x < PG_CTAS) *cl.map_shared_rank(slot + rank, threadIdx.x) = mine;
-    cl.sync();
-    int64_t before = 0, sum = 0;
+    __device__ __forceinline__ int64_t get(int i, int rank, int64_t* all) const {
+        int64_t before = 0, sum = 0;
 #pragma unroll
-    for (int r = 0; r < PG_CTAS; ++r) {
-        const int64_t s = slot[r];
-        before += r < rank ? s : 0;
-        sum += s;
+        for (int r = 0; r < PG_CTAS; ++r) {
+            before += r < rank ? slot[i][r] : 0;
+            sum += slot[i][r];
+        }
+        *all = sum;
+        return before;
     }
-    *all = sum;
-    return before;
-}
+};
 
-constexpr int PG_RUN = 8;   // consecutive pages to a thread
+// Pages of a CTA's part by words of 32, a word to a warp at a time: a lane loads one page's number, a ballot makes the word, and the words'
+// counts are summed up over the block.  N kinds of pages are told apart at once.
+template <int N>
+struct Words {
+    static constexpr int MAX = 2048;        // words at a time: pools of up to 8 x 65536 pages are looked at once
+    unsigned mask[N][MAX];
+    int before[N][MAX];                     // pages of the kind in the words before
 
-// bit i: page first + i (below end) has a count below 0
-__device__ __forceinline__ unsigned unowned(const PageList& pl, int64_t first, int64_t end) {
-    unsigned bits = 0;
+    // words of pages [lo, hi); kind(value, k) says whether a page belongs to kind k.  Ends with a barrier.
+    template <typename F>
+    __device__ __forceinline__ void fill(const int32_t* values, int64_t lo, int64_t hi, F&& kind) {
+        constexpr int AHEAD = 8;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, words = (int)((hi - lo + 31) / 32);
+        for (int w0 = warp; w0 < words; w0 += PG_WARPS * AHEAD) {
+            int v[AHEAD];
 #pragma unroll
-    for (int i = 0; i < PG_RUN; ++i)
-        if (first + i < end && __ldcg(pl.refs + first + i) < 0) bits |= 1u << i;
-    return bits;
-}
-
-// As host_settle, by all CTAs, after the counts are complete (a barrier of the cluster before); *taken becomes the list's new start.
-// Another barrier makes the list visible.
-__device__ __forceinline__ int64_t settle(cg::cluster_group& cl, const PageList& pl, int64_t* slot, int* taken, int64_t* lost) {
-    const Part part(pl.n_pages, cl.block_rank());
-    int64_t mine = 0, total = 0, all;
-    for (int64_t p = part.lo + threadIdx.x * PG_RUN; p < part.hi; p += PG_THREADS * PG_RUN) mine += __popc(unowned(pl, p, part.hi));
-    block_sums(mine, &total);
-    int64_t at = exchange(cl, slot, total, &all);
-    const int64_t n = min(all, (int64_t)*taken);
-    if (total > 0)
-        for (int64_t base = part.lo; base < part.hi; base += PG_THREADS * PG_RUN) {
-            const int64_t p = base + threadIdx.x * PG_RUN;
-            unsigned bits = unowned(pl, p, part.hi);
-            int64_t here;
-            int64_t i = at + block_sums(__popc(bits), &here);
-            at += here;
-            for (; bits; bits &= bits - 1, ++i) {
-                const int64_t page = p + __ffs(bits) - 1;
-                pl.refs[page] = 0;
-                if (i < n) pl.free_pages[*taken - n + i] = (int)page;
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t p = lo + (int64_t)(w0 + u * PG_WARPS) * 32 + lane;
+                v[u] = p < hi ? __ldcg(values + p) : 0;          // 0: of no kind
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int w = w0 + u * PG_WARPS;
+                if (w >= words) break;
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const unsigned m = __ballot_sync(0xffffffffu, kind(v[u], k));
+                    if (lane == 0) mask[k][w] = m;
+                }
             }
         }
-    *lost = all - n;
-    *taken -= (int)n;
-    return all;
+        __syncthreads();
+    }
+    // the sums; total[k]: pages of kind k.  Ends with a barrier.
+    __device__ __forceinline__ void sum(int words, int64_t (&total)[N]) {
+        constexpr int PER = MAX / PG_THREADS;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            int n[PER];
+            int64_t mine = 0, of_warp;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int w = threadIdx.x * PER + i;
+                n[i] = w < words ? __popc(mask[k][w]) : 0;
+                mine += n[i];
+            }
+            const int64_t in_warp = warp_exclusive(mine, &of_warp);
+            int at = (int)(block_sums(of_warp, &total[k]) + in_warp);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int w = threadIdx.x * PER + i;
+                if (w < words) before[k][w] = at;
+                at += n[i];
+            }
+        }
+        __syncthreads();
+    }
+};
+// the part [lo, hi) in stretches that fit
+template <typename F>
+__device__ __forceinline__ void stretches(const Part& part, F&& body) {
+    constexpr int64_t STEP = 32 * Words<1>::MAX;
+    for (int64_t lo = part.lo; lo < part.hi; lo += STEP) body(lo, min(lo + STEP, part.hi), part.hi - part.lo > STEP);
 }
 
-__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) paged_release_kernel(const ReleaseArgs a) {
-    cg::cluster_group cl = cg::this_cluster();
-    __shared__ int64_t slot[PG_CTAS];
-    const int lane = threadIdx.x & 31, warps = PG_CTAS * PG_WARPS;
-    const int first = (threadIdx.x >> 5) * PG_CTAS + cl.block_rank();   // a warp to a row, neighbours on different SMs
-    int taken = start_of(a.pl, __ldcg(a.pl.taken));
+// The pages without an owner, numbered by all CTAs.  count() needs the owners' counts complete (a barrier of the cluster before); between
+// it and write() the CTAs' totals are exchanged.
+struct Settle {
+    Words<1>& words;
+    const Part part;
+    __device__ __forceinline__ Settle(Words<1>& w, const PageList& pl, int rank) : words(w), part(pl.n_pages, 32, rank) {}
+
+    __device__ __forceinline__ int64_t look(const PageList& pl, int64_t lo, int64_t hi) const {
+        int64_t total[1];
+        words.fill(pl.refs, lo, hi, [](int v, int) { return v < 0; });
+        words.sum((int)((hi - lo + 31) / 32), total);
+        return total[0];
+    }
+    __device__ __forceinline__ int64_t count(const PageList& pl) const {
+        int64_t n = 0;
+        stretches(part, [&](int64_t lo, int64_t hi, bool) { n += look(pl, lo, hi); });
+        return n;
+    }
+    // `at`: the number of this CTA's first page; the first n of all go to the places in front of `taken`
+    __device__ __forceinline__ void write(const PageList& pl, int64_t at, int64_t n, int taken) const {
+        const int lane = threadIdx.x & 31;
+        stretches(part, [&](int64_t lo, int64_t hi, bool again) {
+            const int64_t here = again ? look(pl, lo, hi) : 0;
+            for (int w = threadIdx.x >> 5; w < (hi - lo + 31) / 32; w += PG_WARPS) {
+                const unsigned m = words.mask[0][w];
+                if (!(m >> lane & 1)) continue;
+                const int64_t k = at + words.before[0][w] + __popc(m & ((1u << lane) - 1)), page = lo + w * 32 + lane;
+                pl.refs[page] = 0;
+                if (k < n) pl.free_pages[taken - n + k] = (int)page;
+            }
+            at += here;
+            if (again) __syncthreads();
+        });
+    }
+};
+
+// rows of a release: a warp to a row at a time
+__device__ __forceinline__ void drop_rows(const ReleaseArgs& a, int first, int warps) {
+    const int lane = threadIdx.x & 31;
     int keep = 0, held = 0;
     if (first < a.B) { keep = __ldg(a.keep_lens + first); held = __ldcg(a.held + first); }
     for (int b = first; b < a.B; b += warps) {
@@ -299,39 +365,70 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
         }
         if (lane == 0) a.held_out[b] = kept;
     }
+}
+
+// Batches of more rows than a cluster has warps let go of their pages in a launch of their own, over all SMs.
+constexpr int DROP_THREADS = 256;
+__global__ void __launch_bounds__(DROP_THREADS) paged_drop_kernel(const ReleaseArgs a) {
+    let_next_start();
+    drop_rows(a, (threadIdx.x >> 5) * gridDim.x + blockIdx.x, gridDim.x * (DROP_THREADS / 32));
+}
+
+template <bool DROPPED>
+__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) paged_release_kernel(const ReleaseArgs a) {
+    cg::cluster_group cl = cg::this_cluster();
+    __shared__ Exchange ex;
+    __shared__ Words<1> words;
+    const int rank = cl.block_rank();
+    if constexpr (DROPPED) wait_for_previous();
+    const int taken = start_of(a.pl, __ldcg(a.pl.taken));
+    if constexpr (!DROPPED) drop_rows(a, (threadIdx.x >> 5) * PG_CTAS + rank, PG_ALL_WARPS);   // neighbours on different SMs
     cl.sync();
-    int64_t lost;
-    const int64_t freed = settle(cl, a.pl, slot, &taken, &lost);
-    if (cl.block_rank() == 0 && threadIdx.x == 0) {
-        *a.pl.taken = taken;
+    const Settle s(words, a.pl, rank);
+    int64_t freed;
+    const int64_t mine = s.count(a.pl);
+    ex.put(cl, mine, 0);
+    const int64_t at = ex.get(0, rank, &freed), n = min(freed, (int64_t)taken);
+    if (mine > 0) s.write(a.pl, at, n, taken);
+    if (rank == 0 && threadIdx.x == 0) {
+        *a.pl.taken = (int)(taken - n);
         a.counts[0] = 0;
         a.counts[1] = saturate(freed);
-        a.counts[2] = saturate(lost);
+        a.counts[2] = saturate(freed - n);
         a.counts[3] = 0;
     }
 }
 
+// Up to FORK_LOCAL sequences every CTA counts all children for itself, in shared memory; longer batches do it together, in the workspace.
+constexpr int FORK_LOCAL = 2048;
+
 __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) paged_fork_kernel(const ForkArgs a) {
     cg::cluster_group cl = cg::this_cluster();
-    __shared__ int64_t slot[2][PG_CTAS];
-    const int rank = cl.block_rank(), lane = threadIdx.x & 31, warps = PG_CTAS * PG_WARPS;
-    const int first = (threadIdx.x >> 5) * PG_CTAS + rank;
+    __shared__ Exchange ex;
+    __shared__ Words<1> words;
+    __shared__ int32_t s_kids[FORK_LOCAL], s_heir[FORK_LOCAL], s_start[FORK_LOCAL / PG_CTAS];
+    const int rank = cl.block_rank(), lane = threadIdx.x & 31, first = (threadIdx.x >> 5) * PG_CTAS + rank;
     const int64_t me = (int64_t)rank * PG_THREADS + threadIdx.x;
-    int32_t *kids = a.ws, *heir = a.ws + a.B;
-    int taken = start_of(a.pl, __ldcg(a.pl.taken));
-    for (int64_t b = me; b < a.B; b += PG_ALL) { kids[b] = 0; heir[b] = INT_MAX; }
-    cl.sync();
-    for (int64_t b = me; b < a.B; b += PG_ALL) {
+    const bool local = a.B <= FORK_LOCAL;
+    int32_t *kids = local ? s_kids : a.ws, *heir = local ? s_heir : a.ws + a.B;
+    const int64_t b0 = local ? threadIdx.x : me, step = local ? PG_THREADS : PG_ALL;
+    auto together = [&] { if (local) __syncthreads(); else cl.sync(); };
+    const int taken = start_of(a.pl, __ldcg(a.pl.taken));
+    for (int64_t b = b0; b < a.B; b += step) { kids[b] = 0; heir[b] = INT_MAX; }
+    together();
+    for (int64_t b = b0; b < a.B; b += step) {
         const int p = fork_from(a, (int)b);
         if (p < 0) continue;
         atomicAdd(kids + p, 1);
         atomicMin(heir + p, b == p ? -1 : (int)b);
     }
-    cl.sync();
+    together();
+    auto kids_of = [&](int r) { return local ? kids[r] : __ldcg(kids + r); };
+    auto is_heir = [&](int b, int r) { return (local ? heir[r] : __ldcg(heir + r)) == (b == r ? -1 : b); };
     // owners gained and lost
-    for (int r = first; r < a.B; r += warps) {
+    for (int r = first; r < a.B; r += PG_ALL_WARPS) {
         const Parent p = fork_parent(a, r);
-        const int k = __ldcg(kids + r), n = k > 0 ? p.share : p.held;
+        const int k = kids_of(r), n = k > 0 ? p.share : p.held;
         if (k == 1) continue;
         const int32_t* row = a.block_table + (int64_t)r * a.max_pages;
 #pragma unroll 4
@@ -340,31 +437,37 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
             if (in_pool(a.pl, page)) atomicAdd(a.pl.refs + page, k - 1);
         }
     }
-    // pages to draw: this CTA's rows, numbered from the first row of all on.  kids is done with: it takes the first number of a row
-    // (within this CTA's part)
-    const Part part(a.B, rank);
+    // pages to draw, numbered through this CTA's rows; with a batch in the workspace the numbers take the place of kids
     cl.sync();
-    int64_t need_before = 0;
+    const Part part(a.B, 1, rank);
+    int32_t* const start = local ? s_start : kids;
+    const int64_t start0 = local ? part.lo : 0;
+    int64_t need_all = 0;
     for (int64_t base = part.lo; base < part.hi; base += PG_THREADS) {
         const int64_t b = base + threadIdx.x;
         int need = 0;
         if (b < part.hi) {
             const int r = fork_from(a, (int)b);
-            if (r >= 0 && __ldcg(heir + r) != (b == r ? -1 : (int)b)) {
+            if (r >= 0 && !is_heir((int)b, r)) {
                 const Parent p = fork_parent(a, r);
-                need = p.used > p.share ? p.used - p.share : 0;
+                need = p.used - p.share;
             }
         }
-        int64_t total;
-        const int64_t at = need_before + block_sums(need, &total);
-        if (b < part.hi) kids[b] = saturate(at);
-        need_before += total;
+        int64_t of_warp, total;
+        const int64_t in_warp = warp_exclusive(need, &of_warp), before = block_sums(of_warp, &total);
+        if (b < part.hi) start[b - start0] = saturate(need_all + before + in_warp);
+        need_all += total;
     }
-    int64_t drawn, lost;
-    const int64_t draw0 = exchange(cl, slot[0], need_before, &drawn);
-    const int64_t freed = settle(cl, a.pl, slot[1], &taken, &lost);
-    cl.sync();
-    const int64_t room = min((int64_t)a.pl.n_free - taken, (int64_t)a.max_copies), got = min(drawn, room);
+    const Settle s(words, a.pl, rank);
+    int64_t freed, drawn;
+    const int64_t mine = s.count(a.pl);
+    ex.put(cl, mine, need_all);
+    const int64_t at = ex.get(0, rank, &freed), back = min(freed, (int64_t)taken), draw0 = ex.get(1, rank, &drawn);
+    if (mine > 0) s.write(a.pl, at, back, taken);
+    if (freed > 0) cl.sync();                    // pages that came back are drawn from
+    else __syncthreads();
+    const int from = (int)(taken - back);
+    const int64_t room = min((int64_t)a.pl.n_free - from, (int64_t)a.max_copies), got = min(drawn, room);
     for (int64_t b = part.lo + (threadIdx.x >> 5); b < part.hi; b += PG_WARPS) {
         const int r = fork_from(a, (int)b);
         int32_t* out = a.table_out + b * a.max_pages;
@@ -374,20 +477,20 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
             continue;
         }
         const Parent p = fork_parent(a, r);
-        const bool is_heir = __ldcg(heir + r) == (b == r ? -1 : (int)b);
+        const bool all = is_heir((int)b, r);
         const int32_t* row = a.block_table + (int64_t)r * a.max_pages;
-        const int named = is_heir ? p.held : p.share, used = is_heir ? p.held : p.used;
-        const int64_t start = draw0 + kids[b];   // written by this CTA
+        const int named = all ? p.held : p.share, used = all ? p.held : p.used;
+        const int64_t draw = draw0 + start[b - start0];
 #pragma unroll 4
         for (int j = lane; j < a.max_pages; j += 32) {
             int page = j < used ? __ldg(row + j) : -1;
             if (j >= named && j < used) {
-                const int64_t i = start + j - named;
-                const int from = page;
+                const int64_t i = draw + j - named;
+                const int was = page;
                 page = -1;
                 if (i < room) {
-                    page = __ldcg(a.pl.free_pages + taken + i);
-                    a.copy_src[i] = in_pool(a.pl, from) ? from : -1;
+                    page = __ldcg(a.pl.free_pages + from + i);
+                    a.copy_src[i] = in_pool(a.pl, was) ? was : -1;
                     a.copy_dst[i] = page;
                 }
             }
@@ -395,109 +498,149 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
         }
         if (lane == 0) {
             a.lens_out[b] = a.cache_lens[r];
-            a.held_out[b] = named + (int)min(max(room - start, (int64_t)0), (int64_t)(used - named));
+            a.held_out[b] = named + (int)min(max(room - draw, (int64_t)0), (int64_t)(used - named));
         }
     }
     for (int64_t i = got + me; i < a.max_copies; i += PG_ALL) a.copy_src[i] = a.copy_dst[i] = -1;
     if (rank == 0 && threadIdx.x == 0) {
-        *a.pl.taken = (int)(taken + got);
+        *a.pl.taken = (int)(from + got);
         a.counts[0] = saturate(got);
         a.counts[1] = saturate(freed);
-        a.counts[2] = saturate(lost);
+        a.counts[2] = saturate(freed - back);
         a.counts[3] = saturate(drawn - got);
     }
 }
 
-__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) paged_compact_kernel(const CompactArgs a) {
-    cg::cluster_group cl = cg::this_cluster();
-    __shared__ int64_t slot[3][PG_CTAS];
-    const PageList& pl = a.pl;
-    const int rank = cl.block_rank(), lane = threadIdx.x & 31, warps = PG_CTAS * PG_WARPS;
-    const int first = (threadIdx.x >> 5) * PG_CTAS + rank;
-    const int64_t me = (int64_t)rank * PG_THREADS + threadIdx.x;
-    int32_t* state = a.page_map;   // bit 0: free, bit 1: named
-    const int taken = start_of(pl, __ldcg(pl.taken));
-    for (int64_t p = me; p < pl.n_pages; p += PG_ALL) state[p] = 0;
-    cl.sync();
-    for (int64_t i = taken + me; i < pl.n_free; i += PG_ALL) {
-        const int p = pl.free_pages[i];
-        if (in_pool(pl, p)) atomicOr(state + p, 1);
+// Every page's state (bit 0: free, bit 1: named), in page_map, from the free list and the tables; and the tables' new numbers: an entry of
+// page_map is the page's new number, or -1 - i for the source of move i whose number has not been written yet.
+__device__ __forceinline__ void mark_pages(const CompactArgs& a, int64_t thread, int64_t threads, int warp, int warps) {
+    const int lane = threadIdx.x & 31;
+    for (int64_t i = start_of(a.pl, __ldcg(a.pl.taken)) + thread; i < a.pl.n_free; i += threads) {
+        const int p = a.pl.free_pages[i];
+        if (in_pool(a.pl, p)) atomicOr(a.page_map + p, 1);
     }
-    for (int b = first; b < a.B; b += warps) {
+    for (int b = warp; b < a.B; b += warps) {
         const int h = clampi(__ldg(a.held + b), 0, a.max_pages);
 #pragma unroll 4
         for (int j = lane; j < h; j += 32) {
             const int p = a.block_table[(int64_t)b * a.max_pages + j];
-            if (in_pool(pl, p)) atomicOr(state + p, 2);
+            if (in_pool(a.pl, p)) atomicOr(a.page_map + p, 2);
         }
+    }
+}
+__device__ __forceinline__ void rename_pages(const CompactArgs& a, int warp, int warps) {
+    const int lane = threadIdx.x & 31;
+    for (int b = warp; b < a.B; b += warps) {
+        const int h = clampi(__ldg(a.held + b), 0, a.max_pages);
+        int32_t* row = a.block_table + (int64_t)b * a.max_pages;
+#pragma unroll 4
+        for (int j = lane; j < h; j += 32) {
+            const int p = row[j];
+            if (!in_pool(a.pl, p)) continue;
+            const int to = __ldcg(a.page_map + p);
+            row[j] = to >= 0 ? to : __ldcg(a.copy_dst - 1 - to);
+        }
+    }
+}
+
+// Long batches and large pools: clearing, marking and renaming in launches of their own, over all SMs.
+constexpr int WIDE_THREADS = 256;
+__global__ void __launch_bounds__(WIDE_THREADS) paged_clear_kernel(const CompactArgs a) {
+    let_next_start();
+    for (int64_t p = (int64_t)blockIdx.x * WIDE_THREADS + threadIdx.x; p < a.pl.n_pages; p += (int64_t)gridDim.x * WIDE_THREADS) a.page_map[p] = 0;
+}
+__global__ void __launch_bounds__(WIDE_THREADS) paged_mark_kernel(const CompactArgs a) {
+    let_next_start();
+    wait_for_previous();
+    mark_pages(a, (int64_t)blockIdx.x * WIDE_THREADS + threadIdx.x, (int64_t)gridDim.x * WIDE_THREADS, (threadIdx.x >> 5) * gridDim.x + blockIdx.x,
+               gridDim.x * (WIDE_THREADS / 32));
+}
+__global__ void __launch_bounds__(WIDE_THREADS) paged_rename_kernel(const CompactArgs a) {
+    wait_for_previous();
+    if (__ldcg(a.counts) > 0) rename_pages(a, (threadIdx.x >> 5) * gridDim.x + blockIdx.x, gridDim.x * (WIDE_THREADS / 32));
+}
+
+template <bool WIDE>
+__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) paged_compact_kernel(const CompactArgs a) {
+    cg::cluster_group cl = cg::this_cluster();
+    __shared__ Exchange ex[2];
+    __shared__ Words<2> words;
+    const PageList& pl = a.pl;
+    const int rank = cl.block_rank(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first_row = warp * PG_CTAS + rank;
+    const int64_t me = (int64_t)rank * PG_THREADS + threadIdx.x;
+    int32_t* state = a.page_map;
+    if constexpr (WIDE) {
+        let_next_start();
+        wait_for_previous();
+    } else {
+        for (int64_t p = me; p < pl.n_pages; p += PG_ALL) state[p] = 0;
+        cl.sync();
+        mark_pages(a, me, PG_ALL, first_row, PG_ALL_WARPS);
     }
     cl.sync();
-    // bits of PG_RUN pages: free ones in the low half, named ones in the high half
-    const Part part(pl.n_pages, rank);
-    auto run_of = [&](int64_t p) {
-        unsigned bits = 0;
-#pragma unroll
-        for (int i = 0; i < PG_RUN; ++i)
-            if (p + i < part.hi) {
-                const int s = __ldcg(state + p + i);
-                bits |= s & 2 ? 0x10000u << i : (unsigned)(s & 1) << i;
-            }
-        return bits;
+    const Part part(pl.n_pages, 32, rank);
+    // kind 0: named, kind 1: free and not named
+    auto look = [&](int64_t lo, int64_t hi, int64_t (&total)[2]) {
+        words.fill(state, lo, hi, [](int v, int k) { return k == 0 ? (v & 2) != 0 : v == 1; });
+        words.sum((int)((hi - lo + 31) / 32), total);
     };
-    int64_t mine_f = 0, mine_n = 0, tot_f, tot_n, all_f, all_n;
-    for (int64_t p = part.lo + threadIdx.x * PG_RUN; p < part.hi; p += PG_THREADS * PG_RUN) {
-        const unsigned bits = run_of(p);
-        mine_f += __popc(bits & 0xffff);
-        mine_n += __popc(bits >> 16);
-    }
-    block_sums(mine_f, &tot_f);
-    block_sums(mine_n, &tot_n);
-    if (threadIdx.x < PG_CTAS) *cl.map_shared_rank(&slot[0][rank], threadIdx.x) = tot_f;
-    int64_t n0 = exchange(cl, slot[1], tot_n, &all_n), f0 = 0;
-    all_f = 0;
-    for (int r = 0; r < PG_CTAS; ++r) {
-        f0 += r < rank ? slot[0][r] : 0;
-        all_f += slot[0][r];
-    }
+    int64_t mine_n = 0, mine_f = 0, all_n, all_f, here[2];
+    stretches(part, [&](int64_t lo, int64_t hi, bool) {
+        look(lo, hi, here);
+        mine_n += here[0];
+        mine_f += here[1];
+    });
+    ex[0].put(cl, mine_n, mine_f);
+    const int64_t n0 = ex[0].get(0, rank, &all_n), f0 = ex[0].get(1, rank, &all_f);
     // Of the pages that are free or named the lowest all_n are to be the named ones.  Page p, with f free and n named ones before it, is
     // among them if f + n < all_n.  Named pages above move, in order, to the free ones below.
-    int64_t above = 0, tot_above, moves;
-    for (int64_t base = part.lo, f = f0, n = n0; base < part.hi; base += PG_THREADS * PG_RUN) {
-        const int64_t p = base + threadIdx.x * PG_RUN;
-        const unsigned bits = p < part.hi ? run_of(p) : 0;
-        int64_t hf, hn;
-        int64_t pf = f + block_sums(__popc(bits & 0xffff), &hf), pn = n + block_sums(__popc(bits >> 16), &hn);
-        for (int i = 0; i < PG_RUN; ++i) {
-            if (bits >> (16 + i) & 1) { above += pf + pn >= all_n; ++pn; }
-            pf += bits >> i & 1;
-        }
-        f += hf;
-        n += hn;
+    int64_t above = 0, moves;
+    {
+        int64_t n = n0, f = f0, mine = 0;
+        stretches(part, [&](int64_t lo, int64_t hi, bool again) {
+            if (again) look(lo, hi, here);
+            for (int w = threadIdx.x; w < (hi - lo + 31) / 32; w += PG_THREADS) {
+                const unsigned named = words.mask[0][w], free = words.mask[1][w];
+                const int64_t before = n + words.before[0][w] + f + words.before[1][w];
+                if (before + __popc(named | free) <= all_n) continue;
+                for (unsigned m = named; m; m &= m - 1) mine += before + __popc((named | free) & ((m & -m) - 1)) >= all_n;
+            }
+            if (again) { n += here[0]; f += here[1]; __syncthreads(); }
+        });
+        warp_exclusive(mine, &mine);
+        block_sums(mine, &above);
     }
-    block_sums(above, &tot_above);
-    exchange(cl, slot[2], tot_above, &moves);
+    ex[1].put(cl, above, 0);
+    ex[1].get(0, rank, &moves);
     const int64_t count = min(moves, (int64_t)a.max_copies), stay = all_n - moves;   // named pages below: their ranks are 0 .. stay - 1
-    for (int64_t base = part.lo, f = f0, n = n0; base < part.hi; base += PG_THREADS * PG_RUN) {
-        const int64_t p = base + threadIdx.x * PG_RUN;
-        const unsigned bits = p < part.hi ? run_of(p) : 0;
-        int64_t hf, hn;
-        int64_t pf = f + block_sums(__popc(bits & 0xffff), &hf), pn = n + block_sums(__popc(bits >> 16), &hn);
-        for (int i = 0; i < PG_RUN && p + i < part.hi; ++i) {
-            const int page = (int)(p + i);
-            const bool is_free = bits >> i & 1, is_named = bits >> (16 + i) & 1;
-            // of the free pages the first `count` become named (there are that many below), of the named ones those of rank stay ..
-            // stay + count - 1 become free
-            const bool to = is_free && pf < count, from = is_named && pn >= stay && pn - stay < count;
-            if (to) a.copy_dst[pf] = page;
-            if (from) a.copy_src[pn - stay] = page;
-            if ((is_free && !to) || from)
-                pl.free_pages[pl.n_free - all_f + pf - min(pf, count) + min(max(pn - stay, (int64_t)0), count)] = page;
-            state[page] = page;
-            pf += is_free;
-            pn += is_named;
-        }
-        f += hf;
-        n += hn;
+    {
+        int64_t n = n0, f = f0;
+        stretches(part, [&](int64_t lo, int64_t hi, bool again) {
+            if (again) look(lo, hi, here);
+            for (int w = warp; w < (hi - lo + 31) / 32; w += PG_WARPS) {
+                const int64_t page = lo + w * 32 + lane;
+                if (page >= hi) continue;
+                const unsigned wn = words.mask[0][w], wf = words.mask[1][w], below = (1u << lane) - 1;
+                const int64_t pn = n + words.before[0][w] + __popc(wn & below), pf = f + words.before[1][w] + __popc(wf & below);
+                const bool is_named = wn >> lane & 1, is_free = wf >> lane & 1;
+                // of the free pages the first `count` become named (there are that many below), of the named ones those of rank stay ..
+                // stay + count - 1 become free
+                const bool to = is_free && pf < count, from = is_named && pn >= stay && pn - stay < count;
+                if (to) a.copy_dst[pf] = (int)page;
+                if (from) a.copy_src[pn - stay] = (int)page;
+                if ((is_free && !to) || from)
+                    pl.free_pages[pl.n_free - all_f + pf - min(pf, count) + min(max(pn - stay, (int64_t)0), count)] = (int)page;
+                state[page] = from ? (int)(-1 - (pn - stay)) : (int)page;
+            }
+            if (again) { n += here[0]; f += here[1]; __syncthreads(); }
+        });
+    }
+    if (rank == 0 && threadIdx.x == 0) {
+        *pl.taken = (int)(pl.n_free - all_f);
+        a.counts[0] = saturate(count);
+        a.counts[1] = saturate(all_f);
+        a.counts[2] = saturate(all_n);
+        a.counts[3] = saturate(moves - count);
     }
     cl.sync();
     for (int64_t i = me; i < a.max_copies; i += PG_ALL) {
@@ -510,24 +653,7 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
             a.copy_src[i] = a.copy_dst[i] = -1;
         }
     }
-    cl.sync();
-    if (count > 0)
-        for (int b = first; b < a.B; b += warps) {
-            const int h = clampi(__ldg(a.held + b), 0, a.max_pages);
-            int32_t* row = a.block_table + (int64_t)b * a.max_pages;
-#pragma unroll 4
-            for (int j = lane; j < h; j += 32) {
-                const int p = row[j];
-                if (in_pool(pl, p)) row[j] = __ldcg(a.page_map + p);
-            }
-        }
-    if (rank == 0 && threadIdx.x == 0) {
-        *pl.taken = (int)(pl.n_free - all_f);
-        a.counts[0] = saturate(count);
-        a.counts[1] = saturate(all_f);
-        a.counts[2] = saturate(all_n);
-        a.counts[3] = saturate(moves - count);
-    }
+    if (!WIDE && count > 0) rename_pages(a, first_row, PG_ALL_WARPS);
 }
 
 // Copying: a warp takes 4 KB of one page of one pool at a time, eight 16-byte loads per lane in flight, then as many stores.
@@ -560,15 +686,27 @@ __global__ void __launch_bounds__(COPY_THREADS) paged_copy_kernel(const __grid_c
 }
 
 // ------------------------------------------------------------------ host side
-template <typename A>
-static cudaError_t launch_cluster(void (*kernel)(A), const A& a, cudaStream_t st) {
-    kernel<<<PG_CTAS, PG_THREADS, 0, st>>>(a);
-    count_launches(1);
-    return cudaGetLastError();
+// Rows to a cluster's warp beyond which the rows' own work goes over all SMs in launches of its own, each behind the other.
+constexpr int PG_ROWS = 1;
+
+cudaError_t launch_paged_release(const ReleaseArgs& a, cudaStream_t st) {
+    if (a.B <= PG_ROWS * PG_ALL_WARPS) return launch_behind(paged_release_kernel<false>, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
+    const unsigned grid = (unsigned)std::min(148 * 8, (a.B + DROP_THREADS / 32 - 1) / (DROP_THREADS / 32));
+    const cudaError_t e = launch_behind(paged_drop_kernel, dim3(grid), DROP_THREADS, 0, st, false, a);
+    return e == cudaSuccess ? launch_behind(paged_release_kernel<true>, dim3(PG_CTAS), PG_THREADS, 0, st, true, a) : e;
 }
-cudaError_t launch_paged_release(const ReleaseArgs& a, cudaStream_t st) { return launch_cluster(paged_release_kernel, a, st); }
-cudaError_t launch_paged_fork(const ForkArgs& a, cudaStream_t st) { return launch_cluster(paged_fork_kernel, a, st); }
-cudaError_t launch_paged_compact(const CompactArgs& a, cudaStream_t st) { return launch_cluster(paged_compact_kernel, a, st); }
+cudaError_t launch_paged_fork(const ForkArgs& a, cudaStream_t st) {
+    return launch_behind(paged_fork_kernel, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
+}
+cudaError_t launch_paged_compact(const CompactArgs& a, cudaStream_t st) {
+    if (a.B <= PG_ROWS * PG_ALL_WARPS) return launch_behind(paged_compact_kernel<false>, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
+    const dim3 grid(148 * 4);
+    cudaError_t e = launch_behind(paged_clear_kernel, grid, WIDE_THREADS, 0, st, false, a);
+    if (e == cudaSuccess) e = launch_behind(paged_mark_kernel, grid, WIDE_THREADS, 0, st, true, a);
+    if (e == cudaSuccess) e = launch_behind(paged_compact_kernel<true>, dim3(PG_CTAS), PG_THREADS, 0, st, true, a);
+    if (e == cudaSuccess) e = launch_behind(paged_rename_kernel, grid, WIDE_THREADS, 0, st, true, a);
+    return e;
+}
 cudaError_t launch_paged_copy(const CopyArgs& a, cudaStream_t st) {
     paged_copy_kernel<<<COPY_CTAS, COPY_THREADS, 0, st>>>(a);
     count_launches(1);
