@@ -399,34 +399,16 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
     }
 }
 
-// Up to FORK_LOCAL sequences every CTA counts all children for itself, in shared memory; longer batches do it together, in the workspace.
-constexpr int FORK_LOCAL = 2048;
+// Rows to a cluster's warp beyond which the rows' own work goes over all SMs in launches of its own, each behind the other.  Measured (us, one
+// launch against several, up to 1900 entries in pages of 16): 128 sequences: fork 15.9 / 18.0, release 10.1 / 9.6, compaction 25.7 / 26.3; 1000: fork
+// 30.9 / 24.2, release 17.8 / 14.1, compaction 107 / 81.
+constexpr int PG_ROWS = 1, PG_FEW = PG_ROWS * PG_ALL_WARPS;
 
-__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) paged_fork_kernel(const ForkArgs a) {
-    cg::cluster_group cl = cg::this_cluster();
-    __shared__ Exchange ex;
-    __shared__ Words<1> words;
-    __shared__ int32_t s_kids[FORK_LOCAL], s_heir[FORK_LOCAL], s_start[FORK_LOCAL / PG_CTAS];
-    const int rank = cl.block_rank(), lane = threadIdx.x & 31, first = (threadIdx.x >> 5) * PG_CTAS + rank;
-    const int64_t me = (int64_t)rank * PG_THREADS + threadIdx.x;
-    const bool local = a.B <= FORK_LOCAL;
-    int32_t *kids = local ? s_kids : a.ws, *heir = local ? s_heir : a.ws + a.B;
-    const int64_t b0 = local ? threadIdx.x : me, step = local ? PG_THREADS : PG_ALL;
-    auto together = [&] { if (local) __syncthreads(); else cl.sync(); };
-    const int taken = start_of(a.pl, __ldcg(a.pl.taken));
-    for (int64_t b = b0; b < a.B; b += step) { kids[b] = 0; heir[b] = INT_MAX; }
-    together();
-    for (int64_t b = b0; b < a.B; b += step) {
-        const int p = fork_from(a, (int)b);
-        if (p < 0) continue;
-        atomicAdd(kids + p, 1);
-        atomicMin(heir + p, b == p ? -1 : (int)b);
-    }
-    together();
-    auto kids_of = [&](int r) { return local ? kids[r] : __ldcg(kids + r); };
-    auto is_heir = [&](int b, int r) { return (local ? heir[r] : __ldcg(heir + r)) == (b == r ? -1 : b); };
-    // owners gained and lost
-    for (int r = first; r < a.B; r += PG_ALL_WARPS) {
+// rows' owners gained and lost; kids_of: children of a row
+template <typename F>
+__device__ __forceinline__ void change_owners(const ForkArgs& a, int first, int warps, F&& kids_of) {
+    const int lane = threadIdx.x & 31;
+    for (int r = first; r < a.B; r += warps) {
         const Parent p = fork_parent(a, r);
         const int k = kids_of(r), n = k > 0 ? p.share : p.held;
         if (k == 1) continue;
@@ -437,8 +419,77 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
             if (in_pool(a.pl, page)) atomicAdd(a.pl.refs + page, k - 1);
         }
     }
-    // pages to draw, numbered through this CTA's rows; with a batch in the workspace the numbers take the place of kids
-    cl.sync();
+}
+
+// One row of the new table by a warp.  r: its parent or -1; all: it takes over all the parent's pages; draw: the number of its first fresh
+// page, of which `room` can be had, from free_pages[from] on.
+__device__ __forceinline__ void write_row(const ForkArgs& a, int64_t b, int r, bool all, int64_t draw, int64_t room, int from) {
+    const int lane = threadIdx.x & 31;
+    int32_t* out = a.table_out + b * a.max_pages;
+    if (r < 0) {
+        for (int j = lane; j < a.max_pages; j += 32) out[j] = -1;
+        if (lane == 0) { a.lens_out[b] = -1; a.held_out[b] = 0; }
+        return;
+    }
+    const Parent p = fork_parent(a, r);
+    const int32_t* row = a.block_table + (int64_t)r * a.max_pages;
+    const int named = all ? p.held : p.share, used = all ? p.held : p.used;
+#pragma unroll 8
+    for (int j = lane; j < a.max_pages; j += 32) {
+        int page = j < used ? __ldg(row + j) : -1;
+        if (j >= named && j < used) {
+            const int64_t i = draw + j - named;
+            const int was = page;
+            page = -1;
+            if (i < room) {
+                page = __ldcg(a.pl.free_pages + from + i);
+                a.copy_src[i] = in_pool(a.pl, was) ? was : -1;
+                a.copy_dst[i] = page;
+            }
+        }
+        out[j] = page;
+    }
+    if (lane == 0) {
+        a.lens_out[b] = a.cache_lens[r];
+        a.held_out[b] = named + (int)min(max(room - draw, (int64_t)0), (int64_t)(used - named));
+    }
+}
+
+// One launch (ALL: up to PG_FEW rows, whose children every CTA counts for itself in shared memory), or the two parts that need every row's result, with owners and rows in launches over all SMs between and behind them:
+// COUNT (children and heirs into the workspace) and NUMBER (free pages, draws; the workspace's first half takes the draws' numbers).
+enum ForkPart { FORK_ALL, FORK_COUNT, FORK_NUMBER };
+
+template <int PART>
+__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) paged_fork_kernel(const ForkArgs a) {
+    cg::cluster_group cl = cg::this_cluster();
+    __shared__ Exchange ex;
+    __shared__ Words<1> words;
+    __shared__ int32_t s_kids[PG_FEW], s_heir[PG_FEW], s_start[PG_FEW / PG_CTAS];
+    const int rank = cl.block_rank();
+    const int64_t me = (int64_t)rank * PG_THREADS + threadIdx.x;
+    constexpr bool local = PART == FORK_ALL;
+    int32_t *kids = local ? s_kids : a.ws, *heir = local ? s_heir : a.ws + a.B;
+    let_next_start();
+    if constexpr (PART == FORK_NUMBER) wait_for_previous();
+    const int taken = start_of(a.pl, __ldcg(a.pl.taken));
+    if constexpr (PART != FORK_NUMBER) {
+        const int64_t b0 = local ? threadIdx.x : me, step = local ? PG_THREADS : PG_ALL;
+        auto together = [&] { if (local) __syncthreads(); else cl.sync(); };
+        for (int64_t b = b0; b < a.B; b += step) { kids[b] = 0; heir[b] = INT_MAX; }
+        together();
+        for (int64_t b = b0; b < a.B; b += step) {
+            const int p = fork_from(a, (int)b);
+            if (p < 0) continue;
+            atomicAdd(kids + p, 1);
+            atomicMin(heir + p, b == p ? -1 : (int)b);
+        }
+        if constexpr (PART == FORK_COUNT) return;
+        together();
+        change_owners(a, (threadIdx.x >> 5) * PG_CTAS + rank, PG_ALL_WARPS, [&](int r) { return local ? kids[r] : __ldcg(kids + r); });
+        cl.sync();
+    }
+    auto is_heir = [&](int b, int r) { return (local ? heir[r] : __ldcg(heir + r)) == (b == r ? -1 : b); };
+    // pages to draw, numbered through this CTA's rows; in the workspace the numbers take the place of kids
     const Part part(a.B, 1, rank);
     int32_t* const start = local ? s_start : kids;
     const int64_t start0 = local ? part.lo : 0;
@@ -464,42 +515,17 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
     ex.put(cl, mine, need_all);
     const int64_t at = ex.get(0, rank, &freed), back = min(freed, (int64_t)taken), draw0 = ex.get(1, rank, &drawn);
     if (mine > 0) s.write(a.pl, at, back, taken);
-    if (freed > 0) cl.sync();                    // pages that came back are drawn from
+    if (PART == FORK_ALL && freed > 0) cl.sync();        // pages that came back are drawn from
     else __syncthreads();
     const int from = (int)(taken - back);
     const int64_t room = min((int64_t)a.pl.n_free - from, (int64_t)a.max_copies), got = min(drawn, room);
-    for (int64_t b = part.lo + (threadIdx.x >> 5); b < part.hi; b += PG_WARPS) {
-        const int r = fork_from(a, (int)b);
-        int32_t* out = a.table_out + b * a.max_pages;
-        if (r < 0) {
-            for (int j = lane; j < a.max_pages; j += 32) out[j] = -1;
-            if (lane == 0) { a.lens_out[b] = -1; a.held_out[b] = 0; }
-            continue;
+    if constexpr (PART == FORK_ALL) {
+        for (int64_t b = part.lo + (threadIdx.x >> 5); b < part.hi; b += PG_WARPS) {
+            const int r = fork_from(a, (int)b);
+            write_row(a, b, r, r >= 0 && is_heir((int)b, r), draw0 + start[b - start0], room, from);
         }
-        const Parent p = fork_parent(a, r);
-        const bool all = is_heir((int)b, r);
-        const int32_t* row = a.block_table + (int64_t)r * a.max_pages;
-        const int named = all ? p.held : p.share, used = all ? p.held : p.used;
-        const int64_t draw = draw0 + start[b - start0];
-#pragma unroll 4
-        for (int j = lane; j < a.max_pages; j += 32) {
-            int page = j < used ? __ldg(row + j) : -1;
-            if (j >= named && j < used) {
-                const int64_t i = draw + j - named;
-                const int was = page;
-                page = -1;
-                if (i < room) {
-                    page = __ldcg(a.pl.free_pages + from + i);
-                    a.copy_src[i] = in_pool(a.pl, was) ? was : -1;
-                    a.copy_dst[i] = page;
-                }
-            }
-            out[j] = page;
-        }
-        if (lane == 0) {
-            a.lens_out[b] = a.cache_lens[r];
-            a.held_out[b] = named + (int)min(max(room - draw, (int64_t)0), (int64_t)(used - named));
-        }
+    } else {
+        for (int64_t b = part.lo + threadIdx.x; b < part.hi; b += PG_THREADS) kids[b] = saturate(draw0 + kids[b]);
     }
     for (int64_t i = got + me; i < a.max_copies; i += PG_ALL) a.copy_src[i] = a.copy_dst[i] = -1;
     if (rank == 0 && threadIdx.x == 0) {
@@ -508,6 +534,23 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
         a.counts[1] = saturate(freed);
         a.counts[2] = saturate(freed - back);
         a.counts[3] = saturate(drawn - got);
+    }
+}
+
+constexpr int WIDE_THREADS = 256;
+__global__ void __launch_bounds__(WIDE_THREADS) paged_owners_kernel(const ForkArgs a) {
+    let_next_start();
+    wait_for_previous();
+    change_owners(a, (threadIdx.x >> 5) * gridDim.x + blockIdx.x, gridDim.x * (WIDE_THREADS / 32), [&](int r) { return __ldcg(a.ws + r); });
+}
+__global__ void __launch_bounds__(WIDE_THREADS) paged_rows_kernel(const ForkArgs a) {
+    let_next_start();
+    wait_for_previous();
+    const int from = __ldcg(a.pl.taken) - __ldcg(a.counts);
+    const int64_t room = min((int64_t)a.pl.n_free - from, (int64_t)a.max_copies);
+    for (int64_t b = (threadIdx.x >> 5) * gridDim.x + blockIdx.x; b < a.B; b += gridDim.x * (WIDE_THREADS / 32)) {
+        const int r = fork_from(a, (int)b);
+        write_row(a, b, r, r >= 0 && __ldcg(a.ws + a.B + r) == (b == r ? -1 : (int)b), __ldcg(a.ws + b), room, from);
     }
 }
 
@@ -543,8 +586,7 @@ __device__ __forceinline__ void rename_pages(const CompactArgs& a, int warp, int
     }
 }
 
-// Long batches and large pools: clearing, marking and renaming in launches of their own, over all SMs.
-constexpr int WIDE_THREADS = 256;
+// Long batches: clearing, marking and renaming in launches of their own, over all SMs.
 __global__ void __launch_bounds__(WIDE_THREADS) paged_clear_kernel(const CompactArgs a) {
     let_next_start();
     for (int64_t p = (int64_t)blockIdx.x * WIDE_THREADS + threadIdx.x; p < a.pl.n_pages; p += (int64_t)gridDim.x * WIDE_THREADS) a.page_map[p] = 0;
@@ -556,6 +598,7 @@ __global__ void __launch_bounds__(WIDE_THREADS) paged_mark_kernel(const CompactA
                gridDim.x * (WIDE_THREADS / 32));
 }
 __global__ void __launch_bounds__(WIDE_THREADS) paged_rename_kernel(const CompactArgs a) {
+    let_next_start();
     wait_for_previous();
     if (__ldcg(a.counts) > 0) rename_pages(a, (threadIdx.x >> 5) * gridDim.x + blockIdx.x, gridDim.x * (WIDE_THREADS / 32));
 }
@@ -569,8 +612,8 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
     const int rank = cl.block_rank(), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first_row = warp * PG_CTAS + rank;
     const int64_t me = (int64_t)rank * PG_THREADS + threadIdx.x;
     int32_t* state = a.page_map;
+    let_next_start();
     if constexpr (WIDE) {
-        let_next_start();
         wait_for_previous();
     } else {
         for (int64_t p = me; p < pl.n_pages; p += PG_ALL) state[p] = 0;
@@ -661,16 +704,17 @@ constexpr int COPY_THREADS = 256, COPY_BYTES = 4096, COPY_CTAS = 148 * 6;
 
 __global__ void __launch_bounds__(COPY_THREADS) paged_copy_kernel(const __grid_constant__ CopyArgs a) {
     const int lane = threadIdx.x & 31;
-    const int64_t n = min(max(__ldg(a.n), 0), a.max_copies);
     int64_t per = 0;   // pieces of one page in all pools
     for (int k = 0; k < a.n_pools; ++k) per += (a.bytes[k] + COPY_BYTES - 1) / COPY_BYTES;
+    wait_for_previous();   // the list is often the result of the launch before this one
+    const int64_t n = min(max(__ldcg(a.n), 0), a.max_copies);
     const int64_t warps = (int64_t)gridDim.x * (COPY_THREADS / 32);
     for (int64_t u = (int64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x; u < n * per; u += warps) {
         const int64_t i = u / per;
         int64_t piece = u - i * per;
         int k = 0;
         for (int64_t x; piece >= (x = (a.bytes[k] + COPY_BYTES - 1) / COPY_BYTES); ++k) piece -= x;
-        const int s = __ldg(a.src + i), d = __ldg(a.dst + i);
+        const int s = __ldcg(a.src + i), d = __ldcg(a.dst + i);
         if (s < 0 || s >= a.n_pages || d < 0 || d >= a.n_pages || s == d) continue;
         const int64_t at = piece * COPY_BYTES + lane * 16, end = a.bytes[k];
         const uint8_t* from = a.pool[k] + s * end;
@@ -686,20 +730,23 @@ __global__ void __launch_bounds__(COPY_THREADS) paged_copy_kernel(const __grid_c
 }
 
 // ------------------------------------------------------------------ host side
-// Rows to a cluster's warp beyond which the rows' own work goes over all SMs in launches of its own, each behind the other.
-constexpr int PG_ROWS = 1;
-
 cudaError_t launch_paged_release(const ReleaseArgs& a, cudaStream_t st) {
-    if (a.B <= PG_ROWS * PG_ALL_WARPS) return launch_behind(paged_release_kernel<false>, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
+    if (a.B <= PG_FEW) return launch_behind(paged_release_kernel<false>, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
     const unsigned grid = (unsigned)std::min(148 * 8, (a.B + DROP_THREADS / 32 - 1) / (DROP_THREADS / 32));
     const cudaError_t e = launch_behind(paged_drop_kernel, dim3(grid), DROP_THREADS, 0, st, false, a);
     return e == cudaSuccess ? launch_behind(paged_release_kernel<true>, dim3(PG_CTAS), PG_THREADS, 0, st, true, a) : e;
 }
 cudaError_t launch_paged_fork(const ForkArgs& a, cudaStream_t st) {
-    return launch_behind(paged_fork_kernel, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
+    if (a.B <= PG_FEW) return launch_behind(paged_fork_kernel<FORK_ALL>, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
+    const dim3 grid((unsigned)std::min(148 * 8, (a.B + WIDE_THREADS / 32 - 1) / (WIDE_THREADS / 32)));
+    cudaError_t e = launch_behind(paged_fork_kernel<FORK_COUNT>, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
+    if (e == cudaSuccess) e = launch_behind(paged_owners_kernel, grid, WIDE_THREADS, 0, st, true, a);
+    if (e == cudaSuccess) e = launch_behind(paged_fork_kernel<FORK_NUMBER>, dim3(PG_CTAS), PG_THREADS, 0, st, true, a);
+    if (e == cudaSuccess) e = launch_behind(paged_rows_kernel, grid, WIDE_THREADS, 0, st, true, a);
+    return e;
 }
 cudaError_t launch_paged_compact(const CompactArgs& a, cudaStream_t st) {
-    if (a.B <= PG_ROWS * PG_ALL_WARPS) return launch_behind(paged_compact_kernel<false>, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
+    if (a.B <= PG_FEW) return launch_behind(paged_compact_kernel<false>, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
     const dim3 grid(148 * 4);
     cudaError_t e = launch_behind(paged_clear_kernel, grid, WIDE_THREADS, 0, st, false, a);
     if (e == cudaSuccess) e = launch_behind(paged_mark_kernel, grid, WIDE_THREADS, 0, st, true, a);
@@ -708,9 +755,7 @@ cudaError_t launch_paged_compact(const CompactArgs& a, cudaStream_t st) {
     return e;
 }
 cudaError_t launch_paged_copy(const CopyArgs& a, cudaStream_t st) {
-    paged_copy_kernel<<<COPY_CTAS, COPY_THREADS, 0, st>>>(a);
-    count_launches(1);
-    return cudaGetLastError();
+    return launch_behind(paged_copy_kernel, dim3(COPY_CTAS), COPY_THREADS, 0, st, true, a);
 }
 
 }  // namespace loma
