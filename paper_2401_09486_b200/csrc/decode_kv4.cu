@@ -23,22 +23,29 @@ constexpr int KV4_STEP = 32;   // memory entries to a block: two tiles
 struct Kv4Plan {
     int g_rows, g_tiles;   // query heads of a kv head per head tile, head tiles per kv head
     int ctas, workers;     // W, before it is cut down for few blocks
+    bool whole;            // a CTA per unit, whose warps share its blocks and join their parts in shared memory: one launch
     // in the workspace, in floats.  Segment: outputs [g_rows][D], g_rows log2-sum-exps.  cum: int64 [B + 1], blocks before sequence b within
     // one (kv head, head tile)
     int64_t o, lse, cum, total;
     uint32_t ones;         // 0x00010001 (see kv4_pairs)
 };
 
-static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, bool cuda_cores) {
+// Units of so many blocks at most stay with one CTA, as long as all CTAs run at once (B4 H8 D64, 200 entries and tails of 40: WHOLE_A us against
+// WHOLE_B).
+constexpr int KV4_WHOLE = 16;
+
+static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, int max_mem, int max_tail, bool cuda_cores) {
     Kv4Plan p;
     const int g = Hq / Hkv;
     p.g_rows = cuda_cores ? (g < 3 ? g : 4) : (g <= 8 ? g : 16);
     p.g_tiles = (g + p.g_rows - 1) / p.g_rows;
     p.ctas = 148 * (cuda_cores ? (p.g_rows == 4 ? 2 : 4) : p.g_rows <= 8 ? 3 : 2);
     p.workers = p.ctas * KV4_WARPS;
+    const int64_t units = (int64_t)B * Hkv * p.g_tiles, blocks = ((int64_t)max_mem + KV4_STEP - 1) / KV4_STEP + max_tail / KV4_ROWS + 1;
+    p.whole = !cuda_cores && blocks <= KV4_WHOLE && units <= p.ctas;
     int64_t at = 0;
     auto take = [&](int64_t n) { const int64_t o = at; at += (n + 63) / 64 * 64; return o; };
-    const int64_t segments = p.workers + (int64_t)B * Hkv * p.g_tiles;
+    const int64_t segments = p.workers + units;
     p.o = take(segments * p.g_rows * D);
     p.lse = take(segments * p.g_rows);
     p.cum = take(2 * ((int64_t)B + 1));
@@ -461,16 +468,49 @@ __device__ __forceinline__ void group_pairs(int g, uint32_t a, uint32_t b, uint3
     if (g & 1) kv4_pairs<true>(a, b, ones, p); else kv4_pairs<false>(a, b, ones, p);
 }
 
-// R: column tiles of 8 query heads
-template <int D, int R>
+// Partial results joined: a maximum, a sum and four features, result by result in a fixed order.
+struct Kv4Join {
+    float M = -INFINITY, total = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    // N results at a time, e: log2-sum-exps (-inf: no weight: past the last, or scores of -inf, whose values are 0/0)
+    template <int N>
+    __device__ __forceinline__ void add(const float (&e)[N], const float4 (&y)[N]) {
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < N; ++u) top = fmaxf(top, e[u]);
+        const float keep = M == -INFINITY ? 1.f : exp2f(M - top);   // no weight yet, or NaN, which stays
+        M = top;
+        total *= keep;
+        o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            if (e[u] == -INFINITY) continue;
+            const float f = exp2f(e[u] - top);
+            total += f;
+            o.x = fmaf(f, y[u].x, o.x); o.y = fmaf(f, y[u].y, o.y); o.z = fmaf(f, y[u].z, o.z); o.w = fmaf(f, y[u].w, o.w);
+        }
+    }
+    template <typename T, int D>
+    __device__ __forceinline__ void store(const Kv4DecodeArgs& a, int64_t row, int c4) const {   // row = b * Hq + head
+        const float inv = 1.f / total;
+        T* out = static_cast<T*>(a.o) + row * D + c4 * 4;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        else *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        if (a.lse && c4 == 0) a.lse[row] = (M + log2f(total)) * 0.6931471805599453f;
+    }
+};
+
+// R: column tiles of 8 query heads.  WHOLE: p.whole.
+template <int D, int R, bool WHOLE>
 __global__ void __launch_bounds__(KV4_WARPS * 32, R == 1 ? 3 : 2)
 kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     using TL = Kv4Tile<D>;
     constexpr int G = TL::GROUPS, NS = Kv4Ring<D>::NS;
     extern __shared__ __align__(128) uint8_t kv4_smem[];
     __shared__ __align__(8) uint64_t bars[KV4_WARPS][NS];
-    __shared__ int64_t scan[Kv4Blocks::MAX_GROUPS + 1];
+    __shared__ int64_t scan[WHOLE ? 1 : Kv4Blocks::MAX_GROUPS + 1];
     __shared__ int64_t wsum[KV4_WARPS];
+    __shared__ float s_lse[KV4_WARPS][8 * R];
     __shared__ int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, j = lane & 3;
     float* ws = static_cast<float*>(a.ws);
@@ -480,12 +520,27 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     let_next_start();
     const Kv4Blocks kb{a};
-    const int per = kb.scan(scan, wsum, blockIdx.x == 0 ? reinterpret_cast<int64_t*>(ws + p.cum) : nullptr);
-    const int64_t T = scan[(a.B + per - 1) / per] * a.Hkv * p.g_tiles, W = min(T, (int64_t)p.workers);
-    const int64_t w = (int64_t)warp * gridDim.x + blockIdx.x;   // neighbours on different SMs
-    if (w >= W) return;
-    int left = (int)(kv4_first(w + 1, T, W) - kv4_first(w, T, W)), left_f = left;   // blocks of the share still to come, and still to be fetched
-    Kv4Blocks::Cursor c = kb.find(kv4_first(w, T, W), scan, per), f = c;
+    int left;                 // blocks of the share still to come
+    int64_t w = 0;
+    Kv4Blocks::Cursor c;
+    if constexpr (WHOLE) {
+        c.hh = blockIdx.x / a.B;
+        c.b = blockIdx.x - c.hh * a.B;
+        c.s = kv4_seq(a, c.b);
+        if (c.s.n == 0) return;
+        c.blk = c.s.n * warp / KV4_WARPS;
+        left = c.s.n * (warp + 1) / KV4_WARPS - c.blk;
+        __syncthreads();      // barriers and abort flag are set up
+    } else {
+        const int per = kb.scan(scan, wsum, blockIdx.x == 0 ? reinterpret_cast<int64_t*>(ws + p.cum) : nullptr);
+        const int64_t T = scan[(a.B + per - 1) / per] * a.Hkv * p.g_tiles, W = min(T, (int64_t)p.workers);
+        w = (int64_t)warp * gridDim.x + blockIdx.x;   // neighbours on different SMs
+        if (w >= W) return;
+        left = (int)(kv4_first(w + 1, T, W) - kv4_first(w, T, W));
+        c = kb.find(kv4_first(w, T, W), scan, per);
+    }
+    int left_f = left;        // blocks still to be fetched
+    Kv4Blocks::Cursor f = c;
 
     // Fetching goes by runs of blocks that lie behind one another in a page.  Where a page is one tile, lanes 0 and 1 fetch one each.
     const bool small_pages = a.m.log2_ps == 4;
@@ -614,7 +669,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
         }
     };
 
-    for (;;) {   // a segment: blocks of memory, then of the tail
+    while (left > 0) {   // a segment: blocks of memory, then of the tail
         h = p.g_tiles == 1 ? c.hh : c.hh / p.g_tiles;
         gt = c.hh - h * p.g_tiles;
         heads = min(p.g_rows, a.g - gt * p.g_rows);
@@ -780,7 +835,9 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 }
             }
         }
+        // the partial result: in the workspace, or (WHOLE) in place of the ring, which has been used up
         const int64_t seg = w + (int64_t)c.hh * a.B + c.b;
+        float *const o_part = WHOLE ? reinterpret_cast<float*>(ring) : ws + p.o + seg * p.g_rows * D, *const lse_part = WHOLE ? s_lse[warp] : ws + p.lse + seg * p.g_rows;
 #pragma unroll
         for (int x = 0; x < R; ++x)
 #pragma unroll
@@ -791,17 +848,36 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 const int hd = x * 8 + 2 * j + y;
                 if (hd < heads) {
                     const float inv = 1.f / lt;
-                    float* o = ws + p.o + (seg * p.g_rows + hd) * D + 4 * r;   // 8 lanes: 128 contiguous bytes
+                    float* o = o_part + hd * D + 4 * r;   // 8 lanes: 128 contiguous bytes
 #pragma unroll
                     for (int g = 0; g < G; ++g)
                         *reinterpret_cast<float4*>(o + 32 * g) = make_float4(acc[x][2 * g][y] * inv, acc[x][2 * g][2 + y] * inv,
                                                                            acc[x][2 * g + 1][y] * inv, acc[x][2 * g + 1][2 + y] * inv);
-                    if (r == 0) ws[p.lse + seg * p.g_rows + hd] = ref[x][y] + log2f(lt);
+                    if (r == 0) lse_part[hd] = ref[x][y] + log2f(lt);
                 }
             }
         left -= tiles + tails;
-        if (left == 0) break;
-        kb.next_unit(c);
+        if (left > 0) kb.next_unit(c);
+    }
+    if constexpr (WHOLE) {
+        if (c.s.n * (warp + 1) / KV4_WARPS == c.s.n * warp / KV4_WARPS && lane < 8 * R) s_lse[warp][lane] = -INFINITY;   // no blocks
+        __syncthreads();
+        h = c.hh / p.g_tiles;
+        gt = c.hh - h * p.g_tiles;
+        heads = min(p.g_rows, a.g - gt * p.g_rows);
+        for (int i = threadIdx.x; i < heads * (D / 4); i += KV4_WARPS * 32) {
+            const int hd = i / (D / 4), c4 = i % (D / 4);
+            float e[KV4_WARPS];
+            float4 y[KV4_WARPS];
+#pragma unroll
+            for (int u = 0; u < KV4_WARPS; ++u) {
+                e[u] = s_lse[u][hd];
+                y[u] = *reinterpret_cast<const float4*>(kv4_smem + u * Kv4Ring<D>::WARP + (hd * D + c4 * 4) * 4);
+            }
+            Kv4Join join;
+            join.add(e, y);
+            join.store<__nv_bfloat16, D>(a, (int64_t)c.b * a.Hq + h * a.g + gt * p.g_rows + hd, c4);
+        }
     }
     if (!ok) {
         // leaving early: give copies already in flight a bounded time to land in this CTA's shared memory
@@ -826,8 +902,7 @@ kv4_merge_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
     const bool live = there && __ldg(a.tail_lens + b) >= 0;
     const float* ws = static_cast<const float*>(a.ws);
     wait_for_previous();
-    float M = -INFINITY, total = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    Kv4Join join;
     if (live) {
         const int64_t* cum = reinterpret_cast<const int64_t*>(ws + p.cum);
         const int64_t per_head = __ldcg(cum + a.B), hh = (int64_t)h * p.g_tiles + gt, T_all = per_head * a.Hkv * p.g_tiles;
@@ -835,7 +910,7 @@ kv4_merge_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
         const int64_t w0 = kv4_worker(t0, T_all, W), first = w0 + hh * a.B + b;
         const int n = (int)(kv4_worker(t1 - 1, T_all, W) - w0) + 1;
         const float *lse = ws + p.lse + first * p.g_rows + x, *v = ws + p.o + (first * p.g_rows + x) * D + c4 * 4;
-        for (int s0 = way * AT_ONCE; s0 < n; s0 += WAYS * AT_ONCE) {   // results are fetched several at a time: the chain of loads is what takes time
+        for (int s0 = way * AT_ONCE; s0 < n; s0 += WAYS * AT_ONCE) {   // fetched several at a time: the chain of loads is what takes time
             float e[AT_ONCE];
             float4 y[AT_ONCE];
 #pragma unroll
@@ -846,56 +921,34 @@ kv4_merge_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
                     y[u] = __ldcg(reinterpret_cast<const float4*>(v + (int64_t)(s0 + u) * p.g_rows * D));
                 }
             }
-            float top = M;
-#pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) top = fmaxf(top, e[u]);
-            const float keep = M == -INFINITY ? 1.f : exp2f(M - top);   // no weight yet, or NaN, which stays
-            M = top;
-            total *= keep;
-            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
-#pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                if (e[u] == -INFINITY) continue;   // no weight: past the last, or scores of -inf (values 0/0)
-                const float f = exp2f(e[u] - top);
-                total += f;
-                o.x = fmaf(f, y[u].x, o.x); o.y = fmaf(f, y[u].y, o.y); o.z = fmaf(f, y[u].z, o.z); o.w = fmaf(f, y[u].w, o.w);
-            }
+            join.add(e, y);
         }
     }
     if constexpr (WAYS > 1) {
-        __shared__ float s_m[KV4_MERGE_THREADS], s_t[KV4_MERGE_THREADS];
-        __shared__ float4 s_o[KV4_MERGE_THREADS];
-        s_m[threadIdx.x] = M;
-        s_t[threadIdx.x] = total;
-        s_o[threadIdx.x] = o;
+        __shared__ Kv4Join s_part[KV4_MERGE_THREADS];
+        s_part[threadIdx.x] = join;
         __syncthreads();
         if (way > 0) return;
-        for (int y = 1; y < WAYS; ++y) M = fmaxf(M, s_m[threadIdx.x + y * LANES]);
-        total = 0.f;
-        o = make_float4(0.f, 0.f, 0.f, 0.f);
+        Kv4Join all;
+        for (int y = 0; y < WAYS; ++y) all.M = fmaxf(all.M, s_part[threadIdx.x + y * LANES].M);
         for (int y = 0; y < WAYS; ++y) {
-            const int at = threadIdx.x + y * LANES;
-            if (s_t[at] == 0.f) continue;   // took no result, or only ones without weight (one of NaN alone has a total of NaN)
-            const float f = exp2f(s_m[at] - M);
-            total += f * s_t[at];
-            o.x = fmaf(f, s_o[at].x, o.x); o.y = fmaf(f, s_o[at].y, o.y); o.z = fmaf(f, s_o[at].z, o.z); o.w = fmaf(f, s_o[at].w, o.w);
+            const Kv4Join& q = s_part[threadIdx.x + y * LANES];
+            if (q.total == 0.f) continue;   // took no result, or only ones without weight (one of NaN alone has a total of NaN)
+            const float f = exp2f(q.M - all.M);
+            all.total += f * q.total;
+            all.o.x = fmaf(f, q.o.x, all.o.x); all.o.y = fmaf(f, q.o.y, all.o.y); all.o.z = fmaf(f, q.o.z, all.o.z); all.o.w = fmaf(f, q.o.w, all.o.w);
         }
+        join = all;
     }
-    if (!live) return;
-    const float inv = 1.f / total;
-    T* out = static_cast<T*>(a.o) + row * D + c4 * 4;
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-    else *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    if (a.lse && c4 == 0) a.lse[row] = (M + log2f(total)) * 0.6931471805599453f;
+    if (live) join.store<T, D>(a, row, c4);
 }
 
 // ------------------------------------------------------------------ host side
 // both kernels' cuts, array by array, so that a buffer made for the largest call serves the smaller ones
 size_t decode_kv4_workspace_bytes(int B, int Hq, int Hkv, int D, int max_mem, int max_tail) {
-    (void)max_mem; (void)max_tail;   // the cut goes by workers, not by lengths
     int64_t rows = 0;
     for (bool cuda_cores : {false, true}) {
-        const Kv4Plan p = make_kv4_plan(B, Hq, Hkv, D, cuda_cores);
+        const Kv4Plan p = make_kv4_plan(B, Hq, Hkv, D, max_mem, max_tail, cuda_cores);
         rows = std::max(rows, (p.workers + (int64_t)B * Hkv * p.g_tiles) * p.g_rows);
     }
     int64_t n = 0;
@@ -913,7 +966,7 @@ static cudaError_t merge(const Kv4DecodeArgs& a, const Kv4Plan& p, cudaStream_t 
 
 template <typename T, int D>
 static cudaError_t stream(const Kv4DecodeArgs& a, cudaStream_t st) {
-    const Kv4Plan p = make_kv4_plan(a.B, a.Hq, a.Hkv, D, true);
+    const Kv4Plan p = make_kv4_plan(a.B, a.Hq, a.Hkv, D, a.max_mem, a.max_tail, true);
     auto* kernel = p.g_rows == 1 ? kv4_stream_kernel<T, D, 1> : p.g_rows == 2 ? kv4_stream_kernel<T, D, 2> : kv4_stream_kernel<T, D, 4>;
     const cudaError_t e = launch_behind(kernel, dim3(p.ctas), KV4_WARPS * 32, 0, st, false, a, p);
     return e == cudaSuccess ? merge<T, D>(a, p, st) : e;
@@ -921,10 +974,14 @@ static cudaError_t stream(const Kv4DecodeArgs& a, cudaStream_t st) {
 
 template <int D>
 static cudaError_t tensor_cores(const Kv4DecodeArgs& a, cudaStream_t st) {
-    const Kv4Plan p = make_kv4_plan(a.B, a.Hq, a.Hkv, D, false);
+    const Kv4Plan p = make_kv4_plan(a.B, a.Hq, a.Hkv, D, a.max_mem, a.max_tail, false);
     int* status = device_status_word();
     if (!status) return cudaErrorUnknown;
-    auto* kernel = p.g_rows <= 8 ? kv4_decode_kernel<D, 1> : kv4_decode_kernel<D, 2>;
+    if (p.whole) {
+        auto* kernel = p.g_rows <= 8 ? kv4_decode_kernel<D, 1, true> : kv4_decode_kernel<D, 2, true>;
+        return launch_behind(kernel, dim3(a.B * a.Hkv * p.g_tiles), KV4_WARPS * 32, Kv4Ring<D>::TOTAL, st, false, a, p, status);
+    }
+    auto* kernel = p.g_rows <= 8 ? kv4_decode_kernel<D, 1, false> : kv4_decode_kernel<D, 2, false>;
     const cudaError_t e = launch_behind(kernel, dim3(p.ctas), KV4_WARPS * 32, Kv4Ring<D>::TOTAL, st, false, a, p, status);
     return e == cudaSuccess ? merge<__nv_bfloat16, D>(a, p, st) : e;
 }
