@@ -24,9 +24,9 @@ struct Kv4Plan {
     int g_rows, g_tiles;   // query heads of a kv head per head tile, head tiles per kv head
     int ctas, workers;     // W, before it is cut down for few blocks
     bool whole;            // a CTA per unit, whose warps share its blocks and join their parts in shared memory: one launch
-    // in the workspace, in floats.  Segment: outputs [g_rows][D], g_rows log2-sum-exps.  cum: int64 [B + 1], blocks before sequence b within
-    // one (kv head, head tile)
-    int64_t o, lse, cum, total;
+    // in the workspace, in floats.  Segment: outputs [g_rows][D], g_rows log2-sum-exps.  ends: int32 [2][units], the workers of a unit's
+    // first and of its last segment
+    int64_t o, lse, ends, total;
     uint32_t ones;         // 0x00010001 (see kv4_pairs)
 };
 
@@ -48,14 +48,13 @@ static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, int max_mem, int max
     const int64_t segments = p.workers + units;
     p.o = take(segments * p.g_rows * D);
     p.lse = take(segments * p.g_rows);
-    p.cum = take(2 * ((int64_t)B + 1));
+    p.ends = take(2 * units);
     p.total = at;
     p.ones = 0x00010001u;
     return p;
 }
 
-// the worker that block t of T belongs to, and the first block of worker w (W <= T)
-__device__ __forceinline__ int64_t kv4_worker(int64_t t, int64_t T, int64_t W) { return ((t + 1) * W - 1) / T; }
+// the first block of worker w of W <= T
 __device__ __forceinline__ int64_t kv4_first(int64_t w, int64_t T, int64_t W) { return T / W * w + T % W * w / W; }
 
 // One sequence's part of a unit.
@@ -72,6 +71,13 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4DecodeArgs& a, int b) {
     return s;
 }
 
+// a worker that does blocks [from, to) of a unit of n notes where the unit's segments begin and end
+__device__ __forceinline__ void kv4_note(const Kv4DecodeArgs& a, const Kv4Plan& p, int64_t unit, int64_t w, int from, int to, int n) {
+    int32_t* ends = reinterpret_cast<int32_t*>(static_cast<float*>(a.ws) + p.ends);
+    if (from == 0) ends[unit] = (int)w;
+    if (to == n) ends[(int64_t)a.B * a.Hkv * p.g_tiles + unit] = (int)w;
+}
+
 // The numbering of the blocks, found again by every CTA.
 struct Kv4Blocks {
     static constexpr int MAX_GROUPS = 512, THREADS = KV4_WARPS * 32, PER_THREAD = MAX_GROUPS / THREADS;
@@ -81,9 +87,8 @@ struct Kv4Blocks {
     };
     const Kv4DecodeArgs& a;
 
-    // s[i]: blocks before sequence i * per of one (kv head, head tile), i = 0 .. groups; returns per.  out: all B + 1 sums, stored for
-    // the merge kernel (or NULL).  Ends with a barrier.
-    __device__ __forceinline__ int scan(int64_t* s, int64_t* wsum, int64_t* out) const {
+    // s[i]: blocks before sequence i * per of one (kv head, head tile), i = 0 .. groups; returns per.  Ends with a barrier.
+    __device__ __forceinline__ int scan(int64_t* s, int64_t* wsum) const {
         const int per = (a.B + MAX_GROUPS - 1) / MAX_GROUPS, groups = (a.B + per - 1) / per;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         int64_t mine[PER_THREAD], sum = 0;
@@ -108,14 +113,6 @@ struct Kv4Blocks {
         for (int u = 0; u < PER_THREAD; ++u) {
             const int i = threadIdx.x * PER_THREAD + u;
             if (i <= groups) s[i] = at;
-            if (out) {
-                int64_t c = at;
-                for (int b = i * per; b < min(a.B, (i + 1) * per); ++b) {
-                    out[b] = c;
-                    c += kv4_seq(a, b).n;
-                }
-                if (i == groups - 1) out[a.B] = c;
-            }
             at += mine[u];
         }
         if (threadIdx.x == THREADS - 1 && groups == MAX_GROUPS) s[MAX_GROUPS] = at;
@@ -201,7 +198,7 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
     float* ws = static_cast<float*>(a.ws);
     let_next_start();
     const Kv4Blocks kb{a};
-    const int per = kb.scan(scan, wsum, blockIdx.x == 0 ? reinterpret_cast<int64_t*>(ws + p.cum) : nullptr);
+    const int per = kb.scan(scan, wsum);
     const int64_t total = scan[(a.B + per - 1) / per] * a.Hkv * p.g_tiles, W = min(total, (int64_t)p.workers);
     const int64_t w = (int64_t)warp * gridDim.x + blockIdx.x;
     if (w >= W) return;
@@ -381,7 +378,8 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
                 }
             }
         }
-        const int64_t seg = w + (int64_t)c.hh * a.B + c.b;
+        const int64_t unit = (int64_t)c.hh * a.B + c.b, seg = w + unit;
+        if (lane == 0) kv4_note(a, p, unit, w, c.blk, c.blk + blocks + tails, c.s.n);
 #pragma unroll
         for (int o = DUP; o < LH; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
         l += __shfl_xor_sync(0xffffffffu, l, 8);
@@ -424,7 +422,9 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
 // needs over the banks of shared memory (D = 128: no conflict).
 template <int D>
 struct Kv4Ring {
-    static constexpr int NS = D == 128 ? 3 : 6, STAGE = 2 * Kv4Tile<D>::BYTES, WARP = NS * STAGE, TOTAL = KV4_WARPS * WARP;
+    static_assert(KV4_ROWS * D * 2 <= 2 * Kv4Tile<D>::BYTES);
+    static constexpr int NS = D == 128 ? 3 : 6, STAGE = 2 * Kv4Tile<D>::BYTES,   // two tiles, or 16 rows of the tail
+                          WARP = NS * STAGE, TOTAL = KV4_WARPS * WARP;
 };
 
 __device__ __forceinline__ void mma_acc(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -532,7 +532,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
         left = c.s.n * (warp + 1) / KV4_WARPS - c.blk;
         __syncthreads();      // barriers and abort flag are set up
     } else {
-        const int per = kb.scan(scan, wsum, blockIdx.x == 0 ? reinterpret_cast<int64_t*>(ws + p.cum) : nullptr);
+        const int per = kb.scan(scan, wsum);
         const int64_t T = scan[(a.B + per - 1) / per] * a.Hkv * p.g_tiles, W = min(T, (int64_t)p.workers);
         w = (int64_t)warp * gridDim.x + blockIdx.x;   // neighbours on different SMs
         if (w >= W) return;
@@ -542,41 +542,67 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     int left_f = left;        // blocks still to be fetched
     Kv4Blocks::Cursor f = c;
 
-    // Fetching goes by runs of blocks that lie behind one another in a page.  Where a page is one tile, lanes 0 and 1 fetch one each.
+    // Fetching goes by runs: of memory blocks that lie behind one another in a page (where a page is one tile, lanes 0 and 1 fetch one
+    // each), or of a unit's tail blocks, which take two places of the ring, one for the keys' rows and one for the values'; the new token's
+    // row is lane 1's.
     const bool small_pages = a.m.log2_ps == 4;
     const int page_blocks = small_pages ? 1 : 1 << (a.m.log2_ps - 5);
     const uint8_t* src = nullptr;
-    int run = 0, rest = 0, h_f = p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles;   // rest: entries of the sequence from the next block on
+    // rest: entries of the sequence's memory (or tail and new token) from the next block on; values: the next fetch is of a tail block's values
+    int run = 0, rest = 0, h_f = p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles;
+    bool tail_run = false, values = false;
     auto next_run = [&]() {
-        while (left_f > 0 && f.blk >= f.s.nm) {   // past tail blocks
-            left_f -= f.s.n - f.blk;
-            if (left_f > 0) {
-                kb.next_unit(f);
-                h_f = p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles;
-            }
-        }
         if (left_f <= 0) return;
-        rest = f.s.mem - f.blk * KV4_STEP;
-        const int entry = f.blk * KV4_STEP + (small_pages && lane == 1 && rest > KV4_ROWS ? KV4_ROWS : 0);
-        src = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, f.b, entry), h_f, entry);
-        run = min(min(page_blocks - (f.blk & (page_blocks - 1)), f.s.nm - f.blk), left_f);
-        f.blk += run;
-        left_f -= run;
+        if (f.blk == f.s.n) {
+            kb.next_unit(f);
+            h_f = p.g_tiles == 1 ? f.hh : f.hh / p.g_tiles;
+        }
+        int blocks;
+        tail_run = f.blk >= f.s.nm;
+        if (tail_run) {
+            blocks = min(f.s.n - f.blk, left_f);
+            run = 2 * blocks;
+            const int base = (f.blk - f.s.nm) * KV4_ROWS;
+            rest = f.s.tail + 1 - base;
+            src = reinterpret_cast<const uint8_t*>((((int64_t)f.b * a.Hkv + h_f) * a.cap + base) * D * 2);   // from the start of either cache
+        } else {
+            rest = f.s.mem - f.blk * KV4_STEP;
+            const int entry = f.blk * KV4_STEP + (small_pages && lane == 1 && rest > KV4_ROWS ? KV4_ROWS : 0);
+            src = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, f.b, entry), h_f, entry);
+            blocks = run = min(min(page_blocks - (f.blk & (page_blocks - 1)), f.s.nm - f.blk), left_f);
+        }
+        f.blk += blocks;
+        left_f -= blocks;
     };
     uint8_t* const ring = kv4_smem + warp * Kv4Ring<D>::WARP;
     const uint32_t ring_s = smem_u32(ring), bars_s = smem_u32(&bars[warp][0]);
     int slot_f = 0;
+    auto bulk = [&](uint32_t dst, const void* from, int bytes, uint32_t bar) {
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(from), "r"(bytes), "r"(bar) : "memory");
+    };
     auto fetch = [&]() {
-        const int bytes = rest > KV4_ROWS ? 2 * TL::BYTES : TL::BYTES;
-        if (lane == 0) mbar_expect_tx(bars_s + slot_f * 8, bytes);
-        __syncwarp();
-        if (lane == 0 || (small_pages && lane == 1 && rest > KV4_ROWS))
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ring_s + slot_f * Kv4Ring<D>::STAGE + lane * TL::BYTES),
-                         "l"(src), "r"(small_pages ? TL::BYTES : bytes), "r"(bars_s + slot_f * 8)
-                         : "memory");
+        const uint32_t bar = bars_s + slot_f * 8, dst = ring_s + slot_f * Kv4Ring<D>::STAGE;
+        if (tail_run) {
+            const int rows = min(rest, KV4_ROWS), old = rows - (rest <= KV4_ROWS && a.k_new ? 1 : 0);   // without the new token
+            if (lane == 0) mbar_expect_tx(bar, rows * D * 2);
+            __syncwarp();
+            if (lane == 0 && old > 0) bulk(dst, static_cast<const uint8_t*>(values ? a.v_tail : a.k_tail) + reinterpret_cast<uintptr_t>(src), old * D * 2, bar);
+            if (lane == 1 && old < rows)
+                bulk(dst + old * D * 2, static_cast<const uint8_t*>(values ? a.v_new : a.k_new) + ((int64_t)f.b * a.Hkv + h_f) * D * 2, D * 2, bar);
+            if (values) {
+                src += KV4_ROWS * D * 2;
+                rest -= KV4_ROWS;
+            }
+            values = !values;
+        } else {
+            const int bytes = rest > KV4_ROWS ? 2 * TL::BYTES : TL::BYTES;
+            if (lane == 0) mbar_expect_tx(bar, bytes);
+            __syncwarp();
+            if (lane == 0 || (small_pages && lane == 1 && rest > KV4_ROWS)) bulk(dst + lane * TL::BYTES, src, small_pages ? TL::BYTES : bytes, bar);
+            src += 2 * TL::BYTES;
+            rest -= KV4_STEP;
+        }
         slot_f = slot_f + 1 == NS ? 0 : slot_f + 1;
-        src += 2 * TL::BYTES;
-        rest -= KV4_STEP;
         if (--run == 0) next_run();
     };
     next_run();
@@ -626,7 +652,24 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 m[x][y] *= KV4_S;
                 ref[x][y] += KV4_P_LOG2;
             }
+#pragma unroll
+            for (int i = 0; i < 2 * G; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float f = e ? 4 / KV4_Q : 1 / KV4_Q;
+                    qf[x][i][e] = pack_bf16(bf16lo(qf[x][i][e]) * f, bf16hi(qf[x][i][e]) * f);
+                }
         }
+    };
+    // the next place of the ring, once its copies are there; and its use for the next fetch, once every lane is done with it
+    auto arrived = [&]() {
+        ok = __all_sync(0xffffffffu, mbar_wait(bars_s + slot * 8, phase, &abort_flag, status));
+        return ring + slot * Kv4Ring<D>::STAGE;
+    };
+    auto done_with = [&]() {
+        __syncwarp();
+        if (run > 0) fetch();
+        if (++slot == NS) { slot = 0; phase ^= 1; }
     };
     // z: raw products of rows pr (0, 1) and pr + 8 (2, 3) of one or two tiles, heads 2j, 2j + 1 (-inf: no weight) -> weights
     // 2^(z sc - ref)
@@ -688,9 +731,8 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
         int valid = c.s.mem - c.blk * KV4_STEP;   // entries from the block on
 #pragma unroll 1
         for (int i = 0; i < tiles; ++i, valid -= KV4_STEP) {
-            ok = __all_sync(0xffffffffu, mbar_wait(bars_s + slot * 8, phase, &abort_flag, status));
+            const uint8_t* st = arrived();
             if (!ok) break;
-            const uint8_t* st = ring + slot * Kv4Ring<D>::STAGE;
             float s[R][8];   // of the two tiles
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -761,82 +803,68 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                     }
                 }
             }
-            // every lane is done with the block: fetch the next one into its place
-            __syncwarp();
-            if (run > 0) fetch();
-            if (++slot == NS) { slot = 0; phase ^= 1; }
+            done_with();
         }
         if (!ok) break;
-        if (tiles) {
-            to_plain();
-            if (tails) load_q(1.f, 1.f);
-        }
+        if (tiles) to_plain();
 #pragma unroll 1
-        for (int i = 0; i < tails; ++i) {   // 16 entries of the tail, straight from memory; the last one is the new token
-            const int base = (c.blk + tiles + i - c.s.nm) * KV4_ROWS, valid = c.s.tail + 1 - base;
-            const int64_t cell0 = ((int64_t)c.b * a.Hkv + h) * a.cap;
-            auto row_at = [&](const void* cache, const void* fresh_row, int i) {   // no row of another sequence is ever read
-                const int e = min(base + i, c.s.tail);
-                return e == c.s.tail && fresh_row ? static_cast<const __nv_bfloat16*>(fresh_row) + ((int64_t)c.b * a.Hkv + h) * D
-                                                  : static_cast<const __nv_bfloat16*>(cache) + (cell0 + e) * D;
-            };
+        for (int i = 0; i < tails; ++i) {   // 16 entries of the tail; the last one is the new token
+            const int valid = c.s.tail + 1 - (c.blk + tiles + i - c.s.nm) * KV4_ROWS;
+            const int64_t cell = ((((int64_t)c.b * a.Hkv + h) * a.cap + c.s.tail) * D) / 8 + lane;
+            const bool token = valid <= KV4_ROWS && a.k_new && gt == 0 && lane < D / 8;   // its rows go to the cache, where nobody reads them in this launch
+            const uint8_t* st = arrived();
+            if (!ok) break;
             float s[R][4];
 #pragma unroll
-            for (int x = 0; x < R; ++x)
+            for (int g = 0; g < G; ++g) {
+                const uint4 u0 = *reinterpret_cast<const uint4*>(st + (pr * D + 32 * g + 8 * j) * 2), u1 = *reinterpret_cast<const uint4*>(st + ((pr + 8) * D + 32 * g + 8 * j) * 2);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[x][e] = 0.f;
-            {
-                const __nv_bfloat16 *k0 = row_at(a.k_tail, a.k_new, pr) + 8 * j, *k1 = row_at(a.k_tail, a.k_new, pr + 8) + 8 * j;
-                uint4 u0[G], u1[G];
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    u0[g] = *reinterpret_cast<const uint4*>(k0 + 32 * g);
-                    u1[g] = *reinterpret_cast<const uint4*>(k1 + 32 * g);
-                }
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-#pragma unroll
-                    for (int x = 0; x < R; ++x) {
-                        mma_acc(s[x], __byte_perm(u0[g].x, u0[g].z, 0x5410), __byte_perm(u1[g].x, u1[g].z, 0x5410), __byte_perm(u0[g].x, u0[g].z, 0x7632),
-                                __byte_perm(u1[g].x, u1[g].z, 0x7632), qf[x][2 * g][0], qf[x][2 * g][1]);
-                        mma_acc(s[x], __byte_perm(u0[g].y, u0[g].w, 0x5410), __byte_perm(u1[g].y, u1[g].w, 0x5410), __byte_perm(u0[g].y, u0[g].w, 0x7632),
-                                __byte_perm(u1[g].y, u1[g].w, 0x7632), qf[x][2 * g + 1][0], qf[x][2 * g + 1][1]);
-                    }
-            }
-            uint2 v[4][G];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = (i & 1 ? pv1 : pv0) + (i & 2) * 4;
-                const __nv_bfloat16* row = row_at(a.v_tail, a.v_new, e) + 4 * r;
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    v[i][g] = *reinterpret_cast<const uint2*>(row + 32 * g);
-                    if (e >= valid) v[i][g] = make_uint2(0, 0);   // repeated rows have no weight, but 0 x inf is not 0
+                for (int x = 0; x < R; ++x) {
+                    const uint32_t e0[4] = {__byte_perm(u0.x, u0.z, 0x5410), __byte_perm(u0.x, u0.z, 0x7632), __byte_perm(u0.y, u0.w, 0x5410), __byte_perm(u0.y, u0.w, 0x7632)};
+                    const uint32_t e1[4] = {__byte_perm(u1.x, u1.z, 0x5410), __byte_perm(u1.x, u1.z, 0x7632), __byte_perm(u1.y, u1.w, 0x5410), __byte_perm(u1.y, u1.w, 0x7632)};
+                    if (g == 0) mma_new(s[x], e0[0], e1[0], e0[1], e1[1], qf[x][0][0], qf[x][0][1]);
+                    else mma_acc(s[x], e0[0], e1[0], e0[1], e1[1], qf[x][2 * g][0], qf[x][2 * g][1]);
+                    mma_acc(s[x], e0[2], e1[2], e0[3], e1[3], qf[x][2 * g + 1][0], qf[x][2 * g + 1][1]);
                 }
             }
-            if (valid <= KV4_ROWS && a.k_new && gt == 0 && lane < D / 8) {   // entry `tail` of the cache is read by nobody in this launch
-                const int64_t from = (((int64_t)c.b * a.Hkv + h) * D) / 8 + lane, to = (cell0 + c.s.tail) * (D / 8) + lane;
-                static_cast<uint4*>(a.k_tail)[to] = __ldg(static_cast<const uint4*>(a.k_new) + from);
-                static_cast<uint4*>(a.v_tail)[to] = __ldg(static_cast<const uint4*>(a.v_new) + from);
-            }
+            if (token) static_cast<uint4*>(a.k_tail)[cell] = *reinterpret_cast<const uint4*>(st + (valid - 1) * D * 2 + lane * 16);
+            done_with();
+            uint32_t b0[R], b1[R];
 #pragma unroll
             for (int x = 0; x < R; ++x) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (pr + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
                 weights(x, s[x], sc_tail, grow_tail, 0.f);
-                const uint32_t b0 = transposed(pack_bf16(s[x][0], s[x][1])), b1 = transposed(pack_bf16(s[x][2], s[x][3]));
+                b0[x] = transposed(pack_bf16(s[x][0], s[x][1]));
+                b1[x] = transposed(pack_bf16(s[x][2], s[x][3]));
+            }
+            st = arrived();
+            if (!ok) break;
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    mma_acc(acc[x][2 * g], __byte_perm(v[0][g].x, v[1][g].x, 0x5410), __byte_perm(v[0][g].x, v[1][g].x, 0x7632),
-                            __byte_perm(v[2][g].x, v[3][g].x, 0x5410), __byte_perm(v[2][g].x, v[3][g].x, 0x7632), b0, b1);
-                    mma_acc(acc[x][2 * g + 1], __byte_perm(v[0][g].y, v[1][g].y, 0x5410), __byte_perm(v[0][g].y, v[1][g].y, 0x7632),
-                            __byte_perm(v[2][g].y, v[3][g].y, 0x5410), __byte_perm(v[2][g].y, v[3][g].y, 0x7632), b0, b1);
+            for (int g = 0; g < G; ++g) {
+                uint2 v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int e = (k & 1 ? pv1 : pv0) + (k & 2) * 4;
+                    v[k] = *reinterpret_cast<const uint2*>(st + (e * D + 32 * g + 4 * r) * 2);
+                    if (e >= valid) v[k] = make_uint2(0, 0);   // rows past the last one may hold anything, and 0 x NaN is not 0
+                }
+#pragma unroll
+                for (int x = 0; x < R; ++x) {
+                    mma_acc(acc[x][2 * g], __byte_perm(v[0].x, v[1].x, 0x5410), __byte_perm(v[0].x, v[1].x, 0x7632), __byte_perm(v[2].x, v[3].x, 0x5410),
+                            __byte_perm(v[2].x, v[3].x, 0x7632), b0[x], b1[x]);
+                    mma_acc(acc[x][2 * g + 1], __byte_perm(v[0].y, v[1].y, 0x5410), __byte_perm(v[0].y, v[1].y, 0x7632), __byte_perm(v[2].y, v[3].y, 0x5410),
+                            __byte_perm(v[2].y, v[3].y, 0x7632), b0[x], b1[x]);
                 }
             }
+            if (token) static_cast<uint4*>(a.v_tail)[cell] = *reinterpret_cast<const uint4*>(st + (valid - 1) * D * 2 + lane * 16);
+            done_with();
         }
+        if (!ok) break;
         // the partial result: in the workspace, or (WHOLE) in place of the ring, which has been used up
-        const int64_t seg = w + (int64_t)c.hh * a.B + c.b;
+        const int64_t unit = (int64_t)c.hh * a.B + c.b, seg = w + unit;
+        if (!WHOLE && lane == 0) kv4_note(a, p, unit, w, c.blk, c.blk + tiles + tails, c.s.n);
         float *const o_part = WHOLE ? reinterpret_cast<float*>(ring) : ws + p.o + seg * p.g_rows * D, *const lse_part = WHOLE ? s_lse[warp] : ws + p.lse + seg * p.g_rows;
 #pragma unroll
         for (int x = 0; x < R; ++x)
@@ -887,30 +915,30 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
 }
 
 // ------------------------------------------------------------------ merge
-// A row's D features are D / 4 lanes; WAYS sets of lanes share a row's partial results.
+// A row's D features are D / 4 lanes; WAYS sets of lanes share a row's partial results.  Results are fetched several at a time: the chain of
+// loads is what takes time.
 constexpr int KV4_MERGE_THREADS = 128;
 
 template <typename T, int D, int WAYS>
 __global__ void __launch_bounds__(KV4_MERGE_THREADS)
 kv4_merge_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
-    constexpr int LANES = D / 4, ROWS = KV4_MERGE_THREADS / LANES / WAYS, AT_ONCE = 8;
+    constexpr int LANES = D / 4, ROWS = KV4_MERGE_THREADS / LANES / WAYS, AT_ONCE = WAYS > 1 ? 8 : 4;
     const int c4 = threadIdx.x % LANES, set = threadIdx.x / LANES, way = set % WAYS;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + set / WAYS;
-    const bool there = row < (int64_t)a.B * a.Hq;
-    const int b = there ? (int)(row / a.Hq) : 0, hq = there ? (int)(row - (int64_t)b * a.Hq) : 0;
+    const int row = blockIdx.x * ROWS + set / WAYS;       // B * Hq fits 32 bits
+    const bool there = row < a.B * a.Hq;
+    const int b = there ? row / a.Hq : 0, hq = there ? row - b * a.Hq : 0;
     const int h = hq / a.g, j = hq - h * a.g, gt = j / p.g_rows, x = j - gt * p.g_rows;
     const bool live = there && __ldg(a.tail_lens + b) >= 0;
     const float* ws = static_cast<const float*>(a.ws);
     wait_for_previous();
     Kv4Join join;
     if (live) {
-        const int64_t* cum = reinterpret_cast<const int64_t*>(ws + p.cum);
-        const int64_t per_head = __ldcg(cum + a.B), hh = (int64_t)h * p.g_tiles + gt, T_all = per_head * a.Hkv * p.g_tiles;
-        const int64_t W = min(T_all, (int64_t)p.workers), t0 = hh * per_head + __ldcg(cum + b), t1 = hh * per_head + __ldcg(cum + b + 1);
-        const int64_t w0 = kv4_worker(t0, T_all, W), first = w0 + hh * a.B + b;
-        const int n = (int)(kv4_worker(t1 - 1, T_all, W) - w0) + 1;
-        const float *lse = ws + p.lse + first * p.g_rows + x, *v = ws + p.o + (first * p.g_rows + x) * D + c4 * 4;
-        for (int s0 = way * AT_ONCE; s0 < n; s0 += WAYS * AT_ONCE) {   // fetched several at a time: the chain of loads is what takes time
+        const int64_t unit = (int64_t)(h * p.g_tiles + gt) * a.B + b;
+        const int32_t* ends = reinterpret_cast<const int32_t*>(ws + p.ends) + unit;
+        const int w0 = __ldcg(ends), n = __ldcg(ends + (int64_t)a.B * a.Hkv * p.g_tiles) - w0 + 1;
+        const int64_t first = (w0 + unit) * p.g_rows + x;
+        const float *lse = ws + p.lse + first, *v = ws + p.o + first * D + c4 * 4;
+        for (int s0 = way * AT_ONCE; s0 < n; s0 += WAYS * AT_ONCE) {
             float e[AT_ONCE];
             float4 y[AT_ONCE];
 #pragma unroll
@@ -946,22 +974,25 @@ kv4_merge_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
 // ------------------------------------------------------------------ host side
 // both kernels' cuts, array by array, so that a buffer made for the largest call serves the smaller ones
 size_t decode_kv4_workspace_bytes(int B, int Hq, int Hkv, int D, int max_mem, int max_tail) {
-    int64_t rows = 0;
+    int64_t rows = 0, units = 0;
     for (bool cuda_cores : {false, true}) {
         const Kv4Plan p = make_kv4_plan(B, Hq, Hkv, D, max_mem, max_tail, cuda_cores);
+        units = std::max(units, (int64_t)B * Hkv * p.g_tiles);
         rows = std::max(rows, (p.workers + (int64_t)B * Hkv * p.g_tiles) * p.g_rows);
     }
     int64_t n = 0;
-    for (int64_t x : {rows * D, rows, 2 * ((int64_t)B + 1)}) n += (x + 63) / 64 * 64;
+    for (int64_t x : {rows * D, rows, 2 * units}) n += (x + 63) / 64 * 64;
     return (size_t)n * sizeof(float);
 }
 
+// Rows of long lists of partial results are shared by all of a CTA's sets of lanes.
 template <typename T, int D>
 static cudaError_t merge(const Kv4DecodeArgs& a, const Kv4Plan& p, cudaStream_t st) {
-    const int64_t rows = (int64_t)a.B * a.Hq;
     constexpr int SETS = KV4_MERGE_THREADS / (D / 4);
-    const unsigned grid = (unsigned)((rows * SETS + SETS - 1) / SETS);
-    return launch_behind(kv4_merge_kernel<T, D, SETS>, dim3(grid), KV4_MERGE_THREADS, 0, st, true, a, p);
+    const int rows = a.B * a.Hq;
+    if (p.workers > 8 * (int64_t)a.B * a.Hkv * p.g_tiles)
+        return launch_behind(kv4_merge_kernel<T, D, SETS>, dim3(rows), KV4_MERGE_THREADS, 0, st, true, a, p);
+    return launch_behind(kv4_merge_kernel<T, D, 1>, dim3((rows + SETS - 1) / SETS), KV4_MERGE_THREADS, 0, st, true, a, p);
 }
 
 template <typename T, int D>
