@@ -30,9 +30,11 @@ struct Kv4Plan {
     uint32_t ones;         // 0x00010001 (see kv4_pairs)
 };
 
-// Units of so many blocks at most stay with one CTA, as long as all CTAs run at once (B4 H8 D64, 200 entries and tails of 40: WHOLE_A us against
-// WHOLE_B).
-constexpr int KV4_WHOLE = 16;
+// Units of so many blocks at most stay with one CTA: that saves finding the cut and the merge, 5 us together, and costs that sequences of
+// different lengths do not even out.  Measured, whole against cut (D = 128, us): 32 units of up to 10 / 35 / 66 blocks 5.4 / 10.4 / 16.4 against
+// 9.9 / 11.2 / 12.6; 256 units of 35 / 66 16.9 / 27.3 against 20.6 / 27.2; 512 units (more than run at once) of 14 / 35 14.2 / 29.4 against 17.3 / 27.5;
+// 1024 units of 14 27.3 against 24.3; 8 units of 32 9.7 against 8.3, so few units are cut earlier.  (Clusters of two to eight CTAs to a unit gained a microsecond at 32 units and lost up to eight at 256.)
+constexpr int KV4_WHOLE = 40, KV4_WHOLE_SHORT = 16, KV4_WHOLE_FEW = 20;
 
 static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, int max_mem, int max_tail, bool cuda_cores) {
     Kv4Plan p;
@@ -42,7 +44,7 @@ static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, int max_mem, int max
     p.ctas = 148 * (cuda_cores ? (p.g_rows == 4 ? 2 : 4) : p.g_rows <= 8 ? 3 : 2);
     p.workers = p.ctas * KV4_WARPS;
     const int64_t units = (int64_t)B * Hkv * p.g_tiles, blocks = ((int64_t)max_mem + KV4_STEP - 1) / KV4_STEP + max_tail / KV4_ROWS + 1;
-    p.whole = !cuda_cores && blocks <= KV4_WHOLE && units <= p.ctas;
+    p.whole = !cuda_cores && units <= 4 * 148 && blocks <= (units <= 64 ? KV4_WHOLE_FEW : units <= p.ctas ? KV4_WHOLE : KV4_WHOLE_SHORT);
     int64_t at = 0;
     auto take = [&](int64_t n) { const int64_t o = at; at += (n + 63) / 64 * 64; return o; };
     const int64_t segments = p.workers + units;
