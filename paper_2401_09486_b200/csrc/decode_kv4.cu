@@ -210,7 +210,7 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
     const float scale_log2 = a.scale * 1.4426950408889634f;
     float q[G][NG][4], acc[G][NG][4], m, ref, l;   // m (a score in powers of two), ref (what exponents are taken off), l: of head x / LH
     // s: scores of the lane's four entries (rows i * 4 + sub of a tile) for all heads; the weights of all heads come back in it
-    auto weights = [&](float (&s)[M], int valid, float factor, float off) {
+    auto weights = [&](float (&s)[M], int valid, float factor) {
         spread_sum8<M, 4>(s, lane);
         float top = -INFINITY;
 #pragma unroll
@@ -226,7 +226,7 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
         if (__any_sync(0xffffffffu, top > m + 8.f)) {
             const float m_new = fmaxf(m, top), keep = m_new == -INFINITY ? 1.f : exp2f(m - m_new);
             m = m_new;
-            ref = (m == -INFINITY ? 0.f : m) - off;
+            ref = m == -INFINITY ? 0.f : m;
             l *= keep;
 #pragma unroll
             for (int y = 0; y < G; ++y) {
@@ -265,8 +265,7 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
             }
         }
         m = -INFINITY;
-        ref = blocks ? -KV4_P_LOG2 : 0.f;
-        l = 0.f;
+        ref = l = 0.f;
         const int end = min(c.s.mem, (c.blk + blocks) * KV4_STEP);
 #pragma unroll 1
         for (int j0 = c.blk * KV4_STEP; j0 < end; j0 += KV4_ROWS) {
@@ -299,7 +298,7 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
                         s[y * 4 + i] = fmaf(hi, bf16hi(kh[i][g / 2]), fmaf(lo, bf16lo(kh[i][g / 2]), g ? s[y * 4 + i] : 0.f));
                     }
                 }
-            weights(s, valid, scale_log2 * KV4_S, KV4_P_LOG2);
+            weights(s, valid, scale_log2 * KV4_S);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bool there = i * 4 + sub < valid;   // rows past the last entry may hold anything, and 0 x NaN is not 0
@@ -307,7 +306,7 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
                 for (int g = 0; g < NG; g += 2) {
                     uint32_t n[4];
                     kv4_word(vw[i][g / 2], ones, n);
-                    const float h0 = there ? bf16lo(vh[i][g / 2]) : 0.f, h1 = there ? bf16hi(vh[i][g / 2]) : 0.f;
+                    const float h0 = there ? bf16lo(vh[i][g / 2]) * KV4_P : 0.f, h1 = there ? bf16hi(vh[i][g / 2]) * KV4_P : 0.f;
 #pragma unroll
                     for (int y = 0; y < G; ++y) {
                         const float w0 = s[y * 4 + i] * h0, w1 = s[y * 4 + i] * h1;
@@ -330,8 +329,6 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
                         acc[y][g][e] *= e & 1 ? KV4_O / 4 : KV4_O;
                         q[y][g][e] *= e & 1 ? 4 / KV4_Q : 1 / KV4_Q;
                     }
-            l *= KV4_P_INV;
-            ref += KV4_P_LOG2;
         }
 #pragma unroll 1
         for (int t = 0; t < tails; ++t) {   // 16 entries of the tail; the last one is the new token
@@ -357,7 +354,7 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[y * 4 + i] = fmaf(q[y][g][e], k[e], g + e ? s[y * 4 + i] : 0.f);
                 }
-            weights(s, valid, scale_log2, 0.f);
+            weights(s, valid, scale_log2);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -649,11 +646,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 acc[x][i][2] *= KV4_O / 4; acc[x][i][3] *= KV4_O / 4;
             }
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                l[x][y] *= KV4_P_INV;
-                m[x][y] *= KV4_S;
-                ref[x][y] += KV4_P_LOG2;
-            }
+            for (int y = 0; y < 2; ++y) m[x][y] *= KV4_S;
 #pragma unroll
             for (int i = 0; i < 2 * G; ++i)
 #pragma unroll
@@ -676,7 +669,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     // z: raw products of rows pr (0, 1) and pr + 8 (2, 3) of one or two tiles, heads 2j, 2j + 1 (-inf: no weight) -> weights
     // 2^(z sc - ref)
     const float grow_mem = 8.f / sc_mem, grow_tail = 8.f / sc_tail;
-    auto weights = [&](int x, auto& z, float sc, float grow, float off) {
+    auto weights = [&](int x, auto& z, float sc, float grow) {
         constexpr int N = sizeof(z) / sizeof(float);
         float m0 = fmaxf(z[0], z[2]), m1 = fmaxf(z[1], z[3]);
         if constexpr (N > 4) {
@@ -695,8 +688,8 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
             const float f0 = m0 == -INFINITY ? 1.f : fast_ex2((m[x][0] - m0) * sc), f1 = m1 == -INFINITY ? 1.f : fast_ex2((m[x][1] - m1) * sc);
             m[x][0] = m0;
             m[x][1] = m1;
-            ref[x][0] = (m0 == -INFINITY ? 0.f : m0 * sc) - off;
-            ref[x][1] = (m1 == -INFINITY ? 0.f : m1 * sc) - off;
+            ref[x][0] = m0 == -INFINITY ? 0.f : m0 * sc;
+            ref[x][1] = m1 == -INFINITY ? 0.f : m1 * sc;
             l[x][0] *= f0;
             l[x][1] *= f1;
 #pragma unroll
@@ -723,7 +716,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
 #pragma unroll
         for (int x = 0; x < R; ++x) {
             m[x][0] = m[x][1] = -INFINITY;
-            ref[x][0] = ref[x][1] = tiles ? -KV4_P_LOG2 : 0.f;
+            ref[x][0] = ref[x][1] = 0.f;
             l[x][0] = l[x][1] = 0.f;
 #pragma unroll
             for (int i = 0; i < 2 * G; ++i)
@@ -771,7 +764,11 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                         if (pr + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
             }
 #pragma unroll
-            for (int x = 0; x < R; ++x) weights(x, s[x], sc_mem, grow_mem, KV4_P_LOG2);
+            for (int x = 0; x < R; ++x) {
+                weights(x, s[x], sc_mem, grow_mem);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[x][e] *= KV4_P;
+            }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const uint8_t* tile = st + u * TL::BYTES;
@@ -837,7 +834,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (pr + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
-                weights(x, s[x], sc_tail, grow_tail, 0.f);
+                weights(x, s[x], sc_tail, grow_tail);
                 b0[x] = transposed(pack_bf16(s[x][0], s[x][1]));
                 b1[x] = transposed(pack_bf16(s[x][2], s[x][3]));
             }

@@ -113,12 +113,12 @@ __device__ __forceinline__ void kv4_word(uint32_t u, uint32_t ones, uint32_t (&p
     p[2] = ((w << 1) & 0x800E800Eu) | ones;
     p[3] = (w & 0x80388038u) | ones << 2;
 }
-// Powers of two that keep sums over these patterns in the normal range: queries carry 2^64 (2^62 against odd e), weights 2^80, so scores
-// come out times 2^-69 and outputs times 2^-53 (2^-51).
+// Powers of two that keep sums over these patterns in the normal range: queries carry 2^64 (2^62 against odd e), weights 2^80 (after
+// their sum has been taken), so scores come out times 2^-69 and outputs times 2^-53 (2^-51).
 constexpr float KV4_Q = 18446744073709551616.f;                    // 2^64
 constexpr float KV4_S = 590295810358705651712.f;                   // 2^69
+constexpr float KV4_P = 1208925819614629174706176.f;               // 2^80
 constexpr float KV4_O = 9007199254740992.f;                        // 2^53
-constexpr float KV4_P_LOG2 = 80.f, KV4_P_INV = 8.271806125530277e-25f;   // 2^-80
 
 // G half-words (a chunk's bytes, a row's steps) as words
 template <int G>
