@@ -12,8 +12,12 @@
 // lengths are known on the device only, so every CTA finds the cut from them.
 //
 // bf16: kv4_decode_kernel, warp-level products.  fp32, and the second opinion: kv4_stream_kernel on CUDA cores.
+#include <cooperative_groups.h>
+
 #include "kv4.cuh"
 #include "tcgen05_common.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace loma {
 
@@ -23,18 +27,20 @@ constexpr int KV4_STEP = 32;   // memory entries to a block: two tiles
 struct Kv4Plan {
     int g_rows, g_tiles;   // query heads of a kv head per head tile, head tiles per kv head
     int ctas, workers;     // W, before it is cut down for few blocks
-    bool whole;            // a CTA per unit, whose warps share its blocks and join their parts in shared memory: one launch
+    int whole;             // CTAs of a cluster per unit, whose warps share its blocks and join their parts in shared memory: one launch (0: no)
     // in the workspace, in floats.  Segment: outputs [g_rows][D], g_rows log2-sum-exps.  ends: int32 [2][units], the workers of a unit's
     // first and of its last segment
     int64_t o, lse, ends, total;
     uint32_t ones;         // 0x00010001 (see kv4_pairs)
 };
 
-// Units of so many blocks at most stay with one CTA: that saves finding the cut and the merge, 5 us together, and costs that sequences of
-// different lengths do not even out.  Measured, whole against cut (D = 128, us): 32 units of up to 10 / 35 / 66 blocks 5.4 / 10.4 / 16.4 against
-// 9.9 / 11.2 / 12.6; 256 units of 35 / 66 16.9 / 27.3 against 20.6 / 27.2; 512 units (more than run at once) of 14 / 35 14.2 / 29.4 against 17.3 / 27.5;
-// 1024 units of 14 27.3 against 24.3; 8 units of 32 9.7 against 8.3, so few units are cut earlier.  (Clusters of two to eight CTAs to a unit gained a microsecond at 32 units and lost up to eight at 256.)
-constexpr int KV4_WHOLE = 40, KV4_WHOLE_SHORT = 16, KV4_WHOLE_FEW = 20;
+// Units stay whole, with the warps of one CTA or of a cluster of two to eight, while all of them run at once and no warp gets more than
+// KV4_WHOLE blocks: that saves finding the cut, a launch and the merge through memory, 3 to 5 us together, and costs that sequences of different
+// lengths do not even out.  Somewhat more CTAs than run at once will do for short units (up to KV4_WHOLE_SHORT blocks).  Measured, whole
+// against cut (D = 128, us): 32 units of up to 4 / 35 / 66 / 129 blocks 5.8 / 8.7 / 9.6 / 12.0 against 9.9 / 11.1 / 12.4 / 15.3; 128 units of 35 / 66
+// 11.8 / 16.8 against 14.7 / 18.5; 256 units of 35 / 51 16.0 / 22.1 against 20.2 / 24.2; 512 units of 14 14.7 against 17.2; but 64 units of 254, 16 blocks
+// to a warp, 26.4 against 24.9, and 1024 units of 14 27.3 against 24.3.
+constexpr int KV4_WHOLE = 12, KV4_WHOLE_SHORT = 16;
 
 static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, int max_mem, int max_tail, bool cuda_cores) {
     Kv4Plan p;
@@ -44,7 +50,12 @@ static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, int max_mem, int max
     p.ctas = 148 * (cuda_cores ? (p.g_rows == 4 ? 2 : 4) : p.g_rows <= 8 ? 3 : 2);
     p.workers = p.ctas * KV4_WARPS;
     const int64_t units = (int64_t)B * Hkv * p.g_tiles, blocks = ((int64_t)max_mem + KV4_STEP - 1) / KV4_STEP + max_tail / KV4_ROWS + 1;
-    p.whole = !cuda_cores && units <= 4 * 148 && blocks <= (units <= 64 ? KV4_WHOLE_FEW : units <= p.ctas ? KV4_WHOLE : KV4_WHOLE_SHORT);
+    p.whole = 0;
+    if (!cuda_cores) {
+        int c = 8;   // as many CTAs as run at once and have more than a block to a warp; a cluster is not worth it for KV4_WHOLE_SHORT blocks
+        while (c > 1 && (units * c > p.ctas || blocks <= std::max(KV4_WHOLE_SHORT, KV4_WARPS * c))) c /= 2;
+        if (units * c <= p.ctas ? blocks <= (int64_t)KV4_WHOLE * KV4_WARPS * c : units <= 4 * 148 && blocks <= KV4_WHOLE_SHORT) p.whole = c;
+    }
     int64_t at = 0;
     auto take = [&](int64_t n) { const int64_t o = at; at += (n + 63) / 64 * 64; return o; };
     const int64_t segments = p.workers + units;
@@ -470,7 +481,7 @@ __device__ __forceinline__ void group_pairs(int g, uint32_t a, uint32_t b, uint3
 // Partial results joined: a maximum, a sum and four features, result by result in a fixed order.
 struct Kv4Join {
     float M = -INFINITY, total = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 o_ = make_float4(0.f, 0.f, 0.f, 0.f);
     // N results at a time, e: log2-sum-exps (-inf: no weight: past the last, or scores of -inf, whose values are 0/0)
     template <int N>
     __device__ __forceinline__ void add(const float (&e)[N], const float4 (&y)[N]) {
@@ -480,31 +491,45 @@ struct Kv4Join {
         const float keep = M == -INFINITY ? 1.f : exp2f(M - top);   // no weight yet, or NaN, which stays
         M = top;
         total *= keep;
-        o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+        o_.x *= keep; o_.y *= keep; o_.z *= keep; o_.w *= keep;
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             if (e[u] == -INFINITY) continue;
             const float f = exp2f(e[u] - top);
             total += f;
-            o.x = fmaf(f, y[u].x, o.x); o.y = fmaf(f, y[u].y, o.y); o.z = fmaf(f, y[u].z, o.z); o.w = fmaf(f, y[u].w, o.w);
+            o_.x = fmaf(f, y[u].x, o_.x); o_.y = fmaf(f, y[u].y, o_.y); o_.z = fmaf(f, y[u].z, o_.z); o_.w = fmaf(f, y[u].w, o_.w);
         }
+    }
+    // the other lane's results, too (lanes that differ in bit o)
+    __device__ __forceinline__ void exchange(int o) {
+        const float m = __shfl_xor_sync(0xffffffffu, M, o), t = __shfl_xor_sync(0xffffffffu, total, o), top = fmaxf(M, m);
+        // a side that took no result, or only ones without weight, has a total of 0; one of NaN alone a total of NaN
+        const float f = total == 0.f ? 0.f : exp2f(M - top), g = t == 0.f ? 0.f : exp2f(m - top);
+        const float4 y = make_float4(__shfl_xor_sync(0xffffffffu, o_.x, o), __shfl_xor_sync(0xffffffffu, o_.y, o), __shfl_xor_sync(0xffffffffu, o_.z, o),
+                                     __shfl_xor_sync(0xffffffffu, o_.w, o));
+        M = top;
+        total = f * total + g * t;
+        o_.x = f * o_.x + g * y.x; o_.y = f * o_.y + g * y.y; o_.z = f * o_.z + g * y.z; o_.w = f * o_.w + g * y.w;
     }
     template <typename T, int D>
     __device__ __forceinline__ void store(const Kv4DecodeArgs& a, int64_t row, int c4) const {   // row = b * Hq + head
         const float inv = 1.f / total;
         T* out = static_cast<T*>(a.o) + row * D + c4 * 4;
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-        else *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o_.x * inv, o_.y * inv), pack_bf16(o_.z * inv, o_.w * inv));
+        else *reinterpret_cast<float4*>(out) = make_float4(o_.x * inv, o_.y * inv, o_.z * inv, o_.w * inv);
         if (a.lse && c4 == 0) a.lse[row] = (M + log2f(total)) * 0.6931471805599453f;
     }
 };
 
-// R: column tiles of 8 query heads.  WHOLE: p.whole.
-template <int D, int R, bool WHOLE>
+// R: column tiles of 8 query heads.  How units are dealt: CUT to workers, or WHOLE to a CTA, or to a cluster of p.whole CTAs.
+enum Kv4Dealt { KV4_CUT, KV4_CTA, KV4_CLUSTER };
+template <int D, int R, int DEALT>
 __global__ void __launch_bounds__(KV4_WARPS * 32, R == 1 ? 3 : 2)
 kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     using TL = Kv4Tile<D>;
     constexpr int G = TL::GROUPS, NS = Kv4Ring<D>::NS;
+    constexpr bool WHOLE = DEALT != KV4_CUT;
+    const int ctas = DEALT == KV4_CLUSTER ? p.whole : 1;
     extern __shared__ __align__(128) uint8_t kv4_smem[];
     __shared__ __align__(8) uint64_t bars[KV4_WARPS][NS];
     __shared__ int64_t scan[WHOLE ? 1 : Kv4Blocks::MAX_GROUPS + 1];
@@ -523,12 +548,14 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     int64_t w = 0;
     Kv4Blocks::Cursor c;
     if constexpr (WHOLE) {
-        c.hh = blockIdx.x / a.B;
-        c.b = blockIdx.x - c.hh * a.B;
+        const int unit = blockIdx.x / ctas, at = blockIdx.x % ctas * KV4_WARPS + warp;
+        c.hh = unit / a.B;
+        c.b = unit - c.hh * a.B;
         c.s = kv4_seq(a, c.b);
         if (c.s.n == 0) return;
-        c.blk = c.s.n * warp / KV4_WARPS;
-        left = c.s.n * (warp + 1) / KV4_WARPS - c.blk;
+        c.blk = (int)((int64_t)c.s.n * at / (KV4_WARPS * ctas));
+        left = (int)((int64_t)c.s.n * (at + 1) / (KV4_WARPS * ctas)) - c.blk;
+        if (left == 0 && lane < 8 * R) s_lse[warp][lane] = -INFINITY;
         __syncthreads();      // barriers and abort flag are set up
     } else {
         const int per = kb.scan(scan, wsum);
@@ -887,24 +914,35 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
         if (left > 0) kb.next_unit(c);
     }
     if constexpr (WHOLE) {
-        if (c.s.n * (warp + 1) / KV4_WARPS == c.s.n * warp / KV4_WARPS && lane < 8 * R) s_lse[warp][lane] = -INFINITY;   // no blocks
-        __syncthreads();
+        // the unit's rows are dealt to the threads: `ctas` neighbouring lanes to four features of a row, each taking the parts of one CTA
+        cg::cluster_group cl = cg::this_cluster();
+        if constexpr (DEALT == KV4_CLUSTER) cl.sync();
+        else __syncthreads();
         h = c.hh / p.g_tiles;
         gt = c.hh - h * p.g_tiles;
         heads = min(p.g_rows, a.g - gt * p.g_rows);
-        for (int i = threadIdx.x; i < heads * (D / 4); i += KV4_WARPS * 32) {
-            const int hd = i / (D / 4), c4 = i % (D / 4);
+        const int items = heads * (D / 4), cta = lane % ctas, per = KV4_WARPS * 32 / ctas;
+        const float* lse = &s_lse[0][0];
+        const uint8_t* part = kv4_smem;
+        if constexpr (DEALT == KV4_CLUSTER) {
+            lse = cl.map_shared_rank(lse, cta);
+            part = cl.map_shared_rank(part, cta);
+        }
+        for (int i0 = blockIdx.x % ctas * per; i0 < items; i0 += KV4_WARPS * 32) {
+            const int i = min(i0 + (int)threadIdx.x / ctas, items - 1), hd = i / (D / 4), c4 = i % (D / 4);
             float e[KV4_WARPS];
             float4 y[KV4_WARPS];
 #pragma unroll
             for (int u = 0; u < KV4_WARPS; ++u) {
-                e[u] = s_lse[u][hd];
-                y[u] = *reinterpret_cast<const float4*>(kv4_smem + u * Kv4Ring<D>::WARP + (hd * D + c4 * 4) * 4);
+                e[u] = lse[u * 8 * R + hd];
+                y[u] = *reinterpret_cast<const float4*>(part + u * Kv4Ring<D>::WARP + (hd * D + c4 * 4) * 4);
             }
             Kv4Join join;
             join.add(e, y);
-            join.store<__nv_bfloat16, D>(a, (int64_t)c.b * a.Hq + h * a.g + gt * p.g_rows + hd, c4);
+            for (int o = 1; o < ctas; o <<= 1) join.exchange(o);
+            if (cta == 0 && i0 + (int)threadIdx.x / ctas < items) join.store<__nv_bfloat16, D>(a, (int64_t)c.b * a.Hq + h * a.g + gt * p.g_rows + hd, c4);
         }
+        if constexpr (DEALT == KV4_CLUSTER) cl.sync();   // nobody leaves while its results are being read
     }
     if (!ok) {
         // leaving early: give copies already in flight a bounded time to land in this CTA's shared memory
@@ -963,7 +1001,7 @@ kv4_merge_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
             if (q.total == 0.f) continue;   // took no result, or only ones without weight (one of NaN alone has a total of NaN)
             const float f = exp2f(q.M - all.M);
             all.total += f * q.total;
-            all.o.x = fmaf(f, q.o.x, all.o.x); all.o.y = fmaf(f, q.o.y, all.o.y); all.o.z = fmaf(f, q.o.z, all.o.z); all.o.w = fmaf(f, q.o.w, all.o.w);
+            all.o_.x = fmaf(f, q.o_.x, all.o_.x); all.o_.y = fmaf(f, q.o_.y, all.o_.y); all.o_.z = fmaf(f, q.o_.z, all.o_.z); all.o_.w = fmaf(f, q.o_.w, all.o_.w);
         }
         join = all;
     }
@@ -1007,12 +1045,30 @@ static cudaError_t tensor_cores(const Kv4DecodeArgs& a, cudaStream_t st) {
     const Kv4Plan p = make_kv4_plan(a.B, a.Hq, a.Hkv, D, a.max_mem, a.max_tail, false);
     int* status = device_status_word();
     if (!status) return cudaErrorUnknown;
+    const bool narrow = p.g_rows <= 8;
+    const dim3 units(a.B * a.Hkv * p.g_tiles), threads(KV4_WARPS * 32);
+    constexpr int smem = Kv4Ring<D>::TOTAL;
+    if (p.whole == 1) return launch_behind(narrow ? kv4_decode_kernel<D, 1, KV4_CTA> : kv4_decode_kernel<D, 2, KV4_CTA>, units, threads, smem, st, false, a, p, status);
     if (p.whole) {
-        auto* kernel = p.g_rows <= 8 ? kv4_decode_kernel<D, 1, true> : kv4_decode_kernel<D, 2, true>;
-        return launch_behind(kernel, dim3(a.B * a.Hkv * p.g_tiles), KV4_WARPS * 32, Kv4Ring<D>::TOTAL, st, false, a, p, status);
+        auto* kernel = narrow ? kv4_decode_kernel<D, 1, KV4_CLUSTER> : kv4_decode_kernel<D, 2, KV4_CLUSTER>;
+        cudaError_t e = prepare_kernel(reinterpret_cast<const void*>(kernel), smem);
+        if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(units.x * p.whole);
+        cfg.blockDim = threads;
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = p.whole;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, kernel, a, p, status);
+        if (e == cudaSuccess) count_launches(1);
+        return e;
     }
-    auto* kernel = p.g_rows <= 8 ? kv4_decode_kernel<D, 1, false> : kv4_decode_kernel<D, 2, false>;
-    const cudaError_t e = launch_behind(kernel, dim3(p.ctas), KV4_WARPS * 32, Kv4Ring<D>::TOTAL, st, false, a, p, status);
+    const cudaError_t e = launch_behind(narrow ? kv4_decode_kernel<D, 1, KV4_CUT> : kv4_decode_kernel<D, 2, KV4_CUT>, dim3(p.ctas), threads, smem, st, false, a, p, status);
     return e == cudaSuccess ? merge<__nv_bfloat16, D>(a, p, st) : e;
 }
 
