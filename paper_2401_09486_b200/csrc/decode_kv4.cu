@@ -286,10 +286,10 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int row = i * 4 + sub;
-                halves<NG>(tile + kv4_chunk<D>(row, x), kw[i]);
-                halves<NG>(tile + TL::K_STEPS + row * TL::STEPS, kh[i]);
-                halves<NG>(tile + TL::V + kv4_chunk<D>(row, x), vw[i]);
-                halves<NG>(tile + TL::V_STEPS + row * TL::STEPS, vh[i]);
+                kv4_halves<NG>(tile + kv4_k_unit<D>(row, x), x & 1, kw[i]);
+                kv4_steps<NG>(tile + TL::K_STEPS + row * TL::STEPS, kh[i]);
+                kv4_halves<NG>(tile + kv4_v_unit<D>(row, x), row & 1, vw[i]);
+                kv4_steps<NG>(tile + TL::V_STEPS + row * TL::STEPS, vh[i]);
             }
             float s[M];
 #pragma unroll
@@ -427,9 +427,6 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
 //
 // A tile's numbers are n 2^-133 (n odd, up to 15; times 4 for odd e, see kv4.cuh); the powers of two that queries and weights carry are
 // exact and are taken off where memory ends and the tail begins (to_plain), or with the partial result.
-//
-// Row r of the scores is entry pi(r) = r ^ (r >> 1 & 1): with the chunks' places that spreads the four rows whose values a lane
-// needs over the banks of shared memory (D = 128: no conflict).
 template <int D>
 struct Kv4Ring {
     static_assert(KV4_ROWS * D * 2 <= 2 * Kv4Tile<D>::BYTES);
@@ -463,21 +460,6 @@ __device__ __forceinline__ void steps_of(const uint8_t* p, float (&h)[G]) {
         h[0] = bf16lo(u); h[1] = bf16hi(u);
     }
 }
-// the words of two neighbouring chunks: w[chunk][i] holds groups 2 i and 2 i + 1
-template <int G>
-__device__ __forceinline__ void chunk_pair(const uint8_t* p, uint32_t (&w)[2][G / 2]) {
-    if constexpr (G == 4) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
-        w[0][0] = u.x; w[0][1] = u.y; w[1][0] = u.z; w[1][1] = u.w;
-    } else {
-        const uint2 u = *reinterpret_cast<const uint2*>(p);
-        w[0][0] = u.x; w[1][0] = u.y;
-    }
-}
-__device__ __forceinline__ void group_pairs(int g, uint32_t a, uint32_t b, uint32_t ones, uint32_t (&p)[4]) {
-    if (g & 1) kv4_pairs<true>(a, b, ones, p); else kv4_pairs<false>(a, b, ones, p);
-}
-
 // Partial results joined: a maximum, a sum and four features, result by result in a fixed order.
 struct Kv4Join {
     float M = -INFINITY, total = 0.f;
@@ -636,8 +618,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
 
     const uint32_t ones = p.ones;
     const float sc_tail = a.scale * 1.4426950408889634f, sc_mem = sc_tail * KV4_S;
-    const int pr = r ^ (r >> 1 & 1), pv0 = 2 * j ^ (j & 1), pv1 = pv0 ^ 1;   // entries of this lane's rows of scores, and of its pairs of values
-    const int k_at = pr * TL::ROW + (j ^ ((r & 4) >> 1)) * 2 * TL::CHUNK, v_x = (r ^ (j & 2) << 1) * TL::CHUNK;
+    const int k_at = kv4_k_unit<D>(r, 2 * j), v_at = kv4_v_unit<D>(2 * j, r);   // this lane's keys' row r, and its values' rows 2j, 2j + 1
     const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
     uint32_t qf[R][2 * G][2];                    // operand B: column = head x * 8 + r
     float m[R][2], ref[R][2], l[R][2];           // heads x * 8 + 2j, + 1.  m: the reference as a raw product; ref: what exponents are taken off
@@ -693,7 +674,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
         if (run > 0) fetch();
         if (++slot == NS) { slot = 0; phase ^= 1; }
     };
-    // z: raw products of rows pr (0, 1) and pr + 8 (2, 3) of one or two tiles, heads 2j, 2j + 1 (-inf: no weight) -> weights
+    // z: raw products of rows r (0, 1) and r + 8 (2, 3) of one or two tiles, heads 2j, 2j + 1 (-inf: no weight) -> weights
     // 2^(z sc - ref)
     const float grow_mem = 8.f / sc_mem, grow_tail = 8.f / sc_tail;
     auto weights = [&](int x, auto& z, float sc, float grow) {
@@ -759,17 +740,17 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const uint8_t* tile = st + u * TL::BYTES;
-                uint32_t k0[2][G / 2], k1[2][G / 2];
+                uint32_t k0[G], k1[G];
                 float h0[G], h1[G];
-                chunk_pair<G>(tile + k_at, k0);
-                chunk_pair<G>(tile + k_at + 8 * TL::ROW, k1);
-                steps_of<G>(tile + TL::K_STEPS + pr * TL::STEPS, h0);
-                steps_of<G>(tile + TL::K_STEPS + (pr + 8) * TL::STEPS, h1);
+                kv4_unit<G>(tile + k_at, k0);
+                kv4_unit<G>(tile + k_at + 8 * TL::ROW, k1);
+                steps_of<G>(tile + TL::K_STEPS + r * TL::STEPS, h0);
+                steps_of<G>(tile + TL::K_STEPS + (r + 8) * TL::STEPS, h1);
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     uint32_t e0[4], e1[4];
-                    group_pairs(g, k0[0][g / 2], k0[1][g / 2], ones, e0);
-                    group_pairs(g, k1[0][g / 2], k1[1][g / 2], ones, e1);
+                    kv4_word(k0[g], ones, e0);
+                    kv4_word(k1[g], ones, e1);
 #pragma unroll
                     for (int x = 0; x < R; ++x) {
                         float t[4];
@@ -788,7 +769,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 for (int x = 0; x < R; ++x)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (pr + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
+                        if (r + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
             }
 #pragma unroll
             for (int x = 0; x < R; ++x) {
@@ -799,26 +780,24 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const uint8_t* tile = st + u * TL::BYTES;
-                uint32_t v0[G / 2], v1[G / 2], v2[G / 2], v3[G / 2];
+                uint32_t v0[G], v1[G];
                 float h0[G], h1[G];
-                halves<G>(tile + TL::V + pv0 * TL::ROW + v_x, v0);
-                halves<G>(tile + TL::V + pv1 * TL::ROW + v_x, v1);
-                halves<G>(tile + TL::V + (pv0 + 8) * TL::ROW + v_x, v2);
-                halves<G>(tile + TL::V + (pv1 + 8) * TL::ROW + v_x, v3);
-                steps_of<G>(tile + TL::V_STEPS + pr * TL::STEPS, h0);
-                steps_of<G>(tile + TL::V_STEPS + (pr + 8) * TL::STEPS, h1);
+                kv4_unit<G>(tile + v_at, v0);
+                kv4_unit<G>(tile + v_at + 8 * TL::ROW, v1);
+                steps_of<G>(tile + TL::V_STEPS + r * TL::STEPS, h0);
+                steps_of<G>(tile + TL::V_STEPS + (r + 8) * TL::STEPS, h1);
                 if (valid < KV4_STEP) {   // ... and 0 x NaN is not 0
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        if (pr + 16 * u >= valid) h0[g] = 0.f;
-                        if (pr + 16 * u + 8 >= valid) h1[g] = 0.f;
+                        if (r + 16 * u >= valid) h0[g] = 0.f;
+                        if (r + 16 * u + 8 >= valid) h1[g] = 0.f;
                     }
                 }
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     uint32_t e0[4], e1[4];
-                    group_pairs(g, v0[g / 2], v1[g / 2], ones, e0);
-                    group_pairs(g, v2[g / 2], v3[g / 2], ones, e1);
+                    kv4_word(v0[g], ones, e0);
+                    kv4_word(v1[g], ones, e1);
 #pragma unroll
                     for (int x = 0; x < R; ++x) {
                         // weight times step, rounded to bf16: off by 2^-8 of its value at most; the sums stay in fp32
@@ -843,7 +822,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
             float s[R][4];
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                const uint4 u0 = *reinterpret_cast<const uint4*>(st + (pr * D + 32 * g + 8 * j) * 2), u1 = *reinterpret_cast<const uint4*>(st + ((pr + 8) * D + 32 * g + 8 * j) * 2);
+                const uint4 u0 = *reinterpret_cast<const uint4*>(st + (r * D + 32 * g + 8 * j) * 2), u1 = *reinterpret_cast<const uint4*>(st + ((r + 8) * D + 32 * g + 8 * j) * 2);
 #pragma unroll
                 for (int x = 0; x < R; ++x) {
                     const uint32_t e0[4] = {__byte_perm(u0.x, u0.z, 0x5410), __byte_perm(u0.x, u0.z, 0x7632), __byte_perm(u0.y, u0.w, 0x5410), __byte_perm(u0.y, u0.w, 0x7632)};
@@ -860,7 +839,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
             for (int x = 0; x < R; ++x) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (pr + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
+                    if (r + (e >> 1) * 8 >= valid) s[x][e] = -INFINITY;
                 weights(x, s[x], sc_tail, grow_tail);
                 b0[x] = transposed(pack_bf16(s[x][0], s[x][1]));
                 b1[x] = transposed(pack_bf16(s[x][2], s[x][3]));
@@ -872,7 +851,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 uint2 v[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int e = (k & 1 ? pv1 : pv0) + (k & 2) * 4;
+                    const int e = 2 * j + (k & 1) + (k & 2) * 4;
                     v[k] = *reinterpret_cast<const uint2*>(st + (e * D + 32 * g + 4 * r) * 2);
                     if (e >= valid) v[k] = make_uint2(0, 0);   // rows past the last one may hold anything, and 0 x NaN is not 0
                 }

@@ -8,14 +8,16 @@
 // A pool is [n_pages][Hkv][page_size / 16] tiles of 16 entries.  A tile holds, for its 16 rows, the keys' bits, the values' bits, the
 // keys' steps, the values' steps, one behind the other, so one copy fetches it: 2304 bytes for D = 128 (in bf16: 8192).
 //
-// A row's bits are laid out for warp-level m16n8k16 products.  Feature 32 g + 4 x + e (group g, x = 0 .. 7, e = 0 .. 3) lies in
-// chunk x, half-word g, a half-word's 16 bits being
+// The bits are laid out for warp-level m16n8k16 products.  Feature 32 g + 4 x + e (group g, x = 0 .. 7, e = 0 .. 3) lies in half-word (x, g)
+// of its row, whose 16 bits are
 //     m0 m1 s2 s3 | m2 m3 s0 s1        (3 3 1 1 | 3 3 1 1 bits, lowest first; s: sign)
-// With the half-word itself (e = 1), doubled (e = 0), and the same with its bytes exchanged (e = 3, 2), sign and m stand where one
-// AND and one OR make them the bf16 pattern of +-(2 m + 1) 2^-133 (times 4 for odd e): a number below the normal range, which the
-// products take as it is, so turning 4 bits into operands takes two instructions a pair and adds no offset that would have to be
-// taken off again.  Powers of two bring the sums back (see decode_kv4.cu).
-// Chunk x of row k lies at x ^ (4 if k & 4), which spreads the reads of a tile in shared memory over its banks.
+// In a word of two half-words that want to be neighbours in an operand, the word itself (e = 1), doubled (e = 0), and the same with the
+// bytes of each half exchanged (e = 3, 2) have sign and m where one AND and one OR make them the bf16 pattern of +-(2 m + 1) 2^-133
+// (times 4 for odd e): a number below the normal range, which the products take as it is.  So 4 bits turn into operands in under two
+// instructions a pair, with no offset to be taken off again; powers of two bring the sums back (see KV4_Q and the like).
+// Neighbours are, for keys, half-words x and x + 1 (x even) of a row: word g of unit x / 2, four units to a row, row after row.  For
+// values, rows k and k + 1 (k even): word g of unit x, eight units to a pair of rows, unit x of pair p at x ^ 2 (p & 3) (D = 64: p & 2), which
+// spreads the reads of a tile in shared memory over its banks.
 #pragma once
 
 #include <algorithm>
@@ -30,7 +32,7 @@ constexpr int KV4_GROUP = 32;   // features that share a step
 template <int D>
 struct Kv4Tile {
     static constexpr int GROUPS = D / KV4_GROUP;
-    static constexpr int CHUNK = D / 16;                         // bytes: a half-word per group
+    static constexpr int UNIT = 4 * GROUPS;                      // bytes: a word per group
     static constexpr int ROW = D / 2, STEPS = GROUPS * 2;        // bytes of a row's bits and of its steps
     static constexpr int V = KV4_ROWS * ROW, K_STEPS = 2 * V, V_STEPS = K_STEPS + KV4_ROWS * STEPS;   // where they begin
     static constexpr int BYTES = V_STEPS + KV4_ROWS * STEPS;
@@ -57,7 +59,7 @@ struct Kv4LoadArgs {
     void *k = nullptr, *v = nullptr;   // [B, Hkv, cap, D]
     const int32_t* mem_lens = nullptr;
     int B = 0, Hkv = 0, cap = 0;
-    uint32_t ones = 0x00010001u;       // see kv4_pairs
+    uint32_t ones = 0x00010001u;       // see kv4_word
 };
 cudaError_t launch_kv4_append(const Kv4AppendArgs& a, int D, loma_dtype dt, cudaStream_t st);   // kv4_store.cu
 cudaError_t launch_kv4_load(const Kv4LoadArgs& a, int D, loma_dtype dt, cudaStream_t st);
@@ -89,23 +91,17 @@ __device__ __forceinline__ int64_t kv4_tile(const Kv4Pool& m, int Hkv, int page,
     const int tiles = 1 << (m.log2_ps - 4), t = (j & ((1 << m.log2_ps) - 1)) >> 4;
     return (((int64_t)page * Hkv + h) * tiles + t) * Kv4Tile<D>::BYTES;
 }
-// byte offset of chunk x of row k among a tile's bits of keys (or of values)
+// byte offsets of the units that hold half-words x of row k, among a tile's keys and from its beginning (values)
 template <int D>
-__device__ __forceinline__ int kv4_chunk(int k, int x) { return k * Kv4Tile<D>::ROW + (x ^ (k & 4)) * Kv4Tile<D>::CHUNK; }
+__device__ __forceinline__ int kv4_k_unit(int k, int x) { return k * Kv4Tile<D>::ROW + (x >> 1) * Kv4Tile<D>::UNIT; }
+template <int D>
+__device__ __forceinline__ int kv4_v_unit(int k, int x) {
+    return Kv4Tile<D>::V + (k >> 1) * 2 * Kv4Tile<D>::ROW + (x ^ (k & (D == 128 ? 6 : 4))) * Kv4Tile<D>::UNIT;
+}
 
-// A and B: half-words of two chunks (two rows, or two chunks of a row), group by group.  Out: the pair's four elements e as bf16 pairs
-// (A low, B high), +-(2 m + 1) 2^-133, times 4 for odd e.  HI: the upper half-words of the words.  ones: 0x00010001, from a kernel
+// The four elements e of a word's two half-words as bf16 pairs, +-(2 m + 1) 2^-133, times 4 for odd e.  ones: 0x00010001, from a kernel
 // parameter: an AND-OR takes one constant in the instruction, and the other one, where the compiler knows it, is moved to a register
 // before every use.
-template <bool HI>
-__device__ __forceinline__ void kv4_pairs(uint32_t a, uint32_t b, uint32_t ones, uint32_t (&p)[4]) {
-    const uint32_t u = __byte_perm(a, b, HI ? 0x7632 : 0x5410), w = __byte_perm(a, b, HI ? 0x6723 : 0x4501);
-    p[0] = ((u << 1) & 0x800E800Eu) | ones;
-    p[1] = (u & 0x80388038u) | ones << 2;
-    p[2] = ((w << 1) & 0x800E800Eu) | ones;
-    p[3] = (w & 0x80388038u) | ones << 2;
-}
-// the same of one word: elements e of groups 2 i (low) and 2 i + 1 (high) of a chunk
 __device__ __forceinline__ void kv4_word(uint32_t u, uint32_t ones, uint32_t (&p)[4]) {
     const uint32_t w = __byte_perm(u, 0, 0x2301);
     p[0] = ((u << 1) & 0x800E800Eu) | ones;
@@ -120,9 +116,28 @@ constexpr float KV4_S = 590295810358705651712.f;                   // 2^69
 constexpr float KV4_P = 1208925819614629174706176.f;               // 2^80
 constexpr float KV4_O = 9007199254740992.f;                        // 2^53
 
-// G half-words (a chunk's bytes, a row's steps) as words
+// the G words of a unit
 template <int G>
-__device__ __forceinline__ void halves(const uint8_t* p, uint32_t (&w)[G / 2]) {
+__device__ __forceinline__ void kv4_unit(const uint8_t* p, uint32_t (&w)[G]) {
+    if constexpr (G == 4) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+    } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        w[0] = u.x; w[1] = u.y;
+    }
+}
+// one row's half-words of a unit, groups 2 i and 2 i + 1 in word i
+template <int G>
+__device__ __forceinline__ void kv4_halves(const uint8_t* p, bool upper, uint32_t (&w)[G / 2]) {
+    uint32_t u[G];
+    kv4_unit<G>(p, u);
+#pragma unroll
+    for (int i = 0; i < G / 2; ++i) w[i] = __byte_perm(u[2 * i], u[2 * i + 1], upper ? 0x7632 : 0x5410);
+}
+// a row's steps, groups 2 i and 2 i + 1 in word i
+template <int G>
+__device__ __forceinline__ void kv4_steps(const uint8_t* p, uint32_t (&w)[G / 2]) {
     if constexpr (G == 4) {
         const uint2 u = *reinterpret_cast<const uint2*>(p);
         w[0] = u.x; w[1] = u.y;

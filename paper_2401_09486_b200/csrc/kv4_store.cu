@@ -1,7 +1,6 @@
 // Memory entries into a 4-bit pool and back (loma_kv4_append, loma_kv4_load); format in kv4.cuh.
 //
-// Eight lanes share a row: lane x has features 32 g + 4 x .. + 3 of every group g, which are the four of a half-word, so a lane writes
-// one chunk of 8 (or 4) bytes.  Keys and values of an entry go together: eight loads in flight per lane, and the largest magnitudes of
+// Eight lanes share a row: lane x has features 32 g + 4 x .. + 3 of every group g, which are the four of half-word (x, g).  Keys and values of an entry go together: eight loads in flight per lane, and the largest magnitudes of
 // the eight groups are found with results spread over the lanes (seven shuffles), so each lane works out one step.  Both directions are
 // bound by HBM (256 bytes of bf16 against 72 for a row of 128 features) as long as a value costs few instructions: m is the integer part
 // of |x| / (2 h), a product and an addition that rounds towards zero; see kv4_half for why that is exact.
@@ -108,10 +107,9 @@ __device__ __forceinline__ void spread_max8(float* s, int x, unsigned lanes) {
     if constexpr (O > 1) spread_max8<(M > 1 ? M / 2 : 1), O / 2>(s, x, lanes);
 }
 
-// G half-words: a chunk's bytes, or a row's steps
-template <int G>
-__device__ __forceinline__ void put_halves(uint8_t* p, const uint32_t (&w)[G / 2]) {
-    if constexpr (G == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+template <int N>
+__device__ __forceinline__ void put_words(uint8_t* p, const uint32_t (&w)[N]) {
+    if constexpr (N == 2) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint32_t*>(p) = w[0];
 }
 
@@ -156,8 +154,26 @@ __global__ void __launch_bounds__(STORE_THREADS) kv4_append_kernel(const Kv4Appe
 #pragma unroll
             for (int i = 0; i < G / 2; ++i)
                 half[i] = kv4_half(f[w][2 * i], bf16lo(step[w][i])) | kv4_half(f[w][2 * i + 1], bf16hi(step[w][i])) << 16;
-            put_halves<G>(tile + w * TL::V + kv4_chunk<D>(row, x), half);
-            if (x == w) put_halves<G>(tile + TL::K_STEPS + w * (TL::V_STEPS - TL::K_STEPS) + row * TL::STEPS, step[w]);
+            if (w == 0) {
+                // keys: lanes x and x ^ 1 make the unit's words of them, the even lane those of the lower groups, the odd one of the upper
+                const bool odd = x & 1;
+                uint32_t word[G / 2];
+                if constexpr (G == 4) {
+                    const uint32_t other = __shfl_xor_sync(mine, odd ? half[0] : half[1], 1), own = odd ? half[1] : half[0];
+                    word[0] = odd ? __byte_perm(other, own, 0x5410) : __byte_perm(own, other, 0x5410);
+                    word[1] = odd ? __byte_perm(other, own, 0x7632) : __byte_perm(own, other, 0x7632);
+                } else {
+                    const uint32_t other = __shfl_xor_sync(mine, half[0], 1);
+                    word[0] = odd ? __byte_perm(other, half[0], 0x7632) : __byte_perm(half[0], other, 0x5410);
+                }
+                put_words(tile + kv4_k_unit<D>(row, x) + odd * (TL::UNIT / 2), word);
+            } else {
+                // values: the other half of each word is another row's
+                uint8_t* unit = tile + kv4_v_unit<D>(row, x) + (row & 1) * 2;
+#pragma unroll
+                for (int g = 0; g < G; ++g) *reinterpret_cast<uint16_t*>(unit + 4 * g) = (uint16_t)(half[g / 2] >> g % 2 * 16);
+            }
+            if (x == w) put_words(tile + TL::K_STEPS + w * (TL::V_STEPS - TL::K_STEPS) + row * TL::STEPS, step[w]);
         }
     }
 }
@@ -179,8 +195,8 @@ __global__ void __launch_bounds__(STORE_THREADS) kv4_load_kernel(const Kv4LoadAr
         uint32_t half[2][G / 2], step[2][G / 2];
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-            halves<G>(tile + w * TL::V + kv4_chunk<D>(row, x), half[w]);
-            halves<G>(tile + TL::K_STEPS + w * (TL::V_STEPS - TL::K_STEPS) + row * TL::STEPS, step[w]);
+            kv4_halves<G>(tile + (w ? kv4_v_unit<D>(row, x) : kv4_k_unit<D>(row, x)), w ? row & 1 : x & 1, half[w]);
+            kv4_steps<G>(tile + TL::K_STEPS + w * (TL::V_STEPS - TL::K_STEPS) + row * TL::STEPS, step[w]);
         }
         // n 2^-133 times 2^127, the step and 2^6 (2^4 for odd e): exact in this order, whatever the step
         constexpr float UP = 1.7014118346046923e38f;   // 2^127
