@@ -967,8 +967,8 @@ LOMA_API int loma_paged_copy(int n_pools, void* const* pools, const int64_t* pag
  * Page numbers outside the pool are clamped to it where they are read (load, decode).
  * Precision: memory entries are what they stand for, (2 m + 1) h, without a further rounding; scores, the softmax and the sums are
  * fp32.  bf16 calls run on the tensor cores and round each weight (times the step of the value's group) to bf16 for the product
- * with V, off by 2^-8 of itself at most; fp32, and LOMA_FLAG_FORCE_GENERIC, keep it.  On the tensor cores queries up to 2^60 and
- * values up to 2^40 in magnitude.
+ * with V, off by 2^-8 of itself at most; fp32, and LOMA_FLAG_FORCE_GENERIC, keep it.  For queries up to 2^60 and memory values
+ * up to 2^40 in magnitude (sums carry powers of two).
  * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CAPACITY, WORKSPACE, CUDA.  B * Hkv * l == 0, B * Hkv * cap == 0, B * Hq == 0: a no-op.
  * ------------------------------------------------------------------------- */
 LOMA_API size_t loma_kv4_page_bytes(int Hkv, int D, int page_size);

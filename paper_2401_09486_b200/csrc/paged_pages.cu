@@ -14,7 +14,6 @@
 #include <limits.h>
 
 #include <algorithm>
-#include <vector>
 
 #include <cooperative_groups.h>
 

@@ -6,6 +6,9 @@ off by at most (D + 8) 2^-23 of scale * sum |q_d k_d| (twice a half step per ter
 off by that much of itself, and so is the weights' sum: twice.  Exponentials and the merge's factors take 2^-20 together, sums of n weights n 2^-23.  bf16 calls on the tensor
 cores round each weight times its step to bf16 (half a step: 2^-8), and the output once (2^-8 of it); fp32 rounds the output by 2^-24."""
 
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -65,6 +68,19 @@ def test_pages_match_oracle(B, M, ps, n_pages, seed):
         H.check_fork(H.run_fork(case, parents, ps, most, DEV, with_fixed=f is not None, with_held=h is not None),
                      C.fork(parents, lens, f, h, table, ps, refs, free, taken, most))
     H.check_compact(H.run_compact(case, most, DEV), C.compact(held, table, refs, free, taken, most))
+
+
+@pytest.mark.parametrize("B,M", [(40, 30), (300, 20)])
+def test_pages_of_a_pool_looked_at_in_stretches(B, M):
+    """More pages than the words of a cluster's shared memory."""
+    case = H.pool_case(7, B, M, 4, 1200000)
+    lens, fixed, held, table, refs, free, taken, rng = case
+    keep = np.where(rng.random(B) < 0.3, -1, rng.integers(0, M * 4 + 2, B))
+    H.check_release(H.run_release(case, keep, 4, DEV), C.release(keep, held, table, 4, refs, free, taken))
+    parents = H.parents_of(case, "any")
+    H.check_fork(H.run_fork(case, parents, 4, 5000, DEV), C.fork(parents, lens, fixed, held, table, 4, refs, free, taken, 5000))
+    for most in (100, 20000):
+        H.check_compact(H.run_compact(case, most, DEV), C.compact(held, table, refs, free, taken, most))
 
 
 @pytest.mark.parametrize("taken", [-5, 0, 10**6])
@@ -232,6 +248,24 @@ def test_kv4_offsets_beyond_32_bits():
         assert (np.abs(npf(o)[:, :, 0] - want) <= 2.0**-7 * o_abs + 1e-6).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_append_row_by_row_in_any_order(dtype, D):
+    """Rows share words with their neighbours: entry after entry, in any order and in pieces, the pool becomes what one call makes it."""
+    B, Hkv, ps, n = 3, 2, 16, 45
+    k, v = normal((B, Hkv, n, D), 1, dtype), normal((B, Hkv, n, D), 2, dtype)
+    table, whole = table_of(B, 3, 0), new_pool(11, Hkv, D, ps, 255)
+    L.loma_kv4_append(k, v, whole, table, ps, di32([0] * B))
+    rng = np.random.default_rng(0)
+    single, pieces = new_pool(11, Hkv, D, ps, 255), new_pool(11, Hkv, D, ps, 255)
+    for e in rng.permutation(n).tolist():
+        L.loma_kv4_append(k[:, :, e:e + 1], v[:, :, e:e + 1], single, table, ps, di32([e] * B))
+    cuts = [0, 1, 4, 5, 11, 18, 33, 44, n]
+    for e0, e1 in rng.permutation(list(zip(cuts, cuts[1:]))).tolist():
+        L.loma_kv4_append(k[:, :, e0:e1], v[:, :, e0:e1], pieces, table, ps, di32([e0] * B))
+    assert torch.equal(single, whole) and torch.equal(pieces, whole)
+
+
 # ------------------------------------------------------------------------------------------------ decode
 def make(B, Hq, Hkv, D, mems, tails, ps, dtype, seed=0, cap=None, std=1.0, garbage=True):
     """A batch: memory entries stored through the block table, tails in caches; everything no request may see is NaN."""
@@ -331,6 +365,36 @@ def test_decode(case, dtype, flags):
             kt[b, :, n], vt[b, :, n] = s["kn"][b, :, 0], s["vn"][b, :, 0]
     for got, want in ((s["kt"], kt), (s["vt"], vt)):
         assert np.array_equal(npf(got), npf(want), equal_nan=True)
+
+
+CUT = [
+    (2, 24, 2, 128, [3000, 517], [40, 0], 16),
+    (3, 8, 8, 64, [1700, 0, 333], [-1, 17, 5], 32),
+    (1, 40, 2, 64, [2100], [3], 128),
+    (5, 6, 3, 128, [0, 31, 32, 33, 900], [0, 15, 16, 31, 100], 16),
+    (2, 17, 1, 128, [64, 4000], [100, 1], 256),
+]
+
+
+@pytest.mark.parametrize("dtype,flags", KINDS)
+@pytest.mark.parametrize("case", range(len(CUT)))
+def test_decode_cut_into_equal_shares(case, dtype, flags):
+    """Bounds as high as a table's capacity: units are cut among all workers, and joined from the workspace."""
+    s = make(*CUT[case], dtype, seed=100 + case)
+    s["table"] = torch.cat([s["table"], torch.full((s["B"], 200000 // s["ps"]), -1, dtype=torch.int32, device=DEV)], 1).contiguous()
+    top, s["max_mem"] = s["max_mem"], 150000
+    s["ws"] = torch.full((L.loma_decode_kv4_workspace_bytes(s["B"], s["Hq"], s["Hkv"], s["D"], 150000, s["max_tail"]),), 255, dtype=torch.uint8, device=DEV)
+    call(s, flags)
+    s["max_mem"] = top
+    check(s, flags)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,most,ps", [(75, 16, 8, 128, 300, 16), (150, 20, 4, 64, 500, 64), (70, 9, 9, 128, 90, 16)])
+def test_decode_many_units(B, Hq, Hkv, D, most, ps):
+    """More units than run at once: cut, rows joined by one set of lanes each; and short ones, whole."""
+    s = make(B, Hq, Hkv, D, [(37 * b) % most for b in range(B)], [(b * 7) % 40 - 1 for b in range(B)], ps, torch.bfloat16, seed=B)
+    call(s)
+    check(s)
 
 
 @pytest.mark.parametrize("dtype,flags", KINDS)
@@ -669,3 +733,55 @@ def test_prompt_memory_through_load_and_prefill():
         assert np.array_equal(hk[b, :, :n], stored(k, dtype)[b, :, :n])
         want = O.prefill_attn(npf(q)[b:b + 1], npf(kn)[b:b + 1], npf(vn)[b:b + 1], hk[b:b + 1], hv[b:b + 1], n)[0]
         assert (np.abs(npf(o)[b] - want[0]) <= 2e-2).all()
+
+
+
+FIRST_CALL = """
+import sys
+import torch
+from paper_2401_09486_b200 import binding as L
+d, bf, which = "cuda:0", torch.bfloat16, sys.argv[1]
+i = lambda *x: torch.tensor(x, dtype=torch.int32, device=d)
+z = lambda *x: torch.zeros(x, dtype=torch.int32, device=d)
+k, q = torch.randn(2, 2, 20, 64, device=d).to(bf), torch.randn(2, 4, 1, 64, device=d).to(bf)
+kn, vn, o = k[:, :, :1].contiguous(), k[:, :, 1:2].contiguous(), torch.zeros_like(q)
+kc, vc = torch.zeros_like(k), torch.zeros_like(k)
+pool = torch.zeros(8, L.loma_kv4_page_bytes(2, 64, 16), dtype=torch.uint8, device=d)
+some = torch.randint(1, 100, tuple(pool.shape), dtype=torch.uint8, device=d)
+ws = torch.zeros(1 << 24, dtype=torch.uint8, device=d)
+table, wide, long = i(0, 1, 2, 3).view(2, 2), torch.cat([i(0, 1, 2, 3).view(2, 2), z(2, 20000)], 1).contiguous(), z(400, 3)
+lens, tails, held, refs, free, taken, counts, src, dst = i(20, 7), i(3, 0), i(2, 2), z(8), i(7, 6, 5, 4), i(1), z(4), z(6), z(6)
+out, wide_out, l2, h2, l4, h4, none, one4, page_map = z(2, 2), z(400, 3), z(2), z(2), z(400), z(400), z(400) - 1, z(400) + 1, z(8)
+state = (refs, free, taken)
+parents, keep, keep4, one, zero = i(1, 0), z(2), z(400), i(1), i(0)
+decode = lambda bound: L.loma_decode_attn_kv4(q, kn, vn, kc, vc, tails, 3, pool, wide, 16, lens, bound, o, None, workspace=ws)
+calls = {
+    "append": (pool, lambda: L.loma_kv4_append(k, k, pool, table, 16, keep)),
+    "load": (kc, lambda: L.loma_kv4_load(some, table, 16, lens, kc, vc)),
+    "whole": (o, lambda: decode(32)), "cluster": (o, lambda: decode(1000)), "cut": (o, lambda: decode(300000)),
+    "release": (counts, lambda: L.loma_paged_release(keep, held, table, 16, held, *state, counts)),
+    "release_long": (counts, lambda: L.loma_paged_release(keep4, one4, long, 16, one4, *state, counts)),
+    "fork": (out, lambda: L.loma_paged_fork(parents, lens, None, held, table, 16, out, l2, h2, *state, src, dst, counts, workspace=ws)),
+    "fork_long": (counts, lambda: L.loma_paged_fork(none, one4, None, one4, long, 16, wide_out, l4, h4, *state, src, dst, counts, workspace=ws)),
+    "compact": (page_map, lambda: L.loma_paged_compact(held, table, *state, page_map, src, dst, counts)),
+    "compact_long": (page_map, lambda: L.loma_paged_compact(one4, long, *state, page_map, src, dst, counts)),
+    "copy": (pool, lambda: L.loma_paged_copy([pool, some], one, zero, one)),
+}
+if which == "copy":
+    pool[1] = 1
+result, call = calls[which]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    call()
+graph.replay()
+torch.cuda.synchronize()
+assert result.ne(0).any() and (which != "copy" or bool((pool[0] == 1).all()))
+print("captured")
+"""
+
+
+@pytest.mark.parametrize("which", ["append", "load", "whole", "cluster", "cut", "release", "release_long", "fork", "fork_long", "compact", "compact_long", "copy"])
+def test_the_first_call_of_a_process_may_be_captured(which):
+    out = subprocess.run([sys.executable, "-c", FIRST_CALL, which], capture_output=True, text=True, timeout=300, cwd=build.ROOT)
+    assert out.returncode == 0 and "captured" in out.stdout, out.stderr[-2000:]
