@@ -69,8 +69,12 @@ static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, int max_mem, int max
     return p;
 }
 
-// the first block of worker w of W <= T
-__device__ __forceinline__ int64_t kv4_first(int64_t w, int64_t T, int64_t W) { return T / W * w + T % W * w / W; }
+// the first block of worker w of W <= T (W^2 fits 32 bits; a division of 64 bits takes a hundred instructions)
+__device__ __forceinline__ int64_t kv4_first(int64_t w, int64_t T, int64_t W) {
+    if (T > UINT32_MAX) return T / W * w + T % W * w / W;
+    const uint32_t q = (uint32_t)T / (uint32_t)W, r = (uint32_t)T - q * (uint32_t)W;
+    return (int64_t)q * w + r * (uint32_t)w / (uint32_t)W;
+}
 
 // One sequence's part of a unit.
 struct Kv4Seq {
@@ -86,11 +90,13 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4DecodeArgs& a, int b) {
     return s;
 }
 
-// a worker that does blocks [from, to) of a unit of n notes where the unit's segments begin and end
+// A worker that does blocks [from, to) of a unit of n notes where the unit's segments begin and end; a unit that it does all of has none left
+// to be joined.
 __device__ __forceinline__ void kv4_note(const Kv4DecodeArgs& a, const Kv4Plan& p, int64_t unit, int64_t w, int from, int to, int n) {
     int32_t* ends = reinterpret_cast<int32_t*>(static_cast<float*>(a.ws) + p.ends);
-    if (from == 0) ends[unit] = (int)w;
-    if (to == n) ends[(int64_t)a.B * a.Hkv * p.g_tiles + unit] = (int)w;
+    const bool all = from == 0 && to == n;
+    if (from == 0) ends[unit] = all ? 1 : (int)w;
+    if (to == n) ends[(int64_t)a.B * a.Hkv * p.g_tiles + unit] = all ? 0 : (int)w;
 }
 
 // The numbering of the blocks, found again by every CTA.
@@ -138,13 +144,13 @@ struct Kv4Blocks {
     __device__ __forceinline__ Cursor find(int64_t t, const int64_t* s, int per) const {
         const int groups = (a.B + per - 1) / per;
         Cursor c;
-        c.hh = (int)(t / s[groups]);
-        int64_t rem = t - c.hh * s[groups];
-        int lo = 0, hi = groups;   // s[lo] <= rem < s[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (s[mid] <= rem) lo = mid; else hi = mid;
-        }
+        const int64_t n = s[groups];
+        c.hh = t <= UINT32_MAX && n <= UINT32_MAX ? (int)((uint32_t)t / (uint32_t)n) : (int)(t / n);
+        int64_t rem = t - c.hh * n;
+        // the last group with s[lo] <= rem, by a warp: 16 groups to a lane, then one
+        const int lane = threadIdx.x & 31;
+        int lo = 16 * (__popc(__ballot_sync(0xffffffffu, lane * 16 < groups && s[min(lane * 16, groups)] <= rem)) - 1);
+        lo += __popc(__ballot_sync(0xffffffffu, lane < 16 && lo + lane < groups && s[min(lo + lane, groups)] <= rem)) - 1;
         rem -= s[lo];
         for (c.b = lo * per;; ++c.b) {
             c.s = kv4_seq(a, c.b);
@@ -200,6 +206,9 @@ __device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&x)[4]) {
     const uint2 u = *reinterpret_cast<const uint2*>(p);
     x[0] = bf16lo(u.x); x[1] = bf16hi(u.x); x[2] = bf16lo(u.y); x[3] = bf16hi(u.y);
 }
+
+__device__ __forceinline__ void kv4_put(float* p, const float4& o) { *reinterpret_cast<float4*>(p) = o; }
+__device__ __forceinline__ void kv4_put(__nv_bfloat16* p, const float4& o) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w)); }
 
 template <typename T, int D, int G>
 __global__ void __launch_bounds__(KV4_WARPS * 32, G == 4 ? 2 : 4)
@@ -396,7 +405,13 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
         for (int o = DUP; o < LH; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
         l += __shfl_xor_sync(0xffffffffu, l, 8);
         l += __shfl_xor_sync(0xffffffffu, l, 16);
-        if (sub == 0 && x % LH == 0 && x / LH < heads) ws[p.lse + seg * p.g_rows + x / LH] = ref + log2f(l);
+        const bool all = c.blk == 0 && blocks + tails == c.s.n;       // the rows' results, not parts of them
+        const int64_t row0 = (int64_t)c.b * a.Hq + h * a.g + gt * G;
+        if (sub == 0 && x % LH == 0 && x / LH < heads) {
+            const float e = ref + log2f(l);
+            if (!all) ws[p.lse + seg * p.g_rows + x / LH] = e;
+            else if (a.lse) a.lse[row0 + x / LH] = e * 0.6931471805599453f;
+        }
 #pragma unroll
         for (int y = 0; y < G; ++y) {
             const float inv = 1.f / __shfl_sync(0xffffffffu, l, y * LH);
@@ -407,9 +422,11 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
                     acc[y][g][e] += __shfl_xor_sync(0xffffffffu, acc[y][g][e], 8);
                     acc[y][g][e] += __shfl_xor_sync(0xffffffffu, acc[y][g][e], 16);
                 }
-                if (y < heads && sub == 0)
-                    *reinterpret_cast<float4*>(ws + p.o + (seg * p.g_rows + y) * D + 32 * g + 4 * x) =
-                        make_float4(acc[y][g][0] * inv, acc[y][g][1] * inv, acc[y][g][2] * inv, acc[y][g][3] * inv);
+                if (y < heads && sub == 0) {
+                    const float4 o = make_float4(acc[y][g][0] * inv, acc[y][g][1] * inv, acc[y][g][2] * inv, acc[y][g][3] * inv);
+                    if (all) kv4_put(static_cast<T*>(a.o) + (row0 + y) * D + 32 * g + 4 * x, o);
+                    else *reinterpret_cast<float4*>(ws + p.o + (seg * p.g_rows + y) * D + 32 * g + 4 * x) = o;
+                }
             }
         }
         left -= blocks + tails;
@@ -498,9 +515,7 @@ struct Kv4Join {
     template <typename T, int D>
     __device__ __forceinline__ void store(const Kv4DecodeArgs& a, int64_t row, int c4) const {   // row = b * Hq + head
         const float inv = 1.f / total;
-        T* out = static_cast<T*>(a.o) + row * D + c4 * 4;
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o_.x * inv, o_.y * inv), pack_bf16(o_.z * inv, o_.w * inv));
-        else *reinterpret_cast<float4*>(out) = make_float4(o_.x * inv, o_.y * inv, o_.z * inv, o_.w * inv);
+        kv4_put(static_cast<T*>(a.o) + row * D + c4 * 4, make_float4(o_.x * inv, o_.y * inv, o_.z * inv, o_.w * inv));
         if (a.lse && c4 == 0) a.lse[row] = (M + log2f(total)) * 0.6931471805599453f;
     }
 };
@@ -869,7 +884,9 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
             done_with();
         }
         if (!ok) break;
-        // the partial result: in the workspace, or (WHOLE) in place of the ring, which has been used up
+        // the partial result: in the workspace, or (WHOLE) in place of the ring, which has been used up.  A worker that has done all of a unit
+        // has the rows' results
+        const bool all = !WHOLE && c.blk == 0 && tiles + tails == c.s.n;
         const int64_t unit = (int64_t)c.hh * a.B + c.b, seg = w + unit;
         if (!WHOLE && lane == 0) kv4_note(a, p, unit, w, c.blk, c.blk + tiles + tails, c.s.n);
         float *const o_part = WHOLE ? reinterpret_cast<float*>(ring) : ws + p.o + seg * p.g_rows * D, *const lse_part = WHOLE ? s_lse[warp] : ws + p.lse + seg * p.g_rows;
@@ -882,13 +899,16 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
                 for (int o = 4; o < 32; o <<= 1) lt += __shfl_xor_sync(0xffffffffu, lt, o);
                 const int hd = x * 8 + 2 * j + y;
                 if (hd < heads) {
-                    const float inv = 1.f / lt;
-                    float* o = o_part + hd * D + 4 * r;   // 8 lanes: 128 contiguous bytes
+                    const float inv = 1.f / lt, e = ref[x][y] + log2f(lt);
+                    const int64_t row = (int64_t)c.b * a.Hq + h * a.g + gt * p.g_rows + hd;
 #pragma unroll
-                    for (int g = 0; g < G; ++g)
-                        *reinterpret_cast<float4*>(o + 32 * g) = make_float4(acc[x][2 * g][y] * inv, acc[x][2 * g][2 + y] * inv,
-                                                                           acc[x][2 * g + 1][y] * inv, acc[x][2 * g + 1][2 + y] * inv);
-                    if (r == 0) lse_part[hd] = ref[x][y] + log2f(lt);
+                    for (int g = 0; g < G; ++g) {
+                        const float4 o = make_float4(acc[x][2 * g][y] * inv, acc[x][2 * g][2 + y] * inv, acc[x][2 * g + 1][y] * inv, acc[x][2 * g + 1][2 + y] * inv);
+                        if (all) kv4_put(static_cast<__nv_bfloat16*>(a.o) + row * D + 32 * g + 4 * r, o);
+                        else *reinterpret_cast<float4*>(o_part + hd * D + 32 * g + 4 * r) = o;   // 8 lanes: 128 contiguous bytes
+                    }
+                    if (r == 0 && !all) lse_part[hd] = e;
+                    if (r == 0 && all && a.lse) a.lse[row] = e * 0.6931471805599453f;
                 }
             }
         left -= tiles + tails;
@@ -950,10 +970,12 @@ kv4_merge_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
     const float* ws = static_cast<const float*>(a.ws);
     wait_for_previous();
     Kv4Join join;
+    int n = 0;               // partial results; 0: a worker has done all of the unit
     if (live) {
         const int64_t unit = (int64_t)(h * p.g_tiles + gt) * a.B + b;
         const int32_t* ends = reinterpret_cast<const int32_t*>(ws + p.ends) + unit;
-        const int w0 = __ldcg(ends), n = __ldcg(ends + (int64_t)a.B * a.Hkv * p.g_tiles) - w0 + 1;
+        const int w0 = __ldcg(ends);
+        n = __ldcg(ends + (int64_t)a.B * a.Hkv * p.g_tiles) - w0 + 1;
         const int64_t first = (w0 + unit) * p.g_rows + x;
         const float *lse = ws + p.lse + first, *v = ws + p.o + first * D + c4 * 4;
         for (int s0 = way * AT_ONCE; s0 < n; s0 += WAYS * AT_ONCE) {
@@ -986,7 +1008,7 @@ kv4_merge_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
         }
         join = all;
     }
-    if (live) join.store<T, D>(a, row, c4);
+    if (n > 0) join.store<T, D>(a, row, c4);
 }
 
 // ------------------------------------------------------------------ host side
