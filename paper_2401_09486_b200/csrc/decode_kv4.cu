@@ -207,6 +207,12 @@ __device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&x)[4]) {
     x[0] = bf16lo(u.x); x[1] = bf16hi(u.x); x[2] = bf16lo(u.y); x[3] = bf16hi(u.y);
 }
 
+__device__ __forceinline__ uint64_t times2(uint64_t v, float lo, float hi) { return fma2(v, pack2(lo, hi), 0); }
+__device__ __forceinline__ float both(uint64_t v) {
+    float lo, hi;
+    unpack2(v, lo, hi);
+    return lo + hi;
+}
 __device__ __forceinline__ void kv4_put(float* p, const float4& o) { *reinterpret_cast<float4*>(p) = o; }
 __device__ __forceinline__ void kv4_put(__nv_bfloat16* p, const float4& o) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w)); }
 
@@ -230,7 +236,9 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
     Kv4Blocks::Cursor c = kb.find(kv4_first(w, total, W), scan, per);
     const uint32_t ones = p.ones;
     const float scale_log2 = a.scale * 1.4426950408889634f;
-    float q[G][NG][4], acc[G][NG][4], m, ref, l;   // m (a score in powers of two), ref (what exponents are taken off), l: of head x / LH
+    // two-wide arithmetic: groups 2 i and 2 i + 1 go together
+    uint64_t q[G][NG / 2][4], acc[G][NG / 2][4];
+    float m = -INFINITY, ref = 0.f, l = 0.f;       // m (a score in powers of two), ref (what exponents are taken off), l: of head x / LH
     // s: scores of the lane's four entries (rows i * 4 + sub of a tile) for all heads; the weights of all heads come back in it
     auto weights = [&](float (&s)[M], int valid, float factor) {
         spread_sum8<M, 4>(s, lane);
@@ -254,9 +262,9 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
             for (int y = 0; y < G; ++y) {
                 const float f = __shfl_sync(0xffffffffu, keep, y * LH);
 #pragma unroll
-                for (int g = 0; g < NG; ++g)
+                for (int g = 0; g < NG / 2; ++g)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[y][g][e] *= f;
+                    for (int e = 0; e < 4; ++e) acc[y][g][e] = times2(acc[y][g][e], f, f);
             }
         }
         __syncwarp();   // the last tile's weights have been read
@@ -277,22 +285,30 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
         for (int y = 0; y < G; ++y) {
             const T* qp = static_cast<const T*>(a.q) + ((int64_t)c.b * a.Hq + h * a.g + gt * G + min(y, heads - 1)) * D + 4 * x;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                load4(qp + 32 * g, q[y][g]);
+            for (int g = 0; g < NG; g += 2) {
+                float lo[4], hi[4];
+                load4(qp + 32 * g, lo);
+                load4(qp + 32 * g + 32, hi);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (blocks) q[y][g][e] *= e & 1 ? KV4_Q / 4 : KV4_Q;
-                    acc[y][g][e] = 0.f;
+                    const float f = !blocks ? 1.f : e & 1 ? KV4_Q / 4 : KV4_Q;
+                    q[y][g / 2][e] = pack2(lo[e] * f, hi[e] * f);
+                    acc[y][g / 2][e] = 0;
                 }
             }
         }
         m = -INFINITY;
         ref = l = 0.f;
         const int end = min(c.s.mem, (c.blk + blocks) * KV4_STEP);
+        const uint8_t* next = blocks ? a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, c.b, c.blk * KV4_STEP), h, c.blk * KV4_STEP) : nullptr;
 #pragma unroll 1
         for (int j0 = c.blk * KV4_STEP; j0 < end; j0 += KV4_ROWS) {
-            const uint8_t* tile = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, c.b, j0), h, j0);
+            const uint8_t* tile = next;
             const int valid = end - j0;
+            if (valid > KV4_ROWS) {   // the next tile's way from memory begins a tile ahead
+                next = a.m.pool + kv4_tile<D>(a.m, a.Hkv, kv4_page_read(a.m, c.b, j0 + KV4_ROWS), h, j0 + KV4_ROWS);
+                if (lane < (TL::BYTES + 127) / 128) asm volatile("prefetch.global.L1 [%0];" ::"l"(next + min(lane * 128, TL::BYTES - 1)));
+            }
             uint32_t kw[4][NG / 2], vw[4][NG / 2], kh[4][NG / 2], vh[4][NG / 2];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -304,39 +320,44 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
             }
             float s[M];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) {
+                uint64_t sum[G] = {};
 #pragma unroll
-                for (int g = 0; g < NG; g += 2) {
+                for (int g = 0; g < NG / 2; ++g) {
                     uint32_t n[4];
-                    kv4_word(kw[i][g / 2], ones, n);
+                    kv4_word(kw[i][g], ones, n);
+                    uint64_t n2[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) n2[e] = pack2(bf16lo(n[e]), bf16hi(n[e]));
+                    const uint64_t step = pack2(bf16lo(kh[i][g]), bf16hi(kh[i][g]));
 #pragma unroll
                     for (int y = 0; y < G; ++y) {
-                        float lo = 0.f, hi = 0.f;
+                        uint64_t t = fma2(q[y][g][0], n2[0], 0);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            lo = fmaf(q[y][g][e], bf16lo(n[e]), lo);
-                            hi = fmaf(q[y][g + 1][e], bf16hi(n[e]), hi);
-                        }
-                        s[y * 4 + i] = fmaf(hi, bf16hi(kh[i][g / 2]), fmaf(lo, bf16lo(kh[i][g / 2]), g ? s[y * 4 + i] : 0.f));
+                        for (int e = 1; e < 4; ++e) t = fma2(q[y][g][e], n2[e], t);
+                        sum[y] = fma2(t, step, sum[y]);
                     }
                 }
+#pragma unroll
+                for (int y = 0; y < G; ++y) s[y * 4 + i] = both(sum[y]);
+            }
             weights(s, valid, scale_log2 * KV4_S);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bool there = i * 4 + sub < valid;   // rows past the last entry may hold anything, and 0 x NaN is not 0
 #pragma unroll
-                for (int g = 0; g < NG; g += 2) {
+                for (int g = 0; g < NG / 2; ++g) {
                     uint32_t n[4];
-                    kv4_word(vw[i][g / 2], ones, n);
-                    const float h0 = there ? bf16lo(vh[i][g / 2]) * KV4_P : 0.f, h1 = there ? bf16hi(vh[i][g / 2]) * KV4_P : 0.f;
+                    kv4_word(vw[i][g], ones, n);
+                    uint64_t n2[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) n2[e] = pack2(bf16lo(n[e]), bf16hi(n[e]));
+                    const float h0 = there ? bf16lo(vh[i][g]) * KV4_P : 0.f, h1 = there ? bf16hi(vh[i][g]) * KV4_P : 0.f;
 #pragma unroll
                     for (int y = 0; y < G; ++y) {
-                        const float w0 = s[y * 4 + i] * h0, w1 = s[y * 4 + i] * h1;
+                        const uint64_t weight = pack2(s[y * 4 + i] * h0, s[y * 4 + i] * h1);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            acc[y][g][e] = fmaf(w0, bf16lo(n[e]), acc[y][g][e]);
-                            acc[y][g + 1][e] = fmaf(w1, bf16hi(n[e]), acc[y][g + 1][e]);
-                        }
+                        for (int e = 0; e < 4; ++e) acc[y][g][e] = fma2(weight, n2[e], acc[y][g][e]);
                     }
                 }
             }
@@ -345,11 +366,12 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
 #pragma unroll
             for (int y = 0; y < G; ++y)
 #pragma unroll
-                for (int g = 0; g < NG; ++g)
+                for (int g = 0; g < NG / 2; ++g)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        acc[y][g][e] *= e & 1 ? KV4_O / 4 : KV4_O;
-                        q[y][g][e] *= e & 1 ? 4 / KV4_Q : 1 / KV4_Q;
+                        const float f = e & 1 ? KV4_O / 4 : KV4_O, back = e & 1 ? 4 / KV4_Q : 1 / KV4_Q;
+                        acc[y][g][e] = times2(acc[y][g][e], f, f);
+                        q[y][g][e] = times2(q[y][g][e], back, back);
                     }
         }
 #pragma unroll 1
@@ -366,28 +388,36 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
             }
             float s[M];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) {
+                uint64_t sum[G] = {};
 #pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    float k[4];
-                    load4(row[0][i] + 32 * g, k);
+                for (int g = 0; g < NG / 2; ++g) {
+                    float lo[4], hi[4];
+                    load4(row[0][i] + 64 * g, lo);
+                    load4(row[0][i] + 64 * g + 32, hi);
 #pragma unroll
-                    for (int y = 0; y < G; ++y)
+                    for (int e = 0; e < 4; ++e) {
+                        const uint64_t k2 = pack2(lo[e], hi[e]);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[y * 4 + i] = fmaf(q[y][g][e], k[e], g + e ? s[y * 4 + i] : 0.f);
+                        for (int y = 0; y < G; ++y) sum[y] = fma2(q[y][g][e], k2, sum[y]);
+                    }
                 }
+#pragma unroll
+                for (int y = 0; y < G; ++y) s[y * 4 + i] = both(sum[y]);
+            }
             weights(s, valid, scale_log2);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    float v[4];
-                    load4(row[1][i] + 32 * g, v);
+                for (int g = 0; g < NG / 2; ++g) {
+                    float lo[4], hi[4];
+                    load4(row[1][i] + 64 * g, lo);
+                    load4(row[1][i] + 64 * g + 32, hi);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        if (i * 4 + sub >= valid) v[e] = 0.f;   // a repeated row has no weight, but 0 x inf is not 0
+                        const uint64_t v2 = i * 4 + sub < valid ? pack2(lo[e], hi[e]) : 0;   // a repeated row has no weight, but 0 x inf is not 0
 #pragma unroll
-                        for (int y = 0; y < G; ++y) acc[y][g][e] = fmaf(s[y * 4 + i], v[e], acc[y][g][e]);
+                        for (int y = 0; y < G; ++y) acc[y][g][e] = fma2(pack2(s[y * 4 + i], s[y * 4 + i]), v2, acc[y][g][e]);
                     }
                 }
             if (valid <= KV4_ROWS && a.k_new && gt == 0) {   // entry `tail` of the cache is read by nobody in this launch
@@ -416,16 +446,24 @@ kv4_stream_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
         for (int y = 0; y < G; ++y) {
             const float inv = 1.f / __shfl_sync(0xffffffffu, l, y * LH);
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
+            for (int g = 0; g < NG; g += 2) {
+                float lo[4], hi[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    acc[y][g][e] += __shfl_xor_sync(0xffffffffu, acc[y][g][e], 8);
-                    acc[y][g][e] += __shfl_xor_sync(0xffffffffu, acc[y][g][e], 16);
+                    unpack2(acc[y][g / 2][e], lo[e], hi[e]);
+#pragma unroll
+                    for (int o = 8; o < 32; o <<= 1) {
+                        lo[e] += __shfl_xor_sync(0xffffffffu, lo[e], o);
+                        hi[e] += __shfl_xor_sync(0xffffffffu, hi[e], o);
+                    }
                 }
-                if (y < heads && sub == 0) {
-                    const float4 o = make_float4(acc[y][g][0] * inv, acc[y][g][1] * inv, acc[y][g][2] * inv, acc[y][g][3] * inv);
-                    if (all) kv4_put(static_cast<T*>(a.o) + (row0 + y) * D + 32 * g + 4 * x, o);
-                    else *reinterpret_cast<float4*>(ws + p.o + (seg * p.g_rows + y) * D + 32 * g + 4 * x) = o;
+                if (y >= heads || sub != 0) continue;
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const float(&f)[4] = z ? hi : lo;
+                    const float4 o = make_float4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+                    if (all) kv4_put(static_cast<T*>(a.o) + (row0 + y) * D + 32 * (g + z) + 4 * x, o);
+                    else *reinterpret_cast<float4*>(ws + p.o + (seg * p.g_rows + y) * D + 32 * (g + z) + 4 * x) = o;
                 }
             }
         }
@@ -638,7 +676,7 @@ kv4_decode_kernel(const Kv4DecodeArgs a, const Kv4Plan p, int* status) {
     const int k_at = kv4_k_unit<D>(r, 2 * j), v_at = kv4_v_unit<D>(2 * j, r);   // this lane's keys' row r, and its values' rows 2j, 2j + 1
     const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
     uint32_t qf[R][2 * G][2];                    // operand B: column = head x * 8 + r
-    float m[R][2], ref[R][2], l[R][2];           // heads x * 8 + 2j, + 1.  m: the reference as a raw product; ref: what exponents are taken off
+    float m[R][2] = {}, ref[R][2] = {}, l[R][2] = {};   // heads x * 8 + 2j, + 1.  m: the reference as a raw product; ref: what exponents are taken off
     float acc[R][2 * G][4];
     int slot = 0, h = 0, gt = 0, heads = 0;
     uint32_t phase = 0;
