@@ -12,8 +12,8 @@
 // lengths are known on the device only, so every CTA finds the cut from them.  Few or short units are not cut (KV4_WHOLE).
 //
 // bf16: kv4_decode_kernel, warp-level products.  fp32, and the second opinion: kv4_stream_kernel on CUDA cores.
-// Measured: B64 Hq32 Hkv8 D128, up to 16384 entries and tails of up to 127: 165 us, 5.6 TB/s (0.85 of a copy; the copies alone take 134 us);
-// B32 H32, 2048 entries 56 us; B4 H8 D64, 200 entries 5.4 us; fp32 B11 Hq15 Hkv3, 2501 entries 22.7 us.
+// Measured: B64 Hq32 Hkv8 D128, up to 16384 entries and tails of up to 127: 164 us, 5.6 TB/s (0.86 of a copy; the copies alone take 134 us);
+// B32 H32, 2048 entries 56 us; B4 H8 D64, 200 entries 5.4 us; fp32 B11 Hq15 Hkv3, 2501 entries 23 us.
 #include <cooperative_groups.h>
 
 #include "kv4.cuh"
