@@ -2,8 +2,9 @@
 //
 // Eight lanes share a row: lane x has features 32 g + 4 x .. + 3 of every group g, which are the four of half-word (x, g).
 // Keys and values of an entry go together: eight loads in flight per lane, and the largest magnitudes of the eight groups are found with
-// results spread over the lanes (seven shuffles), so each lane works out one step.  Both directions are bound by HBM (256 bytes of bf16 against 72 for a row of 128 features) as long as a value costs few instructions: m is the integer part
-// of |x| / (2 h), a product and an addition that rounds towards zero; see kv4_half for why that is exact.
+// results spread over the lanes (seven shuffles), so each lane works out one step.  Both directions are bound by HBM (256 bytes of bf16
+// against 72 for a row of 128 features) as long as a value costs few instructions: m is the integer part of |x| / (2 h), a product and an
+// addition that rounds towards zero; see kv4_half for why that is exact.
 // Measured (32 x 32 heads, D = 128, bf16): 1.5 million rows stored in 206 us (4.9 TB/s, issue-bound), 1.6 million read back in 158 us (6.5 TB/s).
 #include "kv4.cuh"
 
