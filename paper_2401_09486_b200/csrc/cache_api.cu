@@ -29,6 +29,18 @@ bool apart(std::initializer_list<Range> ins, std::initializer_list<Range> outs, 
     return true;
 }
 
+// Can an array of that many bytes be?  Offsets and ends of arrays are 64-bit sums.
+bool fits(std::initializer_list<int64_t> factors) {
+    int64_t n = 1;
+    for (int64_t x : factors)
+        if (x == 0) return true;
+    for (int64_t x : factors) {
+        if (n > (INT64_MAX >> 3) / x) return false;
+        n *= x;
+    }
+    return true;
+}
+
 // ------------------------------------------------------------------ 4-bit memory
 int kv4_sizes(int B, int Hkv, int D, int page_size, int max_pages, int n_pages, loma_dtype dtype, int* l2) {
     if (B < 0 || Hkv < 0 || max_pages < 0 || n_pages < 0) return LOMA_ERR_INVALID_ARG;
@@ -37,6 +49,7 @@ int kv4_sizes(int B, int Hkv, int D, int page_size, int max_pages, int n_pages, 
     *l2 = log2_exact(page_size);
     if (*l2 < 4 || page_size > 65536) return LOMA_ERR_INVALID_ARG;
     if ((int64_t)max_pages * page_size > INT_MAX) return LOMA_ERR_INVALID_ARG;
+    if (!fits({n_pages, Hkv, page_size, 2 * D}) || !fits({4, B, max_pages})) return LOMA_ERR_INVALID_ARG;
     return LOMA_OK;
 }
 
@@ -65,7 +78,7 @@ int loma_kv4_append(const void* k, const void* v, void* kv_pool, const int32_t* 
     int l2;
     const int rc = kv4_sizes(B, Hkv, D, page_size, max_pages, n_pages, dtype, &l2);
     if (rc != LOMA_OK) return rc;
-    if (l < 0 || l > INT_MAX - 4096) return LOMA_ERR_INVALID_ARG;
+    if (l < 0 || l > INT_MAX - 4096 || !fits({B, Hkv, l, D, 4})) return LOMA_ERR_INVALID_ARG;
     if (B == 0 || Hkv == 0 || l == 0) return LOMA_OK;
     if (!k || !v || !kv_pool || !block_table || !mem_lens || !k_strides || !v_strides || n_pages < 1) return LOMA_ERR_INVALID_ARG;
     Kv4AppendArgs a;
@@ -85,6 +98,7 @@ int loma_kv4_append(const void* k, const void* v, void* kv_pool, const int32_t* 
     for (int i = 0; i < 2; ++i) {
         span[i] = D;
         for (int x = 0; x < 3; ++x) span[i] += (extent[x] - 1) * st[i][x];
+        if (!fits({span[i], 4})) return LOMA_ERR_INVALID_ARG;
     }
     if (!apart({{k, span[0] * (int64_t)elt_bytes(dtype)}, {v, span[1] * (int64_t)elt_bytes(dtype)}, {block_table, 4ll * B * max_pages},
                 {mem_lens, 4ll * B}, {new_lens, 4ll * B}}, {pool})) return LOMA_ERR_INVALID_ARG;
@@ -100,7 +114,7 @@ int loma_kv4_load(const void* kv_pool, const int32_t* block_table, const int32_t
     int l2;
     const int rc = kv4_sizes(B, Hkv, D, page_size, max_pages, n_pages, dtype, &l2);
     if (rc != LOMA_OK) return rc;
-    if (cap < 0 || cap > INT_MAX - 4096) return LOMA_ERR_INVALID_ARG;
+    if (cap < 0 || cap > INT_MAX - 4096 || !fits({B, Hkv, cap, D, 4})) return LOMA_ERR_INVALID_ARG;
     if (B == 0 || Hkv == 0 || cap == 0) return LOMA_OK;
     if (!kv_pool || !block_table || !mem_lens || !k_cache || !v_cache || n_pages < 1) return LOMA_ERR_INVALID_ARG;
     for (const void* p : {kv_pool, (const void*)k_cache, (const void*)v_cache}) if (misaligned(p, 16)) return LOMA_ERR_ALIGNMENT;
@@ -140,7 +154,8 @@ int loma_decode_attn_kv4(const void* q, const void* k_new, const void* v_new, vo
     int l2;
     const int rc = kv4_sizes(B, Hkv, D, page_size, max_pages, n_pages, dtype, &l2);
     if (rc != LOMA_OK) return rc;
-    if (cap < 0 || (k_new == nullptr) != (v_new == nullptr)) return LOMA_ERR_INVALID_ARG;
+    if (cap < 0 || !fits({B, Hkv, cap, D, 4}) || (k_new == nullptr) != (v_new == nullptr)) return LOMA_ERR_INVALID_ARG;
+    if (softmax_scale > 0x1p50f || (softmax_scale > 0.f && softmax_scale < 0x1p-50f)) return LOMA_ERR_INVALID_ARG;   // sums carry powers of two
     if (max_tail_len >= cap || max_mem_len > (int64_t)max_pages * page_size) return LOMA_ERR_CAPACITY;
     if (B == 0 || Hq == 0) return LOMA_OK;
     if (!q || !k_tail || !v_tail || !o || !tail_lens || !mem_lens) return LOMA_ERR_INVALID_ARG;
@@ -170,7 +185,7 @@ int loma_decode_attn_kv4(const void* q, const void* k_new, const void* v_new, vo
 // ------------------------------------------------------------------ pages
 static int page_sizes(int B, int page_size, int max_pages, int n_pages, int n_free, int* l2) {
     if (B < 0 || max_pages < 0 || n_pages < 0 || n_free < 0) return LOMA_ERR_INVALID_ARG;
-    if (B == INT_MAX || n_pages > INT_MAX - 65536 || n_free == INT_MAX) return LOMA_ERR_INVALID_ARG;
+    if (B == INT_MAX || n_pages > INT_MAX - 65536 || n_free == INT_MAX || !fits({4, B, max_pages})) return LOMA_ERR_INVALID_ARG;
     *l2 = log2_exact(page_size);
     if (*l2 < 0 || page_size > 65536) return LOMA_ERR_INVALID_ARG;
     if ((int64_t)max_pages * page_size > INT_MAX) return LOMA_ERR_INVALID_ARG;

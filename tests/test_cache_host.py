@@ -512,3 +512,31 @@ def test_binding_checks_shapes_and_types(lib):
         L.loma_kv4_append(k, k, torch.zeros(2, L.loma_kv4_page_bytes(2, 64, 16), dtype=torch.uint8), z(1, 2), 16, z(1))
     with pytest.raises(ValueError):
         L.loma_paged_copy([torch.zeros(4, 16)], z(2), z(2), z(1))
+
+
+def test_sizes_beyond_64_bit_offsets_are_refused(lib):
+    """Numbers that each pass their own bound but whose product does not fit; nothing is read."""
+    big = 2**31 - 5000
+    x, lens = torch.zeros(64), z(4)
+    a, w = p(x), p(lens)
+    wide = (ctypes.c_int64 * 3)(2**60, 2**29, 128)
+    for B, H, l, n, st in ((big, big, 4, 6, wide), (1, big, 4, big, wide), (2, 1, 4, 6, (ctypes.c_int64 * 3)(2**60, 2**60, 128))):
+        assert lib.loma_kv4_append(a, a, a, w, w, None, B, H, 128, l, 65536, 4, n, st, st, 0, None) == INVALID
+    assert lib.loma_kv4_append(a, a, a, w, w, None, big, 1, 128, 4, 16, 2**27 - 1, 6, wide, wide, 0, None) == INVALID
+    assert lib.loma_kv4_load(a, w, w, a, a, big, 1, 128, big, 16, 4, 6, 0, None) == INVALID
+    assert lib.loma_kv4_load(a, w, w, a, a, 1, big, 128, 16, 65536, 4, big, 0, None) == INVALID
+    assert lib.loma_decode_attn_kv4(a, a, a, a, a, a, w, a, None, 1, 2**20, 2**20, 128, big, w, 8, 65536, 4, big, w, 60, 0, 0.0, 0, a, 2**40, None) == INVALID
+    for on_device in (0, 1):
+        assert lib.loma_paged_release(big, 1, big, 6, 6, w, w, w, w, w, w, w, w, on_device, None) == INVALID
+        assert lib.loma_paged_fork(big, 1, big, 6, 6, 4, *[w] * 15, 2**40, on_device, None) == INVALID
+        assert lib.loma_paged_compact(big, big, 6, 6, 4, *[w] * 9, on_device, None) == INVALID
+
+
+@pytest.mark.parametrize("scale,status", [(2.0**51, INVALID), (float("inf"), INVALID), (2.0**-51, INVALID), (1e-45, INVALID)])
+def test_kv4_decode_refuses_scales_its_sums_cannot_carry(lib, scale, status):
+    B, Hq, H, D, cap = 2, 6, 3, 64, 9
+    q, kt, vt, o, lens, ws = torch.zeros(B, Hq, D), torch.zeros(B, H, cap, D), torch.zeros(B, H, cap, D), torch.zeros(B, Hq, D), z(B), torch.zeros(2**20, dtype=torch.uint8)
+    for flags in (0, L.LOMA_FLAG_FORCE_GENERIC):
+        for dtype in (0, 1):
+            assert lib.loma_decode_attn_kv4(p(q), None, None, p(kt), p(vt), None, None, p(o), None, B, Hq, H, D, cap, p(lens), 8, 16, 0, 0, p(z(B)), 0, dtype, scale, flags, p(ws),
+                                            2**20, None) == status
