@@ -785,3 +785,108 @@ print("captured")
 def test_the_first_call_of_a_process_may_be_captured(which):
     out = subprocess.run([sys.executable, "-c", FIRST_CALL, which], capture_output=True, text=True, timeout=300, cwd=build.ROOT)
     assert out.returncode == 0 and "captured" in out.stdout, out.stderr[-2000:]
+
+
+# ------------------------------------------------------------------------------------------------ calls between others
+@pytest.mark.parametrize("dtype,flags", KINDS)
+@pytest.mark.parametrize("B,live", [(300, {0, 31, 32, 65, 298}), (300, {299}), (97, {0}), (64, {5, 38, 63}), (1100, {3, 600, 1098})])
+def test_decode_few_requests_in_many_slots(B, live, dtype, flags):
+    """Workers pass over the slots without a request, in runs of any length and past the batch's end, cut and whole."""
+    s = make(B, 6, 2, 64, [40 + b % 50 if b in live else 9 for b in range(B)], [b % 33 if b in live else -1 - b % 3 for b in range(B)], 16, dtype, seed=B)
+    call(s, flags)
+    check(s, flags)
+    s["table"] = torch.cat([s["table"], torch.full((B, 2000), -1, dtype=torch.int32, device=DEV)], 1).contiguous()
+    top, s["max_mem"] = s["max_mem"], 30000
+    s["ws"] = torch.full((L.loma_decode_kv4_workspace_bytes(B, 6, 2, 64, 30000, s["max_tail"]),), 255, dtype=torch.uint8, device=DEV)
+    for b in range(B):
+        if b not in live:
+            continue
+        s["kt"][b, :, s["tails"][b]:], s["vt"][b, :, s["tails"][b]:] = float("nan"), float("nan")
+    s["o"].fill_(7.0), s["lse"].fill_(7.0)
+    call(s, flags)
+    s["max_mem"] = top
+    check(s, flags)
+
+
+@pytest.mark.parametrize("before", ["memcpy", "memset", "event", "torch", "nothing"])
+def test_copy_behind_other_work(before):
+    """The copy may be launched early behind a kernel; behind anything else it waits all the same, eager and captured."""
+    pool = torch.randint(0, 256, (9, 1 << 20), dtype=torch.uint8, device=DEV)
+    lists, ready, start = di32([[0, 3, 5], [1, 2, 4]]), di32([[0, 3, 5], [1, 2, 4]]), pool.clone()
+    n, other, big = di32([3]), torch.cuda.Stream(), torch.empty(1 << 27, dtype=torch.uint8, device=DEV)
+    want = start.clone()
+    want[[1, 2, 4]] = start[[0, 3, 5]]
+
+    def step():
+        now = torch.cuda.current_stream()
+        if before == "memcpy":
+            pool.copy_(start)
+            lists.copy_(ready)
+        elif before == "memset":
+            big.zero_()
+        elif before == "event":                    # lists and pool made on another stream, behind 128 MB of other writes
+            other.wait_stream(now)
+            with torch.cuda.stream(other):
+                big.fill_(3)
+                pool.copy_(start)
+                lists.copy_(ready)
+            now.wait_stream(other)
+        elif before == "torch":
+            torch.add(ready, 0, out=lists)
+        L.loma_paged_copy([pool], lists[0], lists[1], n)
+
+    def reset():
+        pool.copy_(start)
+        if before in ("memcpy", "event"):
+            pool.zero_()
+        if before in ("memcpy", "event", "torch"):
+            lists.fill_(-1)
+        torch.cuda.synchronize()
+
+    for _ in range(3):
+        reset()
+        step()
+        assert torch.equal(pool, want)
+    reset()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        step()
+    for _ in range(3):
+        reset()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(pool, want)
+
+
+def test_calls_from_two_threads_at_once():
+    """Threads with streams, workspaces and lists of their own: the results of calls made alone."""
+    sets = [make(5, 8, 2, 128, [(j * 900 + 77 * b) % 1500 for b in range(5)], [5 * b for b in range(5)], 16, torch.bfloat16, seed=90 + j) for j in range(4)]
+    for s in sets:
+        call(s)
+    want = [(s["o"].clone(), s["lse"].clone()) for s in sets]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(s, o, lse, j):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                s["o"].fill_(7.0), s["lse"].fill_(7.0)
+                call(s)
+                pool = torch.arange(12, device=DEV, dtype=torch.int32).repeat(64, 1).t().contiguous().view(torch.uint8)
+                table, held, refs, free, taken, counts = di32([[0, 1, 2], [3, 4, 5]]), di32([3, 3]), di32([0] * 12), di32(list(range(12))), di32([6]), di32([0] * 4)
+                L.loma_paged_release(di32([16 * j % 48, -1]), held, table, 16, held, refs, free, taken, counts)
+                L.loma_paged_copy([pool], di32([7]), di32([8]), di32([1]))
+                stream.synchronize()
+                kept = min(j, 3) if j < 3 else 0
+                if not (torch.equal(s["o"], o) and torch.equal(s["lse"], lse)) or held.tolist() != [kept, 3] or int(taken) != 6 - (3 - kept) or not torch.equal(pool[8], pool[7]):
+                    wrong.append(j)
+
+    import threading
+    threads = [threading.Thread(target=work, args=(s, *w, j)) for j, (s, w) in enumerate(zip(sets, want))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
