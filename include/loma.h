@@ -860,7 +860,8 @@ LOMA_API size_t loma_decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D
  *   counts [4]  [out]              see below.  Counts beyond INT_MAX are stored as INT_MAX
  * Table entries outside [0, n_pages) (loma_paged_extend writes -1 when its list is short) are passed over.
  * on_device != 0: every pointer is [device] and the work is enqueued on `stream`; 0: every pointer is [host], no CUDA call.
- * Each is one launch; a step of extend, append, attention, release and fork needs no host read and can be captured.
+ * Each is one launch (for more than 256 rows, or pages past 2^18 to let go of, up to four); a step of extend, append, attention,
+ * release and fork needs no host read and can be captured.
  *
  * release   row b keeps ceil(keep_lens[b] / ps) of its pages, or all it has if those are fewer; keep_lens[b] negative: the row is
  *           left alone (0 lets go of everything).  The table entries of the others become -1, refs of their pages falls by one per

@@ -9,7 +9,7 @@
 // counts exchanged through each other's shared memory.  Pages and sequences are dealt to the CTAs in contiguous parts, so ranks
 // follow from block-wide sums and the parts' totals, in ascending order of page or sequence: results repeat bit for bit, and the
 // only atomics are additions and ORs of integers.
-// Measured with the launch: release of 64 sequences 5 us, of 2000 with 500 000 pages 32; fork of 8 / 256 sequences 7 / 17; compaction of 16
+// Measured with the launch: release of 64 sequences 5 us, of 2000 with 500 000 pages 29; fork of 8 / 256 sequences 7 / 17; compaction of 16
 // sequences 10, of 500 with 94 500 pages 35; copy of 2 x 386 MB 107 (0.95 to 1.0 of a copy).
 #include <limits.h>
 
@@ -347,7 +347,34 @@ struct Settle {
             if (again) __syncthreads();
         });
     }
+    // in place of write(): the number of a word's lowest page, less 2^31, in the place of its count; list_pages does the rest
+    __device__ __forceinline__ void mark(const PageList& pl, int64_t at) const {
+        stretches(part, [&](int64_t lo, int64_t hi, bool again) {
+            const int64_t here = again ? look(pl, lo, hi) : 0;
+            for (int w = threadIdx.x; w < (hi - lo + 31) / 32; w += PG_THREADS) {
+                const unsigned m = words.mask[0][w];
+                if (m) pl.refs[lo + w * 32 + __ffs(m) - 1] = (int)(INT_MIN + at + words.before[0][w]);
+            }
+            at += here;
+            if (again) __syncthreads();
+        });
+    }
 };
+// the first n of the pages without an owner to the places from `taken` on, a word to a warp at a time
+__device__ __forceinline__ void list_pages(const PageList& pl, int n, int taken, int64_t warp, int64_t warps) {
+    const int lane = threadIdx.x & 31;
+    for (int64_t w = warp; w < (pl.n_pages + 31) / 32; w += warps) {
+        const int64_t page = w * 32 + lane;
+        const int v = page < pl.n_pages ? __ldcg(pl.refs + page) : 0;
+        const unsigned m = __ballot_sync(0xffffffffu, v < 0);
+        const int first = __shfl_sync(0xffffffffu, v, __ffs(m | 1u << 31) - 1) & INT_MAX;
+        if (v < 0) {
+            const int k = first + __popc(m & ((1u << lane) - 1));
+            pl.refs[page] = 0;
+            if (k < n) pl.free_pages[taken + k] = (int)page;
+        }
+    }
+}
 
 // rows of a release: a warp to a row at a time
 __device__ __forceinline__ void drop_rows(const ReleaseArgs& a, int first, int warps) {
@@ -375,12 +402,14 @@ __global__ void __launch_bounds__(DROP_THREADS) paged_drop_kernel(const ReleaseA
     drop_rows(a, (threadIdx.x >> 5) * gridDim.x + blockIdx.x, gridDim.x * (DROP_THREADS / 32));
 }
 
+// list: a launch over all SMs that lists the pages comes behind
 template <bool DROPPED>
-__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) paged_release_kernel(const ReleaseArgs a) {
+__global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) paged_release_kernel(const ReleaseArgs a, const bool list) {
     cg::cluster_group cl = cg::this_cluster();
     __shared__ Exchange ex;
     __shared__ Words<1> words;
     const int rank = cl.block_rank();
+    let_next_start();
     if constexpr (DROPPED) wait_for_previous();
     const int taken = start_of(a.pl, __ldcg(a.pl.taken));
     if constexpr (!DROPPED) drop_rows(a, (threadIdx.x >> 5) * PG_CTAS + rank, PG_ALL_WARPS);   // neighbours on different SMs
@@ -390,7 +419,8 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
     const int64_t mine = s.count(a.pl);
     ex.put(cl, mine, 0);
     const int64_t at = ex.get(0, rank, &freed), n = min(freed, (int64_t)taken);
-    if (mine > 0) s.write(a.pl, at, n, taken);
+    if (mine > 0 && list) s.mark(a.pl, at);
+    else if (mine > 0) s.write(a.pl, at, n, taken);
     if (rank == 0 && threadIdx.x == 0) {
         *a.pl.taken = (int)(taken - n);
         a.counts[0] = 0;
@@ -399,6 +429,17 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
         a.counts[3] = 0;
     }
 }
+
+__global__ void __launch_bounds__(DROP_THREADS) paged_list_kernel(const ReleaseArgs a) {
+    wait_for_previous();
+    const int freed = __ldcg(a.counts + 1);
+    if (freed > 0)
+        list_pages(a.pl, freed - __ldcg(a.counts + 2), __ldcg(a.pl.taken), (int64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x, (int64_t)gridDim.x * (DROP_THREADS / 32));
+}
+
+// Pages that a release may free beyond which they are listed over all SMs: eight SMs store them at 20 bytes a cycle each.  Measured (us, in the
+// cluster against a launch of its own): 125 000 pages 13.2 / 15.9, 250 000 22.3 / 22.7, 500 000 34.1 / 29.5, a million 70 / 56.
+constexpr int PG_LIST = 1 << 18;
 
 // Rows to a cluster's warp beyond which the rows' own work goes over all SMs in launches of its own, each behind the other.  Measured (us, one
 // launch against several, up to 1900 entries in pages of 16): 128 sequences: fork 15.9 / 18.0, release 10.1 / 9.6, compaction 25.7 / 26.3; 1000: fork
@@ -586,6 +627,19 @@ __device__ __forceinline__ void rename_pages(const CompactArgs& a, int warp, int
         }
     }
 }
+// owners of the pages that move, their new numbers, and the end of the list
+__device__ __forceinline__ void move_owners(const CompactArgs& a, int64_t count, int64_t thread, int64_t threads) {
+    for (int64_t i = thread; i < a.max_copies; i += threads) {
+        if (i < count) {
+            const int s = __ldcg(a.copy_src + i), d = __ldcg(a.copy_dst + i);
+            a.page_map[s] = d;
+            a.pl.refs[d] = __ldcg(a.pl.refs + s);
+            a.pl.refs[s] = 0;
+        } else {
+            a.copy_src[i] = a.copy_dst[i] = -1;
+        }
+    }
+}
 
 // Long batches: clearing, marking and renaming in launches of their own, over all SMs.
 __global__ void __launch_bounds__(WIDE_THREADS) paged_clear_kernel(const CompactArgs a) {
@@ -601,7 +655,9 @@ __global__ void __launch_bounds__(WIDE_THREADS) paged_mark_kernel(const CompactA
 __global__ void __launch_bounds__(WIDE_THREADS) paged_rename_kernel(const CompactArgs a) {
     let_next_start();
     wait_for_previous();
-    if (__ldcg(a.counts) > 0) rename_pages(a, (threadIdx.x >> 5) * gridDim.x + blockIdx.x, gridDim.x * (WIDE_THREADS / 32));
+    const int count = __ldcg(a.counts);
+    if (count > 0) rename_pages(a, (threadIdx.x >> 5) * gridDim.x + blockIdx.x, gridDim.x * (WIDE_THREADS / 32));
+    move_owners(a, count, (int64_t)blockIdx.x * WIDE_THREADS + threadIdx.x, (int64_t)gridDim.x * WIDE_THREADS);
 }
 
 template <bool WIDE>
@@ -686,18 +742,10 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
         a.counts[2] = saturate(all_n);
         a.counts[3] = saturate(moves - count);
     }
+    if constexpr (WIDE) return;
     cl.sync();
-    for (int64_t i = me; i < a.max_copies; i += PG_ALL) {
-        if (i < count) {
-            const int s = __ldcg(a.copy_src + i), d = __ldcg(a.copy_dst + i);
-            a.page_map[s] = d;
-            pl.refs[d] = __ldcg(pl.refs + s);
-            pl.refs[s] = 0;
-        } else {
-            a.copy_src[i] = a.copy_dst[i] = -1;
-        }
-    }
-    if (!WIDE && count > 0) rename_pages(a, first_row, PG_ALL_WARPS);
+    move_owners(a, count, me, PG_ALL);
+    if (count > 0) rename_pages(a, first_row, PG_ALL_WARPS);
 }
 
 // Copying: a warp takes 4 KB of one page of one pool at a time, eight 16-byte loads per lane in flight, then as many stores.
@@ -732,10 +780,15 @@ __global__ void __launch_bounds__(COPY_THREADS) paged_copy_kernel(const __grid_c
 
 // ------------------------------------------------------------------ host side
 cudaError_t launch_paged_release(const ReleaseArgs& a, cudaStream_t st) {
-    if (a.B <= PG_FEW) return launch_behind(paged_release_kernel<false>, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);
-    const unsigned grid = (unsigned)std::min(148 * 8, (a.B + DROP_THREADS / 32 - 1) / (DROP_THREADS / 32));
-    const cudaError_t e = launch_behind(paged_drop_kernel, dim3(grid), DROP_THREADS, 0, st, false, a);
-    return e == cudaSuccess ? launch_behind(paged_release_kernel<true>, dim3(PG_CTAS), PG_THREADS, 0, st, true, a) : e;
+    const bool list = std::min<int64_t>(a.pl.n_pages, (int64_t)a.B * a.max_pages) > PG_LIST, dropped = a.B > PG_FEW;
+    cudaError_t e = cudaSuccess;
+    if (dropped) {
+        const unsigned grid = (unsigned)std::min(148 * 8, (a.B + DROP_THREADS / 32 - 1) / (DROP_THREADS / 32));
+        e = launch_behind(paged_drop_kernel, dim3(grid), DROP_THREADS, 0, st, false, a);
+    }
+    if (e == cudaSuccess) e = launch_behind(dropped ? paged_release_kernel<true> : paged_release_kernel<false>, dim3(PG_CTAS), PG_THREADS, 0, st, dropped, a, list);
+    if (e == cudaSuccess && list) e = launch_behind(paged_list_kernel, dim3(148 * 8), DROP_THREADS, 0, st, true, a);
+    return e;
 }
 cudaError_t launch_paged_fork(const ForkArgs& a, cudaStream_t st) {
     if (a.B <= PG_FEW) return launch_behind(paged_fork_kernel<FORK_ALL>, dim3(PG_CTAS), PG_THREADS, 0, st, false, a);

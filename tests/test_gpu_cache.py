@@ -83,6 +83,17 @@ def test_pages_of_a_pool_looked_at_in_stretches(B, M):
         H.check_compact(H.run_compact(case, most, DEV), C.compact(held, table, refs, free, taken, most))
 
 
+@pytest.mark.parametrize("B,M,n_pages,room", [(600, 500, 300000, None), (200, 1400, 270001, None), (600, 500, 1200000, 1000), (600, 500, 300000, 0)])
+def test_many_pages_released_at_once(B, M, n_pages, room):
+    """So many that a launch over all SMs lists them; room: places in the list, fewer than pages that come back."""
+    lens, fixed, held, table, refs, free, taken, rng = H.pool_case(B + M, B, M, 4, n_pages)
+    if room is not None:
+        taken = room
+    case = (lens, fixed, held, table, refs, free, taken, rng)
+    for keep in (np.where(rng.random(B) < 0.3, -1, rng.integers(0, M * 4 + 2, B)), np.zeros(B, dtype=np.int64), np.full(B, -1), np.where(np.arange(B) == 1, 0, -1)):
+        H.check_release(H.run_release(case, keep, 4, DEV), C.release(keep, held, table, 4, refs, free, taken))
+
+
 @pytest.mark.parametrize("taken", [-5, 0, 10**6])
 def test_pages_of_an_empty_batch_and_a_start_out_of_range(taken):
     rf, fr, tk, ct = di32([0] * 5), di32([3, 1, 4]), di32([taken]), di32([-7] * 4)
