@@ -225,7 +225,8 @@ __device__ __forceinline__ int64_t block_sums(int64_t of_warp, int64_t* total) {
 }
 
 // Two numbers of each CTA to every CTA, and a barrier of the cluster; then the sums of the lower ranks' and of everyone's.
-// slot: in shared memory, one set per exchange.
+// slot: in shared memory, one set per exchange.  put() writes to the other CTAs, so a barrier of the cluster comes before it in every kernel:
+// without one a CTA may not have started yet.
 struct Exchange {
     int64_t slot[2][PG_CTAS];
     __device__ __forceinline__ void put(cg::cluster_group& cl, int64_t x, int64_t y) {
@@ -528,8 +529,8 @@ __global__ void __cluster_dims__(PG_CTAS, 1, 1) __launch_bounds__(PG_THREADS) pa
         if constexpr (PART == FORK_COUNT) return;
         together();
         change_owners(a, (threadIdx.x >> 5) * PG_CTAS + rank, PG_ALL_WARPS, [&](int r) { return local ? kids[r] : __ldcg(kids + r); });
-        cl.sync();
     }
+    cl.sync();   // owners' counts are complete (NUMBER: the launch before did that), and every CTA runs, so its shared memory may be written to
     auto is_heir = [&](int b, int r) { return (local ? heir[r] : __ldcg(heir + r)) == (b == r ? -1 : b); };
     // pages to draw, numbered through this CTA's rows; in the workspace the numbers take the place of kids
     const Part part(a.B, 1, rank);

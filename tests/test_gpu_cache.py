@@ -901,3 +901,49 @@ def test_calls_from_two_threads_at_once():
     for t in threads:
         t.join()
     assert not wrong
+
+
+# ------------------------------------------------------------------------------------------------ where the rules change over
+@pytest.mark.parametrize("B", [248, 249, 256, 257, 264, 265, 1024, 1025])
+@pytest.mark.parametrize("ended", [0.0, 0.5])
+def test_forks_on_both_sides_of_the_longest_batch_of_one_launch(B, ended):
+    """Every warp and every place in the shared tables of children and draws in use, and one row more: launches of their own.  ended: the
+    part of the rows that nobody goes on from, whose pages come back and are drawn again in the same call."""
+    case = H.pool_case(B, B, 9, 4, 7 * B)
+    lens, fixed, held, table, refs, free, taken, rng = case
+    some = rng.integers(0, B, B) if ended else np.arange(B)
+    parents = np.where(rng.random(B) < 0.6, some, np.arange(B) // 4 * 4)
+    parents = np.where(rng.random(B) < ended / 4, -1, parents)
+    for most in (5, 20000):
+        H.check_fork(H.run_fork(case, parents, 4, most, DEV), C.fork(parents, lens, fixed, held, table, 4, refs, free, taken, most))
+
+
+def test_a_fork_of_a_long_batch_replayed():
+    """The launches of a long batch in a graph, many times over from the same start: the same numbers every time."""
+    B, M = 700, 12
+    case = H.pool_case(11, B, M, 4, 9000)
+    lens, fixed, held, table, refs, free, taken, rng = case
+    parents = rng.integers(-1, B, B)
+    want = C.fork(parents, lens, fixed, held, table, 4, refs, free, taken, 6000)
+    start = [di32(refs), di32(free), di32([taken])]
+    state = [x.clone() for x in start]
+    new = lambda *s: torch.full(s, -77, dtype=torch.int32, device=DEV)  # noqa: E731
+    out, lo, ho, src, dst, counts = new(B, M), new(B), new(B), new(6000), new(6000), new(4)
+    ws = torch.full((L.loma_paged_fork_workspace_bytes(B),), 171, dtype=torch.uint8, device=DEV)
+    given = [di32(parents), di32(lens), di32(fixed), di32(held), di32(table)]
+
+    def step():
+        for x, y in zip(state, start):
+            x.copy_(y)
+        L.loma_paged_fork(*given, 4, out, lo, ho, *state, src, dst, counts, workspace=ws)
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        step()
+    for _ in range(40):
+        for x in (out, lo, ho, src, dst, counts):
+            x.fill_(-77)
+        graph.replay()
+        torch.cuda.synchronize()
+        H.check_fork((out, lo, ho, *state, (src, dst), counts), want)
