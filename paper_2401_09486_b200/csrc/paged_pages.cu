@@ -377,7 +377,8 @@ __device__ __forceinline__ void list_pages(const PageList& pl, int n, int taken,
     }
 }
 
-// rows of a release: a warp to a row at a time
+// Rows of a release: a warp to a row at a time.  held_out may be held itself: a row's count is written behind a barrier of the warp, when all
+// its lanes have read it (one row ahead), and the count of a row is read and written by one warp alone.
 __device__ __forceinline__ void drop_rows(const ReleaseArgs& a, int first, int warps) {
     const int lane = threadIdx.x & 31;
     int keep = 0, held = 0;
@@ -392,6 +393,7 @@ __device__ __forceinline__ void drop_rows(const ReleaseArgs& a, int first, int w
             if (in_pool(a.pl, page)) atomicSub(a.pl.refs + page, 1);
             row[j] = -1;
         }
+        __syncwarp();
         if (lane == 0) a.held_out[b] = kept;
     }
 }

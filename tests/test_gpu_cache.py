@@ -947,3 +947,23 @@ def test_a_fork_of_a_long_batch_replayed():
         graph.replay()
         torch.cuda.synchronize()
         H.check_fork((out, lo, ho, *state, (src, dst), counts), want)
+
+
+@pytest.mark.parametrize("B,M", [(1, 130), (257, 70), (3000, 37), (12000, 5)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_release_of_rows_whose_lanes_part(B, M, in_place):
+    """Rows that let go of 0, 1, 31, 32, 33 ... pages, so that a warp's lanes go round their loop differently often; several rows to a warp.
+    With held_out = held every count is read before it is replaced."""
+    n = B * M + 3
+    rng = np.random.default_rng(B + M)
+    held = rng.integers(0, M + 1, B)
+    table = np.where(np.arange(M)[None] < held[:, None], rng.permutation(n)[: B * M].reshape(B, M), -1)
+    refs, free, taken = np.zeros(n, dtype=np.int64), np.setdiff1d(np.arange(n), table), 0
+    taken = int(held.sum())
+    free = np.concatenate([np.full(taken, -1), free])
+    case = (held * 4, held * 0, held, table, refs, free, taken, rng)
+    gone = rng.choice([0, 1, 31, 32, 33, 64, 65], B)
+    keep = np.where(rng.random(B) < 0.2, -1, np.maximum(held - gone, 0) * 4)
+    want = C.release(keep, held, table, 4, refs, free, taken)
+    for _ in range(3):
+        H.check_release(H.run_release(case, keep, 4, DEV, in_place=in_place), want)
