@@ -902,8 +902,9 @@ LOMA_API size_t loma_decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D
  *           No page may be a source and a destination of one call, or a destination twice (the lists above have neither), and the
  *           pools lie apart from each other.
  *           One launch for up to 64 pools.
- * Errors: INVALID_ARG (negative sizes, page size not a power of two <= 65536, max_pages * page_size > INT_MAX, a required pointer
- * NULL, outputs that overlap inputs or each other), ALIGNMENT (4 bytes; pools and page_bytes 16), WORKSPACE, UNSUPPORTED, CUDA.
+ * Errors: INVALID_ARG (negative sizes, page size not a power of two <= 65536, max_pages * page_size > INT_MAX, B, max_pages or n_pages
+ * above INT_MAX - 65536, a required pointer NULL, outputs that overlap inputs or each other), ALIGNMENT (4 bytes; pools and page_bytes
+ * 16), WORKSPACE, UNSUPPORTED, CUDA.
  * ------------------------------------------------------------------------- */
 LOMA_API int loma_paged_release(int B, int page_size, int max_pages, int n_pages, int n_free, const int32_t* keep_lens,
                                 const int32_t* held, int32_t* block_table, int32_t* held_out, int32_t* refs,

@@ -185,7 +185,9 @@ int loma_decode_attn_kv4(const void* q, const void* k_new, const void* v_new, vo
 // ------------------------------------------------------------------ pages
 static int page_sizes(int B, int page_size, int max_pages, int n_pages, int n_free, int* l2) {
     if (B < 0 || max_pages < 0 || n_pages < 0 || n_free < 0) return LOMA_ERR_INVALID_ARG;
-    if (B == INT_MAX || n_pages > INT_MAX - 65536 || n_free == INT_MAX || !fits({4, B, max_pages})) return LOMA_ERR_INVALID_ARG;
+    // kernels go over rows, columns and pages in 32-bit steps of up to 9472 (rows: the warps of a full launch)
+    constexpr int TOP = INT_MAX - 65536;
+    if (B > TOP || max_pages > TOP || n_pages > TOP || n_free == INT_MAX || !fits({4, B, max_pages})) return LOMA_ERR_INVALID_ARG;
     *l2 = log2_exact(page_size);
     if (*l2 < 0 || page_size > 65536) return LOMA_ERR_INVALID_ARG;
     if ((int64_t)max_pages * page_size > INT_MAX) return LOMA_ERR_INVALID_ARG;

@@ -540,3 +540,20 @@ def test_kv4_decode_refuses_scales_its_sums_cannot_carry(lib, scale, status):
         for dtype in (0, 1):
             assert lib.loma_decode_attn_kv4(p(q), None, None, p(kt), p(vt), None, None, p(o), None, B, Hq, H, D, cap, p(lens), 8, 16, 0, 0, p(z(B)), 0, dtype, scale, flags, p(ws),
                                             2**20, None) == status
+
+
+def apart_from_each_other(n):
+    """Addresses of arrays that are not there: for calls that end on the host."""
+    return [ctypes.c_void_p((i + 1) << 42) for i in range(n)]
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="where the checks let a call through, the missing device has to end it")
+def test_rows_and_columns_that_32_bit_steps_would_leave_are_refused(lib):
+    """Kernels go over rows and columns in steps of up to 9472 in 32 bits: the last step must not pass INT_MAX."""
+    top = 2**31 - 1 - 65536
+    for B, M, refused in ((top + 1, 1, True), (2**31 - 2, 1, True), (2**31 - 9000, 0, True), (1, top + 1, True), (1, 2**31 - 1, True), (top, 1, False), (1, top, False), (0, top + 1, True)):
+        for name, args in (("loma_paged_release", [B, 1, M, 6, 6, *apart_from_each_other(8), 1, None]),
+                           ("loma_paged_fork", [B, 1, M, 6, 6, 4, *apart_from_each_other(15), 2**40, 1, None]),
+                           ("loma_paged_compact", [B, M, 6, 6, 4, *apart_from_each_other(9), 1, None])):
+            status = getattr(lib, name)(*args)
+            assert (status == INVALID) == refused and status != 0, (name, B, M, status)
