@@ -972,7 +972,8 @@ LOMA_API int loma_paged_copy(int n_pools, void* const* pools, const int64_t* pag
  * fp32.  bf16 calls run on the tensor cores and round each weight (times the step of the value's group) to bf16 for the product
  * with V, off by 2^-8 of itself at most; fp32, and LOMA_FLAG_FORCE_GENERIC, keep it.  For queries up to 2^60 and memory values
  * up to 2^40 in magnitude (sums carry powers of two); a positive softmax_scale lies between 2^-50 and 2^50 (INVALID_ARG).
- * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CAPACITY, WORKSPACE, CUDA.  B * Hkv * l == 0, B * Hkv * cap == 0, B * Hq == 0: a no-op.
+ * Errors: INVALID_ARG (outputs, decode's workspace among them, that overlap inputs or each other, too), UNSUPPORTED, ALIGNMENT, CAPACITY,
+ * WORKSPACE, CUDA.  B * Hkv * l == 0, B * Hkv * cap == 0, B * Hq == 0: a no-op.
  * ------------------------------------------------------------------------- */
 LOMA_API size_t loma_kv4_page_bytes(int Hkv, int D, int page_size);
 LOMA_API int loma_kv4_append(const void* k, const void* v, void* kv_pool, const int32_t* block_table, const int32_t* mem_lens,

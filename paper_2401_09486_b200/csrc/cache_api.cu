@@ -165,10 +165,11 @@ int loma_decode_attn_kv4(const void* q, const void* k_new, const void* v_new, vo
     for (const void* p : {(const void*)block_table, (const void*)lse, (const void*)tail_lens, (const void*)mem_lens})
         if (misaligned(p, 4)) return LOMA_ERR_ALIGNMENT;
     const int64_t es = (int64_t)elt_bytes(dtype), rows = (int64_t)B * Hq * D * es, news = (int64_t)B * Hkv * D * es, tails = news * cap;
+    const size_t need = loma_decode_kv4_workspace_bytes(B, Hq, Hkv, D, max_mem_len, max_tail_len);
     if (!apart({{q, rows}, {k_new, news}, {v_new, news}, {kv_pool, max_mem_len > 0 ? kv4_pool_bytes(Hkv, D, l2, n_pages) : 0},
                 {block_table, max_mem_len > 0 ? 4ll * B * max_pages : 0}, {tail_lens, 4ll * B}, {mem_lens, 4ll * B}},
-               {{k_tail, tails}, {v_tail, tails}, {o, rows}, {lse, 4ll * B * Hq}})) return LOMA_ERR_INVALID_ARG;
-    const size_t need = loma_decode_kv4_workspace_bytes(B, Hq, Hkv, D, max_mem_len, max_tail_len);
+               {{k_tail, tails}, {v_tail, tails}, {o, rows}, {lse, 4ll * B * Hq}, {workspace, (int64_t)std::min(need, workspace_bytes)}}))
+        return LOMA_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < need) return LOMA_ERR_WORKSPACE;
     const int dc = check_device();
     if (dc != LOMA_OK) return dc;

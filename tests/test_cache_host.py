@@ -557,3 +557,27 @@ def test_rows_and_columns_that_32_bit_steps_would_leave_are_refused(lib):
                            ("loma_paged_compact", [B, M, 6, 6, 4, *apart_from_each_other(9), 1, None])):
             status = getattr(lib, name)(*args)
             assert (status == INVALID) == refused and status != 0, (name, B, M, status)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="where the checks let a call through, the missing device has to end it")
+def test_kv4_decode_refuses_a_workspace_that_meets_its_tensors(lib):
+    B, Hq, H, D, cap, ps, M, n = 2, 6, 3, 64, 9, 16, 4, 6
+    need = L.loma_decode_kv4_workspace_bytes(B, Hq, H, D, 60, 8)
+    names = dict(q=B * Hq * D * 4, kn=B * H * D * 4, vn=B * H * D * 4, kt=B * H * cap * D * 4, vt=B * H * cap * D * 4, pool=n * L.loma_kv4_page_bytes(H, D, ps), table=B * M * 4,
+                 o=B * Hq * D * 4, lse=B * Hq * 4, tails=B * 4, mems=B * 4)
+    at = dict(zip((*names, "ws"), (x.value for x in apart_from_each_other(12))))
+
+    def status(ws, size=need, **without):
+        a = {**{k: ctypes.c_void_p(v) for k, v in at.items()}, **without}
+        return lib.loma_decode_attn_kv4(a["q"], a["kn"], a["vn"], a["kt"], a["vt"], a["pool"], a["table"], a["o"], a["lse"], B, Hq, H, D, cap, a["tails"], 8, ps, M, n, a["mems"], 60, 0,
+                                        0.0, 0, ctypes.c_void_p(ws), size, None)
+
+    assert status(at["ws"]) not in (0, INVALID, WORKSPACE)                      # the missing device
+    for k, size in names.items():
+        assert status(at[k]) == INVALID, k                                     # begins where the tensor does
+        assert status(at[k] + size - 4 - (at[k] + size - 4) % 16) == INVALID, k   # ... in its last 16 bytes
+        assert status(at[k] - need + 16) == INVALID, k                         # ends behind its beginning
+        for ws in (at[k] - need // 16 * 16 - 16, at[k] + (size + 15) // 16 * 16):
+            assert status(ws) not in (0, INVALID, WORKSPACE), k                # beside it
+    assert status(at["lse"], lse=None) not in (0, INVALID, WORKSPACE)
+    assert status(at["ws"], need - 1) == WORKSPACE
