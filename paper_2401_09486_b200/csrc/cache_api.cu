@@ -18,11 +18,11 @@ struct Range {
     int64_t n;   // bytes
 };
 
-// no output may meet an input or another output, but for the pairs that are one array on purpose
-bool apart(std::initializer_list<Range> ins, std::initializer_list<Range> outs, const void* same = nullptr) {
+// no output may meet an input or another output
+bool apart(std::initializer_list<Range> ins, std::initializer_list<Range> outs) {
     for (const Range* x = outs.begin(); x != outs.end(); ++x) {
         for (const Range& y : ins)
-            if (overlap(x->p, x->n, y.p, y.n) && !(same && x->p == same && y.p == same)) return false;
+            if (overlap(x->p, x->n, y.p, y.n)) return false;
         for (const Range* y = outs.begin(); y != x; ++y)
             if (overlap(x->p, x->n, y->p, y->n)) return false;
     }
@@ -210,8 +210,9 @@ int loma_paged_release(int B, int page_size, int max_pages, int n_pages, int n_f
     if (B > 0 && (!keep_lens || !held || !held_out || (max_pages > 0 && !block_table))) return LOMA_ERR_INVALID_ARG;
     if (words_misaligned({keep_lens, held, block_table, held_out, refs, free_pages, taken, counts})) return LOMA_ERR_ALIGNMENT;
     const int64_t nb = 4ll * B;
-    if (!apart({{keep_lens, nb}, {held, nb}}, {{block_table, nb * max_pages}, {held_out, nb}, {refs, 4ll * n_pages}, {free_pages, 4ll * n_free},
-                {taken, 4}, {counts, 16}}, held_out == held ? held : nullptr)) return LOMA_ERR_INVALID_ARG;
+    // held_out may be held, and then neither of them keep_lens
+    if (!apart({{keep_lens, nb}, {held_out == held ? nullptr : held, nb}}, {{block_table, nb * max_pages}, {held_out, nb}, {refs, 4ll * n_pages},
+                {free_pages, 4ll * n_free}, {taken, 4}, {counts, 16}})) return LOMA_ERR_INVALID_ARG;
     a.pl.n_pages = n_pages; a.pl.n_free = n_free; a.pl.refs = refs; a.pl.free_pages = free_pages; a.pl.taken = taken;
     a.B = B; a.max_pages = max_pages; a.keep_lens = keep_lens; a.held = held; a.block_table = block_table; a.held_out = held_out; a.counts = counts;
     if (!on_device) {

@@ -581,3 +581,17 @@ def test_kv4_decode_refuses_a_workspace_that_meets_its_tensors(lib):
             assert status(ws) not in (0, INVALID, WORKSPACE), k                # beside it
     assert status(at["lse"], lse=None) not in (0, INVALID, WORKSPACE)
     assert status(at["ws"], need - 1) == WORKSPACE
+
+
+def test_release_refuses_one_array_for_keep_lens_and_the_counts(lib):
+    """held_out may be held; keep_lens is an input of its own."""
+    B, M, n = 3, 4, 8
+    keep, held, table, refs, free, taken, counts = z(B), z(B) + 2, z(B, M), z(n), z(n), z(1), z(4)
+    tail = [p(refs), p(free), p(taken), p(counts), 0, None]
+    for keep_at, held_at, out_at, status in ((keep, held, held, 0), (held, held, held, INVALID), (keep, held, keep, INVALID), (held, held, keep, 0),
+                                             (held, held, None, INVALID)):
+        held.fill_(2)
+        got = lib.loma_paged_release(B, 4, M, n, n, p(keep_at), p(held_at), p(table), p(out_at) if out_at is not None else ctypes.c_void_p(held.data_ptr() + 4), *tail)
+        assert got == status
+        if status:
+            assert held.tolist() == [2] * B
