@@ -33,7 +33,7 @@ struct Kv4Plan {
     // in the workspace, in floats.  Segment: outputs [g_rows][D], g_rows log2-sum-exps.  ends: int32 [2][units], the workers of a unit's
     // first and of its last segment
     int64_t o, lse, ends, total;
-    uint32_t ones;         // 0x00010001 (see kv4_pairs)
+    uint32_t ones;         // 0x00010001 (see kv4_word)
 };
 
 // Units stay whole, with the warps of one CTA or of a cluster of two to eight, while all of them run at once and no warp gets more than
@@ -42,6 +42,9 @@ struct Kv4Plan {
 // against cut (D = 128, us): 32 units of up to 4 / 35 / 66 / 129 blocks 5.8 / 8.7 / 9.6 / 12.0 against 9.9 / 11.1 / 12.4 / 15.3; 128 units of 35 / 66
 // 11.8 / 16.8 against 14.7 / 18.5; 256 units of 35 / 51 16.0 / 22.1 against 20.2 / 24.2; 512 units of 14 14.7 against 17.2; but 64 units of 254, 16 blocks
 // to a warp, 26.4 against 24.9, and 1024 units of 14 27.3 against 24.3.
+// The rule goes by the host's bounds, not by the lengths, which only the device knows: a step captured for a capacity of 150000 entries is cut
+// however short its sequences are (D = 128 but for the first; own bound / capacity, us: 32 units of up to 200 entries, D = 64, 5.6 / 9.2; 32 of 100 5.9 / 10.0;
+// 32 of 1000 8.6 / 11.1; 128 of 1000 11.6 / 14.4; 256 of 1000 15.6 / 19.6).
 constexpr int KV4_WHOLE = 12, KV4_WHOLE_SHORT = 16;
 
 static Kv4Plan make_kv4_plan(int B, int Hq, int Hkv, int D, int max_mem, int max_tail, bool cuda_cores) {
