@@ -5,7 +5,8 @@
 // results spread over the lanes (seven shuffles), so each lane works out one step.  Both directions are bound by HBM (256 bytes of bf16
 // against 72 for a row of 128 features) as long as a value costs few instructions: m is the integer part of |x| / (2 h), a product and an
 // addition that rounds towards zero; see kv4_half for why that is exact.
-// Measured (32 x 32 heads, D = 128, bf16): 1.5 million rows stored in 206 us (4.9 TB/s, issue-bound), 1.6 million read back in 158 us (6.5 TB/s).
+// Measured (D = 128): bf16, 1.36 million rows of keys and as many of values stored in 203 us (4.4 TB/s, issue-bound), 1.41 million read back in 161
+// us (5.8 TB/s); fp32, half as many of each: 135 us (5.9 TB/s) and 138 us (6.0 TB/s).  D = 64, bf16: 141 us (3.2 TB/s) and 90 us (5.2 TB/s).
 #include "kv4.cuh"
 
 namespace loma {

@@ -9,8 +9,8 @@
 // counts exchanged through each other's shared memory.  Pages and sequences are dealt to the CTAs in contiguous parts, so ranks
 // follow from block-wide sums and the parts' totals, in ascending order of page or sequence: results repeat bit for bit, and the
 // only atomics are additions and ORs of integers.
-// Measured with the launch: release of 64 sequences 5 us, of 2000 with 500 000 pages 29; fork of 8 / 256 sequences 7 / 17; compaction of 16
-// sequences 10, of 500 with 94 500 pages 35; copy of 2 x 386 MB 107 (0.95 to 1.0 of a copy).
+// Measured with the launch: release of 64 sequences 6 us, of 2000 with 500 000 pages 25; fork of 8 / 256 sequences 9 / 18; compaction of 16
+// sequences 10, of 500 with 94 500 pages 27; copy of 21 000 pages of 8 KB in two pools (346 MB in, 346 out) 124 (0.85 of a plain copy).
 #include <limits.h>
 
 #include <algorithm>
@@ -441,12 +441,16 @@ __global__ void __launch_bounds__(DROP_THREADS) paged_list_kernel(const ReleaseA
 }
 
 // Pages that a release may free beyond which they are listed over all SMs: eight SMs store them at 20 bytes a cycle each.  Measured (us, in the
-// cluster against a launch of its own): 125 000 pages 13.2 / 15.9, 250 000 22.3 / 22.7, 500 000 34.1 / 29.5, a million 70 / 56.
+// cluster against a launch of its own): 125 000 pages 13.2 / 15.9, 250 000 22.3 / 22.7, 500 000 34.1 / 29.5, a million 70 / 56.  The host
+// knows what may be freed, not what is: 64 pages that come back to a pool pay for the look through its counts and, past this bound, for that
+// launch: pools of 512 / 230 000 / 300 000 / 500 000 / a million pages 6 / 11 / 15 / 18 / 40.
 constexpr int PG_LIST = 1 << 18;
 
 // Rows to a cluster's warp beyond which the rows' own work goes over all SMs in launches of its own, each behind the other.  Measured (us, one
-// launch against several, up to 1900 entries in pages of 16): 128 sequences: fork 15.9 / 18.0, release 10.1 / 9.6, compaction 25.7 / 26.3; 1000: fork
-// 30.9 / 24.2, release 17.8 / 14.1, compaction 107 / 81.
+// launch against several, up to 1900 entries in pages of 16, tables of 128 columns): 128 / 256 / 320 / 1000 sequences: fork 12.5 / 13.4 / 16.1 / 25.7
+// against 14.3 / 15.5 / 15.7 / 18.9; release 8.7 / 9.3 / 9.7 / 18.3 against 8.9 / 9.3 / 9.5 / 12.7; compaction, which would change over
+// at 128 by itself, 17.5 / 21.4 / 25.3 / 54.5 against 17.4 / 18.5 / 19.2 / 27.0.  Columns shift it little: 256 forks with tables of 32 / 512 columns 10.9 /
+// 17.4 against 12.9 / 19.2, 256 releases with 512 columns 17.4 against 16.4.
 constexpr int PG_ROWS = 1, PG_FEW = PG_ROWS * PG_ALL_WARPS;
 
 // rows' owners gained and lost; kids_of: children of a row
