@@ -1027,8 +1027,8 @@ kv4_merge_kernel(const Kv4DecodeArgs a, const Kv4Plan p) {
     if (live) {
         const int64_t unit = (int64_t)(h * p.g_tiles + gt) * a.B + b;
         const int32_t* ends = reinterpret_cast<const int32_t*>(ws + p.ends) + unit;
-        const int w0 = __ldcg(ends);
-        n = __ldcg(ends + (int64_t)a.B * a.Hkv * p.g_tiles) - w0 + 1;
+        int w0;
+        n = kv4_parts(__ldcg(ends), __ldcg(ends + (int64_t)a.B * a.Hkv * p.g_tiles), p.workers, &w0);
         const int64_t first = (w0 + unit) * p.g_rows + x;
         const float *lse = ws + p.lse + first, *v = ws + p.o + first * D + c4 * 4;
         for (int s0 = way * AT_ONCE; s0 < n; s0 += WAYS * AT_ONCE) {

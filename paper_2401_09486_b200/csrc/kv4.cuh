@@ -76,6 +76,13 @@ struct Kv4DecodeArgs {
     float scale = 0.f;
     void* ws = nullptr;
 };
+// The partial results of a cut unit, from the notes of its first and its last worker: how many, and the first one's worker.  first 1, last 0: none,
+// one worker has done all of it.  A worker whose bounded wait has run out leaves its notes as they were in the workspace, so any number may
+// stand there: what is read stays among the workers' slots.
+__host__ __device__ inline int kv4_parts(int first, int last, int workers, int* begin) {
+    *begin = first < 0 ? 0 : first >= workers ? workers - 1 : first;
+    return last < *begin ? 0 : (last >= workers ? workers - 1 : last) - *begin + 1;
+}
 size_t decode_kv4_workspace_bytes(int B, int Hq, int Hkv, int D, int max_mem, int max_tail);   // decode_kv4.cu
 cudaError_t launch_decode_kv4(const Kv4DecodeArgs& a, int D, loma_dtype dt, bool generic, cudaStream_t st);
 

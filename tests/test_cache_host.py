@@ -2,6 +2,8 @@
 forms of the page bookkeeping against the oracle, long lives of a pool, refusals before any CUDA call, workspace sizes."""
 
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -595,3 +597,12 @@ def test_release_refuses_one_array_for_keep_lens_and_the_counts(lib):
         assert got == status
         if status:
             assert held.tolist() == [2] * B
+
+
+def test_merge_reads_slots_of_workers_whatever_the_workspace_holds(lib, tmp_path):
+    """A worker whose wait ran out notes nothing, and the merge behind it must stay in the workspace (tests/c_abi/kv4_parts_check.cu)."""
+    exe = str(tmp_path / "kv4_parts_check")
+    subprocess.run([build._nvcc(), "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", build.INCLUDE, "-I", build.CSRC,
+                    os.path.join(build.ROOT, "tests", "c_abi", "kv4_parts_check.cu"), "-o", exe], check=True)
+    out = subprocess.run([exe], capture_output=True, text=True)
+    assert out.returncode == 0 and "kv4 parts ok" in out.stdout, out.stdout + out.stderr
