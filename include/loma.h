@@ -900,7 +900,7 @@ LOMA_API size_t loma_decode_shared_workspace_bytes(int B, int Hq, int Hkv, int D
  *           [host]: n_pools device pointers (K and V of every layer, say) and the bytes of a page of each (multiples of 16), n_pages
  *           pages each.  n_copies [device]: counts of fork or compact.  Pairs with a number outside [0, n_pages) are passed over.
  *           No page may be a source and a destination of one call, or a destination twice (the lists above have neither), and the
- *           pools lie apart from each other.
+ *           pools lie apart from each other (which is not checked; the lists' place outside the pools is).
  *           One launch for up to 64 pools.
  * Errors: INVALID_ARG (negative sizes, page size not a power of two <= 65536, max_pages * page_size > INT_MAX, B, max_pages or n_pages
  * above INT_MAX - 65536, a required pointer NULL, outputs that overlap inputs or each other), ALIGNMENT (4 bytes; pools and page_bytes
@@ -977,7 +977,8 @@ LOMA_API int loma_paged_copy(int n_pools, void* const* pools, const int64_t* pag
  * Precision: memory entries are what they stand for, (2 m + 1) h, without a further rounding; scores, the softmax and the sums are
  * fp32.  bf16 calls run on the tensor cores and round each weight (times the step of the value's group) to bf16 for the product
  * with V, off by 2^-8 of itself at most; fp32, and LOMA_FLAG_FORCE_GENERIC, keep it.  For queries up to 2^60 and memory values
- * up to 2^40 in magnitude (sums carry powers of two); a positive softmax_scale lies between 2^-50 and 2^50 (INVALID_ARG).
+ * up to 2^40 in magnitude (sums carry powers of two, so what memory adds to an output comes in steps of 2^-96 at the finest); a
+ * positive softmax_scale lies between 2^-50 and 2^50 (INVALID_ARG).
  * Errors: INVALID_ARG (outputs, decode's workspace among them, that overlap inputs or each other, too), UNSUPPORTED, ALIGNMENT, CAPACITY,
  * WORKSPACE, CUDA.  B * Hkv * l == 0, B * Hkv * cap == 0, B * Hq == 0: a no-op.
  * ------------------------------------------------------------------------- */

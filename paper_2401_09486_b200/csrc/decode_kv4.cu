@@ -13,7 +13,7 @@
 //
 // bf16: kv4_decode_kernel, warp-level products.  fp32, and the second opinion: kv4_stream_kernel on CUDA cores.
 // Measured: B64 Hq32 Hkv8 D128, up to 16384 entries and tails of up to 127 (829 MB): 164 us, 5.0 TB/s (0.77 of a copy; the copies alone take 134 us)
-// in a short run; 180 us in a long one, which the power limit holds at 1.8 GHz.  B32 H32, 2048 entries 56 us; B4 H8 D64, 200 entries 5.4 us.
+// in a short run; 169 to 180 us in long ones, which the power limit holds at 1.8 GHz.  B32 H32, 2048 entries 56 us; B4 H8 D64, 200 entries 5.4 us.
 // In between 0.2 to 0.4 of a copy's rate (Hkv 8: B16, 1000 entries 11.5 us; B8, 8000 24; B64, 1000 26).  16 heads to a kv head: B64 Hq128, 8000
 // entries 137 us (0.48).  fp32: B11 Hq15 Hkv3, 2501 entries 23 us; B32 Hq32 Hkv8, 4000 entries 87 us.
 #include <cooperative_groups.h>

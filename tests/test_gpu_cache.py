@@ -967,3 +967,14 @@ def test_release_of_rows_whose_lanes_part(B, M, in_place):
     want = C.release(keep, held, table, 4, refs, free, taken)
     for _ in range(3):
         H.check_release(H.run_release(case, keep, 4, DEV, in_place=in_place), want)
+
+
+@pytest.mark.parametrize("dtype,flags", KINDS)
+def test_decode_of_values_near_the_end_of_what_its_sums_carry(dtype, flags):
+    """Values of 1e-20: sums over memory are kept times 2^-53, in steps of 2^-96 of an output, of which there are 2^26 to these outputs."""
+    s = make(2, 4, 2, 64, [100, 37], [20, 3], 16, dtype)
+    for x in ("v", "vt", "vn"):
+        s[x] = (s[x] * 1e-20).to(dtype)
+    L.loma_kv4_append(s["k"], s["v"], s["pool"], s["table"], s["ps"], di32([0, 0]), di32(s["mems"]))
+    call(s, flags)
+    check(s, flags)
